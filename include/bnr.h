@@ -593,6 +593,53 @@ typedef struct {
 bnr_status bnr_reference_bn_relu(int32_t backward, int64_t m, int32_t c, bnr_dtype dtype,
                                  const bnr_bnrelu_ref_args *a, void *ws, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------- layer normalisation ---- */
+
+/* Layer normalisation: the statistics run over the c channels of each row
+ * (pixel, token) instead of over the pixels of each channel, so a row's result
+ * does not depend on the rest of the batch:
+ *   mean = sum(s)/c, var = sum((s - mean)^2)/c (biased), rstd = 1/sqrt(var+eps),
+ *   y = gamma * (s - mean) * rstd + beta.
+ * Rows are views [m][c] with a row stride in elements.  These calls take any
+ * c up to 16384, any stride >= c and element-aligned pointers (16-byte aligned
+ * views whose c and strides are multiples of the 16-byte vector are faster);
+ * different channel slices of one buffer do not overlap each other.  A row of
+ * one repeated value has rstd = 1/sqrt(eps) and y = beta; an infinity or NaN
+ * makes its own row NaN and no other. */
+typedef struct {
+    const float *gamma;    /* [c] scale, or NULL (1)                               */
+    const float *beta;     /* [c] shift, or NULL (0); not read by the backward     */
+    float *mean;           /* [m] written by the forward, read by the backward     */
+    float *rstd;           /* [m] likewise                                         */
+    float eps;             /* > 0 (forward)                                        */
+} bnr_ln;
+
+/* y = layernorm(x), or, with res and sum (both or neither), of the residual
+ * sum: sum = x + res is written in the storage type and y is the norm of the
+ * values as stored.  One pass: every input is read and every output written
+ * once.  y and sum may coincide exactly with x or res (same pointer and
+ * stride) and may not overlap them otherwise, nor each other.  m >= 1. */
+bnr_status bnr_layernorm_fwd(int64_t m, int32_t c, bnr_dtype dtype, const void *x, int32_t x_ldc, const void *res,
+                             int32_t res_ldc, void *sum, int32_t sum_ldc, const bnr_ln *ln, void *y, int32_t y_ldc,
+                             void *stream);
+
+/* Workspace bytes of bnr_layernorm_bwd. */
+size_t bnr_layernorm_workspace_size(int64_t m, int32_t c, bnr_dtype dtype);
+
+/* Backward of bnr_layernorm_fwd; x is what the forward normalised (sum, where
+ * it had one), ln its gamma and the mean and rstd it wrote:
+ *   g = dy * gamma, xhat = (x - mean) * rstd,
+ *   dx = rstd * (g - sum(g)/c - xhat * sum(g * xhat)/c) + dsum,
+ *   dgamma = sum over rows of dy * xhat, dbeta = sum over rows of dy.
+ * dsum (may be NULL) is the gradient that reaches x by another way (the
+ * residual's); dx is then the gradient of both x and res.  dgamma, dbeta
+ * (float32, overwritten) may be NULL; ws may be NULL when both are.  The sums
+ * have a fixed order: the same call gives the same bits.  dx may coincide
+ * exactly with dy, x or dsum and may not overlap them otherwise. */
+bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy, int32_t dy_ldc, const void *x,
+                             int32_t x_ldc, const bnr_ln *ln, const void *dsum, int32_t dsum_ldc, void *dx,
+                             int32_t dx_ldc, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------ diagnostics ---- */
 
 /* Plain device-to-device copy of `bytes` (multiple of 16) with the same
@@ -611,8 +658,9 @@ bnr_status bnr_hbm_copy(const void *src, void *dst, size_t bytes, void *stream);
  * (1 CONV 1x1, 2 CONV 3x3, 3 weight gradient 1x1, 4 weight gradient 3x3,
  * 5 statistics sweep, 6 element-wise pass, 7 statistics combine, 8 weight
  * packing, 9 split-K sum, 10 pooling, 11 copy, 12 first CONV, 13 first-CONV
- * weight gradient, 14 max pooling, 15 classifier head); it returns the number of
- * launches written.  Not meant for graph capture. */
+ * weight gradient, 14 max pooling, 15 classifier head, 16 layer norm,
+ * 17 orthogonalised update); it returns the number of launches written.  Not
+ * meant for graph capture. */
 bnr_status bnr_trace_begin(int32_t kernel_classes, int32_t capacity);
 int32_t bnr_trace_end(double *ms, double *bytes, double *flops, int32_t *kernel_id, int32_t capacity);
 

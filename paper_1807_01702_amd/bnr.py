@@ -63,6 +63,10 @@ class RefArgs(ctypes.Structure):
                 ("dbeta", c_vp), ("dx", c_vp), ("dx_ldc", c_i32), ("dx_accumulate", c_i32)]
 
 
+class LNStruct(ctypes.Structure):
+    _fields_ = [("gamma", c_vp), ("beta", c_vp), ("mean", c_vp), ("rstd", c_vp), ("eps", c_f)]
+
+
 class AddReluRefArgs(ctypes.Structure):
     _fields_ = [("y", c_vp), ("y_ldc", c_i32), ("bn", ctypes.POINTER(BNStruct)), ("id", c_vp), ("id_ldc", c_i32),
                 ("out", c_vp), ("out_ldc", c_i32), ("tmp", c_vp), ("g", c_vp), ("g_ldc", c_i32), ("gm", c_vp),
@@ -143,6 +147,11 @@ _lib_fns = dict(
     bnr_head_bwd=_sig("bnr_head_bwd", ctypes.c_int, c_i32, c_i32, c_i32, c_i32, c_i32, ctypes.c_int, c_vp, c_i32,
                       _P(BNStruct), c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp,
                       c_sz, c_vp),
+    bnr_layernorm_fwd=_sig("bnr_layernorm_fwd", ctypes.c_int, c_i64, c_i32, ctypes.c_int, c_vp, c_i32, c_vp, c_i32,
+                           c_vp, c_i32, _P(LNStruct), c_vp, c_i32, c_vp),
+    bnr_layernorm_workspace_size=_sig("bnr_layernorm_workspace_size", c_sz, c_i64, c_i32, ctypes.c_int),
+    bnr_layernorm_bwd=_sig("bnr_layernorm_bwd", ctypes.c_int, c_i64, c_i32, ctypes.c_int, c_vp, c_i32, c_vp, c_i32,
+                           _P(LNStruct), c_vp, c_i32, c_vp, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp),
     bnr_trace_begin=_sig("bnr_trace_begin", ctypes.c_int, c_i32, c_i32),
     bnr_trace_end=_sig("bnr_trace_end", c_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double),
                        ctypes.POINTER(ctypes.c_double), ctypes.POINTER(c_i32), c_i32),
@@ -150,7 +159,7 @@ _lib_fns = dict(
 
 KERNEL_IDS = {1: "conv1x1", 2: "conv3x3", 3: "wgrad1x1", 4: "wgrad3x3", 5: "stats_sweep", 6: "elementwise",
               7: "stats_combine", 8: "weight_pack", 9: "splitk_sum", 10: "pool", 11: "copy", 12: "stem_conv",
-              13: "stem_wgrad", 14: "maxpool", 15: "head"}
+              13: "stem_wgrad", 14: "maxpool", 15: "head", 16: "layernorm", 17: "ortho"}
 
 
 class BnrError(RuntimeError):
@@ -653,3 +662,97 @@ def bnr_reference_bn_relu(backward, x, bn, y, z=None, gz=None, dy=None, dgamma=N
     ws, wsb = workspace(bnr_stats_workspace_size(m, c), x.device)
     _check(_lib_fns["bnr_reference_bn_relu"](1 if backward else 0, m, c, dtype_code(x), ctypes.byref(a), ws, wsb,
                                              _stream()))
+
+
+# ------------------------------------------- layer norm, weight updates ----
+# These calls run on the current stream of their tensors' device, which need not
+# be the current device, and take their workspace from torch's allocator per call:
+# calls on two streams share nothing, and a captured graph holds its own.
+class _on_device:
+    """Makes a tensor's device current for a call; yields that device's current stream."""
+
+    def __init__(self, *tensors):
+        tensors = [t for t in tensors if t is not None]
+        dev = tensors[0].device
+        if dev.type != "cuda":
+            raise ValueError("tensors of a GPU are wanted, got one of %s" % dev)
+        for t in tensors[1:]:
+            if t.device != dev:
+                raise ValueError("tensors of two devices: %s and %s" % (dev, t.device))
+        self.index = dev.index
+
+    def __enter__(self):
+        self.before = _current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+        return _stream()
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
+def _scratch(nbytes, device):
+    """Workspace of one call (torch aligns its blocks to 512 bytes); the caller keeps the tensor until the launch."""
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _f32_array(t, n, name):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: a contiguous float32 array of %d values is wanted" % (name, n))
+    return t.data_ptr()
+
+
+def _rows(t, m, c, dtype, name):
+    if t is None:
+        return None, 0
+    p, tm, tc, ld = view(t)
+    if (tm, tc) != (m, c) or t.dtype != dtype:
+        raise ValueError("%s: [%d, %d] rows of %s are wanted, got [%d, %d] of %s" % (name, m, c, dtype, tm, tc, t.dtype))
+    return p, ld if m > 1 else c
+
+
+class LN:
+    """One layer norm: gamma, beta ([c] float32 or None), eps, and the statistics of its m rows (mean, rstd: [m],
+    allocated unless given), which the forward writes and the backward reads."""
+
+    def __init__(self, gamma, beta, m, eps=1e-5, mean=None, rstd=None, device=None):
+        dev = next((t.device for t in (gamma, beta, mean, rstd) if t is not None), None) or torch.device(device or "cuda")
+        self.gamma, self.beta, self.eps = gamma, beta, float(eps)
+        self.mean = mean if mean is not None else torch.empty(m, dtype=torch.float32, device=dev)
+        self.rstd = rstd if rstd is not None else torch.empty(m, dtype=torch.float32, device=dev)
+
+    def struct(self, m, c):
+        return LNStruct(_f32_array(self.gamma, c, "gamma"), _f32_array(self.beta, c, "beta"),
+                        _f32_array(self.mean, m, "mean"), _f32_array(self.rstd, m, "rstd"), self.eps)
+
+
+def bnr_layernorm_fwd(x, ln, y, res=None, sum=None):
+    """y = layernorm(x), or, with res, sum = x + res and y = layernorm(sum) (views [.., c])."""
+    px, m, c, ldx = view(x)
+    py, ldy = _rows(y, m, c, x.dtype, "y")
+    pr, ldr = _rows(res, m, c, x.dtype, "res")
+    ps, lds = _rows(sum, m, c, x.dtype, "sum")
+    s = ln.struct(m, c)
+    with _on_device(x, y, ln.mean, ln.rstd, ln.gamma, ln.beta, res, sum) as stream:
+        _check(_lib_fns["bnr_layernorm_fwd"](m, c, dtype_code(x), px, ldx if m > 1 else c, pr, ldr, ps, lds,
+                                             ctypes.byref(s), py, ldy, stream))
+
+
+def bnr_layernorm_bwd(dy, x, ln, dx, dgamma=None, dbeta=None, dsum=None):
+    """dx (views [.., c]; + dsum), dgamma and dbeta ([c] float32, overwritten) of bnr_layernorm_fwd; x: what it
+    normalised (its sum, where it had one)."""
+    px, m, c, ldx = view(x)
+    pd, ldd = _rows(dy, m, c, x.dtype, "dy")
+    po, ldo = _rows(dx, m, c, x.dtype, "dx")
+    pr, ldr = _rows(dsum, m, c, x.dtype, "dsum")
+    s = ln.struct(m, c)
+    pg, pb = _f32_array(dgamma, c, "dgamma"), _f32_array(dbeta, c, "dbeta")
+    with _on_device(x, dy, dx, ln.mean, ln.rstd, ln.gamma, dsum, dgamma, dbeta) as stream:
+        code = dtype_code(x)
+        nbytes = _lib_fns["bnr_layernorm_workspace_size"](m, c, code) if pg or pb else 0
+        ws = _scratch(nbytes, x.device) if nbytes else None
+        _check(_lib_fns["bnr_layernorm_bwd"](m, c, code, pd, ldd, px, ldx if m > 1 else c, ctypes.byref(s), pr, ldr,
+                                             po, ldo, pg, pb, _ptr(ws), nbytes, stream))

@@ -1645,4 +1645,176 @@ bnr_status bnr_head_bwd(int32_t n, int32_t h, int32_t w, int32_t c, int32_t clas
     return ok();
 }
 
+// ------------------------------------------------- layer normalisation ----
+// A row view of the layer norm: unlike the other views it may have any channel
+// count, stride and element-aligned pointer (16-byte vectors where they fit).
+static bnr_status check_ln_view(const void *p, int32_t ldc, int32_t c, bnr_dtype dtype, const char *name)
+{
+    if (!p) return fail(BNR_ERR_NULL, "%s is NULL", name);
+    if (reinterpret_cast<uintptr_t>(p) % esize(dtype)) return fail(BNR_ERR_ALIGN, "%s is not element-aligned", name);
+    if (ldc < c) return fail(BNR_ERR_SHAPE, "%s: ldc %d < channels %d", name, ldc, c);
+    return BNR_OK;
+}
+
+static bool ln_vec(const void *p, int32_t ldc, bnr_dtype dtype)
+{
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ldc % vec_of(dtype) == 0;
+}
+
+// Whether two row views share an element: apart in memory, or different channel
+// slices of rows of one stride, they do not.
+static bool rows_overlap(const void *a, int32_t a_ldc, const void *b, int32_t b_ldc, int64_t m, int32_t c, int es)
+{
+    if (!overlap(view_range(a, m, c, a_ldc, es), view_range(b, m, c, b_ldc, es))) return false;
+    if (a_ldc != b_ldc || m == 1) return true;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+    const uintptr_t row = (uintptr_t)a_ldc * es, d = pa < pb ? (pb - pa) % row : (row - (pa - pb) % row) % row;
+    return !(d >= (uintptr_t)c * es && d + (uintptr_t)c * es <= row);
+}
+
+// an output view `o` may coincide exactly with the input view `i`, else not overlap it
+static bool ln_clash(const void *o, int32_t o_ldc, const void *i, int32_t i_ldc, int64_t m, int32_t c, int es)
+{
+    return !(o == i && o_ldc == i_ldc) && rows_overlap(o, o_ldc, i, i_ldc, m, c, es);
+}
+
+static bnr_status check_ln(int64_t m, int32_t c, bnr_dtype dtype, const bnr_ln *ln)
+{
+    TRY(check_dtype(dtype));
+    if (m <= 0 || m > ((int64_t)1 << 31)) return fail(BNR_ERR_SHAPE, "m = %lld out of range", (long long)m);
+    if (c <= 0) return fail(BNR_ERR_SHAPE, "channels %d must be positive", c);
+    if (c > kLnMaxC) return fail(BNR_ERR_UNSUPPORTED, "more than %d channels", kLnMaxC);
+    if (!ln) return fail(BNR_ERR_NULL, "ln is NULL");
+    if (ln->gamma) TRY(check_fptr(ln->gamma, "ln.gamma"));
+    if (ln->beta) TRY(check_fptr(ln->beta, "ln.beta"));
+    TRY(check_fptr(ln->mean, "ln.mean"));
+    TRY(check_fptr(ln->rstd, "ln.rstd"));
+    return BNR_OK;
+}
+
+// whether the float32 array f[0 .. n) touches the row view v
+static bool array_in_rows(const float *f, int64_t n, const void *v, int32_t ldc, int64_t m, int32_t c, int es)
+{
+    return f && v && overlap(bytes_range(f, n * 4), view_range(v, m, c, ldc, es));
+}
+
+bnr_status bnr_layernorm_fwd(int64_t m, int32_t c, bnr_dtype dtype, const void *x, int32_t x_ldc, const void *res,
+                             int32_t res_ldc, void *sum, int32_t sum_ldc, const bnr_ln *ln, void *y, int32_t y_ldc,
+                             void *stream)
+{
+    TRY(check_ln(m, c, dtype, ln));
+    if (!(ln->eps > 0.0f)) return fail(BNR_ERR_SHAPE, "ln.eps must be > 0");
+    TRY(check_ln_view(x, x_ldc, c, dtype, "x"));
+    TRY(check_ln_view(y, y_ldc, c, dtype, "y"));
+    if ((res != nullptr) != (sum != nullptr)) return fail(BNR_ERR_NULL, "res and sum go together");
+    const int es = esize(dtype);
+    bool vec = c % vec_of(dtype) == 0 && ln_vec(x, x_ldc, dtype) && ln_vec(y, y_ldc, dtype);
+    if (res) {
+        TRY(check_ln_view(res, res_ldc, c, dtype, "res"));
+        TRY(check_ln_view(sum, sum_ldc, c, dtype, "sum"));
+        vec = vec && ln_vec(res, res_ldc, dtype) && ln_vec(sum, sum_ldc, dtype);
+        if (ln_clash(sum, sum_ldc, x, x_ldc, m, c, es) || ln_clash(sum, sum_ldc, res, res_ldc, m, c, es))
+            return fail(BNR_ERR_ALIAS, "sum overlaps x or res without coinciding with it");
+        if (ln_clash(y, y_ldc, res, res_ldc, m, c, es))
+            return fail(BNR_ERR_ALIAS, "y overlaps res without coinciding with it");
+        if (rows_overlap(y, y_ldc, sum, sum_ldc, m, c, es)) return fail(BNR_ERR_ALIAS, "y overlaps sum");
+    }
+    if (ln_clash(y, y_ldc, x, x_ldc, m, c, es))
+        return fail(BNR_ERR_ALIAS, "y overlaps x without coinciding with it");
+    const Range rm = bytes_range(ln->mean, m * 4), rr = bytes_range(ln->rstd, m * 4);
+    if (overlap(rm, rr)) return fail(BNR_ERR_ALIAS, "ln.mean overlaps ln.rstd");
+    for (const float *st : {(const float *)ln->mean, (const float *)ln->rstd}) {
+        if (array_in_rows(st, m, x, x_ldc, m, c, es) || array_in_rows(st, m, y, y_ldc, m, c, es) ||
+            array_in_rows(st, m, res, res_ldc, m, c, es) || array_in_rows(st, m, sum, sum_ldc, m, c, es))
+            return fail(BNR_ERR_ALIAS, "ln.mean / ln.rstd overlap a row view");
+        const Range r = bytes_range(st, m * 4);
+        if ((ln->gamma && overlap(r, bytes_range(ln->gamma, (int64_t)c * 4))) ||
+            (ln->beta && overlap(r, bytes_range(ln->beta, (int64_t)c * 4))))
+            return fail(BNR_ERR_ALIAS, "ln.mean / ln.rstd overlap ln.gamma / ln.beta");
+    }
+    for (const float *g : {ln->gamma, ln->beta})
+        if (array_in_rows(g, c, y, y_ldc, m, c, es) || array_in_rows(g, c, sum, sum_ldc, m, c, es))
+            return fail(BNR_ERR_ALIAS, "y / sum overlap ln.gamma / ln.beta");
+    LnParams p{};
+    p.m = m; p.c = c; p.eps = ln->eps;
+    p.x = x; p.x_ldc = x_ldc;
+    p.res = res; p.res_ldc = res_ldc;
+    p.sum = sum; p.sum_ldc = sum_ldc;
+    p.gamma = ln->gamma; p.beta = ln->beta; p.mean = ln->mean; p.rstd = ln->rstd;
+    p.y = y; p.y_ldc = y_ldc;
+    TRY_HIP(launch_ln_fwd(dt_of(dtype), p, vec, (hipStream_t)stream), "layer norm");
+    return ok();
+}
+
+// workspace of the backward: partial rows | combine scratch | a stand-in for the one of dgamma, dbeta not asked for
+static size_t ln_part_bytes(int64_t m, int32_t c, bnr_dtype dtype)
+{
+    const int64_t a = ln_bwd_groups(dt_of(dtype), m, c, false),
+                  b = c % vec_of(dtype) == 0 ? ln_bwd_groups(dt_of(dtype), m, c, true) : 0;
+    return align_up((size_t)(a > b ? a : b) * 2 * c * 4);
+}
+
+size_t bnr_layernorm_workspace_size(int64_t m, int32_t c, bnr_dtype dtype)
+{
+    if (m <= 0 || m > ((int64_t)1 << 31) || c <= 0 || c > kLnMaxC || (dtype != BNR_F32 && dtype != BNR_BF16)) return 0;
+    return ln_part_bytes(m, c, dtype) + align_up(stats_red_bytes(c)) + align_up((size_t)c * 4);
+}
+
+bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy, int32_t dy_ldc, const void *x,
+                             int32_t x_ldc, const bnr_ln *ln, const void *dsum, int32_t dsum_ldc, void *dx,
+                             int32_t dx_ldc, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream)
+{
+    TRY(check_ln(m, c, dtype, ln));
+    TRY(check_ln_view(dy, dy_ldc, c, dtype, "dy"));
+    TRY(check_ln_view(x, x_ldc, c, dtype, "x"));
+    TRY(check_ln_view(dx, dx_ldc, c, dtype, "dx"));
+    const int es = esize(dtype);
+    bool vec = c % vec_of(dtype) == 0 && ln_vec(dy, dy_ldc, dtype) && ln_vec(x, x_ldc, dtype) &&
+               ln_vec(dx, dx_ldc, dtype);
+    if (dsum) {
+        TRY(check_ln_view(dsum, dsum_ldc, c, dtype, "dsum"));
+        vec = vec && ln_vec(dsum, dsum_ldc, dtype);
+        if (ln_clash(dx, dx_ldc, dsum, dsum_ldc, m, c, es))
+            return fail(BNR_ERR_ALIAS, "dx overlaps dsum without coinciding with it");
+    }
+    if (ln_clash(dx, dx_ldc, dy, dy_ldc, m, c, es) || ln_clash(dx, dx_ldc, x, x_ldc, m, c, es))
+        return fail(BNR_ERR_ALIAS, "dx overlaps dy or x without coinciding with it");
+    for (const float *st : {(const float *)ln->mean, (const float *)ln->rstd})
+        if (array_in_rows(st, m, dx, dx_ldc, m, c, es))
+            return fail(BNR_ERR_ALIAS, "dx overlaps ln.mean / ln.rstd");
+    if (array_in_rows(ln->gamma, c, dx, dx_ldc, m, c, es)) return fail(BNR_ERR_ALIAS, "dx overlaps ln.gamma");
+    for (float *out : {dgamma, dbeta}) {
+        if (!out) continue;
+        TRY(check_fptr(out, out == dgamma ? "dgamma" : "dbeta"));
+        const Range r = bytes_range(out, (int64_t)c * 4);
+        if (array_in_rows(out, c, dy, dy_ldc, m, c, es) || array_in_rows(out, c, x, x_ldc, m, c, es) ||
+            array_in_rows(out, c, dx, dx_ldc, m, c, es) || array_in_rows(out, c, dsum, dsum_ldc, m, c, es) ||
+            overlap(r, bytes_range(ln->mean, m * 4)) || overlap(r, bytes_range(ln->rstd, m * 4)) ||
+            (ln->gamma && overlap(r, bytes_range(ln->gamma, (int64_t)c * 4))))
+            return fail(BNR_ERR_ALIAS, "dgamma / dbeta overlap another argument");
+    }
+    if (dgamma && dbeta && overlap(bytes_range(dgamma, (int64_t)c * 4), bytes_range(dbeta, (int64_t)c * 4)))
+        return fail(BNR_ERR_ALIAS, "dgamma overlaps dbeta");
+    const bool sums = dgamma || dbeta;
+    if (sums) TRY(check_ws(ws, ws_bytes, bnr_layernorm_workspace_size(m, c, dtype)));
+    char *red = (char *)ws + (sums ? ln_part_bytes(m, c, dtype) : 0);
+    LnParams p{};
+    p.m = m; p.c = c;
+    p.x = x; p.x_ldc = x_ldc;
+    p.res = dsum; p.res_ldc = dsum_ldc;
+    p.dy = dy; p.dy_ldc = dy_ldc;
+    p.gamma = ln->gamma; p.mean = ln->mean; p.rstd = ln->rstd;
+    p.y = dx; p.y_ldc = dx_ldc;
+    p.part = sums ? (float *)ws : nullptr;
+    hipStream_t st = (hipStream_t)stream;
+    TRY_HIP(launch_ln_bwd(dt_of(dtype), p, vec, st), "layer norm backward");
+    if (sums) {
+        float *unused = (float *)(red + align_up(stats_red_bytes(c)));
+        TRY_HIP(launch_stats_finalize(p.part, ln_bwd_groups(dt_of(dtype), m, c, vec), c, m, FIN_BWD, 0.f, nullptr,
+                                      nullptr, nullptr, dbeta ? dbeta : unused, dgamma ? dgamma : unused, red, st),
+                "backward sums combine");
+    }
+    return ok();
+}
+
 }  // extern "C"

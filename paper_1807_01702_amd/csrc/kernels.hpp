@@ -270,4 +270,28 @@ hipError_t launch_head_fwd(int dtype, const HeadParams &p, hipStream_t s);
 hipError_t launch_head_bwd_fc(int dtype, const HeadParams &p, hipStream_t s);
 hipError_t launch_head_bn_bwd(int dtype, const HeadParams &p, int mode, hipStream_t s);
 
+// Layer normalisation of each row's channels.
+struct LnParams {
+    int64_t m;
+    int c;
+    float eps;                    // forward
+    const void *x;                // [m][c] view: forward input; backward: what the forward normalised
+    int64_t x_ldc;
+    const void *res;              // forward: added to x (NULL: none); backward: added to dx (NULL: none)
+    int64_t res_ldc;
+    void *sum;                    // forward: x + res as stored (with res)
+    int64_t sum_ldc;
+    const void *dy;               // backward: gradient of the output
+    int64_t dy_ldc;
+    const float *gamma, *beta;    // [c] or NULL (1 and 0)
+    float *mean, *rstd;           // [m] written by the forward, read by the backward
+    void *y;                      // forward: output; backward: dx
+    int64_t y_ldc;
+    float *part;                  // backward: partial rows [groups][2][c] (NULL: no dgamma, dbeta)
+};
+// vec: every pointer, stride and the channel count fit 16-byte vectors
+int64_t ln_bwd_groups(int dtype, int64_t m, int c, bool vec);            // partial rows
+hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s);
+hipError_t launch_ln_bwd(int dtype, const LnParams &p, bool vec, hipStream_t s);
+
 }  // namespace bnr

@@ -1,0 +1,389 @@
+// layernorm.hip -- layer normalisation over the channels of each row (pixel,
+// token), forward and backward, for float32 and bf16 rows of up to kLnMaxC
+// channels.
+//
+//   forward   s = x, or the stored x + res;  mean = sum(s)/c,
+//             var = sum((s - mean)^2)/c,  rstd = (var + eps)^-1/2,
+//             y = (s - mean) rstd gamma + beta
+//   backward  g = dy gamma,  xhat = (x - mean) rstd,
+//             dx = rstd (g - sum(g)/c - xhat sum(g xhat)/c)  (+ dsum),
+//             dgamma = sum over rows of dy xhat,  dbeta = sum over rows of dy
+//
+// Both passes are bound by HBM: every input is read once and every output
+// written once, with the row held in registers between the reductions (the
+// variance is the sum of squared differences from the mean already known, so
+// a mean far from zero costs no accuracy).  All arithmetic is float32.
+//
+// A row is held by TPR threads with NV loads of V elements each: V is the
+// 16-byte vector where pointers, strides and the channel count allow it, else
+// one element.  Rows of up to 64 TPR-lanes reduce with cross-lane shuffles and
+// need no barrier; longer rows take a workgroup of 256 or 1024 threads.
+#include "common.hpp"
+#include "kernels.hpp"
+#include "tiles.hpp"
+#include "trace.hpp"
+
+#include <type_traits>
+
+namespace bnr {
+
+namespace {
+
+// V elements at p as floats (V = 1 or one 16-byte vector)
+template <typename T, int V> struct LnVec;
+template <> struct LnVec<float, 1> {
+    typedef float raw;
+    __device__ static __forceinline__ raw load(const float *p) { return *p; }
+    __device__ static __forceinline__ void unpack(raw r, float *f) { f[0] = r; }
+    __device__ static __forceinline__ void store(float *p, const float *f) { *p = f[0]; }
+};
+template <> struct LnVec<bf16_t, 1> {
+    typedef bf16_t raw;
+    __device__ static __forceinline__ raw load(const bf16_t *p) { return *p; }
+    __device__ static __forceinline__ void unpack(raw r, float *f) { f[0] = bf2f(r); }
+    __device__ static __forceinline__ void store(bf16_t *p, const float *f) { *p = f2bf(f[0]); }
+};
+template <typename T> struct LnVec16 {
+    typedef vec16 raw;
+    __device__ static __forceinline__ raw load(const T *p) { return ldg16(p); }
+    __device__ static __forceinline__ void unpack(const raw &r, float *f) { Elem<T>::unpack(r, f); }
+    __device__ static __forceinline__ void store(T *p, const float *f) { stg16(p, Elem<T>::pack(f)); }
+};
+template <> struct LnVec<float, 4> : LnVec16<float> {};
+template <> struct LnVec<bf16_t, 8> : LnVec16<bf16_t> {};
+
+// N sums over the TPR threads of a row (every thread gets them).  Rows longer
+// than a wave go through red[N][waves], which the next call may not reuse
+// before a barrier: callers alternate between two or more areas.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float *red)
+{
+    constexpr int W = TPR < 64 ? TPR : 64;
+    #pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1)
+        #pragma unroll
+        for (int k = 0; k < N; k++) v[k] += __shfl_xor(v[k], o, 64);
+    if constexpr (TPR > 64) {
+        constexpr int NW = TPR / 64;
+        const int wave = threadIdx.x / 64, first = wave / NW * NW;      // waves of this row
+        if (threadIdx.x % 64 == 0)
+            #pragma unroll
+            for (int k = 0; k < N; k++) red[wave * N + k] = v[k];
+        __syncthreads();
+        #pragma unroll
+        for (int k = 0; k < N; k++) {
+            float t = 0.f;
+            #pragma unroll
+            for (int q = 0; q < NW; q++) t += red[(first + q) * N + k];
+            v[k] = t;
+        }
+    }
+}
+
+// U rows at a time per row group, GR row groups per workgroup.
+template <typename T, int V, int TPR, int NV, int U, bool RES>
+__global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnParams p)
+{
+    constexpr int WG = TPR > kThreads ? TPR : kThreads, GR = WG / TPR;
+    typedef LnVec<T, V> L;
+    __shared__ float red[2][WG / 64 * U];
+    const int lane = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+    const int nvec = p.c / V;
+    const T *x = (const T *)p.x, *res = (const T *)p.res;
+    T *sum = (T *)p.sum, *y = (T *)p.y;
+    const int64_t row0 = (int64_t)blockIdx.x * (GR * U) + grp;
+    typename L::raw rx[U][NV], rr[U][NV];
+    float f[U][NV][V], acc[U];
+    #pragma unroll
+    for (int u = 0; u < U; u++) {
+        // rows and vectors past the end read the last ones and are dropped
+        const int64_t row = row0 + u * GR < p.m ? row0 + u * GR : p.m - 1;
+        #pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int v = j * TPR + lane < nvec ? j * TPR + lane : nvec - 1;
+            rx[u][j] = L::load(x + row * p.x_ldc + (int64_t)v * V);
+            if (RES) rr[u][j] = L::load(res + row * p.res_ldc + (int64_t)v * V);
+        }
+    }
+    #pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int64_t row = row0 + u * GR;
+        acc[u] = 0.f;
+        #pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const bool in = j * TPR + lane < nvec;
+            L::unpack(rx[u][j], f[u][j]);
+            if (RES) {
+                float r[V];
+                L::unpack(rr[u][j], r);
+                // what is normalised is the sum as it is stored
+                #pragma unroll
+                for (int i = 0; i < V; i++) f[u][j][i] = Elem<T>::round(f[u][j][i] + r[i]);
+                if (in && row < p.m) L::store(sum + row * p.sum_ldc + (int64_t)(j * TPR + lane) * V, f[u][j]);
+            }
+            if (in)
+                #pragma unroll
+                for (int i = 0; i < V; i++) acc[u] += f[u][j][i];
+        }
+    }
+    const float inv_c = 1.f / (float)p.c;
+    row_sums<TPR, U>(acc, red[0]);
+    float sq[U];
+    #pragma unroll
+    for (int u = 0; u < U; u++) {
+        acc[u] *= inv_c;
+        sq[u] = 0.f;
+        #pragma unroll
+        for (int j = 0; j < NV; j++)
+            if (j * TPR + lane < nvec)
+                #pragma unroll
+                for (int i = 0; i < V; i++) {
+                    f[u][j][i] -= acc[u];
+                    sq[u] += f[u][j][i] * f[u][j][i];
+                }
+    }
+    row_sums<TPR, U>(sq, red[1]);
+    #pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int64_t row = row0 + u * GR;
+        if (row >= p.m) continue;
+        const float rstd = 1.f / sqrtf(sq[u] * inv_c + p.eps);
+        if (lane == 0) {
+            p.mean[row] = acc[u];
+            p.rstd[row] = rstd;
+        }
+        #pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int v = j * TPR + lane;
+            if (v >= nvec) continue;
+            float o[V];
+            #pragma unroll
+            for (int i = 0; i < V; i++) {
+                const float g = p.gamma ? p.gamma[v * V + i] : 1.f, b = p.beta ? p.beta[v * V + i] : 0.f;
+                o[i] = f[u][j][i] * rstd * g + b;
+            }
+            L::store(y + row * p.y_ldc + (int64_t)v * V, o);
+        }
+    }
+}
+
+// Backward: workgroup b takes row sets b, b + grid, ...; each thread keeps the
+// sums of dy and dy xhat of its own channels in registers over all its rows
+// and the workgroup writes one partial row [2][c] at the end (float32 sums of
+// at most m / (grid GR) terms; the combine adds the partial rows in float64 in
+// a fixed order).  The next row set is loaded before the current one reduces.
+template <typename T, int V, int TPR, int NV, int WG, bool RES>
+__global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
+{
+    constexpr int GR = WG / TPR;
+    typedef LnVec<T, V> L;
+    __shared__ float red[2][WG / 64 * 2];
+    __shared__ float cols[GR > 1 ? 2 * WG * V : 1];
+    const int lane = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+    const int nvec = p.c / V;
+    const T *x = (const T *)p.x, *dy = (const T *)p.dy, *dsum = (const T *)p.res;
+    T *dx = (T *)p.y;
+    float gam[NV][V], sb[NV][V], sg[NV][V];
+    int col[NV];
+    #pragma unroll
+    for (int j = 0; j < NV; j++) {
+        const int v = j * TPR + lane;
+        col[j] = v < nvec ? v * V : -1;
+        #pragma unroll
+        for (int i = 0; i < V; i++) {
+            gam[j][i] = p.gamma && v < nvec ? p.gamma[v * V + i] : 1.f;
+            sb[j][i] = 0.f;
+            sg[j][i] = 0.f;
+        }
+    }
+    const float inv_c = 1.f / (float)p.c;
+    const int64_t step = (int64_t)gridDim.x * GR;
+    const int64_t sets = (p.m + step - 1) / step;
+    int64_t row = (int64_t)blockIdx.x * GR + grp;
+    typename L::raw rx[NV], rd[NV], rs[NV];
+    float mean = 0.f, rstd = 0.f;
+    auto load = [&](int64_t r) __attribute__((always_inline)) {
+        if (r >= p.m) r = p.m - 1;                    // read and dropped
+        mean = p.mean[r];
+        rstd = p.rstd[r];
+        #pragma unroll
+        for (int j = 0; j < NV; j++) {
+            const int64_t c = col[j] >= 0 ? col[j] : (nvec - 1) * V;
+            rx[j] = L::load(x + r * p.x_ldc + c);
+            rd[j] = L::load(dy + r * p.dy_ldc + c);
+            if (RES) rs[j] = L::load(dsum + r * p.res_ldc + c);
+        }
+    };
+    load(row);
+    for (int64_t it = 0; it < sets; it++, row += step) {
+        float xh[NV][V], d[NV][V], e[RES ? NV : 1][V], s[2] = {0.f, 0.f};
+        const float rs0 = rstd, mu0 = mean;
+        const bool live = row < p.m;
+        #pragma unroll
+        for (int j = 0; j < NV; j++) {
+            L::unpack(rx[j], xh[j]);
+            L::unpack(rd[j], d[j]);
+            if (RES) L::unpack(rs[j], e[j]);
+        }
+        if (it + 1 < sets) load(row + step);
+        #pragma unroll
+        for (int j = 0; j < NV; j++)
+            if (col[j] >= 0)
+                #pragma unroll
+                for (int i = 0; i < V; i++) {
+                    xh[j][i] = (xh[j][i] - mu0) * rs0;
+                    if (live) {
+                        sb[j][i] += d[j][i];
+                        sg[j][i] += d[j][i] * xh[j][i];
+                    }
+                    d[j][i] *= gam[j][i];
+                    s[0] += d[j][i];
+                    s[1] += d[j][i] * xh[j][i];
+                }
+        row_sums<TPR, 2>(s, red[it & 1]);
+        if (live) {
+            const float a = s[0] * inv_c, b = s[1] * inv_c;
+            #pragma unroll
+            for (int j = 0; j < NV; j++) {
+                if (col[j] < 0) continue;
+                float o[V];
+                #pragma unroll
+                for (int i = 0; i < V; i++) {
+                    o[i] = rs0 * (d[j][i] - a - xh[j][i] * b);
+                    if (RES) o[i] += e[j][i];
+                }
+                L::store(dx + row * p.y_ldc + col[j], o);
+            }
+        }
+    }
+    if (!p.part) return;
+    float *part = p.part + (int64_t)blockIdx.x * 2 * p.c;
+    #pragma unroll
+    for (int j = 0; j < NV; j++) {
+        if constexpr (GR == 1) {
+            if (col[j] >= 0)
+                #pragma unroll
+                for (int i = 0; i < V; i++) {
+                    part[col[j] + i] = sb[j][i];
+                    part[p.c + col[j] + i] = sg[j][i];
+                }
+        } else {
+            // column sums over the row groups, in a fixed order
+            constexpr int CW = TPR * V;
+            if (j) __syncthreads();
+            #pragma unroll
+            for (int i = 0; i < V; i++) {
+                cols[grp * CW + lane * V + i] = sb[j][i];
+                cols[WG * V + grp * CW + lane * V + i] = sg[j][i];
+            }
+            __syncthreads();
+            for (int k = threadIdx.x; k < 2 * CW; k += WG) {
+                const int half = k >= CW, q = k - half * CW, c = j * CW + q;
+                if (c < p.c) {
+                    float t = 0.f;
+                    #pragma unroll
+                    for (int g = 0; g < GR; g++) t += cols[half * WG * V + g * CW + q];
+                    part[half * p.c + c] = t;
+                }
+            }
+        }
+    }
+}
+
+// The row layout of a call: threads per row, loads per thread, and in the
+// backward pass the workgroup.
+struct LnPlan { bool vec; int tpr, nv, wg; };
+
+LnPlan ln_plan(int dtype, int c, bool vec)
+{
+    if (!vec) {
+        if (c <= 256) return {false, 64, 4, 256};
+        if (c <= 2048) return {false, 256, 8, 256};
+        if (c <= 8192) return {false, 1024, 8, 1024};
+        return {false, 1024, 16, 1024};
+    }
+    const int n = c / stats_vec(dtype);
+    if (n <= 8) return {true, 8, 1, 256};
+    if (n <= 16) return {true, 16, 1, 256};
+    if (n <= 32) return {true, 32, 1, 256};
+    if (n <= 64) return {true, 64, 1, 256};
+    if (n <= 128) return {true, 64, 2, 256};
+    if (n <= 256) return {true, 256, 1, 512};
+    if (n <= 512) return {true, 256, 2, 512};
+    if (n <= 1024) return {true, 256, 4, 512};
+    return {true, 1024, n <= 2048 ? 2 : 4, 1024};
+}
+
+template <typename F>
+hipError_t ln_dispatch(const LnPlan &q, int dtype, F &&go)
+{
+    auto with = [&](auto tag, auto v, auto tpr, auto nv, auto wg) { return go(tag, v, tpr, nv, wg); };
+#define LN_I(N) std::integral_constant<int, N>{}
+#define LN_CASE(T, V, TPR, NV, WG) \
+    if (q.tpr == TPR && q.nv == NV) return with((T *)nullptr, LN_I(V), LN_I(TPR), LN_I(NV), LN_I(WG))
+#define LN_VECTORS(T, V) \
+    LN_CASE(T, V, 8, 1, 256);   LN_CASE(T, V, 16, 1, 256);  LN_CASE(T, V, 32, 1, 256);  LN_CASE(T, V, 64, 1, 256); \
+    LN_CASE(T, V, 64, 2, 256);  LN_CASE(T, V, 256, 1, 512); LN_CASE(T, V, 256, 2, 512); LN_CASE(T, V, 256, 4, 512); \
+    LN_CASE(T, V, 1024, 2, 1024)
+#define LN_SCALARS(T) \
+    LN_CASE(T, 1, 64, 4, 256); LN_CASE(T, 1, 256, 8, 256); LN_CASE(T, 1, 1024, 8, 1024); LN_CASE(T, 1, 1024, 16, 1024)
+    if (dtype == DT_BF16) {
+        if (q.vec) { LN_VECTORS(bf16_t, 8); }
+        else { LN_SCALARS(bf16_t); }
+    } else {
+        if (q.vec) { LN_VECTORS(float, 4); LN_CASE(float, 4, 1024, 4, 1024); }
+        else { LN_SCALARS(float); }
+    }
+#undef LN_SCALARS
+#undef LN_VECTORS
+#undef LN_CASE
+#undef LN_I
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+// Partial rows (= workgroups) of the backward: enough workgroups to fill the
+// chip, few enough that writing and adding the partial rows stays small next
+// to the data (c = 4096: 512 rows are 16 MiB).
+int64_t ln_bwd_groups(int dtype, int64_t m, int c, bool vec)
+{
+    const LnPlan q = ln_plan(dtype, c, vec);
+    const int64_t sets = ceil_div(m, q.wg / q.tpr);
+    const int64_t most = q.wg == 256 ? 1024 : (q.wg == 512 ? 512 : 256);
+    return sets < most ? sets : most;
+}
+
+hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s)
+{
+    const LnPlan q = ln_plan(dtype, p.c, vec);
+    const double n = (double)p.m * p.c * (dtype == DT_BF16 ? 2 : 4);
+    TraceScope tr(KC_SWEEP, KID_LAYERNORM, s, (p.res ? 4.0 : 2.0) * n + 8.0 * p.m + 8.0 * p.c, 0.0);
+    return ln_dispatch(q, dtype, [&](auto *tag, auto v, auto tpr, auto nv, auto) {
+        using T = std::remove_pointer_t<decltype(tag)>;
+        constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, V = decltype(v)::value;
+        constexpr int WG = TPR > kThreads ? TPR : kThreads, U = NV == 1 && TPR <= 64 ? 2 : 1;
+        const dim3 grid((unsigned)ceil_div(p.m, WG / TPR * U));
+        if (p.res) hipLaunchKernelGGL((k_ln_fwd<T, V, TPR, NV, U, true>), grid, dim3(WG), 0, s, p);
+        else hipLaunchKernelGGL((k_ln_fwd<T, V, TPR, NV, U, false>), grid, dim3(WG), 0, s, p);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_ln_bwd(int dtype, const LnParams &p, bool vec, hipStream_t s)
+{
+    const LnPlan q = ln_plan(dtype, p.c, vec);
+    const double n = (double)p.m * p.c * (dtype == DT_BF16 ? 2 : 4);
+    const int64_t R = ln_bwd_groups(dtype, p.m, p.c, vec);
+    TraceScope tr(KC_SWEEP, KID_LAYERNORM, s, (p.res ? 4.0 : 3.0) * n + 8.0 * p.m + 4.0 * p.c + 8.0 * R * p.c, 0.0);
+    return ln_dispatch(q, dtype, [&](auto *tag, auto v, auto tpr, auto nv, auto wg) {
+        using T = std::remove_pointer_t<decltype(tag)>;
+        constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, V = decltype(v)::value;
+        constexpr int WG = decltype(wg)::value;
+        if (p.res) hipLaunchKernelGGL((k_ln_bwd<T, V, TPR, NV, WG, true>), dim3((unsigned)R), dim3(WG), 0, s, p);
+        else hipLaunchKernelGGL((k_ln_bwd<T, V, TPR, NV, WG, false>), dim3((unsigned)R), dim3(WG), 0, s, p);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace bnr

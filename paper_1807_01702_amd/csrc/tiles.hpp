@@ -217,4 +217,7 @@ inline WgTrPlan wgrad_f32_plan(int64_t m, int n, int h, int w, int c_in, int c_o
     return p;
 }
 
+// ---- layer normalisation ---------------------------------------------------
+constexpr int kLnMaxC = 16384;             // 16 channels a thread of a 1024-thread workgroup
+
 }  // namespace bnr

@@ -1,0 +1,364 @@
+"""Layer normalisation (bnr_layernorm_fwd / bnr_layernorm_bwd) against its
+definition in float64.
+
+Tolerances are element-wise and counted in float32 half steps u = 2^-24 (and one
+half step of the storage type for a stored result).  A row sum adds at most 16
+terms per thread and then at most 10 levels of a tree, so it is off by at most
+K u times the sum of its terms' magnitudes, K = 32 with room for the terms' own
+roundings.  From there:
+  mean   K u mean|s|
+  rstd   relative: half the variance's relative error (K + 4) u, the mean's error
+         entering squared, and 4 u for the square root, the quotient and the product
+  y      |gamma| rstd (mean's error + |s - mean| (K + 8) u) + 4 u (|y| + |beta|)
+  dx     rstd (K + 8) u (|g| + mean|g| + |xhat| mean|g xhat|) + 4 u (|dx| + |dsum|)
+  dgamma (n + K) u sum|dy xhat| for n rows added one after another by a thread
+"""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U, K = 2.0 ** -24, 32
+EPS = 1e-5
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+
+
+def _B():
+    from paper_1807_01702_amd import bnr
+    return bnr
+
+
+def _rand(seed, *shape, std=1.0, mean=0.0):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g, dtype=torch.float64) * std + mean
+
+
+def _view(t, dtype, pad=0, shift=0):
+    """t [m, c] on the GPU as rows of a wider buffer (stride c + pad), its first element `shift` past a 16-byte
+    boundary; the rest of the buffer holds a marker."""
+    m, c = t.shape
+    buf = torch.full((m * (c + pad) + shift + 8,), 777.0, dtype=dtype, device="cuda")
+    v = buf[shift:shift + m * (c + pad)].view(m, c + pad)[:, :c]
+    v.copy_(t.to(dtype))
+    return buf, v
+
+
+def _untouched(buf, v, pad, shift):
+    m, c = v.shape
+    rest = buf.clone()
+    rest[shift:shift + m * (c + pad)].view(m, c + pad)[:, :c] = 777.0
+    assert bool((rest == 777.0).all()), "wrote outside the view"
+
+
+def _d(t):
+    return t.detach().double().cpu()
+
+
+def _check(name, got, ref, tol):
+    got = _d(got)
+    bad = ~((got - ref).abs() <= tol)
+    assert not bool(bad.any()), "%s: %d values off, worst %.3g of the tolerance" % (
+        name, int(bad.sum()), float(((got - ref).abs() / tol.clamp_min(1e-300)).max()))
+
+
+def _fwd_reference(s, gamma, beta):
+    c = s.shape[1]
+    mean = s.sum(1, keepdim=True) / c
+    d = s - mean
+    var = (d * d).sum(1, keepdim=True) / c
+    rstd = 1.0 / torch.sqrt(var + EPS)
+    g = torch.ones(c, dtype=torch.float64) if gamma is None else _d(gamma)
+    b = torch.zeros(c, dtype=torch.float64) if beta is None else _d(beta)
+    y = g * d * rstd + b
+    dm = K * U * s.abs().sum(1, keepdim=True) / c
+    rel = 0.5 * ((K + 4) * U + dm * dm * rstd * rstd) + 4 * U
+    return mean[:, 0], dm[:, 0] + 1e-300, rstd[:, 0], (rel * rstd)[:, 0], y, \
+        g.abs() * rstd * (dm + d.abs() * (rel + 4 * U)) + 4 * U * (y.abs() + b.abs()) + 1e-300
+
+
+def _run_fwd(x, gamma, beta, dtype, res=None, pad=0, shift=0, inplace=False):
+    B = _B()
+    m, c = x.shape
+    bx, vx = _view(x, dtype, pad, shift)
+    by, vy = _view(torch.zeros(m, c), dtype, pad, shift)
+    if inplace:
+        by, vy = bx, vx
+    ln = B.LN(gamma, beta, m, EPS, device="cuda")
+    vr = vs = None
+    xin = vx.clone()
+    if res is not None:
+        br, vr = _view(res, dtype, pad, shift)
+        bs, vs = _view(torch.zeros(m, c), dtype, pad, shift)
+    B.bnr_layernorm_fwd(vx, ln, vy, res=vr, sum=vs)
+    torch.cuda.synchronize()
+    _untouched(by, vy, pad, shift)
+    s = _d(xin)
+    if res is not None:
+        _untouched(bs, vs, pad, shift)
+        exact = s + _d(vr)
+        _check("sum", vs, exact, (HALF[dtype] * (1 + U) + U) * exact.abs() + 1e-300)
+        s = _d(vs)
+    mean, tm, rstd, tr, y, ty = _fwd_reference(s, gamma, beta)
+    _check("mean", ln.mean, mean, tm)
+    _check("rstd", ln.rstd, rstd, tr)
+    _check("y", vy, y, ty + HALF[dtype] * (y.abs() + ty))
+    return ln, vy
+
+
+# m, c: one row, one channel, every row layout and the widths around its ends, odd sizes, the widest row
+SIZES = [(1, 1), (5, 1), (1, 8), (3, 7), (130, 8), (67, 64), (9, 72), (33, 128), (64, 200), (31, 256), (17, 257),
+         (300, 264), (7, 512), (5, 1001), (9, 1024), (3, 1032), (4, 2048), (3, 2049), (5, 2056), (2, 4096), (3, 4104),
+         (2, 8192), (3, 8193), (2, 12000), (2, 16384), (1000, 96)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,c", SIZES)
+def test_forward_sizes(m, c, dtype):
+    x = _rand(c * 7 + m, m, c, mean=0.3)
+    gamma, beta = _rand(1, c, mean=1.0, std=0.3).float().cuda(), _rand(2, c).float().cuda()
+    _run_fwd(x, gamma, beta, dtype)
+    _run_fwd(x, gamma, beta, dtype, res=_rand(3, m, c, std=2.0))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (5, 0), (0, 1), (64, 8), (3, 7)])
+def test_forward_strides_and_alignment(pad, shift, dtype):
+    for m, c in ((9, 40), (5, 328), (3, 1032), (2, 4360), (2, 9000)):
+        gamma, beta = _rand(4, c).float().cuda(), _rand(5, c).float().cuda()
+        _run_fwd(_rand(6, m, c), gamma, beta, dtype, res=_rand(7, m, c), pad=pad, shift=shift)
+        _run_fwd(_rand(8, m, c), gamma, beta, dtype, pad=pad, shift=shift, inplace=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_forward_without_affine_parameters(dtype):
+    for m, c in ((4, 96), (3, 1001), (2, 5000)):
+        x, gamma, beta = _rand(9, m, c), _rand(10, c).float().cuda(), _rand(11, c).float().cuda()
+        _run_fwd(x, None, None, dtype)
+        _run_fwd(x, gamma, None, dtype)
+        _run_fwd(x, None, beta, dtype)
+
+
+def test_forward_offsets_and_flat_rows():
+    """A mean far from zero (float32, 10^4 standard deviations), rows of one repeated value, all zeros."""
+    c = 1536
+    x = _rand(12, 6, c) + 1e4
+    x[2] = 3.7
+    x[3] = 0.0
+    x[4] = -1e30
+    beta = _rand(13, c).float().cuda()
+    ln, y = _run_fwd(x[:4], None, beta, torch.float32)
+    assert bool((y[3] == beta).all()), "a row of zeros gives beta"
+    ln, y = _run_fwd(x[4:5] * 0 + 2.0, None, beta, torch.bfloat16)
+    assert bool((y[0] == beta.bfloat16()).all())
+
+
+@pytest.mark.parametrize("m,c", [(6, 48), (5, 1001), (4, 1024), (3, 9000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_non_finite_values_stay_in_their_row(m, c, dtype):
+    B = _B()
+    x = _rand(14, m, c).to(dtype).cuda()
+    clean = torch.empty_like(x)
+    ln = B.LN(None, None, m, EPS, device="cuda")
+    B.bnr_layernorm_fwd(x, ln, clean)
+    bad = x.clone()
+    bad[1, c // 2] = float("nan")
+    bad[2, 0] = float("inf")
+    y = torch.empty_like(x)
+    B.bnr_layernorm_fwd(bad, ln, y)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(y[1]).all()) and bool(torch.isnan(y[2]).all())
+    keep = [r for r in range(m) if r not in (1, 2)]
+    assert torch.equal(y[keep], clean[keep])
+
+
+def _run_bwd(m, c, dtype, gamma, res, pad=0, shift=0, alias=None, want=(True, True), seed=20):
+    B = _B()
+    x, dy = _rand(seed, m, c, mean=0.5), _rand(seed + 1, m, c)
+    bx, vx = _view(x, dtype, pad, shift)
+    bd, vd = _view(dy, dtype, pad, shift)
+    vr = _view(_rand(seed + 2, m, c), dtype, pad, shift)[1] if res else None
+    bo, vo = _view(torch.zeros(m, c), dtype, pad, shift)
+    s = _d(vx)
+    mean = s.mean(1)
+    rstd = 1.0 / torch.sqrt(((s - mean[:, None]) ** 2).mean(1) + EPS)
+    ln = B.LN(gamma, None, m, EPS, mean=mean.float().cuda(), rstd=rstd.float().cuda())
+    d, e = _d(vd), _d(vr) if res else torch.zeros(m, c, dtype=torch.float64)
+    if alias == "dy":
+        bo, vo = bd, vd
+    elif alias == "x":
+        bo, vo = bx, vx
+    elif alias == "dsum":
+        vo = vr
+        bo = None
+    dgamma = torch.full((c,), 5.0, device="cuda") if want[0] else None
+    dbeta = torch.full((c,), 5.0, device="cuda") if want[1] else None
+    B.bnr_layernorm_bwd(vd, vx, ln, vo, dgamma, dbeta, dsum=vr)
+    torch.cuda.synchronize()
+    if bo is not None:
+        _untouched(bo, vo, pad, shift)
+    mean, rstd = _d(ln.mean)[:, None], _d(ln.rstd)[:, None]        # the statistics the call was given
+    xhat = (s - mean) * rstd
+    g = d * (torch.ones(c, dtype=torch.float64) if gamma is None else _d(gamma))
+    dx = rstd * (g - g.mean(1, keepdim=True) - xhat * (g * xhat).mean(1, keepdim=True)) + e
+    tol = rstd * (K + 8) * U * (g.abs() + g.abs().mean(1, keepdim=True) + xhat.abs() * (g * xhat).abs().mean(1, keepdim=True))
+    tol = tol + 4 * U * (dx.abs() + e.abs()) + 1e-300
+    _check("dx", vo, dx, tol + HALF[dtype] * (dx.abs() + tol))
+    n = m // 256 + 33                                # rows a thread adds, and the row groups of a workgroup
+    if want[0]:
+        _check("dgamma", dgamma, (d * xhat).sum(0), (n + K) * U * (d * xhat).abs().sum(0) + 1e-300)
+    if want[1]:
+        _check("dbeta", dbeta, d.sum(0), (n + K) * U * d.abs().sum(0) + 1e-300)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,c", SIZES + [(5000, 40), (3000, 256), (1500, 1024), (700, 4096), (600, 333)])
+def test_backward_sizes(m, c, dtype):
+    gamma = _rand(30, c, mean=1.0, std=0.3).float().cuda()
+    _run_bwd(m, c, dtype, gamma, res=False)
+    _run_bwd(m, c, dtype, gamma, res=True, seed=40)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (5, 0), (0, 1), (64, 8), (3, 7)])
+def test_backward_strides_alignment_and_aliases(pad, shift, dtype):
+    for m, c in ((9, 40), (5, 328), (3, 1032), (2, 4360), (2, 9000)):
+        gamma = _rand(31, c).float().cuda()
+        _run_bwd(m, c, dtype, gamma, True, pad, shift)
+        for alias in ("dy", "x", "dsum"):
+            _run_bwd(m, c, dtype, gamma, True, pad, shift, alias=alias)
+
+
+@pytest.mark.parametrize("want", [(True, False), (False, True), (False, False)])
+def test_backward_optional_outputs(want):
+    for m, c in ((40, 96), (300, 1001), (33, 2048)):
+        _run_bwd(m, c, torch.float32, None, False, want=want)
+        _run_bwd(m, c, torch.bfloat16, None, True, want=want)
+
+
+def test_backward_against_differences():
+    """<dx, v> and <dgamma, w> against central differences of L = sum(y dy) of the forward kernel.  The step's own
+    truncation is taken from the same difference of the float64 definition; what is left is the forward's rounding
+    over the step."""
+    B = _B()
+    m, c, h = 4, 48, 2.0 ** -6
+    x, dy, v = (_rand(50 + i, m, c).float().cuda() for i in range(3))
+    gamma, beta, w = (_rand(60 + i, c).float().cuda() for i in range(3))
+
+    def loss(xx, gg):
+        y = torch.empty_like(xx)
+        B.bnr_layernorm_fwd(xx, B.LN(gg, beta, m, EPS), y)
+        ref = _fwd_reference(_d(xx), gg, beta)
+        return float((_d(y) * _d(dy)).sum()), float((ref[4] * _d(dy)).sum()), float((ref[5] * _d(dy).abs()).sum())
+
+    ln = B.LN(gamma, beta, m, EPS)
+    y, dx, dg, db = torch.empty_like(x), torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)
+    B.bnr_layernorm_fwd(x, ln, y)
+    B.bnr_layernorm_bwd(dy, x, ln, dx, dg, db)
+    xd, g = _d(x), _d(dy) * _d(gamma)
+    _, _, rstd, _, _, _ = _fwd_reference(xd, gamma, beta)
+    xhat = (xd - xd.mean(1, keepdim=True)) * rstd[:, None]
+    dx64 = rstd[:, None] * (g - g.mean(1, keepdim=True) - xhat * (g * xhat).mean(1, keepdim=True))
+    dg64 = (_d(dy) * xhat).sum(0)
+    for name, moved, along, got, ref in (
+            ("x", lambda t: (x + t * v, gamma), v, dx, dx64), ("gamma", lambda t: (x, gamma + t * w), w, dg, dg64)):
+        hi, lo = loss(*moved(h)), loss(*moved(-h))
+        fd, fd64, noise = (hi[0] - lo[0]) / (2 * h), (hi[1] - lo[1]) / (2 * h), (hi[2] + lo[2]) / (2 * h)
+        dot, dot64 = float((_d(got) * _d(along)).sum()), float((ref * _d(along)).sum())
+        slack = (2 * K) * U * float((ref.abs() * _d(along).abs()).sum()) * 4
+        assert abs(fd - dot) <= abs(fd64 - dot64) + noise + slack, (name, fd, dot, fd64, dot64, noise)
+
+
+def test_offsets_past_32_bits():
+    """Rows 2^30 elements apart: the third starts past 2^31 elements."""
+    B = _B()
+    ld, c = (1 << 30) + 8, 40
+    buf = torch.empty(2 * ld + c, dtype=torch.bfloat16, device="cuda")
+    rows = torch.as_strided(buf, (3, c), (ld, 1))
+    x = _rand(70, 3, c)
+    rows.copy_(x.bfloat16())
+    gamma, beta = _rand(71, c).float().cuda(), _rand(72, c).float().cuda()
+    ln, y = B.LN(gamma, beta, 3, EPS), torch.empty(3, c, dtype=torch.bfloat16, device="cuda")
+    B.bnr_layernorm_fwd(rows, ln, y)
+    near = torch.empty_like(y)
+    ln2 = B.LN(gamma, beta, 3, EPS)
+    B.bnr_layernorm_fwd(rows.contiguous(), ln2, near)
+    assert torch.equal(y, near) and torch.equal(ln.mean, ln2.mean)
+    dx, dg, db = torch.empty_like(y), torch.empty_like(gamma), torch.empty_like(gamma)
+    near_dx, dg2, db2 = torch.empty_like(y), torch.empty_like(gamma), torch.empty_like(gamma)
+    dy = _rand(73, 3, c).bfloat16().cuda()
+    B.bnr_layernorm_bwd(dy, rows.contiguous(), ln, near_dx, dg2, db2)
+    B.bnr_layernorm_bwd(dy, rows, ln, rows, dg, db)                 # dx over x, in the far rows
+    assert torch.equal(rows, near_dx) and torch.equal(dg, dg2) and torch.equal(db, db2)
+
+
+def test_slices_of_one_buffer():
+    """x and y as different channel slices of one buffer, as in a concatenation."""
+    B = _B()
+    buf = torch.randn(50, 96, device="cuda")
+    x, y = buf[:, :40], buf[:, 40:80]
+    ref = torch.empty(50, 40, device="cuda")
+    ln = B.LN(None, None, 50, EPS, device="cuda")
+    B.bnr_layernorm_fwd(x.contiguous(), ln, ref)
+    B.bnr_layernorm_fwd(x, ln, y)
+    assert torch.equal(y, ref)
+
+
+@pytest.mark.parametrize("m,c,dtype", [(3000, 256, torch.bfloat16), (700, 4096, torch.bfloat16), (90, 1001, torch.float32)])
+def test_repeats_streams_and_graphs(m, c, dtype):
+    """The same call gives the same bits: again, on another stream with both streams at work, and replayed from two
+    graphs that were captured one after another."""
+    B = _B()
+    x, dy = _rand(80, m, c).to(dtype).cuda(), _rand(81, m, c).to(dtype).cuda()
+    gamma, beta = _rand(82, c).float().cuda(), _rand(83, c).float().cuda()
+
+    def outs():
+        return dict(ln=B.LN(gamma, beta, m, EPS), y=torch.empty_like(x), dx=torch.empty_like(x),
+                    dg=torch.empty_like(gamma), db=torch.empty_like(beta))
+
+    def step(o, xx=x):
+        B.bnr_layernorm_fwd(xx, o["ln"], o["y"])
+        B.bnr_layernorm_bwd(dy, xx, o["ln"], o["dx"], o["dg"], o["db"])
+
+    def same(a, b):
+        return all(torch.equal(a[k], b[k]) for k in ("y", "dx", "dg", "db"))
+
+    ref, again, a, b = outs(), outs(), outs(), outs()
+    step(ref)
+    step(again)
+    torch.cuda.synchronize()
+    assert same(ref, again)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        with torch.cuda.stream(s1):
+            step(a)
+        with torch.cuda.stream(s2):
+            step(b)
+    torch.cuda.synchronize()
+    assert same(ref, a) and same(ref, b)
+    graphs = []
+    for o in (a, b):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(o)
+        graphs.append(g)
+    for _ in range(3):
+        for o, g in zip((a, b), graphs):
+            for k in ("y", "dx", "dg", "db"):
+                o[k].fill_(float("nan"))
+            g.replay()
+        step(again)
+        torch.cuda.synchronize()
+        assert same(ref, a) and same(ref, b) and same(ref, again)
+
+
+def test_numpy_cross_check():
+    """One small case written out with numpy, apart from the reference above."""
+    B = _B()
+    x = np.array([[1.0, 2.0, 4.0, 9.0]], np.float32)
+    y = torch.empty(1, 4, device="cuda")
+    ln = B.LN(torch.tensor([1.0, 2.0, 3.0, 4.0], device="cuda"), torch.tensor([0.5, 0, 0, -1], device="cuda"), 1, EPS)
+    B.bnr_layernorm_fwd(torch.from_numpy(x).cuda(), ln, y)
+    # mean 4, squared differences 9 + 4 + 0 + 25 = 38, variance 9.5
+    r = 1 / np.sqrt(9.5 + EPS)
+    np.testing.assert_allclose(y.cpu().numpy()[0], [-3 * r + 0.5, -4 * r, 0.0, 20 * r - 1], rtol=1e-6, atol=1e-6)
