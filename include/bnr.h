@@ -602,7 +602,8 @@ bnr_status bnr_reference_bn_relu(int32_t backward, int64_t m, int32_t c, bnr_dty
  *   y = gamma * (s - mean) * rstd + beta.
  * Rows are views [m][c] with a row stride in elements.  These calls take any
  * c up to 16384, any stride >= c and element-aligned pointers (16-byte aligned
- * views whose c and strides are multiples of the 16-byte vector are faster);
+ * views and parameters whose c and strides are multiples of the 16-byte vector
+ * are faster);
  * different channel slices of one buffer do not overlap each other.  A row of
  * one repeated value has rstd = 1/sqrt(eps) and y = beta; an infinity or NaN
  * makes its own row NaN and no other. */
@@ -639,6 +640,76 @@ size_t bnr_layernorm_workspace_size(int64_t m, int32_t c, bnr_dtype dtype);
 bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy, int32_t dy_ldc, const void *x,
                              int32_t x_ldc, const bnr_ln *ln, const void *dsum, int32_t dsum_ldc, void *dx,
                              int32_t dx_ldc, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
+/* --------------------------------------- orthogonalised weight updates ---- */
+
+/* Newton-Schulz orthogonalisation of a matrix U [rows][cols]:
+ *   X = U / (||U||_F + eps);  `steps` times  X <- a X + b (X X^T) X + c (X X^T)^2 X
+ * (X^T X in the place of X X^T's side where rows > cols: the products run on the
+ * shorter side, the result is the same).  Every singular value s of X becomes
+ * s (a + b s^2 + c s^4) per step, its singular vectors stay; with the usual
+ * coefficients five steps bring all but the smallest near 1.
+ * The calls take a list of matrices of any shapes, up to 1024, each with its
+ * shorter side up to 16384 and its longer one up to 2^20, and run every stage of
+ * all of them in one launch.  Sums and products carry float32 accuracy (absolute
+ * accuracy 2^-37 of the norm for entries far below it).  Coefficients that could
+ * take a singular value of some X to 3.5 or a + b s^2 + c s^4 to 15 are refused
+ * (BNR_ERR_UNSUPPORTED).  A zero matrix gives zeros; an infinity or NaN makes its
+ * own matrix NaN and no other.  Row strides are in elements; pointers are
+ * element-aligned. */
+typedef struct {
+    int32_t steps;         /* 1..32 (usually 5)                                    */
+    float a, b, c;         /* usually 3.4445, -4.7750, 2.0315                      */
+    float eps;             /* >= 0; with 0 a zero matrix gives NaN                 */
+} bnr_ns_params;
+
+typedef struct {
+    int32_t rows, cols;
+    const void *x;         /* [rows][cols] (x_dtype)                               */
+    int32_t x_ld;
+    void *out;             /* [rows][cols] (out_dtype); may overlap any x          */
+    int32_t out_ld;
+} bnr_ortho_item;
+
+/* out = the orthogonalised x, for every matrix of the list.  The outs must not
+ * overlap each other (BNR_ERR_ALIAS).  An empty list is nothing to do. */
+size_t bnr_orthogonalize_workspace_size(const bnr_ortho_item *items, int32_t count);
+bnr_status bnr_orthogonalize(const bnr_ortho_item *items, int32_t count, bnr_dtype x_dtype, bnr_dtype out_dtype,
+                             const bnr_ns_params *ns, void *ws, size_t ws_bytes, void *stream);
+
+typedef struct {
+    int32_t rows, cols;    /* e.g. k k c_in and c_out of a CONV filter             */
+    void *w;               /* weights (w_dtype), updated                           */
+    int32_t w_ld;
+    const void *g;         /* gradient (g_dtype)                                   */
+    int32_t g_ld;
+    float *buf;            /* momentum, updated                                    */
+    int32_t buf_ld;
+    void *copy;            /* bf16 copy of the new weights, or NULL                */
+    int32_t copy_ld;
+    float scale;           /* factor of this matrix's step                         */
+} bnr_muon_item;
+
+typedef struct {
+    float lr;
+    const float *lr_dev;   /* device value in the place of lr, read when the call  */
+                           /* runs (a captured call follows it), or NULL           */
+    float momentum;        /* in [0, 1)                                            */
+    int32_t nesterov;
+    float weight_decay;    /* decoupled                                            */
+    bnr_ns_params ns;
+} bnr_muon_params;
+
+/* One optimizer step for every matrix of the list:
+ *   buf <- momentum buf + g
+ *   O   =  orthogonalised u, u = g + momentum buf (nesterov) or buf
+ *   w   <- w (1 - lr weight_decay) - lr scale O    (rounded once to w_dtype)
+ * and the bf16 copy of w where asked for (float32 weights for the update, bf16
+ * ones for the CONVs).  Weights, momentum and copies must not overlap each
+ * other, any gradient or lr_dev (BNR_ERR_ALIAS). */
+size_t bnr_muon_workspace_size(const bnr_muon_item *items, int32_t count);
+bnr_status bnr_muon_update(const bnr_muon_item *items, int32_t count, bnr_dtype w_dtype, bnr_dtype g_dtype,
+                           const bnr_muon_params *p, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------ diagnostics ---- */
 

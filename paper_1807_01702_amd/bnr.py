@@ -67,6 +67,24 @@ class LNStruct(ctypes.Structure):
     _fields_ = [("gamma", c_vp), ("beta", c_vp), ("mean", c_vp), ("rstd", c_vp), ("eps", c_f)]
 
 
+class NSParams(ctypes.Structure):
+    _fields_ = [("steps", c_i32), ("a", c_f), ("b", c_f), ("c", c_f), ("eps", c_f)]
+
+
+class OrthoItem(ctypes.Structure):
+    _fields_ = [("rows", c_i32), ("cols", c_i32), ("x", c_vp), ("x_ld", c_i32), ("out", c_vp), ("out_ld", c_i32)]
+
+
+class MuonItem(ctypes.Structure):
+    _fields_ = [("rows", c_i32), ("cols", c_i32), ("w", c_vp), ("w_ld", c_i32), ("g", c_vp), ("g_ld", c_i32),
+                ("buf", c_vp), ("buf_ld", c_i32), ("copy", c_vp), ("copy_ld", c_i32), ("scale", c_f)]
+
+
+class MuonParams(ctypes.Structure):
+    _fields_ = [("lr", c_f), ("lr_dev", c_vp), ("momentum", c_f), ("nesterov", c_i32), ("weight_decay", c_f),
+                ("ns", NSParams)]
+
+
 class AddReluRefArgs(ctypes.Structure):
     _fields_ = [("y", c_vp), ("y_ldc", c_i32), ("bn", ctypes.POINTER(BNStruct)), ("id", c_vp), ("id_ldc", c_i32),
                 ("out", c_vp), ("out_ldc", c_i32), ("tmp", c_vp), ("g", c_vp), ("g_ldc", c_i32), ("gm", c_vp),
@@ -152,6 +170,12 @@ _lib_fns = dict(
     bnr_layernorm_workspace_size=_sig("bnr_layernorm_workspace_size", c_sz, c_i64, c_i32, ctypes.c_int),
     bnr_layernorm_bwd=_sig("bnr_layernorm_bwd", ctypes.c_int, c_i64, c_i32, ctypes.c_int, c_vp, c_i32, c_vp, c_i32,
                            _P(LNStruct), c_vp, c_i32, c_vp, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp),
+    bnr_orthogonalize_workspace_size=_sig("bnr_orthogonalize_workspace_size", c_sz, _P(OrthoItem), c_i32),
+    bnr_orthogonalize=_sig("bnr_orthogonalize", ctypes.c_int, _P(OrthoItem), c_i32, ctypes.c_int, ctypes.c_int,
+                           _P(NSParams), c_vp, c_sz, c_vp),
+    bnr_muon_workspace_size=_sig("bnr_muon_workspace_size", c_sz, _P(MuonItem), c_i32),
+    bnr_muon_update=_sig("bnr_muon_update", ctypes.c_int, _P(MuonItem), c_i32, ctypes.c_int, ctypes.c_int,
+                         _P(MuonParams), c_vp, c_sz, c_vp),
     bnr_trace_begin=_sig("bnr_trace_begin", ctypes.c_int, c_i32, c_i32),
     bnr_trace_end=_sig("bnr_trace_end", c_i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double),
                        ctypes.POINTER(ctypes.c_double), ctypes.POINTER(c_i32), c_i32),
@@ -756,3 +780,81 @@ def bnr_layernorm_bwd(dy, x, ln, dx, dgamma=None, dbeta=None, dsum=None):
         ws = _scratch(nbytes, x.device) if nbytes else None
         _check(_lib_fns["bnr_layernorm_bwd"](m, c, code, pd, ldd, px, ldx if m > 1 else c, ctypes.byref(s), pr, ldr,
                                              po, ldo, pg, pb, _ptr(ws), nbytes, stream))
+
+
+NS_COEF = (3.4445, -4.7750, 2.0315)
+
+
+def _matrix(t, shape, dtype, name):
+    """(data pointer, row stride) of a tensor whose leading dimensions collapse to rows (a CONV filter
+    [k, k, c_in, c_out] is the matrix [k k c_in, c_out])."""
+    p, r, c, ld = view(t)
+    if (r, c) != shape or t.dtype != dtype:
+        raise ValueError("%s: [%d, %d] of %s is wanted, got [%d, %d] of %s" % (name, *shape, dtype, r, c, t.dtype))
+    return p, ld if r > 1 else c
+
+
+def bnr_orthogonalize(xs, outs, steps=5, coef=NS_COEF, eps=1e-7):
+    """Orthogonalises every matrix of xs (a tensor or a list; leading dimensions collapse to rows) into outs."""
+    xs, outs = ([xs], [outs]) if isinstance(xs, torch.Tensor) else (list(xs), list(outs))
+    if len(xs) != len(outs):
+        raise ValueError("%d matrices and %d outputs" % (len(xs), len(outs)))
+    if not xs:
+        return
+    items = (OrthoItem * len(xs))()
+    for it, x, o in zip(items, xs, outs):
+        _, it.rows, it.cols, _ = view(x)
+        it.x, it.x_ld = _matrix(x, (it.rows, it.cols), xs[0].dtype, "matrix")
+        it.out, it.out_ld = _matrix(o, (it.rows, it.cols), outs[0].dtype, "output")
+    ns = NSParams(steps, *coef, eps)
+    with _on_device(*xs, *outs) as stream:
+        nbytes = _lib_fns["bnr_orthogonalize_workspace_size"](items, len(xs))
+        ws = _scratch(nbytes, xs[0].device)
+        _check(_lib_fns["bnr_orthogonalize"](items, len(xs), dtype_code(xs[0]), dtype_code(outs[0]), ctypes.byref(ns),
+                                             _ptr(ws), nbytes, stream))
+
+
+class MuonGroup:
+    """The weight matrices that one bnr_muon_update call updates, with their gradients, momentum buffers (float32),
+    and optionally bf16 copies and step factors (default: sqrt(max(1, outputs / inputs)) for [inputs, outputs]).
+    Leading dimensions collapse to rows.  The group holds the tensors; their values are read at every update."""
+
+    def __init__(self, weights, grads, bufs, copies=None, scales=None):
+        self.tensors = (list(weights), list(grads), list(bufs), list(copies) if copies is not None else None)
+        ws, gs, bs, cs = self.tensors
+        n = len(ws)
+        if not (len(gs) == len(bs) == n and (cs is None or len(cs) == n) and (scales is None or len(scales) == n)):
+            raise ValueError("one gradient, momentum buffer (copy, scale) for each weight matrix")
+        self.count, self.items = n, (MuonItem * max(n, 1))()
+        for i, it in enumerate(self.items[:n]):
+            _, r, c, _ = view(ws[i])
+            it.rows, it.cols = r, c
+            it.w, it.w_ld = _matrix(ws[i], (r, c), ws[0].dtype, "weight")
+            it.g, it.g_ld = _matrix(gs[i], (r, c), gs[0].dtype, "gradient")
+            it.buf, it.buf_ld = _matrix(bs[i], (r, c), torch.float32, "momentum")
+            if cs is not None:
+                it.copy, it.copy_ld = _matrix(cs[i], (r, c), torch.bfloat16, "copy")
+            it.scale = max(1.0, c / r) ** 0.5 if scales is None else scales[i]
+        if n:
+            self.w_code, self.g_code = dtype_code(ws[0]), dtype_code(gs[0])
+            self.on = _on_device(*(t for part in self.tensors if part is not None for t in part))
+            self.ws_bytes = _lib_fns["bnr_muon_workspace_size"](self.items, n)
+
+
+def bnr_muon_update(group, lr, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, coef=NS_COEF, eps=1e-7):
+    """One optimizer step of a MuonGroup.  lr: a number, or a float32 tensor of one value on the group's device that
+    is read when the step runs (a captured step follows it)."""
+    if not group.count:
+        return
+    p = MuonParams(0.0, None, momentum, 1 if nesterov else 0, weight_decay, NSParams(steps, *coef, eps))
+    device = group.tensors[0][0].device
+    if isinstance(lr, torch.Tensor):
+        if lr.device != device:
+            raise ValueError("lr on %s, weights on %s" % (lr.device, device))
+        p.lr_dev = _f32_array(lr, 1, "lr")
+    else:
+        p.lr = lr
+    with group.on as stream:
+        ws = _scratch(group.ws_bytes, device)
+        _check(_lib_fns["bnr_muon_update"](group.items, group.count, group.w_code, group.g_code, ctypes.byref(p),
+                                           _ptr(ws), group.ws_bytes, stream))

@@ -6,6 +6,7 @@
 // on any error it returns without launching anything.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cstdarg>
 #include <cstdio>
@@ -1656,6 +1657,8 @@ static bnr_status check_ln_view(const void *p, int32_t ldc, int32_t c, bnr_dtype
     return BNR_OK;
 }
 
+// per-channel parameters that a row of vectors reads as vectors
+static bool ln_vec(const float *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 static bool ln_vec(const void *p, int32_t ldc, bnr_dtype dtype)
 {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ldc % vec_of(dtype) == 0;
@@ -1708,7 +1711,8 @@ bnr_status bnr_layernorm_fwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
     TRY(check_ln_view(y, y_ldc, c, dtype, "y"));
     if ((res != nullptr) != (sum != nullptr)) return fail(BNR_ERR_NULL, "res and sum go together");
     const int es = esize(dtype);
-    bool vec = c % vec_of(dtype) == 0 && ln_vec(x, x_ldc, dtype) && ln_vec(y, y_ldc, dtype);
+    bool vec = c % vec_of(dtype) == 0 && ln_vec(x, x_ldc, dtype) && ln_vec(y, y_ldc, dtype) &&
+               ln_vec(ln->gamma) && ln_vec(ln->beta);
     if (res) {
         TRY(check_ln_view(res, res_ldc, c, dtype, "res"));
         TRY(check_ln_view(sum, sum_ldc, c, dtype, "sum"));
@@ -1770,7 +1774,7 @@ bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
     TRY(check_ln_view(dx, dx_ldc, c, dtype, "dx"));
     const int es = esize(dtype);
     bool vec = c % vec_of(dtype) == 0 && ln_vec(dy, dy_ldc, dtype) && ln_vec(x, x_ldc, dtype) &&
-               ln_vec(dx, dx_ldc, dtype);
+               ln_vec(dx, dx_ldc, dtype) && ln_vec(ln->gamma);
     if (dsum) {
         TRY(check_ln_view(dsum, dsum_ldc, c, dtype, "dsum"));
         vec = vec && ln_vec(dsum, dsum_ldc, dtype);
@@ -1814,6 +1818,214 @@ bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
                                       nullptr, nullptr, dbeta ? dbeta : unused, dgamma ? dgamma : unused, red, st),
                 "backward sums combine");
     }
+    return ok();
+}
+
+}  // extern "C"
+
+// ------------------------------------------ orthogonalised weight updates ----
+static bnr_status check_ns_matrix(int i, int32_t rows, int32_t cols)
+{
+    if (rows <= 0 || cols <= 0) return fail(BNR_ERR_SHAPE, "matrix %d: %d x %d", i, rows, cols);
+    const int32_t lo = rows < cols ? rows : cols, hi = rows < cols ? cols : rows;
+    if (lo > kNsMaxShort || hi > kNsMaxLong)
+        return fail(BNR_ERR_UNSUPPORTED, "matrix %d: %d x %d exceeds %d x %d", i, rows, cols, kNsMaxShort, kNsMaxLong);
+    return BNR_OK;
+}
+
+static bnr_status check_ns_view(int i, const char *name, const void *p, int32_t ld, int32_t cols, int es)
+{
+    if (!p) return fail(BNR_ERR_NULL, "matrix %d: %s is NULL", i, name);
+    if (reinterpret_cast<uintptr_t>(p) % es) return fail(BNR_ERR_ALIGN, "matrix %d: %s is not element-aligned", i, name);
+    if (ld < cols) return fail(BNR_ERR_SHAPE, "matrix %d: %s stride %d < %d columns", i, name, ld, cols);
+    return BNR_OK;
+}
+
+// The iteration maps a singular value s of X to s q(s), q = a + b s^2 + c s^4,
+// from [0, 1] on (||X||_F <= 1).  X, X X^T and q(X X^T) are held with a range of
+// 16: the largest s of any step must stay below 3.5 (12.25 for its square) and
+// |q| below 15, sampled finely with room for the spacing and for rounding.
+static bnr_status check_ns_params(const bnr_ns_params *n)
+{
+    if (n->steps < 1 || n->steps > 32) return fail(BNR_ERR_SHAPE, "steps %d not in 1..32", n->steps);
+    if (!(n->eps >= 0.0f)) return fail(BNR_ERR_SHAPE, "eps must be >= 0");
+    double top = 1.0;
+    for (int k = 0; k < n->steps; k++) {
+        double next = 0.0, q = 0.0;
+        top *= 1.02;
+        for (int i = 0; i <= 128; i++) {
+            const double x = top * i / 128, x2 = x * x, f = n->a + x2 * (n->b + x2 * n->c);
+            const double af = f < 0 ? -f : f;
+            if (!(af <= 15.0)) { q = 1e30; break; }
+            if (af > q) q = af;
+            if (af * x > next) next = af * x;
+        }
+        if (q > 15.0 || !(next < 3.5) || !(top < 3.5))
+            return fail(BNR_ERR_UNSUPPORTED, "coefficients (%g, %g, %g): step %d of %d leaves the range of the products",
+                        n->a, n->b, n->c, k + 1, n->steps);
+        top = next;
+    }
+    return BNR_OK;
+}
+
+// a row-major matrix in memory
+struct NsArea { uintptr_t lo; int64_t rows, width, pitch; bool written; int item; };   // bytes
+static uintptr_t area_end(const NsArea &a) { return a.lo + (uintptr_t)((a.rows - 1) * a.pitch + a.width); }
+static bool areas_share(const NsArea &a, const NsArea &b)
+{
+    if (a.lo >= area_end(b) || b.lo >= area_end(a)) return false;
+    if (a.pitch != b.pitch) return true;
+    // column slices of rows of one stride: apart if their columns are
+    const uintptr_t row = (uintptr_t)a.pitch, d = a.lo <= b.lo ? (b.lo - a.lo) % row : (row - (a.lo - b.lo) % row) % row;
+    return !(d >= (uintptr_t)a.width && d + (uintptr_t)b.width <= row);
+}
+
+// Refuses a list in which a written matrix shares memory with another one of
+// the list's.  area(i) gives the i-th of n; the indices are sorted by address,
+// so matrices that lie apart cost n log n.
+template <typename F>
+static bnr_status check_ns_areas(int n, F &&area)
+{
+    static_assert(kNsMaxCount * 4 <= 4096, "index buffer");
+    uint16_t order[kNsMaxCount * 4];
+    for (int i = 0; i < n; i++) order[i] = (uint16_t)i;
+    std::sort(order, order + n, [&](uint16_t x, uint16_t y) { return area(x).lo < area(y).lo; });
+    for (int i = 0; i < n; i++) {
+        const NsArea a = area(order[i]);
+        const uintptr_t end = area_end(a);
+        for (int j = i + 1; j < n; j++) {
+            const NsArea b = area(order[j]);
+            if (b.lo >= end) break;
+            if ((a.written || b.written) && areas_share(a, b))
+                return fail(BNR_ERR_ALIAS, "matrices %d and %d: an output shares memory with another argument", a.item,
+                            b.item);
+        }
+    }
+    return BNR_OK;
+}
+
+static bnr_status check_ns_plan(const NsPlan &p)
+{
+    for (int64_t w : p.work)
+        if (w > (int64_t)1 << 30) return fail(BNR_ERR_UNSUPPORTED, "list too large for one call");
+    return BNR_OK;
+}
+
+static NsIn ortho_in(const void *arg, int i)
+{
+    const bnr_ortho_item &t = ((const bnr_ortho_item *)arg)[i];
+    return NsIn{t.x, t.out, nullptr, nullptr, t.rows, t.cols, t.x_ld, t.out_ld, 0, 0, 1.f};
+}
+
+static NsIn muon_in(const void *arg, int i)
+{
+    const bnr_muon_item &t = ((const bnr_muon_item *)arg)[i];
+    return NsIn{t.g, t.w, t.buf, (uint16_t *)t.copy, t.rows, t.cols, t.g_ld, t.w_ld, t.buf_ld, t.copy_ld, t.scale};
+}
+
+template <typename T>
+static size_t ns_workspace(const T *items, int32_t count)
+{
+    if (!items || count <= 0 || count > kNsMaxCount) return 0;
+    NsPlan p{};
+    for (int i = 0; i < count; i++) {
+        if (check_ns_matrix(i, items[i].rows, items[i].cols) != BNR_OK) return 0;
+        ns_plan_add(p, items[i].rows, items[i].cols);
+    }
+    return ns_plan_bytes(p);
+}
+
+extern "C" {
+
+size_t bnr_orthogonalize_workspace_size(const bnr_ortho_item *items, int32_t count) { return ns_workspace(items, count); }
+size_t bnr_muon_workspace_size(const bnr_muon_item *items, int32_t count) { return ns_workspace(items, count); }
+
+static bnr_status check_ns_count(const void *items, int32_t count)
+{
+    if (count < 0) return fail(BNR_ERR_SHAPE, "count %d is negative", count);
+    if (count > kNsMaxCount) return fail(BNR_ERR_UNSUPPORTED, "more than %d matrices", kNsMaxCount);
+    if (count && !items) return fail(BNR_ERR_NULL, "items is NULL");
+    return BNR_OK;
+}
+
+bnr_status bnr_orthogonalize(const bnr_ortho_item *items, int32_t count, bnr_dtype x_dtype, bnr_dtype out_dtype,
+                             const bnr_ns_params *ns, void *ws, size_t ws_bytes, void *stream)
+{
+    TRY(check_ns_count(items, count));
+    TRY(check_dtype(x_dtype));
+    TRY(check_dtype(out_dtype));
+    if (!ns) return fail(BNR_ERR_NULL, "ns is NULL");
+    TRY(check_ns_params(ns));
+    NsPlan plan{};
+    for (int i = 0; i < count; i++) {
+        const bnr_ortho_item &t = items[i];
+        TRY(check_ns_matrix(i, t.rows, t.cols));
+        TRY(check_ns_view(i, "x", t.x, t.x_ld, t.cols, esize(x_dtype)));
+        TRY(check_ns_view(i, "out", t.out, t.out_ld, t.cols, esize(out_dtype)));
+        ns_plan_add(plan, t.rows, t.cols);
+    }
+    const int64_t es = esize(out_dtype);
+    TRY(check_ns_areas(count, [&](int i) {
+        const bnr_ortho_item &t = items[i];
+        return NsArea{reinterpret_cast<uintptr_t>(t.out), t.rows, t.cols * es, t.out_ld * es, true, i};
+    }));
+    if (!count) return ok();
+    TRY(check_ns_plan(plan));
+    TRY(check_ws(ws, ws_bytes, ns_plan_bytes(plan)));
+    NsStep s{};
+    s.steps = ns->steps; s.a = ns->a; s.b = ns->b; s.c = ns->c; s.eps = ns->eps;
+    TRY_HIP(launch_ns(plan, ortho_in, items, s, dt_of(x_dtype), dt_of(out_dtype), ws, (hipStream_t)stream),
+            "orthogonalisation");
+    return ok();
+}
+
+bnr_status bnr_muon_update(const bnr_muon_item *items, int32_t count, bnr_dtype w_dtype, bnr_dtype g_dtype,
+                           const bnr_muon_params *p, void *ws, size_t ws_bytes, void *stream)
+{
+    TRY(check_ns_count(items, count));
+    TRY(check_dtype(w_dtype));
+    TRY(check_dtype(g_dtype));
+    if (!p) return fail(BNR_ERR_NULL, "params is NULL");
+    TRY(check_ns_params(&p->ns));
+    if (!(p->momentum >= 0.0f && p->momentum < 1.0f)) return fail(BNR_ERR_SHAPE, "momentum must be in [0, 1)");
+    if (p->lr_dev) TRY(check_fptr(p->lr_dev, "lr_dev"));
+    NsPlan plan{};
+    for (int i = 0; i < count; i++) {
+        const bnr_muon_item &t = items[i];
+        TRY(check_ns_matrix(i, t.rows, t.cols));
+        TRY(check_ns_view(i, "w", t.w, t.w_ld, t.cols, esize(w_dtype)));
+        TRY(check_ns_view(i, "g", t.g, t.g_ld, t.cols, esize(g_dtype)));
+        TRY(check_ns_view(i, "buf", t.buf, t.buf_ld, t.cols, 4));
+        if (t.copy) TRY(check_ns_view(i, "copy", t.copy, t.copy_ld, t.cols, 2));
+        ns_plan_add(plan, t.rows, t.cols);
+    }
+    const int64_t ws_w = esize(w_dtype), es_g = esize(g_dtype);
+    const auto area = [&](int k) {
+        const bnr_muon_item &t = items[k / 4];
+        switch (k % 4) {
+        case 0: return NsArea{reinterpret_cast<uintptr_t>(t.w), t.rows, t.cols * ws_w, t.w_ld * ws_w, true, k / 4};
+        case 1: return NsArea{reinterpret_cast<uintptr_t>(t.buf), t.rows, t.cols * (int64_t)4, t.buf_ld * (int64_t)4, true, k / 4};
+        case 2: return NsArea{reinterpret_cast<uintptr_t>(t.g), t.rows, t.cols * es_g, t.g_ld * es_g, false, k / 4};
+        // without a copy the gradient stands in once more
+        default: return t.copy ? NsArea{reinterpret_cast<uintptr_t>(t.copy), t.rows, t.cols * (int64_t)2, t.copy_ld * (int64_t)2, true, k / 4}
+                               : NsArea{reinterpret_cast<uintptr_t>(t.g), t.rows, t.cols * es_g, t.g_ld * es_g, false, k / 4};
+        }
+    };
+    TRY(check_ns_areas(count * 4, area));
+    if (p->lr_dev)
+        for (int k = 0; k < count * 4; k++) {
+            const NsArea a = area(k), l{reinterpret_cast<uintptr_t>(p->lr_dev), 1, 4, 4, false, k / 4};
+            if (a.written && areas_share(a, l)) return fail(BNR_ERR_ALIAS, "lr_dev lies in an output of matrix %d", k / 4);
+        }
+    if (!count) return ok();
+    TRY(check_ns_plan(plan));
+    TRY(check_ws(ws, ws_bytes, ns_plan_bytes(plan)));
+    NsStep s{};
+    s.update = 1; s.nesterov = p->nesterov != 0; s.momentum = p->momentum;
+    s.decay = p->weight_decay; s.lr = p->lr; s.lr_dev = p->lr_dev;
+    s.steps = p->ns.steps; s.a = p->ns.a; s.b = p->ns.b; s.c = p->ns.c; s.eps = p->ns.eps;
+    TRY_HIP(launch_ns(plan, muon_in, items, s, dt_of(g_dtype), dt_of(w_dtype), ws, (hipStream_t)stream),
+            "orthogonalised update");
     return ok();
 }
 

@@ -294,4 +294,31 @@ int64_t ln_bwd_groups(int dtype, int64_t m, int c, bool vec);            // part
 hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s);
 hipError_t launch_ln_bwd(int dtype, const LnParams &p, bool vec, hipStream_t s);
 
+// Newton-Schulz orthogonalisation of a list of matrices (newton_schulz.hip).
+struct NsIn {                     // one matrix as the caller gives it, row-major
+    const void *src;              // matrix to orthogonalise, or gradient
+    void *dst;                    // result, or weights
+    float *buf;                   // momentum (update)
+    uint16_t *copy;               // bf16 copy of the weights (update; NULL: none)
+    int rows, cols, ld_src, ld_dst, ld_buf, ld_copy;
+    float scale;
+};
+struct NsStep {                   // one call's numbers
+    int update, nesterov, steps;
+    float momentum, decay, lr;
+    const float *lr_dev;          // in the place of lr (NULL: lr)
+    float eps, a, b, c;
+};
+// what a list needs: filled matrix by matrix, then the workspace and the grids follow
+struct NsPlan {
+    int count;
+    int64_t bytes, work[4];
+    double flops, values;
+};
+typedef NsIn (*NsFill)(const void *arg, int i);
+void ns_plan_add(NsPlan &p, int rows, int cols);
+size_t ns_plan_bytes(const NsPlan &p);
+hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep &s, int src_dtype, int dst_dtype,
+                     void *ws, hipStream_t st);
+
 }  // namespace bnr

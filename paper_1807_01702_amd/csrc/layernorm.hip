@@ -52,6 +52,22 @@ template <typename T> struct LnVec16 {
 template <> struct LnVec<float, 4> : LnVec16<float> {};
 template <> struct LnVec<bf16_t, 8> : LnVec16<bf16_t> {};
 
+// V per-channel parameters at p (16-byte aligned where V > 1), or the constant
+// `other` where there are none
+template <int V>
+__device__ __forceinline__ void ln_param(const float *p, int c, float other, float *f)
+{
+    if constexpr (V == 1) {
+        f[0] = p ? p[c] : other;
+    } else {
+        #pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 t = p ? *reinterpret_cast<const float4 *>(p + c + i) : make_float4(other, other, other, other);
+            f[i] = t.x; f[i + 1] = t.y; f[i + 2] = t.z; f[i + 3] = t.w;
+        }
+    }
+}
+
 // N sums over the TPR threads of a row (every thread gets them).  Rows longer
 // than a wave go through red[N][waves], which the next call may not reuse
 // before a barrier: callers alternate between two or more areas.
@@ -93,7 +109,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
     T *sum = (T *)p.sum, *y = (T *)p.y;
     const int64_t row0 = (int64_t)blockIdx.x * (GR * U) + grp;
     typename L::raw rx[U][NV], rr[U][NV];
-    float f[U][NV][V], acc[U];
+    float f[U][NV][V], gam[NV][V], bet[NV][V], acc[U];
     #pragma unroll
     for (int u = 0; u < U; u++) {
         // rows and vectors past the end read the last ones and are dropped
@@ -104,6 +120,12 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
             rx[u][j] = L::load(x + row * p.x_ldc + (int64_t)v * V);
             if (RES) rr[u][j] = L::load(res + row * p.res_ldc + (int64_t)v * V);
         }
+    }
+    #pragma unroll
+    for (int j = 0; j < NV; j++) {
+        const int v = j * TPR + lane < nvec ? j * TPR + lane : nvec - 1;
+        ln_param<V>(p.gamma, v * V, 1.f, gam[j]);
+        ln_param<V>(p.beta, v * V, 0.f, bet[j]);
     }
     #pragma unroll
     for (int u = 0; u < U; u++) {
@@ -158,10 +180,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
             if (v >= nvec) continue;
             float o[V];
             #pragma unroll
-            for (int i = 0; i < V; i++) {
-                const float g = p.gamma ? p.gamma[v * V + i] : 1.f, b = p.beta ? p.beta[v * V + i] : 0.f;
-                o[i] = f[u][j][i] * rstd * g + b;
-            }
+            for (int i = 0; i < V; i++) o[i] = f[u][j][i] * rstd * gam[j][i] + bet[j][i];
             L::store(y + row * p.y_ldc + (int64_t)v * V, o);
         }
     }
@@ -189,9 +208,9 @@ __global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
     for (int j = 0; j < NV; j++) {
         const int v = j * TPR + lane;
         col[j] = v < nvec ? v * V : -1;
+        ln_param<V>(p.gamma, (v < nvec ? v : nvec - 1) * V, 1.f, gam[j]);
         #pragma unroll
         for (int i = 0; i < V; i++) {
-            gam[j][i] = p.gamma && v < nvec ? p.gamma[v * V + i] : 1.f;
             sb[j][i] = 0.f;
             sg[j][i] = 0.f;
         }

@@ -1,0 +1,218 @@
+"""Host-side checks of the layer-norm and orthogonalised-update entry points (CPU only, no kernel launches): bad
+arguments get the documented status before anything is launched."""
+import ctypes
+
+import pytest
+
+# addresses that are never dereferenced (validation fails first)
+A = 0x10000000
+MB = 1 << 20
+F32, BF16 = 0, 1
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1807_01702_amd import bnr
+    return bnr
+
+
+def _fwd(B, **kw):
+    a = dict(m=10, c=24, dtype=BF16, x=A, x_ldc=24, res=None, res_ldc=0, sum=None, sum_ldc=0, gamma=A + 40 * MB,
+             beta=A + 41 * MB, mean=A + 42 * MB, rstd=A + 43 * MB, eps=1e-5, y=A + MB, y_ldc=24, ln=True)
+    a.update(kw)
+    ln = B.LNStruct(a["gamma"], a["beta"], a["mean"], a["rstd"], a["eps"])
+    return B.STATUS[B._lib_fns["bnr_layernorm_fwd"](a["m"], a["c"], a["dtype"], a["x"], a["x_ldc"], a["res"], a["res_ldc"],
+                                                    a["sum"], a["sum_ldc"], ctypes.byref(ln) if a["ln"] else None, a["y"],
+                                                    a["y_ldc"], None)]
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(m=0), "BNR_ERR_SHAPE"), (dict(m=-3), "BNR_ERR_SHAPE"), (dict(m=(1 << 31) + 1), "BNR_ERR_SHAPE"),
+    (dict(c=0), "BNR_ERR_SHAPE"), (dict(c=16385, x_ldc=20000, y_ldc=20000), "BNR_ERR_UNSUPPORTED"),
+    (dict(dtype=2), "BNR_ERR_DTYPE"), (dict(ln=False), "BNR_ERR_NULL"), (dict(x=None), "BNR_ERR_NULL"),
+    (dict(y=None), "BNR_ERR_NULL"), (dict(mean=None), "BNR_ERR_NULL"), (dict(rstd=None), "BNR_ERR_NULL"),
+    (dict(x=A + 1), "BNR_ERR_ALIGN"), (dict(y=A + MB + 1), "BNR_ERR_ALIGN"), (dict(dtype=F32, x=A + 2), "BNR_ERR_ALIGN"),
+    (dict(gamma=A + 40 * MB + 2), "BNR_ERR_ALIGN"), (dict(mean=A + 42 * MB + 1), "BNR_ERR_ALIGN"),
+    (dict(x_ldc=23), "BNR_ERR_SHAPE"), (dict(y_ldc=8), "BNR_ERR_SHAPE"), (dict(eps=0.0), "BNR_ERR_SHAPE"),
+    (dict(eps=float("nan")), "BNR_ERR_SHAPE"), (dict(res=A + 2 * MB, res_ldc=24), "BNR_ERR_NULL"),
+    (dict(sum=A + 2 * MB, sum_ldc=24), "BNR_ERR_NULL"),
+    (dict(res=A + 2 * MB, res_ldc=23, sum=A + 3 * MB, sum_ldc=24), "BNR_ERR_SHAPE"),
+    (dict(res=A + 2 * MB, res_ldc=24, sum=A + 3 * MB + 1, sum_ldc=24), "BNR_ERR_ALIGN"),
+    (dict(y=A + 48), "BNR_ERR_ALIAS"),                                   # a row later: not the same view
+    (dict(y=A, y_ldc=32), "BNR_ERR_ALIAS"),                              # the same start, another stride
+    (dict(x_ldc=40, y=A + 32, y_ldc=40), "BNR_ERR_ALIAS"),               # slices of one buffer that share channels
+    (dict(res=A + 2 * MB, res_ldc=24, sum=A + MB, sum_ldc=24), "BNR_ERR_ALIAS"),     # y over sum
+    (dict(res=A + 2 * MB, res_ldc=24, sum=A + 48, sum_ldc=24), "BNR_ERR_ALIAS"),
+    (dict(res=A + 2 * MB, res_ldc=24, sum=A + 3 * MB, sum_ldc=24, y=A + 2 * MB + 48), "BNR_ERR_ALIAS"),
+    (dict(rstd=A + 42 * MB), "BNR_ERR_ALIAS"), (dict(mean=A + 100 - 100 % 4), "BNR_ERR_ALIAS"),
+    (dict(mean=A + 40 * MB), "BNR_ERR_ALIAS"), (dict(gamma=A + MB), "BNR_ERR_ALIAS"),
+])
+def test_layernorm_fwd_refuses(B, kw, status):
+    assert _fwd(B, **kw) == status, B._lib_fns["bnr_last_error"]()
+
+
+def _bwd(B, **kw):
+    a = dict(m=10, c=24, dtype=F32, dy=A, dy_ldc=24, x=A + MB, x_ldc=24, gamma=A + 40 * MB, mean=A + 42 * MB,
+             rstd=A + 43 * MB, dsum=None, dsum_ldc=0, dx=A + 2 * MB, dx_ldc=24, dgamma=A + 50 * MB, dbeta=A + 51 * MB,
+             ws=A + 60 * MB, ws_bytes=1 << 30)
+    a.update(kw)
+    ln = B.LNStruct(a["gamma"], None, a["mean"], a["rstd"], 0.0)
+    return B.STATUS[B._lib_fns["bnr_layernorm_bwd"](a["m"], a["c"], a["dtype"], a["dy"], a["dy_ldc"], a["x"], a["x_ldc"],
+                                                    ctypes.byref(ln), a["dsum"], a["dsum_ldc"], a["dx"], a["dx_ldc"],
+                                                    a["dgamma"], a["dbeta"], a["ws"], a["ws_bytes"], None)]
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(m=0), "BNR_ERR_SHAPE"), (dict(c=16385, dy_ldc=20000, x_ldc=20000, dx_ldc=20000), "BNR_ERR_UNSUPPORTED"),
+    (dict(dtype=-1), "BNR_ERR_DTYPE"), (dict(dy=None), "BNR_ERR_NULL"), (dict(x=None), "BNR_ERR_NULL"),
+    (dict(dx=None), "BNR_ERR_NULL"), (dict(rstd=None), "BNR_ERR_NULL"), (dict(dx=A + 2 * MB + 2), "BNR_ERR_ALIGN"),
+    (dict(dgamma=A + 50 * MB + 1), "BNR_ERR_ALIGN"), (dict(dsum=A + 3 * MB, dsum_ldc=8), "BNR_ERR_SHAPE"),
+    (dict(dx=A + 96), "BNR_ERR_ALIAS"), (dict(dx=A + MB, dx_ldc=28), "BNR_ERR_ALIAS"),
+    (dict(dsum=A + 2 * MB + 4, dsum_ldc=24), "BNR_ERR_ALIAS"), (dict(dgamma=A + 51 * MB + 8), "BNR_ERR_ALIAS"),
+    (dict(dgamma=A + 64), "BNR_ERR_ALIAS"), (dict(dbeta=A + 42 * MB), "BNR_ERR_ALIAS"),
+    (dict(dbeta=A + 40 * MB), "BNR_ERR_ALIAS"), (dict(dx=A + 42 * MB - 16), "BNR_ERR_ALIAS"),
+    (dict(ws=None), "BNR_ERR_WORKSPACE"), (dict(ws=A + 60 * MB + 16), "BNR_ERR_ALIGN"), (dict(ws_bytes=64), "BNR_ERR_WORKSPACE"),
+])
+def test_layernorm_bwd_refuses(B, kw, status):
+    assert _bwd(B, **kw) == status, B._lib_fns["bnr_last_error"]()
+
+
+def test_layernorm_workspace_size(B):
+    f = B._lib_fns["bnr_layernorm_workspace_size"]
+    assert f(100, 64, BF16) > 0 and f(1, 1, F32) > 0 and f(401408, 16384, BF16) > 0
+    for m, c, t in ((0, 64, BF16), (10, 0, F32), (10, 16385, F32), (10, 64, 5), (-1, 8, F32)):
+        assert f(m, c, t) == 0
+
+
+def _ortho(B, items, ns=(5, 3.4445, -4.7750, 2.0315, 1e-7), xt=F32, ot=F32, ws=A + (1 << 40), ws_bytes=1 << 40, count=None):
+    n = len(items)
+    arr = (B.OrthoItem * max(n, 1))(*[B.OrthoItem(*i) for i in items])
+    p = B.NSParams(*ns)
+    return B.STATUS[B._lib_fns["bnr_orthogonalize"](arr, n if count is None else count, xt, ot, ctypes.byref(p), ws, ws_bytes,
+                                                    None)]
+
+
+ONE = (8, 16, A, 16, A + MB, 16)
+
+
+@pytest.mark.parametrize("item,status", [
+    ((0, 16, A, 16, A + MB, 16), "BNR_ERR_SHAPE"), ((8, -1, A, 16, A + MB, 16), "BNR_ERR_SHAPE"),
+    ((8, 16, None, 16, A + MB, 16), "BNR_ERR_NULL"), ((8, 16, A, 16, None, 16), "BNR_ERR_NULL"),
+    ((8, 16, A + 2, 16, A + MB, 16), "BNR_ERR_ALIGN"), ((8, 16, A, 15, A + MB, 16), "BNR_ERR_SHAPE"),
+    ((8, 16, A, 16, A + MB, 8), "BNR_ERR_SHAPE"), ((16385, 16385, A, 20000, A + 1 << 36, 20000), "BNR_ERR_UNSUPPORTED"),
+    ((1, (1 << 20) + 1, A, 1 << 21, A + MB, 1 << 21), "BNR_ERR_UNSUPPORTED"),
+])
+def test_orthogonalize_refuses_matrices(B, item, status):
+    assert _ortho(B, [ONE, item]) == status, B._lib_fns["bnr_last_error"]()
+
+
+@pytest.mark.parametrize("ns,status", [
+    ((0, 3.4, -4.7, 2.0, 1e-7), "BNR_ERR_SHAPE"), ((33, 1.5, -0.5, 0.0, 1e-7), "BNR_ERR_SHAPE"),
+    ((5, 3.4, -4.7, 2.0, -1e-7), "BNR_ERR_SHAPE"), ((5, 3.4, -4.7, 2.0, float("nan")), "BNR_ERR_SHAPE"),
+    ((5, 4.0, 0.0, 0.0, 0.0), "BNR_ERR_UNSUPPORTED"), ((1, 16.0, -16.0, 0.0, 0.0), "BNR_ERR_UNSUPPORTED"),
+    ((5, float("nan"), 0.0, 0.0, 0.0), "BNR_ERR_UNSUPPORTED"), ((5, float("inf"), 0.0, 0.0, 0.0), "BNR_ERR_UNSUPPORTED"),
+    ((32, 1.5, 0.5, 0.0, 0.0), "BNR_ERR_UNSUPPORTED"),
+])
+def test_orthogonalize_refuses_coefficients(B, ns, status):
+    assert _ortho(B, [ONE], ns=ns) == status, B._lib_fns["bnr_last_error"]()
+
+
+def test_orthogonalize_refuses_lists(B):
+    assert _ortho(B, [ONE], count=-1) == "BNR_ERR_SHAPE"
+    assert _ortho(B, [ONE], count=1025) == "BNR_ERR_UNSUPPORTED"
+    assert _ortho(B, [], count=0) == "BNR_OK"                          # nothing to do
+    assert _ortho(B, [ONE], xt=3) == "BNR_ERR_DTYPE" and _ortho(B, [ONE], ot=-2) == "BNR_ERR_DTYPE"
+    assert _ortho(B, [ONE], ws=None) == "BNR_ERR_WORKSPACE"
+    assert _ortho(B, [ONE], ws_bytes=1024) == "BNR_ERR_WORKSPACE"
+    assert _ortho(B, [ONE], ws=A + 8) == "BNR_ERR_ALIGN"
+    f, p = B._lib_fns["bnr_orthogonalize"], B.NSParams(5, 3.4445, -4.7750, 2.0315, 1e-7)
+    assert B.STATUS[f(None, 1, F32, F32, ctypes.byref(p), A, 1 << 30, None)] == "BNR_ERR_NULL"
+    arr = (B.OrthoItem * 1)(B.OrthoItem(*ONE))
+    assert B.STATUS[f(arr, 1, F32, F32, None, A, 1 << 30, None)] == "BNR_ERR_NULL"
+    # outputs that share memory: the same one, a later row, slices that share a column; apart, they pass to the workspace
+    for other in (A + MB, A + MB + 64, A + MB + 60, A + MB - 4):
+        assert _ortho(B, [ONE, (8, 16, A, 16, other, 16)], ws=None) == "BNR_ERR_ALIAS", other
+    wide = lambda p: (8, 16, A, 16, p, 40)  # noqa: E731
+    assert _ortho(B, [wide(A + MB), wide(A + MB + 60)], ws=None) == "BNR_ERR_ALIAS"
+    assert _ortho(B, [wide(A + MB + 64), wide(A + MB)], ws=None) == "BNR_ERR_WORKSPACE"
+    many = [(8, 16, A, 16, A + MB + 64 * 16 * i, 16) for i in range(1024)]
+    assert _ortho(B, many, ws=None) == "BNR_ERR_WORKSPACE"
+    assert _ortho(B, many[:-1] + [many[500]], ws=None) == "BNR_ERR_ALIAS"
+
+
+def _muon(B, items, lr_dev=None, momentum=0.95, wt=F32, gt=F32, ws=A + (1 << 40), ws_bytes=1 << 40, ns=None):
+    arr = (B.MuonItem * max(len(items), 1))(*[B.MuonItem(*i) for i in items])
+    p = B.MuonParams(0.1, lr_dev, momentum, 1, 0.0, ns or B.NSParams(5, 3.4445, -4.7750, 2.0315, 1e-7))
+    return B.STATUS[B._lib_fns["bnr_muon_update"](arr, len(items), wt, gt, ctypes.byref(p), ws, ws_bytes, None)]
+
+
+def _item(rows=8, cols=16, w=A, w_ld=16, g=A + MB, g_ld=16, buf=A + 2 * MB, buf_ld=16, copy=None, copy_ld=0, scale=1.0):
+    return rows, cols, w, w_ld, g, g_ld, buf, buf_ld, copy, copy_ld, scale
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(w=None), "BNR_ERR_NULL"), (dict(g=None), "BNR_ERR_NULL"), (dict(buf=None), "BNR_ERR_NULL"),
+    (dict(rows=0), "BNR_ERR_SHAPE"), (dict(w_ld=15), "BNR_ERR_SHAPE"), (dict(g_ld=15), "BNR_ERR_SHAPE"),
+    (dict(buf_ld=15), "BNR_ERR_SHAPE"), (dict(copy=A + 3 * MB, copy_ld=15), "BNR_ERR_SHAPE"),
+    (dict(w=A + 2), "BNR_ERR_ALIGN"), (dict(buf=A + 2 * MB + 2), "BNR_ERR_ALIGN"),
+    (dict(copy=A + 3 * MB + 1, copy_ld=16), "BNR_ERR_ALIGN"), (dict(g=A), "BNR_ERR_ALIAS"), (dict(g=A + 2 * MB + 64), "BNR_ERR_ALIAS"),
+    (dict(buf=A), "BNR_ERR_ALIAS"), (dict(copy=A, copy_ld=16), "BNR_ERR_ALIAS"),
+    (dict(copy=A + MB + 2, copy_ld=16), "BNR_ERR_ALIAS"), (dict(copy=A + 2 * MB, copy_ld=16), "BNR_ERR_ALIAS"),
+])
+def test_muon_update_refuses_matrices(B, kw, status):
+    assert _muon(B, [_item(w=A + 8 * MB, g=A + 9 * MB, buf=A + 10 * MB), _item(**kw)]) == status, B._lib_fns["bnr_last_error"]()
+
+
+def test_muon_update_refuses(B):
+    one = _item()
+    assert _muon(B, []) == "BNR_OK"
+    assert _muon(B, [one], ws=None) == "BNR_ERR_WORKSPACE" and _muon(B, [one], ws_bytes=100) == "BNR_ERR_WORKSPACE"
+    assert _muon(B, [one], wt=4) == "BNR_ERR_DTYPE" and _muon(B, [one], gt=4) == "BNR_ERR_DTYPE"
+    for m in (1.0, -0.1, float("nan")):
+        assert _muon(B, [one], momentum=m) == "BNR_ERR_SHAPE"
+    assert _muon(B, [one], ns=B.NSParams(0, 1, 0, 0, 0)) == "BNR_ERR_SHAPE"
+    assert _muon(B, [one], ns=B.NSParams(5, 9, 0, 0, 0)) == "BNR_ERR_UNSUPPORTED"
+    assert _muon(B, [one], lr_dev=A + 2) == "BNR_ERR_ALIGN"
+    for p in (A + 4, A + 2 * MB + 100):
+        assert _muon(B, [one], lr_dev=p) == "BNR_ERR_ALIAS"
+    assert _muon(B, [one], lr_dev=A + MB, ws=None) == "BNR_ERR_WORKSPACE"      # beside a gradient: only read
+    assert _muon(B, [one, one]) == "BNR_ERR_ALIAS"                               # the same matrix twice
+    # two matrices may take their gradients from one tensor
+    assert _muon(B, [one, _item(w=A + 8 * MB, buf=A + 10 * MB)], ws=None) == "BNR_ERR_WORKSPACE"
+    f = B._lib_fns["bnr_muon_update"]
+    arr = (B.MuonItem * 1)(B.MuonItem(*one))
+    assert B.STATUS[f(arr, 1, F32, F32, None, A, 1 << 30, None)] == "BNR_ERR_NULL"
+
+
+def test_workspace_sizes_of_lists(B):
+    fo, fm = B._lib_fns["bnr_orthogonalize_workspace_size"], B._lib_fns["bnr_muon_workspace_size"]
+    arr = (B.OrthoItem * 2)(B.OrthoItem(*ONE), B.OrthoItem(300, 70, A, 70, A, 70))
+    mu = (B.MuonItem * 2)(B.MuonItem(*_item()), B.MuonItem(*_item(rows=300, cols=70)))
+    assert 0 < fo(arr, 1) < fo(arr, 2) == fm(mu, 2)
+    assert fo(arr, 0) == 0 and fo(None, 1) == 0 and fo(arr, -1) == 0 and fo(arr, 2000) == 0
+    arr[1].rows = 0
+    assert fo(arr, 2) == 0
+
+
+def test_binding_refuses_host_tensors_and_wrong_shapes(B):
+    import torch
+    x, y = torch.zeros(4, 8), torch.zeros(4, 8)
+    ln = B.LN(torch.ones(8), None, 4, device="cpu")
+    with pytest.raises(ValueError, match="GPU"):
+        B.bnr_layernorm_fwd(x, ln, y)
+    with pytest.raises(ValueError, match="rows of"):
+        B.bnr_layernorm_fwd(x, ln, torch.zeros(4, 9))
+    with pytest.raises(ValueError, match="rows of"):
+        B.bnr_layernorm_fwd(x, ln, y.bfloat16())
+    with pytest.raises(ValueError, match="mean"):
+        B.bnr_layernorm_fwd(x, B.LN(torch.ones(8), None, 5, device="cpu"), y)
+    with pytest.raises(ValueError, match="gamma"):
+        B.bnr_layernorm_fwd(x, B.LN(torch.ones(7), None, 4, device="cpu"), y)
+    with pytest.raises(ValueError, match="unit-stride"):
+        B.bnr_layernorm_fwd(torch.zeros(8, 4).t(), ln, y)
+    with pytest.raises(ValueError, match="GPU"):
+        B.bnr_orthogonalize(x, y)
+    with pytest.raises(ValueError, match="outputs"):
+        B.bnr_orthogonalize([x], [])
+    with pytest.raises(ValueError, match="wanted"):
+        B.bnr_orthogonalize([x, x.bfloat16()], [y, y])
