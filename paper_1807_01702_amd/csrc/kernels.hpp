@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "tiles.hpp"
+
 namespace bnr {
 
 // k_stats_partial modes
@@ -312,8 +314,8 @@ struct NsStep {                   // one call's numbers
 // what a list needs: filled matrix by matrix, then the workspace and the grids follow
 struct NsPlan {
     int count;
-    int64_t bytes, work[4];
-    double flops, values;
+    int64_t bytes, work[kNsStages];
+    double flops, narrow_flops, values;    // per step: wide, narrow matrices; matrix elements
 };
 typedef NsIn (*NsFill)(const void *arg, int i);
 void ns_plan_add(NsPlan &p, int rows, int cols);

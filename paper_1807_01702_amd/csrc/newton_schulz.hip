@@ -29,7 +29,11 @@
 #include "common.hpp"
 #include "kernels.hpp"
 #include "tiles.hpp"
+#include "mfma.hpp"
 #include "trace.hpp"
+
+#include <atomic>
+#include <type_traits>
 
 namespace bnr {
 
@@ -42,84 +46,126 @@ typedef uint16_t h16;                                // fp16 storage word
 constexpr float kS = 4096.f, kInvS = 1.f / 4096.f;   // see the precision note
 constexpr int kTile = kNsTile;
 
+// Stages of a call and their work items: momentum and squares; the narrow
+// matrices' blocks and the sums of their partial Gram matrices; the wide ones'
+// conversion, symmetric product tiles and general product tiles.
+enum { PRE_SQ = 0, PRE_NARROW = 1, PRE_SUM = 2, PRE_PREP = 3, PRE_GRAM = 4, PRE_APPLY = 5, kPre = kNsStages };
+
 // one matrix of the list on the device: the caller's arguments and its place in the workspace
 struct NsDev {
     NsIn in;
     int p, q, P, Q, flip;          // short and long side, padded; flip: X is the transpose of the caller's matrix
-    int parts;                     // partial sums of squares
+    int parts, blocks;             // partial sums of squares; column blocks of a narrow matrix (0: wide)
     double *sq;                    // [parts]
-    h16 *x, *xt[2], *g, *r;        // pair matrices [P][Q], [Q][P], [P][P]
+    h16 *x, *xt[2], *g, *r;        // wide: pair matrices [P][Q], [Q][P] twice, [P][P] twice; narrow: xt[0] = the blocks
+    float *part[2], *sum;          // narrow: partial Gram matrices [blocks][P][P], their sum
 };
 // the device table: the matrices and the running counts of work items per stage
-struct NsTable { NsDev *items; int *pre[4]; };
-enum { PRE_SQ = 0, PRE_PREP = 1, PRE_GRAM = 2, PRE_APPLY = 3 };
+struct NsTable { NsDev *items; int *pre[kPre]; };
 
 // Sizes of one matrix, the same on the host (workspace, grids) and on the device.
 struct NsSize {
-    int p, q, P, Q, flip, parts;
-    int64_t work[4];               // work items per stage
+    int p, q, P, Q, flip, parts, blocks;
+    int work[kPre];                // work items per stage
     int64_t bytes;                 // workspace
 };
+constexpr int kMaxParts = 1024;    // partial sums of squares of a matrix
+constexpr int kNarrow = 128;       // short sides up to this take the narrow path
+constexpr int kBlock = 16384;      // values of a narrow matrix's block: [kBlock / P][P]
+// Blocks of one narrow matrix up to which every block adds the partial Gram
+// matrices itself; past it a launch of its own adds them once.
+constexpr int kSumBlocks = 8;
+
 __host__ __device__ inline NsSize ns_size(int rows, int cols)
 {
     NsSize z;
     z.flip = rows > cols;
     z.p = z.flip ? cols : rows;
     z.q = z.flip ? rows : cols;
+    // 16384 values a partial sum, whole rows, at most kMaxParts partial sums
+    const int64_t want = ((int64_t)rows * cols + 16383) >> 14;
+    unsigned n = want > kMaxParts ? kMaxParts : (unsigned)want;
+    if (n > (unsigned)rows) n = rows;
+    const unsigned rp = ((unsigned)rows + n - 1) / n;
+    z.parts = (int)(((unsigned)rows + rp - 1) / rp);
+    z.work[PRE_SQ] = z.parts;
+    for (int k = 1; k < kPre; k++) z.work[k] = 0;
+    z.blocks = 0;
+    if (z.p <= kNarrow) {
+        z.P = z.p <= 32 ? 32 : (z.p <= 64 ? 64 : 128);
+        const int qb = kBlock / z.P;
+        z.blocks = (z.q + qb - 1) / qb;
+        z.Q = z.blocks * qb;
+        z.work[PRE_NARROW] = z.blocks;
+        if (z.blocks > kSumBlocks) z.work[PRE_SUM] = z.P * z.P / 256;
+        z.bytes = kMaxParts * 8 + (int64_t)z.blocks * (kBlock * 4 + 2 * z.P * z.P * 4) + z.P * z.P * 4;
+        return z;
+    }
     z.P = (z.p + kTile - 1) / kTile * kTile;
     z.Q = (z.q + kTile - 1) / kTile * kTile;
-    // 16384 values a partial sum, whole rows, at most 256 partial sums
-    int64_t n = ((int64_t)rows * cols + 16383) / 16384;
-    if (n > 256) n = 256;
-    if (n > rows) n = rows;
-    const int rp = (int)((rows + n - 1) / n);
-    z.parts = (rows + rp - 1) / rp;
-    const int64_t tp = z.P / kTile, tq = z.Q / kTile;
-    z.work[PRE_SQ] = z.parts;
-    z.work[PRE_PREP] = (int64_t)(z.P / 64) * (z.Q / 64);
+    const int tp = z.P / kTile, tq = z.Q / kTile;
+    z.work[PRE_PREP] = (z.P / 64) * (z.Q / 64);
     z.work[PRE_GRAM] = tp * (tp + 1) / 2;
     z.work[PRE_APPLY] = tp * tq;
-    z.bytes = 256 * 8 + (int64_t)z.P * z.Q * 4 * 3 + (int64_t)z.P * z.P * 4 * 2;
+    z.bytes = kMaxParts * 8 + (int64_t)z.P * z.Q * 4 * 3 + (int64_t)z.P * z.P * 4 * 2;
     return z;
 }
 
 struct NsChunk {                   // by value: the next matrices of the list
     int first, count;
     int64_t at;                    // workspace offset and running counts in front of them
-    int work[4];
+    int work[kPre];
     NsIn in[kNsChunk];
 };
 
+// One wave, one matrix a lane; the places come from running sums across the lanes.
 __global__ __launch_bounds__(64) void k_ns_table(NsChunk c, NsTable t, char *base)
 {
     const int i = threadIdx.x;
-    if (i >= c.count) return;
-    int64_t at = c.at;
-    int work[4] = {c.work[0], c.work[1], c.work[2], c.work[3]};
-    for (int j = 0; j < i; j++) {
-        const NsSize z = ns_size(c.in[j].rows, c.in[j].cols);
-        at += z.bytes;
-        for (int k = 0; k < 4; k++) work[k] += (int)z.work[k];
-    }
-    const NsSize z = ns_size(c.in[i].rows, c.in[i].cols);
+    const bool in = i < c.count;
     NsDev d;
-    d.in = c.in[i];
-    d.p = z.p; d.q = z.q; d.P = z.P; d.Q = z.Q; d.flip = z.flip; d.parts = z.parts;
-    char *b = base + at;
-    const int64_t pq = (int64_t)z.P * z.Q * 4, pp = (int64_t)z.P * z.P * 4;
+    d.in = c.in[in ? i : 0];
+    NsSize z = ns_size(d.in.rows, d.in.cols);
+    int64_t at = in ? z.bytes : 0;
+    int work[kPre];
+    for (int k = 0; k < kPre; k++) work[k] = in ? z.work[k] : 0;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t a = __shfl_up((long long)at, o, 64);
+        if (i >= o) at += a;
+        for (int k = 0; k < kPre; k++) {
+            const int w = __shfl_up(work[k], o, 64);
+            if (i >= o) work[k] += w;
+        }
+    }
+    if (!in) return;
+    d.p = z.p; d.q = z.q; d.P = z.P; d.Q = z.Q; d.flip = z.flip; d.parts = z.parts; d.blocks = z.blocks;
+    char *b = base + c.at + at - z.bytes;
     d.sq = (double *)b;
-    b += 256 * 8;
-    d.x = (h16 *)b;
-    d.xt[0] = (h16 *)(b + pq);
-    d.xt[1] = (h16 *)(b + 2 * pq);
-    d.g = (h16 *)(b + 3 * pq);
-    d.r = (h16 *)(b + 3 * pq + pp);
+    b += kMaxParts * 8;
+    d.x = d.xt[0] = d.xt[1] = d.g = d.r = nullptr;
+    d.part[0] = d.part[1] = d.sum = nullptr;
+    const int64_t pp = (int64_t)z.P * z.P * 4;
+    if (z.blocks) {
+        d.xt[0] = (h16 *)b;
+        b += (int64_t)z.blocks * kBlock * 4;
+        d.part[0] = (float *)b;
+        d.part[1] = (float *)(b + z.blocks * pp);
+        d.sum = (float *)(b + 2 * z.blocks * pp);
+    } else {
+        const int64_t pq = (int64_t)z.P * z.Q * 4;
+        d.x = (h16 *)b;
+        d.xt[0] = (h16 *)(b + pq);
+        d.xt[1] = (h16 *)(b + 2 * pq);
+        d.g = (h16 *)(b + 3 * pq);
+        d.r = (h16 *)(b + 3 * pq + pp);
+    }
     t.items[c.first + i] = d;
-    for (int k = 0; k < 4; k++) t.pre[k][c.first + i] = work[k];
+    for (int k = 0; k < kPre; k++) t.pre[k][c.first + i] = c.work[k] + work[k] - z.work[k];
 }
 
 // The matrix a work item belongs to: the last one whose running count is not
-// past it (the counts ascend; the wave compares 64 of them at a time).
+// past it (the counts ascend, matrices without work in a stage repeat their
+// successor's; the wave compares 64 of them at a time).
 __device__ __forceinline__ int ns_find(const int *pre, int count, int item)
 {
     const int lane = threadIdx.x & 63;
@@ -147,34 +193,70 @@ __device__ __forceinline__ float ns_u(float g, float buf, const NsStep &s)
 
 // Stage 1: the momentum (buf <- momentum buf + g) and the partial sums of u^2
 // (in float64: the squares of float32 values neither overflow nor vanish there).
+// A thread takes every 256th value of the part's rows, eight in flight, and
+// steps its row and column along without dividing.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_ns_squares(NsTable t, int count, NsStep s)
 {
+    constexpr int U = 8;
     __shared__ double red[kThreads / 64];
     const int it = ns_find(t.pre[PRE_SQ], count, blockIdx.x);
     const NsDev &d = t.items[it];
     const int part = blockIdx.x - t.pre[PRE_SQ][it];
     const int rows = d.in.rows, cols = d.in.cols, rp = (rows + d.parts - 1) / d.parts;
-    const int r0 = part * rp, r1 = min(rows, r0 + rp);
+    const int r1 = min(rows, part * rp + rp);
+    const int dr = kThreads / cols, dc = kThreads % cols;
+    int r = part * rp + (int)threadIdx.x / cols, c = (int)threadIdx.x % cols;
+    const void *src = d.in.src;
+    float *buf = d.in.buf;
+    const int64_t ls = d.in.ld_src, lb = d.in.ld_buf;
     double acc = 0.0;
-    const int64_t n = (int64_t)(r1 - r0) * cols;
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-        const int64_t r = r0 + i / cols;
-        const int c = (int)(i % cols);
-        const float g = ns_load<T>(d.in.src, r * d.in.ld_src + c);
-        float b = 0.f;
-        if (s.update) {
-            float *pb = d.in.buf + r * d.in.ld_buf + c;
-            b = __builtin_fmaf(s.momentum, *pb, g);
-            *pb = b;
+    while (r < r1) {
+        float g[U], b[U];
+        int64_t at[U];
+        bool in[U];
+        #pragma unroll
+        for (int u = 0; u < U; u++) {
+            in[u] = r < r1;
+            const int rr = in[u] ? r : r1 - 1, cc = in[u] ? c : 0;       // read and dropped
+            g[u] = ns_load<T>(src, rr * ls + cc);
+            at[u] = rr * lb + cc;
+            b[u] = s.update ? buf[at[u]] : 0.f;
+            r += dr;
+            c += dc;
+            if (c >= cols) { c -= cols; r++; }
         }
-        const double u = (double)ns_u(g, b, s);
-        acc += u * u;
+        #pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (!in[u]) continue;
+            if (s.update) {
+                b[u] = __builtin_fmaf(s.momentum, b[u], g[u]);
+                buf[at[u]] = b[u];
+            }
+            const double v = (double)ns_u(g[u], b[u], s);
+            acc += v * v;
+        }
     }
     for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
     if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = acc;
     __syncthreads();
     if (threadIdx.x == 0) d.sq[part] = red[0] + red[1] + red[2] + red[3];
+}
+
+// S / (||u||_F + eps) of a matrix, by all threads of the workgroup; red: one
+// double per wave.  Starts and ends without a barrier of its own around the
+// caller's LDS; contains one.
+template <int NT>
+__device__ __forceinline__ float ns_factor(const NsDev &d, float eps, double *red)
+{
+    double acc = 0.0;
+    for (int i = threadIdx.x; i < d.parts; i += NT) acc += d.sq[i];
+    for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
+    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = acc;
+    __syncthreads();
+    double sum = red[0];
+    for (int i = 1; i < NT / 64; i++) sum += red[i];
+    return (float)((double)kS / (sqrt(sum) + (double)eps));
 }
 
 // The pair of a value already scaled by S.  The empty asm makes v one float32
@@ -209,9 +291,6 @@ __global__ __launch_bounds__(kThreads) void k_ns_prepare(NsTable t, int count, N
     const int RP = d.flip ? d.Q : d.P, CP = d.flip ? d.P : d.Q;
     const int rb = w / (CP / 64) * 64, cb = w % (CP / 64) * 64;
     const int tid = threadIdx.x;
-    double acc = tid < d.parts ? d.sq[tid] : 0.0;
-    for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
-    if (tid % 64 == 0) red[tid / 64] = acc;
     for (int e = tid; e < 64 * 64; e += kThreads) {
         const int r = rb + e / 64, c = cb + e % 64;
         float u = 0.f;
@@ -221,9 +300,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_prepare(NsTable t, int count, N
         }
         tile[e / 64][e % 64] = u;
     }
-    __syncthreads();
-    const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
-    const float scale = (float)((double)kS / (norm + (double)s.eps));
+    const float scale = ns_factor<kThreads>(d, s.eps, red);              // (its barrier covers the tile)
     // as it is: [RP rows][K = CP]; turned: [CP rows][K = RP]
     h16 *straight = d.flip ? d.xt[0] : d.x, *turned = d.flip ? d.x : d.xt[0];
     for (int v = tid; v < 64 * 8; v += kThreads) {
@@ -239,6 +316,22 @@ __global__ __launch_bounds__(kThreads) void k_ns_prepare(NsTable t, int count, N
         *reinterpret_cast<vec16 *>(o + 32) = *reinterpret_cast<vec16 *>(lo);
     }
 }
+
+// The result o of element (row, col) of the caller's matrix: itself, or the
+// weight it steps (and the weight's bf16 copy).  lr is 0 without an update.
+template <typename W>
+__device__ __forceinline__ void ns_result(const NsIn &in, const NsStep &s, float lr, int64_t row, int col, float o)
+{
+    W *dst = (W *)in.dst + row * in.ld_dst + col;
+    float res = o;
+    if (s.update) {
+        res = __builtin_fmaf(-lr * in.scale, o, ns_load<W>(dst, 0) * (1.f - lr * s.decay));
+        if (in.copy) in.copy[row * in.ld_copy + col] = f2bf(res);
+    }
+    if constexpr (sizeof(W) == 4) *dst = res;
+    else *dst = f2bf(res);
+}
+__device__ __forceinline__ float ns_rate(const NsStep &s) { return !s.update ? 0.f : (s.lr_dev ? *s.lr_dev : s.lr); }
 
 // One product stage over the whole list.
 //   NS_GRAM    G = X X^T            (lower-triangle tiles, mirrored)
@@ -341,6 +434,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_ns_product(NsTable t, int coun
     }
 
     // lane l holds rows 4 (l / 16) .. + 3 of column l % 16 of each 16 x 16 block
+    const float lr = MODE == NS_LAST ? ns_rate(s) : 0.f;
     const int i0 = ti * BT + wm * TM + 4 * fc, j0 = tj * BT + wn * TN + fr;
     #pragma unroll
     for (int mi = 0; mi < MI; mi++)
@@ -352,22 +446,10 @@ __global__ __launch_bounds__(WM * WN * 64) void k_ns_product(NsTable t, int coun
             for (int e = 0; e < 4; e++) v[e] = acc[mi][nj][e] * kInvS;        // S times the product
             if constexpr (MODE == NS_LAST) {
                 if (j >= d.q) continue;
-                const float lr = s.update ? (s.lr_dev ? *s.lr_dev : s.lr) : 0.f;
                 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    if (i + e >= d.p) continue;
-                    const float o = v[e] * kInvS;
-                    const int64_t r = d.flip ? j : i + e, c = d.flip ? i + e : j;
-                    W *dst = (W *)d.in.dst + r * d.in.ld_dst + c;
-                    float res = o;
-                    if (s.update) {
-                        const float old = ns_load<W>(dst, 0);
-                        res = __builtin_fmaf(-lr * d.in.scale, o, old * (1.f - lr * s.decay));
-                        if (d.in.copy) d.in.copy[r * d.in.ld_copy + c] = f2bf(res);
-                    }
-                    if constexpr (sizeof(W) == 4) *dst = res;
-                    else *dst = f2bf(res);
-                }
+                for (int e = 0; e < 4; e++)
+                    if (i + e < d.p)
+                        ns_result<W>(d.in, s, lr, d.flip ? j : i + e, d.flip ? i + e : j, v[e] * kInvS);
             } else {
                 // straight: [i][j] with j along k; turned: [j][i]
                 h16 *st = MODE == NS_GRAM ? d.g : (MODE == NS_SQUARE ? d.r : d.x);
@@ -399,9 +481,357 @@ __global__ __launch_bounds__(WM * WN * 64) void k_ns_product(NsTable t, int coun
         }
 }
 
+// ---- narrow matrices (short side up to 128) --------------------------------
+// A workgroup owns a block of kBlock / P columns of X and keeps it, transposed,
+// in LDS ([column][P] pairs, 64 KiB) together with G or R.  One launch is one
+// whole step: the workgroup adds the partial Gram matrices of all blocks of its
+// matrix, forms R = a I + b G + c G G (each block for itself: 128^3 products
+// cost less than a launch), Y = R X over its block and the block's partial Gram
+// matrix of Y for the next step.  So a list of narrow matrices of any number
+// takes one launch per step where the wide path takes three.
+constexpr int kNwThreads = 512;
+template <int P> struct Nw {
+    static constexpr int QB = kBlock / P;
+    // row pitches in halves: 16 and 32 bytes past the pairs, so that the 16 rows
+    // of a fragment and the rows of a transposing read start in different banks
+    static constexpr int GP = 2 * P + 8, XP = 2 * P + 16;
+    static constexpr int XBytes = QB * XP * 2, LBytes = XBytes + P * GP * 2;
+    // waves over a P x P product and over R X
+    static constexpr int TM = P == 128 ? 32 : 16, TN = P == 128 ? 64 : (P == 64 ? 32 : 16), WN = P / TN;
+    static constexpr int YM = 32, YN = 64, YWN = QB / YN;
+    static_assert(P / YM * YWN == kNwThreads / 64, "R X tiles fill the waves");
+};
+constexpr int nw_max(int a, int b) { return a > b ? a : b; }
+constexpr int kNwLds = nw_max(Nw<128>::LBytes, nw_max(Nw<64>::LBytes, Nw<32>::LBytes));
+
+// halves offset of k (0 .. K) within a pair row
+__device__ __forceinline__ int nw_k(int k) { return (k >> 5) * 64 + (k & 31); }
+
+__device__ __forceinline__ f16x8 nw_frag(const h16 *p) { return *reinterpret_cast<const f16x8 *>(p); }
+
+// acc += A B^T over KS k steps, A rows at a, B rows at b (both contiguous along k)
+template <int MI, int NI, int KS>
+__device__ __forceinline__ void nw_product(const h16 *a, int pa, const h16 *b, int pb, f32x4 (&acc)[MI][NI])
+{
+    const int lane = threadIdx.x & 63, fr = lane % 16, fc = lane / 16;
+    a += fr * pa + fc * 8;
+    b += fr * pb + fc * 8;
+    #pragma unroll
+    for (int k = 0; k < KS; k++) {
+        f16x8 ah[MI], al[MI], bh[NI], bl[NI];
+        #pragma unroll
+        for (int i = 0; i < MI; i++) {
+            ah[i] = nw_frag(a + i * 16 * pa + k * 64);
+            al[i] = nw_frag(a + i * 16 * pa + k * 64 + 32);
+        }
+        #pragma unroll
+        for (int j = 0; j < NI; j++) {
+            bh[j] = nw_frag(b + j * 16 * pb + k * 64);
+            bl[j] = nw_frag(b + j * 16 * pb + k * 64 + 32);
+        }
+        #pragma unroll
+        for (int i = 0; i < MI; i++)
+            #pragma unroll
+            for (int j = 0; j < NI; j++) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
+            }
+    }
+}
+
+template <int MI, int NI>
+__device__ __forceinline__ void nw_zero(f32x4 (&acc)[MI][NI])
+{
+    #pragma unroll
+    for (int i = 0; i < MI; i++)
+        #pragma unroll
+        for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+// four consecutive values of a pair row
+__device__ __forceinline__ void nw_store4(h16 *p, const float *v)
+{
+    h16 hi[4], lo[4];
+    #pragma unroll
+    for (int e = 0; e < 4; e++) ns_pair(v[e], hi[e], lo[e]);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
+    *reinterpret_cast<uint2 *>(p + 32) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+}
+__device__ __forceinline__ void nw_load4(const h16 *p, float *v)
+{
+    const f16x4 hi = *reinterpret_cast<const f16x4 *>(p), lo = *reinterpret_cast<const f16x4 *>(p + 32);
+    #pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = (float)hi[e] + (float)lo[e];
+}
+
+// The block in LDS to the workspace, and its partial Gram matrix (S^2 times it).
+template <int P>
+__device__ __forceinline__ void nw_gram(const NsDev &d, int block, const h16 *xs, float *part)
+{
+    using N = Nw<P>;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    h16 *out = d.xt[0] + (int64_t)block * kBlock * 2;
+    #pragma unroll
+    for (int l = 0; l < kBlock * 4 / 16 / kNwThreads; l++) {
+        const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
+        *reinterpret_cast<vec16 *>(out + (int64_t)v * 8) = *reinterpret_cast<const vec16 *>(xs + row * N::XP + c * 8);
+    }
+    constexpr int MI = N::TM / 16, NI = N::TN / 16;
+    const int wm = wave / N::WN, wn = wave % N::WN;
+    if (wm * N::TM >= P) return;                 // P = 32: four waves have a tile
+    f32x4 acc[MI][NI];
+    nw_zero(acc);
+    // fragments of 8 consecutive block columns of one row of X: transposing reads
+    const int g = lane / 16, q = lane % 16;
+    const h16 *base = xs + (8 * g + q / 4) * N::XP + 4 * (q % 4);
+    auto frag = [&](int k, int i, int part_) __attribute__((always_inline)) {
+        return __builtin_bit_cast(f16x8, tr_frag(base + k * 32 * N::XP + nw_k(i) + part_ * 32, N::XP));
+    };
+    #pragma unroll 4
+    for (int k = 0; k < N::QB / 32; k++) {
+        f16x8 ah[MI], al[MI], bh[NI], bl[NI];
+        #pragma unroll
+        for (int i = 0; i < MI; i++) {
+            ah[i] = frag(k, wm * N::TM + i * 16, 0);
+            al[i] = frag(k, wm * N::TM + i * 16, 1);
+        }
+        #pragma unroll
+        for (int j = 0; j < NI; j++) {
+            bh[j] = frag(k, wn * N::TN + j * 16, 0);
+            bl[j] = frag(k, wn * N::TN + j * 16, 1);
+        }
+        #pragma unroll
+        for (int i = 0; i < MI; i++)
+            #pragma unroll
+            for (int j = 0; j < NI; j++) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
+            }
+    }
+    // symmetric: element (i, j) goes to row j, where a lane's four i are consecutive
+    float *o = part + (int64_t)block * P * P;
+    #pragma unroll
+    for (int i = 0; i < MI; i++)
+        #pragma unroll
+        for (int j = 0; j < NI; j++)
+            *reinterpret_cast<f32x4 *>(o + (wn * N::TN + j * 16 + q) * P + wm * N::TM + i * 16 + 4 * g) = acc[i][j];
+}
+
+// Stage 2 of a narrow matrix: X's block as pairs, and its partial Gram matrix.
+template <int P, typename T>
+__device__ __forceinline__ void nw_prepare(const NsDev &d, int block, const NsStep &s, h16 *xs, double *red)
+{
+    using N = Nw<P>;
+    const int tid = threadIdx.x, j0 = block * N::QB;
+    const float scale = ns_factor<kNwThreads>(d, s.eps, red);
+    // e runs along the caller's rows: over P where X is its transpose, else over the block's columns
+    constexpr int U = 8;
+    for (int e0 = tid; e0 < kBlock; e0 += U * kNwThreads) {
+        float u[U];
+        #pragma unroll
+        for (int k = 0; k < U; k++) {
+            const int e = e0 + k * kNwThreads;
+            const int i = d.flip ? e % P : e / N::QB, j = d.flip ? e / P : e % N::QB;
+            const bool in = i < d.p && j0 + j < d.q;
+            const int64_t r = in ? (d.flip ? j0 + j : i) : 0, c = in ? (d.flip ? i : j0 + j) : 0;
+            const float g = ns_load<T>(d.in.src, r * d.in.ld_src + c);
+            const float b = s.update ? d.in.buf[r * d.in.ld_buf + c] : 0.f;
+            u[k] = in ? ns_u(g, b, s) : 0.f;
+        }
+        #pragma unroll
+        for (int k = 0; k < U; k++) {
+            const int e = e0 + k * kNwThreads;
+            const int i = d.flip ? e % P : e / N::QB, j = d.flip ? e / P : e % N::QB;
+            h16 hi, lo;
+            ns_pair(u[k] * scale, hi, lo);
+            h16 *o = xs + j * N::XP + nw_k(i);
+            o[0] = hi;
+            o[32] = lo;
+        }
+    }
+    __syncthreads();
+    nw_gram<P>(d, block, xs, d.part[0]);
+}
+
+template <int P, bool LAST, typename W>
+__device__ __forceinline__ void nw_step(const NsDev &d, int block, const NsStep &s, int turn, h16 *xs)
+{
+    using N = Nw<P>;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int g = lane / 16, q = lane % 16;
+    h16 *gs = xs + N::QB * N::XP;
+    // the block and the partial sums, all loads before the first use
+    constexpr int XL = kBlock * 4 / 16 / kNwThreads;
+    vec16 xv[XL];
+    const h16 *xin = d.xt[0] + (int64_t)block * kBlock * 2;
+    #pragma unroll
+    for (int l = 0; l < XL; l++) xv[l] = ldg16(xin + (int64_t)(l * kNwThreads + tid) * 8);
+    const bool summed = d.blocks > kSumBlocks;
+    const float *part = summed ? d.sum : d.part[turn];
+    const int np = summed ? 1 : d.blocks;
+    constexpr int GV = P * P / 4, GL = (GV + kNwThreads - 1) / kNwThreads;
+    f32x4 gv[GL];
+    #pragma unroll
+    for (int l = 0; l < GL; l++) {
+        const int v = l * kNwThreads + tid;
+        gv[l] = *reinterpret_cast<const f32x4 *>(part + (int64_t)(v < GV ? v : 0) * 4);
+    }
+    for (int b = 1; b < np; b++)
+        #pragma unroll
+        for (int l = 0; l < GL; l++) {
+            const int v = l * kNwThreads + tid;
+            const f32x4 w = *reinterpret_cast<const f32x4 *>(part + (int64_t)b * P * P + (int64_t)(v < GV ? v : 0) * 4);
+            gv[l][0] += w[0]; gv[l][1] += w[1]; gv[l][2] += w[2]; gv[l][3] += w[3];
+        }
+    #pragma unroll
+    for (int l = 0; l < XL; l++) {
+        const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
+        *reinterpret_cast<vec16 *>(xs + row * N::XP + c * 8) = xv[l];
+    }
+    #pragma unroll
+    for (int l = 0; l < GL; l++) {
+        const int v = l * kNwThreads + tid;
+        if (v < GV) {
+            const int row = v / (P / 4), c = v % (P / 4) * 4;
+            float f[4];
+            #pragma unroll
+            for (int e = 0; e < 4; e++) f[e] = gv[l][e] * kInvS;
+            nw_store4(gs + row * N::GP + nw_k(c), f);
+        }
+    }
+    __syncthreads();
+    // R = a I + b G + c G G, over G's place
+    {
+        constexpr int MI = N::TM / 16, NI = N::TN / 16;
+        const int wm = wave / N::WN, wn = wave % N::WN;
+        const bool has = wm * N::TM < P;
+        f32x4 acc[MI][NI];
+        nw_zero(acc);
+        if (has) {
+            nw_product<MI, NI, P / 32>(gs + wm * N::TM * N::GP, N::GP, gs + wn * N::TN * N::GP, N::GP, acc);
+            #pragma unroll
+            for (int i = 0; i < MI; i++)
+                #pragma unroll
+                for (int j = 0; j < NI; j++) {
+                    const int row = wn * N::TN + j * 16 + q, col = wm * N::TM + i * 16 + 4 * g;
+                    float gg[4];
+                    nw_load4(gs + row * N::GP + nw_k(col), gg);
+                    #pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        acc[i][j][e] = __builtin_fmaf(s.c, acc[i][j][e] * kInvS, s.b * gg[e]) +
+                                       (row == col + e ? s.a * kS : 0.f);
+                }
+        }
+        __syncthreads();
+        if (has)
+            #pragma unroll
+            for (int i = 0; i < MI; i++)
+                #pragma unroll
+                for (int j = 0; j < NI; j++) {
+                    const int row = wn * N::TN + j * 16 + q, col = wm * N::TM + i * 16 + 4 * g;
+                    const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                    nw_store4(gs + row * N::GP + nw_k(col), v);
+                }
+        __syncthreads();
+    }
+    // Y = R X
+    constexpr int MI = N::YM / 16, NI = N::YN / 16;
+    const int ym = wave / N::YWN * N::YM, yn = wave % N::YWN * N::YN;
+    f32x4 acc[MI][NI];
+    nw_zero(acc);
+    nw_product<MI, NI, P / 32>(gs + ym * N::GP, N::GP, xs + yn * N::XP, N::XP, acc);
+    __syncthreads();
+    if constexpr (!LAST) {
+        #pragma unroll
+        for (int i = 0; i < MI; i++)
+            #pragma unroll
+            for (int j = 0; j < NI; j++) {
+                float v[4];
+                #pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = acc[i][j][e] * kInvS;
+                nw_store4(xs + (yn + j * 16 + q) * N::XP + nw_k(ym + i * 16 + 4 * g), v);
+            }
+        __syncthreads();
+        nw_gram<P>(d, block, xs, d.part[turn ^ 1]);
+    } else {
+        // through LDS, so that rows of the caller's matrix are written whole
+        constexpr int FP = P + 1;
+        float *fs = (float *)xs;
+        #pragma unroll
+        for (int i = 0; i < MI; i++)
+            #pragma unroll
+            for (int j = 0; j < NI; j++)
+                #pragma unroll
+                for (int e = 0; e < 4; e++)
+                    fs[(yn + j * 16 + q) * FP + ym + i * 16 + 4 * g + e] = acc[i][j][e] * (kInvS * kInvS);
+        __syncthreads();
+        const float lr = ns_rate(s);
+        const int j0 = block * N::QB;
+        for (int e = tid; e < kBlock; e += kNwThreads) {
+            const int i = d.flip ? e % P : e / N::QB, j = d.flip ? e / P : e % N::QB;
+            if (i < d.p && j0 + j < d.q)
+                ns_result<W>(d.in, s, lr, d.flip ? j0 + j : i, d.flip ? i : j0 + j, fs[j * FP + i]);
+        }
+    }
+}
+static_assert(Nw<128>::QB * (128 + 1) * 4 <= Nw<128>::XBytes && Nw<64>::QB * (64 + 1) * 4 <= Nw<64>::XBytes &&
+              Nw<32>::QB * (32 + 1) * 4 <= Nw<32>::XBytes, "the result's staging fits the block's place");
+
+enum { NW_PREPARE = 0, NW_STEP = 1, NW_LAST = 2 };
+
+// T: the source type (NW_PREPARE) or the result type (NW_LAST)
+template <int STAGE, typename T>
+__global__ __launch_bounds__(kNwThreads) void k_ns_narrow(NsTable t, int count, NsStep s, int turn)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ double red[kNwThreads / 64];
+    h16 *xs = (h16 *)smem;
+    const int work = xcd_remap(blockIdx.x, gridDim.x);
+    const int it = ns_find(t.pre[PRE_NARROW], count, work);
+    const NsDev &d = t.items[it];
+    const int block = work - t.pre[PRE_NARROW][it];
+    auto go = [&](auto tag) __attribute__((always_inline)) {
+        constexpr int P = decltype(tag)::value;
+        if constexpr (STAGE == NW_PREPARE) nw_prepare<P, T>(d, block, s, xs, red);
+        else nw_step<P, STAGE == NW_LAST, T>(d, block, s, turn, xs);
+    };
+    if (d.P == 128) go(std::integral_constant<int, 128>{});
+    else if (d.P == 64) go(std::integral_constant<int, 64>{});
+    else go(std::integral_constant<int, 32>{});
+}
+
+// The sum of a narrow matrix's partial Gram matrices: 64 float4 outputs a
+// workgroup, each added by four threads over a quarter of the blocks.
+__global__ __launch_bounds__(kThreads) void k_ns_sum(NsTable t, int count, int turn)
+{
+    __shared__ f32x4 red[kThreads];
+    const int it = ns_find(t.pre[PRE_SUM], count, blockIdx.x);
+    const NsDev &d = t.items[it];
+    const int w = blockIdx.x - t.pre[PRE_SUM][it], tid = threadIdx.x;
+    const int64_t pp = (int64_t)d.P * d.P;
+    const float *src = d.part[turn] + ((int64_t)w * 64 + tid % 64) * 4;
+    const int quarter = tid / 64;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    #pragma unroll 4
+    for (int b = quarter; b < d.blocks; b += 4) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(src + b * pp);
+        acc[0] += v[0]; acc[1] += v[1]; acc[2] += v[2]; acc[3] += v[3];
+    }
+    red[tid] = acc;
+    __syncthreads();
+    if (tid < 64) {
+        f32x4 o = red[tid];
+        for (int k = 1; k < 4; k++)
+            for (int e = 0; e < 4; e++) o[e] += red[k * 64 + tid][e];
+        *reinterpret_cast<f32x4 *>(d.sum + ((int64_t)w * 64 + tid) * 4) = o;
+    }
+}
+
 size_t table_bytes(int count)
 {
-    const size_t a = (size_t)count * sizeof(NsDev), b = (size_t)count * 4 * sizeof(int);
+    const size_t a = (size_t)count * sizeof(NsDev), b = (size_t)count * kPre * sizeof(int);
     return (a + b + 255) / 256 * 256;
 }
 
@@ -412,8 +842,8 @@ void ns_plan_add(NsPlan &p, int rows, int cols)
     const NsSize z = ns_size(rows, cols);
     p.count++;
     p.bytes += z.bytes;
-    for (int k = 0; k < 4; k++) p.work[k] += z.work[k];
-    p.flops += (double)z.p * (z.p + 1) * z.q + (double)z.p * z.p * (z.p + 1) + 2.0 * z.p * z.p * z.q;
+    for (int k = 0; k < kPre; k++) p.work[k] += z.work[k];
+    (z.blocks ? p.narrow_flops : p.flops) += (double)z.p * (z.p + 1) * z.q + (double)z.p * z.p * (z.p + 1) + 2.0 * z.p * z.p * z.q;
     p.values += (double)rows * cols;
 }
 
@@ -426,7 +856,7 @@ NsTable ns_table(void *ws, int count)
     NsTable t;
     t.items = (NsDev *)ws;
     int *pre = (int *)((char *)ws + (size_t)count * sizeof(NsDev));
-    for (int k = 0; k < 4; k++) t.pre[k] = pre + (size_t)k * count;
+    for (int k = 0; k < kPre; k++) t.pre[k] = pre + (size_t)k * count;
     return t;
 }
 
@@ -439,6 +869,34 @@ hipError_t ns_product(const NsPlan &p, const NsTable &t, const NsStep &s, int tu
     return hipGetLastError();
 }
 
+// p: the kernel's launch over the narrow matrices (more LDS than the default limit)
+template <int STAGE, typename T>
+hipError_t ns_narrow(const NsPlan &p, const NsTable &t, const NsStep &s, int turn, hipStream_t st)
+{
+    auto kern = k_ns_narrow<STAGE, T>;
+    static std::atomic<uint64_t> ready{0};       // one bit per device
+    int dev = 0;
+    if (hipError_t e = hipGetDevice(&dev)) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(ready.load(std::memory_order_relaxed) & bit)) {
+        if (hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kNwLds))
+            return e;
+        ready.fetch_or(bit, std::memory_order_relaxed);
+    }
+    TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, STAGE == NW_PREPARE ? 0.0 : p.narrow_flops);
+    hipLaunchKernelGGL(kern, dim3((unsigned)p.work[PRE_NARROW]), dim3(kNwThreads), kNwLds, st, t, p.count, s, turn);
+    return hipGetLastError();
+}
+
+// the sums in front of a narrow step, where a matrix has many blocks
+hipError_t ns_sum(const NsPlan &p, const NsTable &t, int turn, hipStream_t st)
+{
+    if (!p.work[PRE_SUM]) return hipSuccess;
+    TraceScope tr(KC_SMALL, KID_ORTHO, st, 0.0, 0.0);
+    hipLaunchKernelGGL(k_ns_sum, dim3((unsigned)p.work[PRE_SUM]), dim3(kThreads), 0, st, t, p.count, turn);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep &s, int src_dtype, int dst_dtype,
@@ -447,7 +905,7 @@ hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep
     const NsTable t = ns_table(ws, p.count);
     NsChunk c;
     c.at = (int64_t)table_bytes(p.count);
-    for (int k = 0; k < 4; k++) c.work[k] = 0;
+    for (int k = 0; k < kPre; k++) c.work[k] = 0;
     for (c.first = 0; c.first < p.count; c.first += kNsChunk) {
         c.count = p.count - c.first < kNsChunk ? p.count - c.first : kNsChunk;
         for (int i = 0; i < c.count; i++) c.in[i] = fill(arg, c.first + i);
@@ -457,7 +915,7 @@ hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep
         for (int i = 0; i < c.count; i++) {
             const NsSize z = ns_size(c.in[i].rows, c.in[i].cols);
             c.at += z.bytes;
-            for (int k = 0; k < 4; k++) c.work[k] += (int)z.work[k];
+            for (int k = 0; k < kPre; k++) c.work[k] += z.work[k];
         }
     }
     const double es = src_dtype == DT_BF16 ? 2.0 : 4.0;
@@ -467,6 +925,19 @@ hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep
         hipLaunchKernelGGL(kern, dim3((unsigned)p.work[PRE_SQ]), dim3(kThreads), 0, st, t, p.count, s);
         if (hipError_t e = hipGetLastError()) return e;
     }
+    if (p.work[PRE_NARROW]) {
+        hipError_t e = src_dtype == DT_BF16 ? ns_narrow<NW_PREPARE, bf16_t>(p, t, s, 0, st)
+                                            : ns_narrow<NW_PREPARE, float>(p, t, s, 0, st);
+        for (int k = 0, turn = 0; k < s.steps && e == hipSuccess; k++, turn ^= 1) {
+            e = ns_sum(p, t, turn, st);
+            if (e != hipSuccess) break;
+            if (k + 1 < s.steps) e = ns_narrow<NW_STEP, float>(p, t, s, turn, st);
+            else if (dst_dtype == DT_BF16) e = ns_narrow<NW_LAST, bf16_t>(p, t, s, turn, st);
+            else e = ns_narrow<NW_LAST, float>(p, t, s, turn, st);
+        }
+        if (e != hipSuccess) return e;
+    }
+    if (!p.work[PRE_GRAM]) return hipSuccess;
     {
         TraceScope tr(KC_SWEEP, KID_ORTHO, st, p.values * (es + (s.update ? 4.0 : 0.0) + 8.0), 0.0);
         auto kern = src_dtype == DT_BF16 ? k_ns_prepare<bf16_t> : k_ns_prepare<float>;

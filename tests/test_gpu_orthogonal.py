@@ -68,7 +68,8 @@ def _strided(t, dtype, pad):
 
 SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (1, 5000), (16, 16), (17, 33), (31, 32), (33, 31), (64, 64), (65, 63),
           (96, 128), (128, 96), (127, 129), (128, 128), (129, 200), (1152, 32), (255, 257), (256, 256), (300, 40),
-          (64, 1000), (513, 130), (260, 700), (1025, 515), (513, 1200)]
+          (64, 1000), (513, 130), (260, 700), (1025, 515), (513, 1200), (100, 1500), (1100, 128), (20, 5000), (3000, 60),
+          (128, 2100)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
