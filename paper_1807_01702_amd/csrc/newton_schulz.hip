@@ -388,6 +388,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_ns_product(NsTable t, int coun
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(src[l] + (int64_t)step * kRow),
                                              (__attribute__((address_space(3))) uint32_t *)(stage + (l * NT + wave * 64) * 16),
                                              16, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);       // (the scheduler would sink them to the barrier that waits for them)
     };
     const int wm = wave / WN, wn = wave % WN;
     const int fr = lane % 16, fc = lane / 16;    // fragment row and k chunk of this lane
