@@ -313,7 +313,7 @@ struct NsStep {                   // one call's numbers
 };
 // what a list needs: filled matrix by matrix, then the workspace and the grids follow
 struct NsPlan {
-    int count;
+    int count, short_side, long_side;             // longest padded sides of the wide matrices
     int64_t bytes, work[kNsStages];
     double flops, narrow_flops, values;    // per step: wide, narrow matrices; matrix elements
 };

@@ -339,35 +339,154 @@ __device__ __forceinline__ float ns_rate(const NsStep &s) { return !s.update ? 0
 //   NS_APPLY   X, X^T <- R X
 //   NS_LAST    R X into the caller's matrix
 enum { NS_GRAM = 0, NS_SQUARE = 1, NS_APPLY = 2, NS_LAST = 3 };
+constexpr bool ns_sym(int mode) { return mode == NS_GRAM || mode == NS_SQUARE; }
 
-// Workgroup: BT x BT outputs by WM x WN waves.  Two LDS stages of 2 BT rows of
-// 128 bytes (one k step of both operands); the 16-byte chunks of a row are
-// stored in the order chunk ^ (row % 8), so the 16 rows of a fragment read lie
-// in different banks.  The next step's lines are loaded straight into LDS while
-// the current step multiplies.
-template <int BT, int WM, int WN, int MODE, typename W>
-__global__ __launch_bounds__(WM * WN * 64) void k_ns_product(NsTable t, int count, NsStep s, int turn)
+// How a stage's tiles run.  The chip holds kNsSlots workgroups of the product
+// kernel at once.  Whole tiles fill as many rounds of that as they can; the rest
+// (tiles [whole, tiles)) would leave most of the chip idle for a round, so each
+// of them is cut into `pieces` along k: a piece's float32 sums go to the
+// workspace and k_ns_finish adds them in a fixed order.
+struct NsCut { int tiles, whole, pieces; float *part; };
+constexpr int kPart = kTile * kTile;             // values of a piece
+
+// the tile of a stage: its matrix and its block row and column
+struct NsPlace { int it, ti, tj; };
+template <int MODE>
+__device__ __forceinline__ NsPlace ns_place(const NsTable &t, int count, int tile)
 {
-    constexpr int NT = WM * WN * 64, TM = BT / WM, TN = BT / WN, MI = TM / 16, NI = TN / 16;
-    constexpr int kRow = 128, kStage = 2 * BT * kRow, kLoads = kStage / (NT * 16);
-    constexpr bool SYM = MODE == NS_GRAM || MODE == NS_SQUARE;
-    __shared__ __align__(16) unsigned char lds0[kStage], lds1[kStage];
-    const int work = xcd_remap(blockIdx.x, gridDim.x);
-    const int *pre = t.pre[SYM ? PRE_GRAM : PRE_APPLY];
-    const int it = ns_find(pre, count, work);
-    const NsDev &d = t.items[it];
-    const int w = work - pre[it];
-    const int P = d.P, Q = d.Q;
-    int ti, tj;
-    if (SYM) {                                   // row i of the triangle starts at i (i + 1) / 2
-        ti = (int)((sqrtf(8.f * (float)w + 1.f) - 1.f) * 0.5f);
+    const int *pre = t.pre[ns_sym(MODE) ? PRE_GRAM : PRE_APPLY];
+    NsPlace pl;
+    pl.it = ns_find(pre, count, tile);
+    const int w = tile - pre[pl.it];
+    if (ns_sym(MODE)) {                          // row i of the triangle starts at i (i + 1) / 2
+        int ti = (int)((sqrtf(8.f * (float)w + 1.f) - 1.f) * 0.5f);
         while ((ti + 1) * (ti + 2) / 2 <= w) ti++;
         while (ti * (ti + 1) / 2 > w) ti--;
-        tj = w - ti * (ti + 1) / 2;
+        pl.ti = ti;
+        pl.tj = w - ti * (ti + 1) / 2;
     } else {
-        ti = w % (P / BT);
-        tj = w / (P / BT);
+        const int tp = t.items[pl.it].P / kTile;
+        pl.ti = w % tp;
+        pl.tj = w / tp;
     }
+    return pl;
+}
+
+// 64 x 64 results in LDS, turned: row j holds the 64 i as pairs (two k blocks of
+// [hi 32 | lo 32], 256 bytes) or as float32, its 16-byte chunks in the order
+// chunk ^ (j % 16), so that 16 rows of one column lie in different banks.
+constexpr int kSub = 64, kSubBytes = kSub * 256;
+__device__ __forceinline__ int sub_at(int j, int byte) { return j * 256 + ((byte >> 4 ^ (j & 15)) << 4) + (byte & 15); }
+
+// Results [MI][NI] of 16 x 16 blocks (a lane holds rows 4 g .. + 3 of column q)
+// into the sub-tile at block column nj0.  v(e, value, i, j) gives what is kept
+// of S times the product at (i, j) of the sub-tile.
+template <int MODE, int MI, int NI>
+__device__ __forceinline__ void sub_put(unsigned char *sub, const f32x4 (&acc)[MI][NI], int nj0, const NsDev &d,
+                                        const NsStep &s, int i0, int j0)
+{
+    const int lane = threadIdx.x & 63, g = lane / 16, q = lane % 16;
+    #pragma unroll
+    for (int nj = 0; nj < NI; nj++)
+        #pragma unroll
+        for (int mi = 0; mi < MI; mi++) {
+            const int i = mi * 16 + 4 * g, j = (nj0 + nj) * 16 + q;
+            float v[4];
+            #pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = acc[mi][nj][e] * kInvS;
+            if constexpr (MODE == NS_SQUARE) {
+                float gg[4];                     // G is symmetric: row j holds the four i together
+                const h16 *p = d.g + ns_at(j0 + j, i0 + i, d.P);
+                const f16x4 hi = *reinterpret_cast<const f16x4 *>(p), lo = *reinterpret_cast<const f16x4 *>(p + 32);
+                #pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    gg[e] = (float)hi[e] + (float)lo[e];
+                    v[e] = __builtin_fmaf(s.c, v[e], s.b * gg[e]) + (i0 + i + e == j0 + j ? s.a * kS : 0.f);
+                }
+            }
+            if constexpr (MODE == NS_LAST) {
+                f32x4 o = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
+                *reinterpret_cast<f32x4 *>(sub + sub_at(j, i * 4)) = o;
+            } else {
+                h16 hi[4], lo[4];
+                #pragma unroll
+                for (int e = 0; e < 4; e++) ns_pair(v[e], hi[e], lo[e]);
+                const int byte = (i >> 5) * 128 + (i & 31) * 2;
+                *reinterpret_cast<uint2 *>(sub + sub_at(j, byte)) =
+                    make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
+                *reinterpret_cast<uint2 *>(sub + sub_at(j, byte + 64)) =
+                    make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+            }
+        }
+}
+
+// The sub-tile to memory by waves first .. first + NW - 1 of the workgroup, w
+// this wave's number among them: rows of 256 bytes as they lie, and the other
+// orientation through transposing reads.  i0, j0: the sub-tile's place in the result.
+template <int MODE, int NW, typename W>
+__device__ __forceinline__ void sub_out(const unsigned char *sub, int w, const NsDev &d, const NsStep &s, int turn,
+                                        bool mirror, int i0, int j0)
+{
+    const int lane = threadIdx.x & 63, g = lane / 16, q = lane % 16;
+    if constexpr (MODE == NS_LAST) {
+        const float lr = ns_rate(s);
+        #pragma unroll 4
+        for (int k = w; k < kSub; k += NW) {     // one row of the caller's matrix a step
+            const int i = d.flip ? lane : k, j = d.flip ? k : lane;
+            const float o = *reinterpret_cast<const float *>(sub + sub_at(j, i * 4));
+            if (i0 + i < d.p && j0 + j < d.q)
+                ns_result<W>(d.in, s, lr, d.flip ? j0 + j : i0 + i, d.flip ? i0 + i : j0 + j, o);
+        }
+    } else {
+        h16 *straight = MODE == NS_GRAM ? d.g : (MODE == NS_SQUARE ? d.r : d.x);
+        h16 *turned = MODE == NS_APPLY ? d.xt[turn ^ 1] : straight;
+        const int ks = ns_sym(MODE) ? d.P : d.Q;
+        #pragma unroll
+        for (int k = w; k < 16; k += NW) {
+            const int j = k * 4 + lane / 16, c = lane % 16;
+            const vec16 v = *reinterpret_cast<const vec16 *>(sub + sub_at(j, c * 16));
+            *reinterpret_cast<vec16 *>(turned + ns_at(j0 + j, i0, d.P) + c * 8) = v;
+        }
+        if (!mirror) return;
+        // 16 i x 32 j a step: a lane gets 8 consecutive j of one i
+        #pragma unroll
+        for (int k = w; k < 16; k += NW) {
+            const int i = (k >> 2) * 16, jb = (k >> 1 & 1) * 32, part = k & 1;
+            const int byte = (i >> 5) * 128 + (i & 31) * 2 + part * 64 + 8 * (q % 4), j = jb + 8 * g + q / 4;
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sub + sub_at(j, byte)));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sub + sub_at(j + 4, byte)));
+            const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            *reinterpret_cast<s16x8 *>(straight + ns_at(i0 + i + q, j0 + jb + 8 * g, ks) + part * 32) = v;
+        }
+    }
+}
+
+// Workgroup: a tile of 128 x 128 outputs by 2 x 2 waves of 64 x 64, or a piece
+// of one.  Two LDS stages of 256 rows of 128 bytes (one k step of both
+// operands); the 16-byte chunks of a row are stored in the order
+// chunk ^ (row % 8), so the 16 rows of a fragment read lie in different banks.
+// The next step's lines are loaded straight into LDS while the current step
+// multiplies.
+template <int MODE, typename W>
+__global__ __launch_bounds__(256) void k_ns_product(NsTable t, int count, NsStep s, int turn, NsCut cut)
+{
+    constexpr int BT = kTile, NT = 256, TM = 64, TN = 64, MI = TM / 16, NI = TN / 16;
+    constexpr int kRow = 128, kStage = 2 * BT * kRow, kLoads = kStage / (NT * 16);
+    static_assert(kStage == 2 * kSubBytes, "two waves' results fit a stage");
+    __shared__ __align__(16) unsigned char lds0[kStage], lds1[kStage];
+    int tile, piece = 0, pieces = 1;
+    if ((int)blockIdx.x < cut.whole) {
+        tile = xcd_remap(blockIdx.x, cut.whole);
+    } else {
+        const int u = blockIdx.x - cut.whole;
+        pieces = cut.pieces;
+        tile = cut.whole + u / pieces;
+        piece = u % pieces;
+    }
+    const NsPlace pl = ns_place<MODE>(t, count, tile);
+    const NsDev &d = t.items[pl.it];
+    const int P = d.P, Q = d.Q, ti = pl.ti, tj = pl.tj;
     const int K = MODE == NS_GRAM ? Q : P;
     const h16 *pa = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.r);
     const h16 *pb = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.xt[turn]);
@@ -390,7 +509,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_ns_product(NsTable t, int coun
                                              16, 0, 0);
         __builtin_amdgcn_sched_barrier(0);       // (the scheduler would sink them to the barrier that waits for them)
     };
-    const int wm = wave / WN, wn = wave % WN;
+    const int wm = wave / 2, wn = wave % 2;
     const int fr = lane % 16, fc = lane / 16;    // fragment row and k chunk of this lane
     f32x4 acc[MI][NI];
     #pragma unroll
@@ -422,64 +541,63 @@ __global__ __launch_bounds__(WM * WN * 64) void k_ns_product(NsTable t, int coun
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
             }
     };
-    const int steps = K / 32;                    // even: K is a multiple of 64
-    load(lds0, 0);
-    __syncthreads();
-    for (int k = 0; k < steps; k += 2) {
-        load(lds1, k + 1);
-        multiply(lds0);
+    // steps in pairs (K is a multiple of 128); a piece may have none
+    const int pairs = K / 64, k0 = piece * pairs / pieces * 2, k1 = (piece + 1) * pairs / pieces * 2;
+    if (k0 < k1) {
+        load(lds0, k0);
         __syncthreads();
-        if (k + 2 < steps) load(lds0, k + 2);
-        multiply(lds1);
-        __syncthreads();
-    }
-
-    // lane l holds rows 4 (l / 16) .. + 3 of column l % 16 of each 16 x 16 block
-    const float lr = MODE == NS_LAST ? ns_rate(s) : 0.f;
-    const int i0 = ti * BT + wm * TM + 4 * fc, j0 = tj * BT + wn * TN + fr;
-    #pragma unroll
-    for (int mi = 0; mi < MI; mi++)
-        #pragma unroll
-        for (int nj = 0; nj < NI; nj++) {
-            const int i = i0 + mi * 16, j = j0 + nj * 16;
-            float v[4];
-            #pragma unroll
-            for (int e = 0; e < 4; e++) v[e] = acc[mi][nj][e] * kInvS;        // S times the product
-            if constexpr (MODE == NS_LAST) {
-                if (j >= d.q) continue;
-                #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (i + e < d.p)
-                        ns_result<W>(d.in, s, lr, d.flip ? j : i + e, d.flip ? i + e : j, v[e] * kInvS);
-            } else {
-                // straight: [i][j] with j along k; turned: [j][i]
-                h16 *st = MODE == NS_GRAM ? d.g : (MODE == NS_SQUARE ? d.r : d.x);
-                h16 *tu = MODE == NS_GRAM ? d.g : (MODE == NS_SQUARE ? d.r : d.xt[turn ^ 1]);
-                const int ks = SYM ? P : Q;
-                if constexpr (MODE == NS_SQUARE) {
-                    #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const h16 *g = d.g + ns_at(i + e, j, P);
-                        const float gv = (float)__builtin_bit_cast(_Float16, g[0]) + (float)__builtin_bit_cast(_Float16, g[32]);
-                        v[e] = __builtin_fmaf(s.c, v[e], s.b * gv) + (i + e == j ? s.a * kS : 0.f);
-                    }
-                }
-                h16 hi[4], lo[4];
-                #pragma unroll
-                for (int e = 0; e < 4; e++) ns_pair(v[e], hi[e], lo[e]);
-                #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    h16 *o = st + ns_at(i + e, j, ks);
-                    o[0] = hi[e];
-                    o[32] = lo[e];
-                }
-                if (!SYM || ti != tj) {
-                    h16 *o = tu + ns_at(j, i, P);
-                    *reinterpret_cast<uint2 *>(o) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
-                    *reinterpret_cast<uint2 *>(o + 32) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
-                }
-            }
+        for (int k = k0; k < k1; k += 2) {
+            load(lds1, k + 1);
+            multiply(lds0);
+            __syncthreads();
+            if (k + 2 < k1) load(lds0, k + 2);
+            multiply(lds1);
+            __syncthreads();
         }
+    }
+    if (pieces > 1) {                            // in the order of the fragments: [wave][block][lane]
+        float *o = cut.part + (int64_t)(blockIdx.x - cut.whole) * kPart + wave * (kSub * kSub);
+        #pragma unroll
+        for (int i = 0; i < MI; i++)
+            #pragma unroll
+            for (int j = 0; j < NI; j++)
+                *reinterpret_cast<f32x4 *>(o + ((j * MI + i) * 64 + lane) * 4) = acc[i][j];
+        return;
+    }
+    // every wave stages its 64 x 64 results in its own part of the stages
+    unsigned char *sub = (wave < 2 ? lds0 : lds1) + (wave & 1) * kSubBytes;
+    const int i0 = ti * BT + wm * TM, j0 = tj * BT + wn * TN;
+    sub_put<MODE>(sub, acc, 0, d, s, i0, j0);
+    __syncthreads();
+    sub_out<MODE, 1, W>(sub, 0, d, s, turn, !ns_sym(MODE) || ti != tj, i0, j0);
+}
+
+// The results of the tiles that ran in pieces: a workgroup adds the pieces of a
+// 64 x 64 quarter, wave w its block column w, in order.
+template <int MODE, typename W>
+__global__ __launch_bounds__(256) void k_ns_finish(NsTable t, int count, NsStep s, int turn, NsCut cut)
+{
+    __shared__ __align__(16) unsigned char sub[kSubBytes];
+    const int tile = cut.whole + blockIdx.x / 4, quarter = blockIdx.x % 4;
+    const NsPlace pl = ns_place<MODE>(t, count, tile);
+    const NsDev &d = t.items[pl.it];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float *src = cut.part + (int64_t)(blockIdx.x / 4) * cut.pieces * kPart + quarter * (kSub * kSub) +
+                       (wave * 4 * 64 + lane) * 4;
+    f32x4 acc[4][1];
+    #pragma unroll
+    for (int i = 0; i < 4; i++) acc[i][0] = *reinterpret_cast<const f32x4 *>(src + i * 256);
+    #pragma unroll 4
+    for (int k = 1; k < cut.pieces; k++)
+        #pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(src + (int64_t)k * kPart + i * 256);
+            acc[i][0][0] += v[0]; acc[i][0][1] += v[1]; acc[i][0][2] += v[2]; acc[i][0][3] += v[3];
+        }
+    const int i0 = pl.ti * kTile + quarter / 2 * kSub, j0 = pl.tj * kTile + quarter % 2 * kSub;
+    sub_put<MODE>(sub, acc, wave, d, s, i0, j0);
+    __syncthreads();
+    sub_out<MODE, 4, W>(sub, wave, d, s, turn, !ns_sym(MODE) || pl.ti != pl.tj, i0, j0);
 }
 
 // ---- narrow matrices (short side up to 128) --------------------------------
@@ -836,6 +954,31 @@ size_t table_bytes(int count)
     return (a + b + 255) / 256 * 256;
 }
 
+// The cut of a stage of `tiles` tiles whose longest product has `steps` k steps.
+// A piece keeps at least kMinSteps: below that its own start and the extra
+// launch cost more than the idle part of the chip.
+constexpr int kMinSteps = 8;
+NsCut ns_cut(int64_t tiles, int steps)
+{
+    NsCut c{(int)tiles, (int)tiles, 1, nullptr};
+    const int rest = (int)(tiles % kNsSlots);
+    if (!rest) return c;
+    int pieces = kNsSlots / rest;
+    if (pieces > steps / kMinSteps) pieces = steps / kMinSteps;
+    if (pieces < 2) return c;
+    c.whole = (int)tiles - rest;
+    c.pieces = pieces;
+    return c;
+}
+int64_t cut_bytes(const NsCut &c) { return c.pieces > 1 ? (int64_t)(c.tiles - c.whole) * c.pieces * kPart * 4 : 0; }
+
+struct NsCuts { NsCut gram, square, apply; };
+NsCuts ns_cuts(const NsPlan &p)
+{
+    return NsCuts{ns_cut(p.work[PRE_GRAM], p.long_side / 32), ns_cut(p.work[PRE_GRAM], p.short_side / 32),
+                  ns_cut(p.work[PRE_APPLY], p.short_side / 32)};
+}
+
 }  // namespace
 
 void ns_plan_add(NsPlan &p, int rows, int cols)
@@ -846,9 +989,18 @@ void ns_plan_add(NsPlan &p, int rows, int cols)
     for (int k = 0; k < kPre; k++) p.work[k] += z.work[k];
     (z.blocks ? p.narrow_flops : p.flops) += (double)z.p * (z.p + 1) * z.q + (double)z.p * z.p * (z.p + 1) + 2.0 * z.p * z.p * z.q;
     p.values += (double)rows * cols;
+    if (z.blocks) return;
+    if (z.P > p.short_side) p.short_side = z.P;
+    if (z.Q > p.long_side) p.long_side = z.Q;
 }
 
-size_t ns_plan_bytes(const NsPlan &p) { return table_bytes(p.count) + (size_t)p.bytes; }
+size_t ns_plan_bytes(const NsPlan &p)
+{
+    const NsCuts c = ns_cuts(p);
+    int64_t part = 0;
+    for (const NsCut *k : {&c.gram, &c.square, &c.apply}) part = cut_bytes(*k) > part ? cut_bytes(*k) : part;
+    return table_bytes(p.count) + (size_t)p.bytes + (size_t)part;
+}
 
 namespace {
 
@@ -862,11 +1014,18 @@ NsTable ns_table(void *ws, int count)
 }
 
 template <int MODE, typename W>
-hipError_t ns_product(const NsPlan &p, const NsTable &t, const NsStep &s, int turn, double flops, hipStream_t st)
+hipError_t ns_product(const NsPlan &p, const NsTable &t, const NsStep &s, int turn, const NsCut &cut, hipStream_t st)
 {
-    const int64_t work = p.work[MODE == NS_GRAM || MODE == NS_SQUARE ? PRE_GRAM : PRE_APPLY];
-    TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, flops);
-    hipLaunchKernelGGL((k_ns_product<kTile, 2, 2, MODE, W>), dim3((unsigned)work), dim3(256), 0, st, t, p.count, s, turn);
+    const int rest = cut.tiles - cut.whole;
+    {
+        TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, ns_sym(MODE) ? 0.0 : p.flops);
+        hipLaunchKernelGGL((k_ns_product<MODE, W>), dim3((unsigned)(cut.whole + rest * cut.pieces)), dim3(256), 0, st, t,
+                           p.count, s, turn, cut);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    if (cut.pieces == 1) return hipSuccess;
+    TraceScope tr(KC_SMALL, KID_ORTHO, st, (double)cut_bytes(cut), 0.0);
+    hipLaunchKernelGGL((k_ns_finish<MODE, W>), dim3((unsigned)rest * 4), dim3(256), 0, st, t, p.count, s, turn, cut);
     return hipGetLastError();
 }
 
@@ -945,13 +1104,16 @@ hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep
         hipLaunchKernelGGL(kern, dim3((unsigned)p.work[PRE_PREP]), dim3(kThreads), 0, st, t, p.count, s);
         if (hipError_t e = hipGetLastError()) return e;
     }
+    NsCuts cuts = ns_cuts(p);
+    float *part = (float *)((char *)ws + table_bytes(p.count) + p.bytes);
+    for (NsCut *k : {&cuts.gram, &cuts.square, &cuts.apply}) k->part = part;
     for (int k = 0, turn = 0; k < s.steps; k++, turn ^= 1) {
-        hipError_t e = ns_product<NS_GRAM, float>(p, t, s, turn, 0.0, st);
-        if (e == hipSuccess) e = ns_product<NS_SQUARE, float>(p, t, s, turn, 0.0, st);
+        hipError_t e = ns_product<NS_GRAM, float>(p, t, s, turn, cuts.gram, st);
+        if (e == hipSuccess) e = ns_product<NS_SQUARE, float>(p, t, s, turn, cuts.square, st);
         if (e == hipSuccess) {
-            if (k + 1 < s.steps) e = ns_product<NS_APPLY, float>(p, t, s, turn, p.flops, st);
-            else if (dst_dtype == DT_BF16) e = ns_product<NS_LAST, bf16_t>(p, t, s, turn, p.flops, st);
-            else e = ns_product<NS_LAST, float>(p, t, s, turn, p.flops, st);
+            if (k + 1 < s.steps) e = ns_product<NS_APPLY, float>(p, t, s, turn, cuts.apply, st);
+            else if (dst_dtype == DT_BF16) e = ns_product<NS_LAST, bf16_t>(p, t, s, turn, cuts.apply, st);
+            else e = ns_product<NS_LAST, float>(p, t, s, turn, cuts.apply, st);
         }
         if (e != hipSuccess) return e;
     }
