@@ -41,15 +41,18 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef uint16_t h16;                                // fp16 storage word
 
 constexpr float kS = 4096.f, kInvS = 1.f / 4096.f;   // see the precision note
-constexpr int kTile = kNsTile;
+constexpr int kSub = 64;                             // wide matrices are padded to multiples of it
 
 // Stages of a call and their work items: momentum and squares; the narrow
 // matrices' blocks and the sums of their partial Gram matrices; the wide ones'
-// conversion, symmetric product tiles and general product tiles.
-enum { PRE_SQ = 0, PRE_NARROW = 1, PRE_SUM = 2, PRE_PREP = 3, PRE_GRAM = 4, PRE_APPLY = 5, kPre = kNsStages };
+// conversion, symmetric product tiles and general product tiles, and the same in
+// large and in small tiles.
+enum { PRE_SQ = 0, PRE_NARROW = 1, PRE_SUM = 2, PRE_PREP = 3, PRE_GRAM = 4, PRE_APPLY = 5, PRE_GRAM_L = 6, PRE_APPLY_L = 7,
+       PRE_GRAM_S = 8, PRE_APPLY_S = 9, kPre = kNsStages };
 
 // one matrix of the list on the device: the caller's arguments and its place in the workspace
 struct NsDev {
@@ -72,9 +75,10 @@ struct NsSize {
 constexpr int kMaxParts = 1024;    // partial sums of squares of a matrix
 constexpr int kNarrow = 128;       // short sides up to this take the narrow path
 constexpr int kBlock = 16384;      // values of a narrow matrix's block: [kBlock / P][P]
-// Blocks of one narrow matrix up to which every block adds the partial Gram
-// matrices itself; past it a launch of its own adds them once.
-constexpr int kSumBlocks = 8;
+// Values of one narrow matrix's partial Gram matrices up to which every block
+// adds them itself; past it a launch of its own adds them once.
+constexpr int kSumValues = 2 * 128 * 128;
+__host__ __device__ inline bool ns_summed(int blocks, int P) { return blocks * (int64_t)(P * P) > kSumValues; }
 
 __host__ __device__ inline NsSize ns_size(int rows, int cols)
 {
@@ -97,16 +101,20 @@ __host__ __device__ inline NsSize ns_size(int rows, int cols)
         z.blocks = (z.q + qb - 1) / qb;
         z.Q = z.blocks * qb;
         z.work[PRE_NARROW] = z.blocks;
-        if (z.blocks > kSumBlocks) z.work[PRE_SUM] = z.P * z.P / 256;
+        if (ns_summed(z.blocks, z.P)) z.work[PRE_SUM] = z.P * z.P / 256;
         z.bytes = kMaxParts * 8 + (int64_t)z.blocks * (kBlock * 4 + 2 * z.P * z.P * 4) + z.P * z.P * 4;
         return z;
     }
-    z.P = (z.p + kTile - 1) / kTile * kTile;
-    z.Q = (z.q + kTile - 1) / kTile * kTile;
-    const int tp = z.P / kTile, tq = z.Q / kTile;
-    z.work[PRE_PREP] = (z.P / 64) * (z.Q / 64);
-    z.work[PRE_GRAM] = tp * (tp + 1) / 2;
-    z.work[PRE_APPLY] = tp * tq;
+    const int up = (z.p + 63) / 64, uq = (z.q + 63) / 64;
+    z.P = up * 64;
+    z.Q = uq * 64;
+    z.work[PRE_PREP] = up * uq;
+    for (int l = 0; l < 3; l++) {                // tiles of 64, 128, 256
+        const int tp = (up + (1 << l) - 1) >> l, tq = (uq + (1 << l) - 1) >> l;
+        const int at = l == 0 ? PRE_GRAM_S : (l == 1 ? PRE_GRAM : PRE_GRAM_L);
+        z.work[at] = tp * (tp + 1) / 2;
+        z.work[at + 1] = tp * tq;
+    }
     z.bytes = kMaxParts * 8 + (int64_t)z.P * z.Q * 4 * 3 + (int64_t)z.P * z.P * 4 * 2;
     return z;
 }
@@ -179,10 +187,21 @@ __device__ __forceinline__ int ns_find(const int *pre, int count, int item)
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
+// Accesses through a pointer that was read from memory (the table's), or chosen
+// between two LDS arrays: the compiler does not know its address space and would
+// make flat accesses, which wait for the global and the LDS side both (250 ns a
+// step where LDS reads and global stores alternate).  These name the space.
+#define NS_GLOBAL __attribute__((address_space(1)))
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+template <typename V> __device__ __forceinline__ V gld(const void *p) { return *(const NS_GLOBAL V *)p; }
+template <typename V> __device__ __forceinline__ void gst(void *p, V v) { *(NS_GLOBAL V *)p = v; }
+template <typename V> __device__ __forceinline__ V lld(const lds_byte *p) { return *(const __attribute__((address_space(3))) V *)p; }
+template <typename V> __device__ __forceinline__ void lst(lds_byte *p, V v) { *(__attribute__((address_space(3))) V *)p = v; }
+
 template <typename T> __device__ __forceinline__ float ns_load(const void *p, int64_t i)
 {
-    if constexpr (sizeof(T) == 4) return ((const float *)p)[i];
-    else return bf2f(((const bf16_t *)p)[i]);
+    if constexpr (sizeof(T) == 4) return gld<float>((const float *)p + i);
+    else return bf2f(gld<bf16_t>((const bf16_t *)p + i));
 }
 
 // u of element i of a gradient row: the gradient itself, or what the momentum step makes of it
@@ -221,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_squares(NsTable t, int count, N
             const int rr = in[u] ? r : r1 - 1, cc = in[u] ? c : 0;       // read and dropped
             g[u] = ns_load<T>(src, rr * ls + cc);
             at[u] = rr * lb + cc;
-            b[u] = s.update ? buf[at[u]] : 0.f;
+            b[u] = s.update ? gld<float>(buf + at[u]) : 0.f;
             r += dr;
             c += dc;
             if (c >= cols) { c -= cols; r++; }
@@ -231,7 +250,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_squares(NsTable t, int count, N
             if (!in[u]) continue;
             if (s.update) {
                 b[u] = __builtin_fmaf(s.momentum, b[u], g[u]);
-                buf[at[u]] = b[u];
+                gst(buf + at[u], b[u]);
             }
             const double v = (double)ns_u(g[u], b[u], s);
             acc += v * v;
@@ -240,7 +259,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_squares(NsTable t, int count, N
     for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
     if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = acc;
     __syncthreads();
-    if (threadIdx.x == 0) d.sq[part] = red[0] + red[1] + red[2] + red[3];
+    if (threadIdx.x == 0) gst(d.sq + part, red[0] + red[1] + red[2] + red[3]);
 }
 
 // S / (||u||_F + eps) of a matrix, by all threads of the workgroup; red: one
@@ -250,7 +269,7 @@ template <int NT>
 __device__ __forceinline__ float ns_factor(const NsDev &d, float eps, double *red)
 {
     double acc = 0.0;
-    for (int i = threadIdx.x; i < d.parts; i += NT) acc += d.sq[i];
+    for (int i = threadIdx.x; i < d.parts; i += NT) acc += gld<double>(d.sq + i);
     for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
     if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = acc;
     __syncthreads();
@@ -270,6 +289,11 @@ __device__ __forceinline__ void ns_pair(float v, h16 &hi, h16 &lo)
     const _Float16 l = (_Float16)(v - (float)h);
     hi = __builtin_bit_cast(h16, h);
     lo = __builtin_bit_cast(h16, l);
+}
+// four halves as two words
+__device__ __forceinline__ u32x2_t ns_words(const h16 *v)
+{
+    return u32x2_t{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16};
 }
 // element offset of (row, k) of a pair matrix with K columns: hi there, lo 32 further on
 __device__ __forceinline__ int64_t ns_at(int64_t row, int k, int K)
@@ -296,7 +320,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_prepare(NsTable t, int count, N
         float u = 0.f;
         if (r < d.in.rows && c < d.in.cols) {
             const float g = ns_load<T>(d.in.src, (int64_t)r * d.in.ld_src + c);
-            u = ns_u(g, s.update ? d.in.buf[(int64_t)r * d.in.ld_buf + c] : 0.f, s);
+            u = ns_u(g, s.update ? gld<float>(d.in.buf + (int64_t)r * d.in.ld_buf + c) : 0.f, s);
         }
         tile[e / 64][e % 64] = u;
     }
@@ -308,12 +332,12 @@ __global__ __launch_bounds__(kThreads) void k_ns_prepare(NsTable t, int count, N
         __align__(16) h16 hi[8], lo[8];
         for (int i = 0; i < 8; i++) ns_pair(tile[a][k8 + i] * scale, hi[i], lo[i]);
         h16 *o = straight + ns_at(rb + a, cb + k8, CP);
-        *reinterpret_cast<vec16 *>(o) = *reinterpret_cast<vec16 *>(hi);
-        *reinterpret_cast<vec16 *>(o + 32) = *reinterpret_cast<vec16 *>(lo);
+        gst(o, *reinterpret_cast<u32x4 *>(hi));
+        gst(o + 32, *reinterpret_cast<u32x4 *>(lo));
         for (int i = 0; i < 8; i++) ns_pair(tile[k8 + i][a] * scale, hi[i], lo[i]);
         o = turned + ns_at(cb + a, rb + k8, RP);
-        *reinterpret_cast<vec16 *>(o) = *reinterpret_cast<vec16 *>(hi);
-        *reinterpret_cast<vec16 *>(o + 32) = *reinterpret_cast<vec16 *>(lo);
+        gst(o, *reinterpret_cast<u32x4 *>(hi));
+        gst(o + 32, *reinterpret_cast<u32x4 *>(lo));
     }
 }
 
@@ -326,12 +350,12 @@ __device__ __forceinline__ void ns_result(const NsIn &in, const NsStep &s, float
     float res = o;
     if (s.update) {
         res = __builtin_fmaf(-lr * in.scale, o, ns_load<W>(dst, 0) * (1.f - lr * s.decay));
-        if (in.copy) in.copy[row * in.ld_copy + col] = f2bf(res);
+        if (in.copy) gst(in.copy + row * in.ld_copy + col, f2bf(res));
     }
-    if constexpr (sizeof(W) == 4) *dst = res;
-    else *dst = f2bf(res);
+    if constexpr (sizeof(W) == 4) gst<float>(dst, res);
+    else gst<bf16_t>(dst, f2bf(res));
 }
-__device__ __forceinline__ float ns_rate(const NsStep &s) { return !s.update ? 0.f : (s.lr_dev ? *s.lr_dev : s.lr); }
+__device__ __forceinline__ float ns_rate(const NsStep &s) { return !s.update ? 0.f : (s.lr_dev ? gld<float>(s.lr_dev) : s.lr); }
 
 // One product stage over the whole list.
 //   NS_GRAM    G = X X^T            (lower-triangle tiles, mirrored)
@@ -341,20 +365,19 @@ __device__ __forceinline__ float ns_rate(const NsStep &s) { return !s.update ? 0
 enum { NS_GRAM = 0, NS_SQUARE = 1, NS_APPLY = 2, NS_LAST = 3 };
 constexpr bool ns_sym(int mode) { return mode == NS_GRAM || mode == NS_SQUARE; }
 
-// How a stage's tiles run.  The chip holds kNsSlots workgroups of the product
-// kernel at once.  Whole tiles fill as many rounds of that as they can; the rest
+// How a stage's tiles run.  The chip holds ns_slots workgroups of the product
+// kernel at once (512 of the small tile, two a CU, 256 of the large).  Whole tiles fill as many rounds of that as they can; the rest
 // (tiles [whole, tiles)) would leave most of the chip idle for a round, so each
 // of them is cut into `pieces` along k: a piece's float32 sums go to the
 // workspace and k_ns_finish adds them in a fixed order.
-struct NsCut { int tiles, whole, pieces; float *part; };
-constexpr int kPart = kTile * kTile;             // values of a piece
+struct NsCut { int bt, tiles, whole, pieces; float *part; };
 
 // the tile of a stage: its matrix and its block row and column
 struct NsPlace { int it, ti, tj; };
-template <int MODE>
+template <int BT, int MODE>
 __device__ __forceinline__ NsPlace ns_place(const NsTable &t, int count, int tile)
 {
-    const int *pre = t.pre[ns_sym(MODE) ? PRE_GRAM : PRE_APPLY];
+    const int *pre = t.pre[(BT == 64 ? PRE_GRAM_S : (BT == 128 ? PRE_GRAM : PRE_GRAM_L)) + !ns_sym(MODE)];
     NsPlace pl;
     pl.it = ns_find(pre, count, tile);
     const int w = tile - pre[pl.it];
@@ -365,24 +388,31 @@ __device__ __forceinline__ NsPlace ns_place(const NsTable &t, int count, int til
         pl.ti = ti;
         pl.tj = w - ti * (ti + 1) / 2;
     } else {
-        const int tp = t.items[pl.it].P / kTile;
+        const int tp = (t.items[pl.it].P + BT - 1) / BT;
         pl.ti = w % tp;
         pl.tj = w / tp;
     }
     return pl;
 }
 
+// Orders a wave's LDS accesses of other lanes' values (the wave's own area: no barrier needed).
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // 64 x 64 results in LDS, turned: row j holds the 64 i as pairs (two k blocks of
 // [hi 32 | lo 32], 256 bytes) or as float32, its 16-byte chunks in the order
 // chunk ^ (j % 16), so that 16 rows of one column lie in different banks.
-constexpr int kSub = 64, kSubBytes = kSub * 256;
+constexpr int kSubBytes = kSub * 256;
 __device__ __forceinline__ int sub_at(int j, int byte) { return j * 256 + ((byte >> 4 ^ (j & 15)) << 4) + (byte & 15); }
 
 // Results [MI][NI] of 16 x 16 blocks (a lane holds rows 4 g .. + 3 of column q)
 // into the sub-tile at block column nj0.  v(e, value, i, j) gives what is kept
 // of S times the product at (i, j) of the sub-tile.
 template <int MODE, int MI, int NI>
-__device__ __forceinline__ void sub_put(unsigned char *sub, const f32x4 (&acc)[MI][NI], int nj0, const NsDev &d,
+__device__ __forceinline__ void sub_put(lds_byte *sub, const f32x4 (&acc)[MI][NI], int nj0, const NsDev &d,
                                         const NsStep &s, int i0, int j0)
 {
     const int lane = threadIdx.x & 63, g = lane / 16, q = lane % 16;
@@ -397,7 +427,7 @@ __device__ __forceinline__ void sub_put(unsigned char *sub, const f32x4 (&acc)[M
             if constexpr (MODE == NS_SQUARE) {
                 float gg[4];                     // G is symmetric: row j holds the four i together
                 const h16 *p = d.g + ns_at(j0 + j, i0 + i, d.P);
-                const f16x4 hi = *reinterpret_cast<const f16x4 *>(p), lo = *reinterpret_cast<const f16x4 *>(p + 32);
+                const f16x4 hi = gld<f16x4>(p), lo = gld<f16x4>(p + 32);
                 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     gg[e] = (float)hi[e] + (float)lo[e];
@@ -406,16 +436,14 @@ __device__ __forceinline__ void sub_put(unsigned char *sub, const f32x4 (&acc)[M
             }
             if constexpr (MODE == NS_LAST) {
                 f32x4 o = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
-                *reinterpret_cast<f32x4 *>(sub + sub_at(j, i * 4)) = o;
+                lst(sub + sub_at(j, i * 4), o);
             } else {
                 h16 hi[4], lo[4];
                 #pragma unroll
                 for (int e = 0; e < 4; e++) ns_pair(v[e], hi[e], lo[e]);
                 const int byte = (i >> 5) * 128 + (i & 31) * 2;
-                *reinterpret_cast<uint2 *>(sub + sub_at(j, byte)) =
-                    make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
-                *reinterpret_cast<uint2 *>(sub + sub_at(j, byte + 64)) =
-                    make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+                lst(sub + sub_at(j, byte), ns_words(hi));
+                lst(sub + sub_at(j, byte + 64), ns_words(lo));
             }
         }
 }
@@ -424,7 +452,7 @@ __device__ __forceinline__ void sub_put(unsigned char *sub, const f32x4 (&acc)[M
 // this wave's number among them: rows of 256 bytes as they lie, and the other
 // orientation through transposing reads.  i0, j0: the sub-tile's place in the result.
 template <int MODE, int NW, typename W>
-__device__ __forceinline__ void sub_out(const unsigned char *sub, int w, const NsDev &d, const NsStep &s, int turn,
+__device__ __forceinline__ void sub_out(const lds_byte *sub, int w, const NsDev &d, const NsStep &s, int turn,
                                         bool mirror, int i0, int j0)
 {
     const int lane = threadIdx.x & 63, g = lane / 16, q = lane % 16;
@@ -433,7 +461,7 @@ __device__ __forceinline__ void sub_out(const unsigned char *sub, int w, const N
         #pragma unroll 4
         for (int k = w; k < kSub; k += NW) {     // one row of the caller's matrix a step
             const int i = d.flip ? lane : k, j = d.flip ? k : lane;
-            const float o = *reinterpret_cast<const float *>(sub + sub_at(j, i * 4));
+            const float o = lld<float>(sub + sub_at(j, i * 4));
             if (i0 + i < d.p && j0 + j < d.q)
                 ns_result<W>(d.in, s, lr, d.flip ? j0 + j : i0 + i, d.flip ? i0 + i : j0 + j, o);
         }
@@ -444,8 +472,7 @@ __device__ __forceinline__ void sub_out(const unsigned char *sub, int w, const N
         #pragma unroll
         for (int k = w; k < 16; k += NW) {
             const int j = k * 4 + lane / 16, c = lane % 16;
-            const vec16 v = *reinterpret_cast<const vec16 *>(sub + sub_at(j, c * 16));
-            *reinterpret_cast<vec16 *>(turned + ns_at(j0 + j, i0, d.P) + c * 8) = v;
+            gst(turned + ns_at(j0 + j, i0, d.P) + c * 8, lld<u32x4>(sub + sub_at(j, c * 16)));
         }
         if (!mirror) return;
         // 16 i x 32 j a step: a lane gets 8 consecutive j of one i
@@ -453,27 +480,29 @@ __device__ __forceinline__ void sub_out(const unsigned char *sub, int w, const N
         for (int k = w; k < 16; k += NW) {
             const int i = (k >> 2) * 16, jb = (k >> 1 & 1) * 32, part = k & 1;
             const int byte = (i >> 5) * 128 + (i & 31) * 2 + part * 64 + 8 * (q % 4), j = jb + 8 * g + q / 4;
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sub + sub_at(j, byte)));
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sub + sub_at(j + 4, byte)));
             const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            *reinterpret_cast<s16x8 *>(straight + ns_at(i0 + i + q, j0 + jb + 8 * g, ks) + part * 32) = v;
+            gst(straight + ns_at(i0 + i + q, j0 + jb + 8 * g, ks) + part * 32, v);
         }
     }
 }
 
-// Workgroup: a tile of 128 x 128 outputs by 2 x 2 waves of 64 x 64, or a piece
-// of one.  Two LDS stages of 256 rows of 128 bytes (one k step of both
-// operands); the 16-byte chunks of a row are stored in the order
-// chunk ^ (row % 8), so the 16 rows of a fragment read lie in different banks.
-// The next step's lines are loaded straight into LDS while the current step
-// multiplies.
-template <int MODE, typename W>
-__global__ __launch_bounds__(256) void k_ns_product(NsTable t, int count, NsStep s, int turn, NsCut cut)
+// Workgroup: a tile of BT x BT outputs, or a piece of one.  BT = 128: 2 x 2
+// waves of 64 x 64, two workgroups a CU; BT = 256: 2 x 4 waves of 128 x 64, one a
+// CU, for which a k step's operands are half of the lines per product and its
+// fragment reads three quarters (a tile may hang over the matrix by 128 rows or
+// columns: those rows are read again from inside and not written).  Two LDS
+// stages of 2 BT rows of 128 bytes (one k step of both operands); the 16-byte
+// chunks of a row are stored in the order chunk ^ (row % 8), so the 16 rows of a
+// fragment read lie in different banks.  The next step's lines are loaded
+// straight into LDS while the current step multiplies.
+template <int BT, int MODE, typename W>
+__global__ __launch_bounds__(BT * 2) void k_ns_product(NsTable t, int count, NsStep s, int turn, NsCut cut)
 {
-    constexpr int BT = kTile, NT = 256, TM = 64, TN = 64, MI = TM / 16, NI = TN / 16;
+    constexpr int NT = BT * 2, WN = BT / 64, TM = BT / 2, TN = 64, MI = TM / 16, NI = TN / 16;
     constexpr int kRow = 128, kStage = 2 * BT * kRow, kLoads = kStage / (NT * 16);
-    static_assert(kStage == 2 * kSubBytes, "two waves' results fit a stage");
+    static_assert(kStage == NT / 128 * kSubBytes, "half of the waves' results fit a stage");
     __shared__ __align__(16) unsigned char lds0[kStage], lds1[kStage];
     int tile, piece = 0, pieces = 1;
     if ((int)blockIdx.x < cut.whole) {
@@ -484,7 +513,7 @@ __global__ __launch_bounds__(256) void k_ns_product(NsTable t, int count, NsStep
         tile = cut.whole + u / pieces;
         piece = u % pieces;
     }
-    const NsPlace pl = ns_place<MODE>(t, count, tile);
+    const NsPlace pl = ns_place<BT, MODE>(t, count, tile);
     const NsDev &d = t.items[pl.it];
     const int P = d.P, Q = d.Q, ti = pl.ti, tj = pl.tj;
     const int K = MODE == NS_GRAM ? Q : P;
@@ -498,7 +527,9 @@ __global__ __launch_bounds__(256) void k_ns_product(NsTable t, int count, NsStep
     #pragma unroll
     for (int l = 0; l < kLoads; l++) {
         const int row = l * (NT / 8) + lrow;
-        const h16 *base = row < BT ? pa + (int64_t)(ti * BT + row) * 2 * K : pb + (int64_t)(tj * BT + row - BT) * 2 * K;
+        const int end_a = P - 1, end_b = (ns_sym(MODE) ? P : Q) - 1;
+        const h16 *base = row < BT ? pa + (int64_t)min(ti * BT + row, end_a) * 2 * K
+                                   : pb + (int64_t)min(tj * BT + row - BT, end_b) * 2 * K;
         src[l] = (const char *)base + lchunk * 16;
     }
     auto load = [&](unsigned char *stage, int step) __attribute__((always_inline)) {
@@ -509,7 +540,7 @@ __global__ __launch_bounds__(256) void k_ns_product(NsTable t, int count, NsStep
                                              16, 0, 0);
         __builtin_amdgcn_sched_barrier(0);       // (the scheduler would sink them to the barrier that waits for them)
     };
-    const int wm = wave / 2, wn = wave % 2;
+    const int wm = wave / WN, wn = wave % WN;
     const int fr = lane % 16, fc = lane / 16;    // fragment row and k chunk of this lane
     f32x4 acc[MI][NI];
     #pragma unroll
@@ -541,7 +572,7 @@ __global__ __launch_bounds__(256) void k_ns_product(NsTable t, int count, NsStep
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
             }
     };
-    // steps in pairs (K is a multiple of 128); a piece may have none
+    // steps in pairs (K is a multiple of 64); a piece may have none
     const int pairs = K / 64, k0 = piece * pairs / pieces * 2, k1 = (piece + 1) * pairs / pieces * 2;
     if (k0 < k1) {
         load(lds0, k0);
@@ -556,48 +587,139 @@ __global__ __launch_bounds__(256) void k_ns_product(NsTable t, int count, NsStep
         }
     }
     if (pieces > 1) {                            // in the order of the fragments: [wave][block][lane]
-        float *o = cut.part + (int64_t)(blockIdx.x - cut.whole) * kPart + wave * (kSub * kSub);
+        float *o = cut.part + (int64_t)(blockIdx.x - cut.whole) * (BT * BT) + wave * (TM * TN);
         #pragma unroll
         for (int i = 0; i < MI; i++)
             #pragma unroll
             for (int j = 0; j < NI; j++)
-                *reinterpret_cast<f32x4 *>(o + ((j * MI + i) * 64 + lane) * 4) = acc[i][j];
+                gst(o + ((j * MI + i) * 64 + lane) * 4, acc[i][j]);
         return;
     }
-    // every wave stages its 64 x 64 results in its own part of the stages
-    unsigned char *sub = (wave < 2 ? lds0 : lds1) + (wave & 1) * kSubBytes;
-    const int i0 = ti * BT + wm * TM, j0 = tj * BT + wn * TN;
-    sub_put<MODE>(sub, acc, 0, d, s, i0, j0);
-    __syncthreads();
-    sub_out<MODE, 1, W>(sub, 0, d, s, turn, !ns_sym(MODE) || ti != tj, i0, j0);
+    // every wave stages 64 x 64 results at a time in its own part of the stages
+    lds_byte *sub = (wave < NT / 128 ? (lds_byte *)lds0 : (lds_byte *)lds1) + wave % (NT / 128) * kSubBytes;
+    const int j0 = tj * BT + wn * TN;
+    const bool in = j0 < (ns_sym(MODE) ? P : Q);
+    #pragma unroll
+    for (int h = 0; h < TM / kSub; h++) {
+        const int i0 = ti * BT + wm * TM + h * kSub;
+        if (!in || i0 >= P) continue;
+        f32x4 part[4][NI];
+        #pragma unroll
+        for (int i = 0; i < 4; i++)
+            #pragma unroll
+            for (int j = 0; j < NI; j++) part[i][j] = acc[h * 4 + i][j];
+        sub_put<MODE>(sub, part, 0, d, s, i0, j0);
+        wave_sync();
+        // both orientations already
+        sub_out<MODE, 1, W>(sub, 0, d, s, turn, !ns_sym(MODE) || ti != tj, i0, j0);
+        wave_sync();
+    }
 }
 
-// The results of the tiles that ran in pieces: a workgroup adds the pieces of a
-// 64 x 64 quarter, wave w its block column w, in order.
-template <int MODE, typename W>
+// The results of the tiles that ran in pieces: a workgroup adds the pieces of
+// 64 x 64 results, wave w their block column w, in order.
+template <int BT, int MODE, typename W>
 __global__ __launch_bounds__(256) void k_ns_finish(NsTable t, int count, NsStep s, int turn, NsCut cut)
 {
+    constexpr int WN = BT / 64, TM = BT / 2, MI = TM / 16, kSubs = BT * BT / (kSub * kSub), kHalves = TM / kSub;
     __shared__ __align__(16) unsigned char sub[kSubBytes];
-    const int tile = cut.whole + blockIdx.x / 4, quarter = blockIdx.x % 4;
-    const NsPlace pl = ns_place<MODE>(t, count, tile);
+    const int tile = cut.whole + blockIdx.x / kSubs, q = blockIdx.x % kSubs, from = q / kHalves, h = q % kHalves;
+    const NsPlace pl = ns_place<BT, MODE>(t, count, tile);
     const NsDev &d = t.items[pl.it];
+    const int i0 = pl.ti * BT + from / WN * TM + h * kSub, j0 = pl.tj * BT + from % WN * kSub;
+    if (i0 >= d.P || j0 >= (ns_sym(MODE) ? d.P : d.Q)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float *src = cut.part + (int64_t)(blockIdx.x / 4) * cut.pieces * kPart + quarter * (kSub * kSub) +
-                       (wave * 4 * 64 + lane) * 4;
+    const float *src = cut.part + (int64_t)(blockIdx.x / kSubs) * cut.pieces * (BT * BT) + from * (TM * 64) +
+                       ((wave * MI + h * 4) * 64 + lane) * 4;
     f32x4 acc[4][1];
     #pragma unroll
-    for (int i = 0; i < 4; i++) acc[i][0] = *reinterpret_cast<const f32x4 *>(src + i * 256);
+    for (int i = 0; i < 4; i++) acc[i][0] = gld<f32x4>(src + i * 256);
     #pragma unroll 4
     for (int k = 1; k < cut.pieces; k++)
         #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(src + (int64_t)k * kPart + i * 256);
+            const f32x4 v = gld<f32x4>(src + (int64_t)k * (BT * BT) + i * 256);
             acc[i][0][0] += v[0]; acc[i][0][1] += v[1]; acc[i][0][2] += v[2]; acc[i][0][3] += v[3];
         }
-    const int i0 = pl.ti * kTile + quarter / 2 * kSub, j0 = pl.tj * kTile + quarter % 2 * kSub;
-    sub_put<MODE>(sub, acc, wave, d, s, i0, j0);
+    sub_put<MODE>((lds_byte *)sub, acc, wave, d, s, i0, j0);
     __syncthreads();
-    sub_out<MODE, 4, W>(sub, wave, d, s, turn, !ns_sym(MODE) || pl.ti != pl.tj, i0, j0);
+    sub_out<MODE, 4, W>((lds_byte *)sub, wave, d, s, turn, !ns_sym(MODE) || pl.ti != pl.tj, i0, j0);
+}
+
+// Workgroup: a tile of 64 x 64 outputs whose k steps are split over its four
+// waves.  Nothing is shared between the waves, so the operands' fragments are
+// loaded straight into registers, four steps ahead, without LDS or barriers:
+// for few tiles, where the time of a stage is the round trip of its loads.  The
+// waves' sums are added through LDS in a fixed order.
+template <int MODE, typename W>
+__global__ __launch_bounds__(256, 1) void k_ns_direct(NsTable t, int count, NsStep s, int turn)
+{
+    constexpr int AHEAD = 4;
+    __shared__ __align__(16) unsigned char lds[4 * kSubBytes];
+    const NsPlace pl = ns_place<64, MODE>(t, count, xcd_remap(blockIdx.x, gridDim.x));
+    const NsDev &d = t.items[pl.it];
+    const int K = MODE == NS_GRAM ? d.Q : d.P;
+    const h16 *pa = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.r);
+    const h16 *pb = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.xt[turn]);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane % 16, fc = lane / 16;
+    const int i0 = pl.ti * 64, j0 = pl.tj * 64;
+    const int steps = K / 32, k0 = wave * steps / 4, n = (wave + 1) * steps / 4 - k0;
+    const int64_t block = (int64_t)16 * 2 * K;
+    const h16 *a = pa + (int64_t)(i0 + fr) * 2 * K + k0 * 64 + fc * 8, *b = pb + (int64_t)(j0 + fr) * 2 * K + k0 * 64 + fc * 8;
+    f16x8 f[AHEAD][16];                          // a hi, lo; b hi, lo of four blocks each
+    auto load = [&](f16x8 (&o)[16], int k) __attribute__((always_inline)) {
+        #pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const h16 *p = a + i * block + k * 64, *q = b + i * block + k * 64;
+            o[2 * i] = gld<f16x8>(p);
+            o[2 * i + 1] = gld<f16x8>(p + 32);
+            o[8 + 2 * i] = gld<f16x8>(q);
+            o[9 + 2 * i] = gld<f16x8>(q + 32);
+        }
+    };
+    f32x4 acc[4][4];
+    #pragma unroll
+    for (int i = 0; i < 4; i++)
+        #pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    #pragma unroll
+    for (int u = 0; u < AHEAD; u++)
+        if (u < n) load(f[u], u);
+    for (int k = 0; k < n; k += AHEAD)
+        #pragma unroll
+        for (int u = 0; u < AHEAD; u++) {
+            if (k + u < n)
+                #pragma unroll
+                for (int i = 0; i < 4; i++)
+                    #pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[u][2 * i], f[u][9 + 2 * j], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[u][2 * i + 1], f[u][8 + 2 * j], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[u][2 * i], f[u][8 + 2 * j], acc[i][j], 0, 0, 0);
+                    }
+            if (k + u + AHEAD < n) load(f[u], k + u + AHEAD);
+        }
+    // in the order of the fragments, [wave][block][lane]; wave w adds block column w
+    f32x4 *red = reinterpret_cast<f32x4 *>(lds);
+    #pragma unroll
+    for (int i = 0; i < 4; i++)
+        #pragma unroll
+        for (int j = 0; j < 4; j++) red[(wave * 16 + j * 4 + i) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    f32x4 sum[4][1];
+    #pragma unroll
+    for (int i = 0; i < 4; i++) {
+        sum[i][0] = red[(wave * 4 + i) * 64 + lane];
+        #pragma unroll
+        for (int w = 1; w < 4; w++) {
+            const f32x4 v = red[(w * 16 + wave * 4 + i) * 64 + lane];
+            sum[i][0][0] += v[0]; sum[i][0][1] += v[1]; sum[i][0][2] += v[2]; sum[i][0][3] += v[3];
+        }
+    }
+    __syncthreads();
+    sub_put<MODE>((lds_byte *)lds, sum, wave, d, s, i0, j0);
+    __syncthreads();
+    sub_out<MODE, 4, W>((lds_byte *)lds, wave, d, s, turn, !ns_sym(MODE) || pl.ti != pl.tj, i0, j0);
 }
 
 // ---- narrow matrices (short side up to 128) --------------------------------
@@ -674,8 +796,8 @@ __device__ __forceinline__ void nw_store4(h16 *p, const float *v)
     h16 hi[4], lo[4];
     #pragma unroll
     for (int e = 0; e < 4; e++) ns_pair(v[e], hi[e], lo[e]);
-    *reinterpret_cast<uint2 *>(p) = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
-    *reinterpret_cast<uint2 *>(p + 32) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+    *reinterpret_cast<u32x2_t *>(p) = ns_words(hi);
+    *reinterpret_cast<u32x2_t *>(p + 32) = ns_words(lo);
 }
 __device__ __forceinline__ void nw_load4(const h16 *p, float *v)
 {
@@ -694,7 +816,7 @@ __device__ __forceinline__ void nw_gram(const NsDev &d, int block, const h16 *xs
     #pragma unroll
     for (int l = 0; l < kBlock * 4 / 16 / kNwThreads; l++) {
         const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
-        *reinterpret_cast<vec16 *>(out + (int64_t)v * 8) = *reinterpret_cast<const vec16 *>(xs + row * N::XP + c * 8);
+        gst(out + (int64_t)v * 8, *reinterpret_cast<const u32x4 *>(xs + row * N::XP + c * 8));
     }
     constexpr int MI = N::TM / 16, NI = N::TN / 16;
     const int wm = wave / N::WN, wn = wave % N::WN;
@@ -735,7 +857,7 @@ __device__ __forceinline__ void nw_gram(const NsDev &d, int block, const h16 *xs
     for (int i = 0; i < MI; i++)
         #pragma unroll
         for (int j = 0; j < NI; j++)
-            *reinterpret_cast<f32x4 *>(o + (wn * N::TN + j * 16 + q) * P + wm * N::TM + i * 16 + 4 * g) = acc[i][j];
+            gst(o + (wn * N::TN + j * 16 + q) * P + wm * N::TM + i * 16 + 4 * g, acc[i][j]);
 }
 
 // Stage 2 of a narrow matrix: X's block as pairs, and its partial Gram matrix.
@@ -756,7 +878,7 @@ __device__ __forceinline__ void nw_prepare(const NsDev &d, int block, const NsSt
             const bool in = i < d.p && j0 + j < d.q;
             const int64_t r = in ? (d.flip ? j0 + j : i) : 0, c = in ? (d.flip ? i : j0 + j) : 0;
             const float g = ns_load<T>(d.in.src, r * d.in.ld_src + c);
-            const float b = s.update ? d.in.buf[r * d.in.ld_buf + c] : 0.f;
+            const float b = s.update ? gld<float>(d.in.buf + r * d.in.ld_buf + c) : 0.f;
             u[k] = in ? ns_u(g, b, s) : 0.f;
         }
         #pragma unroll
@@ -783,11 +905,11 @@ __device__ __forceinline__ void nw_step(const NsDev &d, int block, const NsStep 
     h16 *gs = xs + N::QB * N::XP;
     // the block and the partial sums, all loads before the first use
     constexpr int XL = kBlock * 4 / 16 / kNwThreads;
-    vec16 xv[XL];
+    u32x4 xv[XL];
     const h16 *xin = d.xt[0] + (int64_t)block * kBlock * 2;
     #pragma unroll
-    for (int l = 0; l < XL; l++) xv[l] = ldg16(xin + (int64_t)(l * kNwThreads + tid) * 8);
-    const bool summed = d.blocks > kSumBlocks;
+    for (int l = 0; l < XL; l++) xv[l] = gld<u32x4>(xin + (int64_t)(l * kNwThreads + tid) * 8);
+    const bool summed = ns_summed(d.blocks, P);
     const float *part = summed ? d.sum : d.part[turn];
     const int np = summed ? 1 : d.blocks;
     constexpr int GV = P * P / 4, GL = (GV + kNwThreads - 1) / kNwThreads;
@@ -795,19 +917,19 @@ __device__ __forceinline__ void nw_step(const NsDev &d, int block, const NsStep 
     #pragma unroll
     for (int l = 0; l < GL; l++) {
         const int v = l * kNwThreads + tid;
-        gv[l] = *reinterpret_cast<const f32x4 *>(part + (int64_t)(v < GV ? v : 0) * 4);
+        gv[l] = gld<f32x4>(part + (int64_t)(v < GV ? v : 0) * 4);
     }
     for (int b = 1; b < np; b++)
         #pragma unroll
         for (int l = 0; l < GL; l++) {
             const int v = l * kNwThreads + tid;
-            const f32x4 w = *reinterpret_cast<const f32x4 *>(part + (int64_t)b * P * P + (int64_t)(v < GV ? v : 0) * 4);
+            const f32x4 w = gld<f32x4>(part + (int64_t)b * P * P + (int64_t)(v < GV ? v : 0) * 4);
             gv[l][0] += w[0]; gv[l][1] += w[1]; gv[l][2] += w[2]; gv[l][3] += w[3];
         }
     #pragma unroll
     for (int l = 0; l < XL; l++) {
         const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
-        *reinterpret_cast<vec16 *>(xs + row * N::XP + c * 8) = xv[l];
+        *reinterpret_cast<u32x4 *>(xs + row * N::XP + c * 8) = xv[l];
     }
     #pragma unroll
     for (int l = 0; l < GL; l++) {
@@ -935,7 +1057,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_sum(NsTable t, int count, int t
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     #pragma unroll 4
     for (int b = quarter; b < d.blocks; b += 4) {
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(src + b * pp);
+        const f32x4 v = gld<f32x4>(src + b * pp);
         acc[0] += v[0]; acc[1] += v[1]; acc[2] += v[2]; acc[3] += v[3];
     }
     red[tid] = acc;
@@ -944,7 +1066,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_sum(NsTable t, int count, int t
         f32x4 o = red[tid];
         for (int k = 1; k < 4; k++)
             for (int e = 0; e < 4; e++) o[e] += red[k * 64 + tid][e];
-        *reinterpret_cast<f32x4 *>(d.sum + ((int64_t)w * 64 + tid) * 4) = o;
+        gst(d.sum + ((int64_t)w * 64 + tid) * 4, o);
     }
 }
 
@@ -954,29 +1076,59 @@ size_t table_bytes(int count)
     return (a + b + 255) / 256 * 256;
 }
 
-// The cut of a stage of `tiles` tiles whose longest product has `steps` k steps.
-// A piece keeps at least kMinSteps: below that its own start and the extra
-// launch cost more than the idle part of the chip.
-constexpr int kMinSteps = 8;
-NsCut ns_cut(int64_t tiles, int steps)
+constexpr int ns_slots(int bt) { return bt == 128 ? kNsSlots : kNsSlots / 2; }
+int64_t cut_bytes(const NsCut &c) { return c.pieces > 1 ? (int64_t)(c.tiles - c.whole) * c.pieces * c.bt * c.bt * 4 : 0; }
+
+// The time of a stage in us as measured (kernel traces of 256 x 256 to
+// 4096 x 4096, alone and in lists): per round of workgroups a part for finding
+// the matrix, the first loads and leaving the results (16 bytes an element at 26
+// GB/s a CU), and a part per k step, which depends on whether the CU is shared;
+// for cut tiles the launch that adds the pieces (5 us + 0.27 us per MB).
+//   256 x 256 (8 steps): 64-tiles 8.9, 128-tiles 14.3, 256-tiles 23.8
+//   1024 x 1024 (32 steps): 20.9, 13.5 + 5.5, 22.7 + 5.6
+//   4096 x 4096, R X (128 steps): 973, 421, 321
+double cut_time(const NsCut &c, int steps)
 {
-    NsCut c{(int)tiles, (int)tiles, 1, nullptr};
-    const int rest = (int)(tiles % kNsSlots);
-    if (!rest) return c;
-    int pieces = kNsSlots / rest;
-    if (pieces > steps / kMinSteps) pieces = steps / kMinSteps;
-    if (pieces < 2) return c;
-    c.whole = (int)tiles - rest;
-    c.pieces = pieces;
-    return c;
+    const int slots = ns_slots(c.bt), rest = c.tiles - c.whole;
+    if (c.bt == 64) {
+        const int rounds = (c.tiles + slots - 1) / slots;
+        return 5.5 + rounds * steps * (rounds > 1 ? 0.6 : 0.45);
+    }
+    const double step = c.bt == 128 ? 1.56 : 2.38, alone = c.bt == 128 ? 0.75 : 1.6, leave = c.bt == 128 ? 10.0 : 16.0;
+    const int units = rest * c.pieces;
+    double t = 2.0 + c.whole / slots * (leave + step * steps);
+    if (units) t += leave + (steps + c.pieces - 1) / c.pieces * (units * 2 <= slots ? alone : step);
+    if (c.pieces > 1) t += 5.0 + cut_bytes(c) * 0.27e-6;
+    return t;
 }
-int64_t cut_bytes(const NsCut &c) { return c.pieces > 1 ? (int64_t)(c.tiles - c.whole) * c.pieces * kPart * 4 : 0; }
+
+// The tile and the cut of a stage: tiles are counted over the whole list, steps
+// are those of the longest product.  Small tiles spread the operands of few
+// products over many CUs; large ones read and stage fewer bytes a product.
+NsCut ns_stage(const NsPlan &p, int sym, int steps)
+{
+    NsCut best{};
+    double least = 1e30;
+    for (int l = 0; l < 3; l++) {
+        const int bt = 64 << l, tiles = (int)p.work[(l == 0 ? PRE_GRAM_S : (l == 1 ? PRE_GRAM : PRE_GRAM_L)) + !sym];
+        const int rest = tiles % ns_slots(bt), most = l == 0 || !rest ? 1 : ns_slots(bt) / rest;
+        for (int pieces = 1; pieces <= most && (pieces == 1 || pieces * 4 <= steps); pieces += (pieces + 3) / 4) {
+            const NsCut c{bt, tiles, l == 0 ? tiles : tiles - rest, pieces, nullptr};
+            const double t = cut_time(c, steps);
+            if (t < least) {
+                least = t;
+                best = c;
+            }
+        }
+    }
+    if (best.pieces == 1) best.whole = best.tiles;
+    return best;
+}
 
 struct NsCuts { NsCut gram, square, apply; };
 NsCuts ns_cuts(const NsPlan &p)
 {
-    return NsCuts{ns_cut(p.work[PRE_GRAM], p.long_side / 32), ns_cut(p.work[PRE_GRAM], p.short_side / 32),
-                  ns_cut(p.work[PRE_APPLY], p.short_side / 32)};
+    return NsCuts{ns_stage(p, 1, p.long_side / 32), ns_stage(p, 1, p.short_side / 32), ns_stage(p, 0, p.short_side / 32)};
 }
 
 }  // namespace
@@ -1013,19 +1165,29 @@ NsTable ns_table(void *ws, int count)
     return t;
 }
 
-template <int MODE, typename W>
-hipError_t ns_product(const NsPlan &p, const NsTable &t, const NsStep &s, int turn, const NsCut &cut, hipStream_t st)
+template <int BT, int MODE, typename W>
+hipError_t ns_product_bt(const NsPlan &p, const NsTable &t, const NsStep &s, int turn, const NsCut &cut, hipStream_t st)
 {
     const int rest = cut.tiles - cut.whole;
     {
         TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, ns_sym(MODE) ? 0.0 : p.flops);
-        hipLaunchKernelGGL((k_ns_product<MODE, W>), dim3((unsigned)(cut.whole + rest * cut.pieces)), dim3(256), 0, st, t,
-                           p.count, s, turn, cut);
+        hipLaunchKernelGGL((k_ns_product<BT, MODE, W>), dim3((unsigned)(cut.whole + rest * cut.pieces)), dim3(BT * 2), 0, st,
+                           t, p.count, s, turn, cut);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (cut.pieces == 1) return hipSuccess;
     TraceScope tr(KC_SMALL, KID_ORTHO, st, (double)cut_bytes(cut), 0.0);
-    hipLaunchKernelGGL((k_ns_finish<MODE, W>), dim3((unsigned)rest * 4), dim3(256), 0, st, t, p.count, s, turn, cut);
+    hipLaunchKernelGGL((k_ns_finish<BT, MODE, W>), dim3((unsigned)rest * (BT * BT / (kSub * kSub))), dim3(256), 0, st, t,
+                       p.count, s, turn, cut);
+    return hipGetLastError();
+}
+template <int MODE, typename W>
+hipError_t ns_product(const NsPlan &p, const NsTable &t, const NsStep &s, int turn, const NsCut &cut, hipStream_t st)
+{
+    if (cut.bt == 128) return ns_product_bt<128, MODE, W>(p, t, s, turn, cut, st);
+    if (cut.bt == 256) return ns_product_bt<256, MODE, W>(p, t, s, turn, cut, st);
+    TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, ns_sym(MODE) ? 0.0 : p.flops);
+    hipLaunchKernelGGL((k_ns_direct<MODE, W>), dim3((unsigned)cut.tiles), dim3(256), 0, st, t, p.count, s, turn);
     return hipGetLastError();
 }
 

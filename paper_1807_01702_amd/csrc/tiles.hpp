@@ -221,9 +221,8 @@ inline WgTrPlan wgrad_f32_plan(int64_t m, int n, int h, int w, int c_in, int c_o
 constexpr int kLnMaxC = 16384;             // 16 channels a thread of a 1024-thread workgroup
 
 // ---- Newton-Schulz orthogonalisation ---------------------------------------
-constexpr int kNsTile = 128;               // outputs of a product tile, and the padding of both sides
 constexpr int kNsSlots = 512;               // product workgroups the chip holds (2 a CU)
-constexpr int kNsStages = 6;               // stages with work items of their own
+constexpr int kNsStages = 10;               // stages with work items of their own
 constexpr int kNsChunk = 48;               // matrices per table launch (kernel arguments below 4 KiB)
 constexpr int kNsMaxCount = 1024;          // matrices of a call
 constexpr int kNsMaxShort = 16384, kNsMaxLong = 1 << 20;

@@ -44,8 +44,8 @@ def _ns64(u, steps=5, coef=COEF, eps=1e-7):
     x = x / (torch.sqrt((x * x).sum()) + eps)
     a, b, c = coef
     for _ in range(steps):
-        g = x @ x.t()
-        x = a * x + (b * g + c * (g @ g)) @ x
+        g = x @ x.t().contiguous()
+        x = a * x + (b * g + c * (g @ g)) @ x.contiguous()
     return x if u.shape[0] <= u.shape[1] else x.t()
 
 
@@ -57,6 +57,31 @@ def _close(name, got, ref, dtype, rel=REL):
     err = float((_d(got) - ref).norm())
     tol = (rel + HALF[dtype]) * float(ref.norm())
     assert err <= tol, "%s: off by %.3g, tolerance %.3g" % (name, err, tol)
+
+
+# lists whose tiles run whole and in pieces, in each tile size, and hang over the matrices' ends
+LARGE = [[(1024, 1024)] * 8, [(2048, 2048)], [(2048, 2048)] * 4, [(1024, 4096)] * 6, [(1300, 2900)] * 3, [(1023, 4093)],
+         [(520, 2000), (2700, 1100), (130, 4000)], [(700, 700), (64, 300), (200, 1900), (1500, 129)], [(4096, 1000)],
+         [(3000, 2990)]]
+
+
+@pytest.mark.parametrize("shapes", LARGE, ids=lambda s: "%dx%dx%d" % (len(s), *s[0]))
+def test_large_lists(shapes):
+    """The reference runs on the GPU in float64 (library products)."""
+    B = _B()
+    xs = [_rand(i * 31 + r, r, c).float().cuda() for i, (r, c) in enumerate(shapes)]
+    outs = [torch.full_like(x, 5.0) for x in xs]
+    B.bnr_orthogonalize(xs, outs)
+    again = [torch.empty_like(x) for x in xs]
+    B.bnr_orthogonalize(xs, again)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, again))
+    for x, o in zip(xs, outs):
+        ref = _ns64(x.double())
+        err = float((o.double() - ref).norm() / ref.norm())
+        # longer sums: sqrt(q / 32) 2^-24 per product past q = 2048
+        tol = REL * max(1.0, (max(x.shape) / 2048) ** 0.5) + HALF[torch.float32]
+        assert err <= tol, (tuple(x.shape), err)
 
 
 def _strided(t, dtype, pad):
