@@ -667,12 +667,13 @@ typedef struct {
     int32_t rows, cols;
     const void *x;         /* [rows][cols] (x_dtype)                               */
     int32_t x_ld;
-    void *out;             /* [rows][cols] (out_dtype); may overlap any x          */
+    void *out;             /* [rows][cols] (out_dtype); may overlap its own x      */
     int32_t out_ld;
 } bnr_ortho_item;
 
-/* out = the orthogonalised x, for every matrix of the list.  The outs must not
- * overlap each other (BNR_ERR_ALIAS).  An empty list is nothing to do. */
+/* out = the orthogonalised x, for every matrix of the list.  An out must not
+ * overlap another one, nor another matrix's x (BNR_ERR_ALIAS).  An empty list is
+ * nothing to do. */
 size_t bnr_orthogonalize_workspace_size(const bnr_ortho_item *items, int32_t count);
 bnr_status bnr_orthogonalize(const bnr_ortho_item *items, int32_t count, bnr_dtype x_dtype, bnr_dtype out_dtype,
                              const bnr_ns_params *ns, void *ws, size_t ws_bytes, void *stream);

@@ -1881,10 +1881,11 @@ static bool areas_share(const NsArea &a, const NsArea &b)
 }
 
 // Refuses a list in which a written matrix shares memory with another one of
-// the list's.  area(i) gives the i-th of n; the indices are sorted by address,
-// so matrices that lie apart cost n log n.
+// the list's (own: another item's; an item's own may overlap).  area(i) gives
+// the i-th of n; the indices are sorted by address, so matrices that lie apart
+// cost n log n.
 template <typename F>
-static bnr_status check_ns_areas(int n, F &&area)
+static bnr_status check_ns_areas(int n, bool own, F &&area)
 {
     static_assert(kNsMaxCount * 4 <= 4096, "index buffer");
     uint16_t order[kNsMaxCount * 4];
@@ -1896,7 +1897,7 @@ static bnr_status check_ns_areas(int n, F &&area)
         for (int j = i + 1; j < n; j++) {
             const NsArea b = area(order[j]);
             if (b.lo >= end) break;
-            if ((a.written || b.written) && areas_share(a, b))
+            if ((a.written || b.written) && !(own && a.item == b.item) && areas_share(a, b))
                 return fail(BNR_ERR_ALIAS, "matrices %d and %d: an output shares memory with another argument", a.item,
                             b.item);
         }
@@ -1964,10 +1965,11 @@ bnr_status bnr_orthogonalize(const bnr_ortho_item *items, int32_t count, bnr_dty
         TRY(check_ns_view(i, "out", t.out, t.out_ld, t.cols, esize(out_dtype)));
         ns_plan_add(plan, t.rows, t.cols);
     }
-    const int64_t es = esize(out_dtype);
-    TRY(check_ns_areas(count, [&](int i) {
-        const bnr_ortho_item &t = items[i];
-        return NsArea{reinterpret_cast<uintptr_t>(t.out), t.rows, t.cols * es, t.out_ld * es, true, i};
+    const int64_t eo = esize(out_dtype), ex = esize(x_dtype);
+    TRY(check_ns_areas(count * 2, true, [&](int k) {
+        const bnr_ortho_item &t = items[k / 2];
+        return k % 2 ? NsArea{reinterpret_cast<uintptr_t>(t.x), t.rows, t.cols * ex, t.x_ld * ex, false, k / 2}
+                     : NsArea{reinterpret_cast<uintptr_t>(t.out), t.rows, t.cols * eo, t.out_ld * eo, true, k / 2};
     }));
     if (!count) return ok();
     TRY(check_ns_plan(plan));
@@ -2011,7 +2013,7 @@ bnr_status bnr_muon_update(const bnr_muon_item *items, int32_t count, bnr_dtype 
                                : NsArea{reinterpret_cast<uintptr_t>(t.g), t.rows, t.cols * es_g, t.g_ld * es_g, false, k / 4};
         }
     };
-    TRY(check_ns_areas(count * 4, area));
+    TRY(check_ns_areas(count * 4, false, area));
     if (p->lr_dev)
         for (int k = 0; k < count * 4; k++) {
             const NsArea a = area(k), l{reinterpret_cast<uintptr_t>(p->lr_dev), 1, 4, 4, false, k / 4};

@@ -314,7 +314,9 @@ struct NsStep {                   // one call's numbers
 // what a list needs: filled matrix by matrix, then the workspace and the grids follow
 struct NsPlan {
     int count, short_side, long_side;             // longest padded sides of the wide matrices
+    int stepwise;                                 // narrow matrices all take a launch a step
     int64_t bytes, work[kNsStages];
+    int64_t ride_bytes, ride_work[kNsStages];     // single-block matrices, if they do
     double flops, narrow_flops, values;    // per step: wide, narrow matrices; matrix elements
 };
 typedef NsIn (*NsFill)(const void *arg, int i);

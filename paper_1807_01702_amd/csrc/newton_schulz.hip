@@ -50,9 +50,9 @@ constexpr int kSub = 64;                             // wide matrices are padded
 // Stages of a call and their work items: momentum and squares; the narrow
 // matrices' blocks and the sums of their partial Gram matrices; the wide ones'
 // conversion, symmetric product tiles and general product tiles, and the same in
-// large and in small tiles.
+// large and in small tiles; the matrices of a single block, whole.
 enum { PRE_SQ = 0, PRE_NARROW = 1, PRE_SUM = 2, PRE_PREP = 3, PRE_GRAM = 4, PRE_APPLY = 5, PRE_GRAM_L = 6, PRE_APPLY_L = 7,
-       PRE_GRAM_S = 8, PRE_APPLY_S = 9, kPre = kNsStages };
+       PRE_GRAM_S = 8, PRE_APPLY_S = 9, PRE_TINY = 10, kPre = kNsStages };
 
 // one matrix of the list on the device: the caller's arguments and its place in the workspace
 struct NsDev {
@@ -80,7 +80,8 @@ constexpr int kBlock = 16384;      // values of a narrow matrix's block: [kBlock
 constexpr int kSumValues = 2 * 128 * 128;
 __host__ __device__ inline bool ns_summed(int blocks, int P) { return blocks * (int64_t)(P * P) > kSumValues; }
 
-__host__ __device__ inline NsSize ns_size(int rows, int cols)
+// whole: a matrix of a single block runs as a launch of its own over all steps.
+__host__ __device__ inline NsSize ns_size(int rows, int cols, int whole)
 {
     NsSize z;
     z.flip = rows > cols;
@@ -92,14 +93,20 @@ __host__ __device__ inline NsSize ns_size(int rows, int cols)
     if (n > (unsigned)rows) n = rows;
     const unsigned rp = ((unsigned)rows + n - 1) / n;
     z.parts = (int)(((unsigned)rows + rp - 1) / rp);
+    for (int k = 0; k < kPre; k++) z.work[k] = 0;
     z.work[PRE_SQ] = z.parts;
-    for (int k = 1; k < kPre; k++) z.work[k] = 0;
     z.blocks = 0;
     if (z.p <= kNarrow) {
         z.P = z.p <= 32 ? 32 : (z.p <= 64 ? 64 : 128);
         const int qb = kBlock / z.P;
         z.blocks = (z.q + qb - 1) / qb;
         z.Q = z.blocks * qb;
+        if (z.blocks == 1 && whole) {            // nothing of it passes through the workspace
+            z.work[PRE_SQ] = 0;
+            z.work[PRE_TINY] = 1;
+            z.bytes = 0;
+            return z;
+        }
         z.work[PRE_NARROW] = z.blocks;
         if (ns_summed(z.blocks, z.P)) z.work[PRE_SUM] = z.P * z.P / 256;
         z.bytes = kMaxParts * 8 + (int64_t)z.blocks * (kBlock * 4 + 2 * z.P * z.P * 4) + z.P * z.P * 4;
@@ -120,7 +127,7 @@ __host__ __device__ inline NsSize ns_size(int rows, int cols)
 }
 
 struct NsChunk {                   // by value: the next matrices of the list
-    int first, count;
+    int first, count, whole;
     int64_t at;                    // workspace offset and running counts in front of them
     int work[kPre];
     NsIn in[kNsChunk];
@@ -133,7 +140,7 @@ __global__ __launch_bounds__(64) void k_ns_table(NsChunk c, NsTable t, char *bas
     const bool in = i < c.count;
     NsDev d;
     d.in = c.in[in ? i : 0];
-    NsSize z = ns_size(d.in.rows, d.in.cols);
+    NsSize z = ns_size(d.in.rows, d.in.cols, c.whole);
     int64_t at = in ? z.bytes : 0;
     int work[kPre];
     for (int k = 0; k < kPre; k++) work[k] = in ? z.work[k] : 0;
@@ -806,22 +813,16 @@ __device__ __forceinline__ void nw_load4(const h16 *p, float *v)
     for (int e = 0; e < 4; e++) v[e] = (float)hi[e] + (float)lo[e];
 }
 
-// The block in LDS to the workspace, and its partial Gram matrix (S^2 times it).
-template <int P>
-__device__ __forceinline__ void nw_gram(const NsDev &d, int block, const h16 *xs, float *part)
+// The block's partial Gram matrix over `steps` k steps of 32 columns (S^2 times
+// it): the wave's tile in acc.  False for a wave without one (P = 32: four waves
+// have a tile).
+template <int P, int MI, int NI>
+__device__ __forceinline__ bool nw_gram(const h16 *xs, int steps, f32x4 (&acc)[MI][NI])
 {
     using N = Nw<P>;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    h16 *out = d.xt[0] + (int64_t)block * kBlock * 2;
-    #pragma unroll
-    for (int l = 0; l < kBlock * 4 / 16 / kNwThreads; l++) {
-        const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
-        gst(out + (int64_t)v * 8, *reinterpret_cast<const u32x4 *>(xs + row * N::XP + c * 8));
-    }
-    constexpr int MI = N::TM / 16, NI = N::TN / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wm = wave / N::WN, wn = wave % N::WN;
-    if (wm * N::TM >= P) return;                 // P = 32: four waves have a tile
-    f32x4 acc[MI][NI];
+    if (wm * N::TM >= P) return false;
     nw_zero(acc);
     // fragments of 8 consecutive block columns of one row of X: transposing reads
     const int g = lane / 16, q = lane % 16;
@@ -830,7 +831,7 @@ __device__ __forceinline__ void nw_gram(const NsDev &d, int block, const h16 *xs
         return __builtin_bit_cast(f16x8, tr_frag(base + k * 32 * N::XP + nw_k(i) + part_ * 32, N::XP));
     };
     #pragma unroll 4
-    for (int k = 0; k < N::QB / 32; k++) {
+    for (int k = 0; k < steps; k++) {
         f16x8 ah[MI], al[MI], bh[NI], bl[NI];
         #pragma unroll
         for (int i = 0; i < MI; i++) {
@@ -851,13 +852,39 @@ __device__ __forceinline__ void nw_gram(const NsDev &d, int block, const h16 *xs
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
             }
     }
-    // symmetric: element (i, j) goes to row j, where a lane's four i are consecutive
-    float *o = part + (int64_t)block * P * P;
+    return true;
+}
+
+// What a symmetric P x P product's tiles hold at (i, j) goes to row j, where a
+// lane's four i are consecutive: put(row, col, values).
+template <int P, int MI, int NI, typename F>
+__device__ __forceinline__ void nw_tiles(const f32x4 (&acc)[MI][NI], F &&put)
+{
+    using N = Nw<P>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane / 16, q = lane % 16;
+    const int wm = wave / N::WN, wn = wave % N::WN;
     #pragma unroll
     for (int i = 0; i < MI; i++)
         #pragma unroll
-        for (int j = 0; j < NI; j++)
-            gst(o + (wn * N::TN + j * 16 + q) * P + wm * N::TM + i * 16 + 4 * g, acc[i][j]);
+        for (int j = 0; j < NI; j++) put(wn * N::TN + j * 16 + q, wm * N::TM + i * 16 + 4 * g, acc[i][j]);
+}
+
+// The block in LDS to the workspace, and its partial Gram matrix.
+template <int P>
+__device__ __forceinline__ void nw_leave(const NsDev &d, int block, const h16 *xs, float *part)
+{
+    using N = Nw<P>;
+    const int tid = threadIdx.x;
+    h16 *out = d.xt[0] + (int64_t)block * kBlock * 2;
+    #pragma unroll
+    for (int l = 0; l < kBlock * 4 / 16 / kNwThreads; l++) {
+        const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
+        gst(out + (int64_t)v * 8, *reinterpret_cast<const u32x4 *>(xs + row * N::XP + c * 8));
+    }
+    f32x4 acc[N::TM / 16][N::TN / 16];
+    float *o = part + (int64_t)block * P * P;
+    if (nw_gram<P>(xs, N::QB / 32, acc))
+        nw_tiles<P>(acc, [&](int row, int col, const f32x4 &v) { gst(o + row * P + col, v); });
 }
 
 // Stage 2 of a narrow matrix: X's block as pairs, and its partial Gram matrix.
@@ -893,15 +920,97 @@ __device__ __forceinline__ void nw_prepare(const NsDev &d, int block, const NsSt
         }
     }
     __syncthreads();
-    nw_gram<P>(d, block, xs, d.part[0]);
+    nw_leave<P>(d, block, xs, d.part[0]);
+}
+
+// R = a I + b G + c G G over G's place in LDS.  Starts after a barrier, ends with one.
+template <int P>
+__device__ __forceinline__ void nw_polynomial(const NsStep &s, h16 *gs)
+{
+    using N = Nw<P>;
+    constexpr int MI = N::TM / 16, NI = N::TN / 16;
+    const int wave = threadIdx.x >> 6, wm = wave / N::WN, wn = wave % N::WN;
+    const bool has = wm * N::TM < P;
+    f32x4 acc[MI][NI];
+    nw_zero(acc);
+    if (has) nw_product<MI, NI, P / 32>(gs + wm * N::TM * N::GP, N::GP, gs + wn * N::TN * N::GP, N::GP, acc);
+    float v[MI * NI][4];
+    int at = 0;
+    if (has)
+        nw_tiles<P>(acc, [&](int row, int col, const f32x4 &t) {
+            float gg[4];
+            nw_load4(gs + row * N::GP + nw_k(col), gg);
+            #pragma unroll
+            for (int e = 0; e < 4; e++)
+                v[at][e] = __builtin_fmaf(s.c, t[e] * kInvS, s.b * gg[e]) + (row == col + e ? s.a * kS : 0.f);
+            at++;
+        });
+    __syncthreads();
+    at = 0;
+    if (has) nw_tiles<P>(acc, [&](int row, int col, const f32x4 &) { nw_store4(gs + row * N::GP + nw_k(col), v[at++]); });
+    __syncthreads();
+}
+
+// Y = R X of the block: this wave's YM x YN tile.
+template <int P, int MI, int NI>
+__device__ __forceinline__ void nw_apply(const h16 *xs, const h16 *gs, f32x4 (&acc)[MI][NI])
+{
+    using N = Nw<P>;
+    const int wave = threadIdx.x >> 6, ym = wave / N::YWN * N::YM, yn = wave % N::YWN * N::YN;
+    nw_zero(acc);
+    nw_product<MI, NI, P / 32>(gs + ym * N::GP, N::GP, xs + yn * N::XP, N::XP, acc);
+}
+// Y over X's place.  The caller has had a barrier since the last read of X.
+template <int P, int MI, int NI>
+__device__ __forceinline__ void nw_keep(h16 *xs, const f32x4 (&acc)[MI][NI])
+{
+    using N = Nw<P>;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane / 16, q = lane % 16;
+    const int ym = wave / N::YWN * N::YM, yn = wave % N::YWN * N::YN;
+    #pragma unroll
+    for (int i = 0; i < MI; i++)
+        #pragma unroll
+        for (int j = 0; j < NI; j++) {
+            float v[4];
+            #pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = acc[i][j][e] * kInvS;
+            nw_store4(xs + (yn + j * 16 + q) * N::XP + nw_k(ym + i * 16 + 4 * g), v);
+        }
+}
+// Y into the caller's matrix, through X's place so that rows are written whole
+// (the same barrier as above).
+template <int P, typename W, int MI, int NI>
+__device__ __forceinline__ void nw_result(const NsDev &d, int block, const NsStep &s, h16 *xs, const f32x4 (&acc)[MI][NI])
+{
+    using N = Nw<P>;
+    constexpr int FP = P + 1;
+    static_assert(N::QB * FP * 4 <= N::XBytes, "the results fit the block's place");
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane / 16, q = lane % 16;
+    const int ym = wave / N::YWN * N::YM, yn = wave % N::YWN * N::YN;
+    float *fs = (float *)xs;
+    #pragma unroll
+    for (int i = 0; i < MI; i++)
+        #pragma unroll
+        for (int j = 0; j < NI; j++)
+            #pragma unroll
+            for (int e = 0; e < 4; e++)
+                fs[(yn + j * 16 + q) * FP + ym + i * 16 + 4 * g + e] = acc[i][j][e] * (kInvS * kInvS);
+    __syncthreads();
+    const float lr = ns_rate(s);
+    const int j0 = block * N::QB;
+    #pragma unroll 4
+    for (int e = tid; e < kBlock; e += kNwThreads) {
+        const int i = d.flip ? e % P : e / N::QB, j = d.flip ? e / P : e % N::QB;
+        if (i < d.p && j0 + j < d.q)
+            ns_result<W>(d.in, s, lr, d.flip ? j0 + j : i, d.flip ? i : j0 + j, fs[j * FP + i]);
+    }
 }
 
 template <int P, bool LAST, typename W>
 __device__ __forceinline__ void nw_step(const NsDev &d, int block, const NsStep &s, int turn, h16 *xs)
 {
     using N = Nw<P>;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int g = lane / 16, q = lane % 16;
+    const int tid = threadIdx.x;
     h16 *gs = xs + N::QB * N::XP;
     // the block and the partial sums, all loads before the first use
     constexpr int XL = kBlock * 4 / 16 / kNwThreads;
@@ -943,82 +1052,96 @@ __device__ __forceinline__ void nw_step(const NsDev &d, int block, const NsStep 
         }
     }
     __syncthreads();
-    // R = a I + b G + c G G, over G's place
-    {
-        constexpr int MI = N::TM / 16, NI = N::TN / 16;
-        const int wm = wave / N::WN, wn = wave % N::WN;
-        const bool has = wm * N::TM < P;
-        f32x4 acc[MI][NI];
-        nw_zero(acc);
-        if (has) {
-            nw_product<MI, NI, P / 32>(gs + wm * N::TM * N::GP, N::GP, gs + wn * N::TN * N::GP, N::GP, acc);
-            #pragma unroll
-            for (int i = 0; i < MI; i++)
-                #pragma unroll
-                for (int j = 0; j < NI; j++) {
-                    const int row = wn * N::TN + j * 16 + q, col = wm * N::TM + i * 16 + 4 * g;
-                    float gg[4];
-                    nw_load4(gs + row * N::GP + nw_k(col), gg);
-                    #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        acc[i][j][e] = __builtin_fmaf(s.c, acc[i][j][e] * kInvS, s.b * gg[e]) +
-                                       (row == col + e ? s.a * kS : 0.f);
-                }
-        }
-        __syncthreads();
-        if (has)
-            #pragma unroll
-            for (int i = 0; i < MI; i++)
-                #pragma unroll
-                for (int j = 0; j < NI; j++) {
-                    const int row = wn * N::TN + j * 16 + q, col = wm * N::TM + i * 16 + 4 * g;
-                    const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                    nw_store4(gs + row * N::GP + nw_k(col), v);
-                }
-        __syncthreads();
-    }
-    // Y = R X
-    constexpr int MI = N::YM / 16, NI = N::YN / 16;
-    const int ym = wave / N::YWN * N::YM, yn = wave % N::YWN * N::YN;
-    f32x4 acc[MI][NI];
-    nw_zero(acc);
-    nw_product<MI, NI, P / 32>(gs + ym * N::GP, N::GP, xs + yn * N::XP, N::XP, acc);
+    nw_polynomial<P>(s, gs);
+    f32x4 acc[N::YM / 16][N::YN / 16];
+    nw_apply<P>(xs, gs, acc);
     __syncthreads();
     if constexpr (!LAST) {
-        #pragma unroll
-        for (int i = 0; i < MI; i++)
-            #pragma unroll
-            for (int j = 0; j < NI; j++) {
-                float v[4];
-                #pragma unroll
-                for (int e = 0; e < 4; e++) v[e] = acc[i][j][e] * kInvS;
-                nw_store4(xs + (yn + j * 16 + q) * N::XP + nw_k(ym + i * 16 + 4 * g), v);
-            }
+        nw_keep<P>(xs, acc);
         __syncthreads();
-        nw_gram<P>(d, block, xs, d.part[turn ^ 1]);
+        nw_leave<P>(d, block, xs, d.part[turn ^ 1]);
     } else {
-        // through LDS, so that rows of the caller's matrix are written whole
-        constexpr int FP = P + 1;
-        float *fs = (float *)xs;
-        #pragma unroll
-        for (int i = 0; i < MI; i++)
-            #pragma unroll
-            for (int j = 0; j < NI; j++)
-                #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    fs[(yn + j * 16 + q) * FP + ym + i * 16 + 4 * g + e] = acc[i][j][e] * (kInvS * kInvS);
+        nw_result<P, W>(d, block, s, xs, acc);
+    }
+}
+
+// A matrix of one block, all of it in one workgroup: momentum, norm, every step
+// and the result, X and G in LDS throughout.
+template <int P, typename T, typename W>
+__device__ __forceinline__ void nw_tiny(const NsDev &d, const NsStep &s, h16 *xs, double *red)
+{
+    using N = Nw<P>;
+    const int tid = threadIdx.x;
+    h16 *gs = xs + N::QB * N::XP;
+    constexpr int U = kBlock / kNwThreads;
+    float u[U], b[U];
+    auto at = [&](int k, int &i, int &j) __attribute__((always_inline)) {
+        const int e = tid + k * kNwThreads;      // along the caller's rows
+        i = d.flip ? e % P : e / N::QB;
+        j = d.flip ? e / P : e % N::QB;
+        return i < d.p && j < d.q;
+    };
+    #pragma unroll
+    for (int k = 0; k < U; k++) {
+        int i, j;
+        const bool in = at(k, i, j);
+        const int64_t r = in ? (d.flip ? j : i) : 0, c = in ? (d.flip ? i : j) : 0;
+        u[k] = ns_load<T>(d.in.src, r * d.in.ld_src + c);
+        b[k] = s.update ? gld<float>(d.in.buf + r * d.in.ld_buf + c) : 0.f;
+    }
+    double sum = 0.0;
+    #pragma unroll
+    for (int k = 0; k < U; k++) {
+        int i, j;
+        if (!at(k, i, j)) {
+            u[k] = 0.f;
+            continue;
+        }
+        if (s.update) {
+            b[k] = __builtin_fmaf(s.momentum, b[k], u[k]);
+            gst(d.in.buf + (int64_t)(d.flip ? j : i) * d.in.ld_buf + (d.flip ? i : j), b[k]);
+        }
+        u[k] = ns_u(u[k], b[k], s);
+        sum += (double)u[k] * (double)u[k];
+    }
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (tid % 64 == 0) red[tid / 64] = sum;
+    __syncthreads();
+    sum = red[0];
+    for (int w = 1; w < kNwThreads / 64; w++) sum += red[w];
+    const float scale = (float)((double)kS / (sqrt(sum) + (double)s.eps));
+    #pragma unroll
+    for (int k = 0; k < U; k++) {
+        int i, j;
+        at(k, i, j);
+        h16 hi, lo;
+        ns_pair(u[k] * scale, hi, lo);
+        h16 *o = xs + j * N::XP + nw_k(i);
+        o[0] = hi;
+        o[32] = lo;
+    }
+    __syncthreads();
+    const int columns = (d.q + 31) / 32;
+    for (int k = 0; k < s.steps; k++) {
+        f32x4 gram[N::TM / 16][N::TN / 16];
+        if (nw_gram<P>(xs, columns, gram))
+            nw_tiles<P>(gram, [&](int row, int col, const f32x4 &v) {
+                const float f[4] = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
+                nw_store4(gs + row * N::GP + nw_k(col), f);
+            });
         __syncthreads();
-        const float lr = ns_rate(s);
-        const int j0 = block * N::QB;
-        for (int e = tid; e < kBlock; e += kNwThreads) {
-            const int i = d.flip ? e % P : e / N::QB, j = d.flip ? e / P : e % N::QB;
-            if (i < d.p && j0 + j < d.q)
-                ns_result<W>(d.in, s, lr, d.flip ? j0 + j : i, d.flip ? i : j0 + j, fs[j * FP + i]);
+        nw_polynomial<P>(s, gs);
+        f32x4 acc[N::YM / 16][N::YN / 16];
+        nw_apply<P>(xs, gs, acc);
+        __syncthreads();
+        if (k + 1 < s.steps) {
+            nw_keep<P>(xs, acc);
+            __syncthreads();
+        } else {
+            nw_result<P, W>(d, 0, s, xs, acc);
         }
     }
 }
-static_assert(Nw<128>::QB * (128 + 1) * 4 <= Nw<128>::XBytes && Nw<64>::QB * (64 + 1) * 4 <= Nw<64>::XBytes &&
-              Nw<32>::QB * (32 + 1) * 4 <= Nw<32>::XBytes, "the result's staging fits the block's place");
 
 enum { NW_PREPARE = 0, NW_STEP = 1, NW_LAST = 2 };
 
@@ -1041,6 +1164,19 @@ __global__ __launch_bounds__(kNwThreads) void k_ns_narrow(NsTable t, int count, 
     if (d.P == 128) go(std::integral_constant<int, 128>{});
     else if (d.P == 64) go(std::integral_constant<int, 64>{});
     else go(std::integral_constant<int, 32>{});
+}
+
+// T: source type, W: result type
+template <typename T, typename W>
+__global__ __launch_bounds__(kNwThreads) void k_ns_tiny(NsTable t, int count, NsStep s)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ double red[kNwThreads / 64];
+    const int it = ns_find(t.pre[PRE_TINY], count, blockIdx.x);
+    const NsDev &d = t.items[it];
+    if (d.P == 128) nw_tiny<128, T, W>(d, s, (h16 *)smem, red);
+    else if (d.P == 64) nw_tiny<64, T, W>(d, s, (h16 *)smem, red);
+    else nw_tiny<32, T, W>(d, s, (h16 *)smem, red);
 }
 
 // The sum of a narrow matrix's partial Gram matrices: 64 float4 outputs a
@@ -1135,10 +1271,25 @@ NsCuts ns_cuts(const NsPlan &p)
 
 void ns_plan_add(NsPlan &p, int rows, int cols)
 {
-    const NsSize z = ns_size(rows, cols);
+    // Single-block matrices run whole (128 x 128: 57 us against 85 in a launch a
+    // step), unless the list has narrow matrices of several blocks: those take a
+    // launch a step anyway, and the others ride along (dense block 1's filters:
+    // 105 us against 163 with a launch of their own first).
+    const NsSize z = ns_size(rows, cols, !p.stepwise);
+    if (z.blocks > 1 && !p.stepwise) {
+        p.stepwise = 1;
+        for (int k = 0; k < kPre; k++) p.work[k] += p.ride_work[k];
+        p.work[PRE_TINY] = 0;
+        p.bytes += p.ride_bytes;
+    }
     p.count++;
     p.bytes += z.bytes;
     for (int k = 0; k < kPre; k++) p.work[k] += z.work[k];
+    if (z.work[PRE_TINY]) {
+        const NsSize r = ns_size(rows, cols, 0);
+        p.ride_bytes += r.bytes;
+        for (int k = 0; k < kPre; k++) p.ride_work[k] += r.work[k];
+    }
     (z.blocks ? p.narrow_flops : p.flops) += (double)z.p * (z.p + 1) * z.q + (double)z.p * z.p * (z.p + 1) + 2.0 * z.p * z.p * z.q;
     p.values += (double)rows * cols;
     if (z.blocks) return;
@@ -1191,20 +1342,37 @@ hipError_t ns_product(const NsPlan &p, const NsTable &t, const NsStep &s, int tu
     return hipGetLastError();
 }
 
-// p: the kernel's launch over the narrow matrices (more LDS than the default limit)
+// Lets a kernel take kNwLds bytes of LDS, more than the default limit, on the current device.
+template <typename K>
+hipError_t allow_lds(K kern, std::atomic<uint64_t> &ready)
+{
+    int dev = 0;
+    if (hipError_t e = hipGetDevice(&dev)) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (ready.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    if (hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kNwLds)) return e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+    return hipSuccess;
+}
+
+template <typename T, typename W>
+hipError_t ns_tiny(const NsPlan &p, const NsTable &t, const NsStep &s, hipStream_t st)
+{
+    auto kern = k_ns_tiny<T, W>;
+    static std::atomic<uint64_t> ready{0};       // one bit per device
+    if (hipError_t e = allow_lds(kern, ready)) return e;
+    TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, 0.0);
+    hipLaunchKernelGGL(kern, dim3((unsigned)p.work[PRE_TINY]), dim3(kNwThreads), kNwLds, st, t, p.count, s);
+    return hipGetLastError();
+}
+
+// one stage of the narrow matrices
 template <int STAGE, typename T>
 hipError_t ns_narrow(const NsPlan &p, const NsTable &t, const NsStep &s, int turn, hipStream_t st)
 {
     auto kern = k_ns_narrow<STAGE, T>;
     static std::atomic<uint64_t> ready{0};       // one bit per device
-    int dev = 0;
-    if (hipError_t e = hipGetDevice(&dev)) return e;
-    const uint64_t bit = 1ull << (dev & 63);
-    if (!(ready.load(std::memory_order_relaxed) & bit)) {
-        if (hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kNwLds))
-            return e;
-        ready.fetch_or(bit, std::memory_order_relaxed);
-    }
+    if (hipError_t e = allow_lds(kern, ready)) return e;
     TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, STAGE == NW_PREPARE ? 0.0 : p.narrow_flops);
     hipLaunchKernelGGL(kern, dim3((unsigned)p.work[PRE_NARROW]), dim3(kNwThreads), kNwLds, st, t, p.count, s, turn);
     return hipGetLastError();
@@ -1226,6 +1394,7 @@ hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep
 {
     const NsTable t = ns_table(ws, p.count);
     NsChunk c;
+    c.whole = !p.stepwise;
     c.at = (int64_t)table_bytes(p.count);
     for (int k = 0; k < kPre; k++) c.work[k] = 0;
     for (c.first = 0; c.first < p.count; c.first += kNsChunk) {
@@ -1235,11 +1404,18 @@ hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep
         hipLaunchKernelGGL(k_ns_table, dim3(1), dim3(64), 0, st, c, t, (char *)ws);
         if (hipError_t e = hipGetLastError()) return e;
         for (int i = 0; i < c.count; i++) {
-            const NsSize z = ns_size(c.in[i].rows, c.in[i].cols);
+            const NsSize z = ns_size(c.in[i].rows, c.in[i].cols, c.whole);
             c.at += z.bytes;
             for (int k = 0; k < kPre; k++) c.work[k] += z.work[k];
         }
     }
+    if (p.work[PRE_TINY]) {
+        const bool b = dst_dtype == DT_BF16;
+        const hipError_t e = src_dtype == DT_BF16 ? (b ? ns_tiny<bf16_t, bf16_t>(p, t, s, st) : ns_tiny<bf16_t, float>(p, t, s, st))
+                                                  : (b ? ns_tiny<float, bf16_t>(p, t, s, st) : ns_tiny<float, float>(p, t, s, st));
+        if (e != hipSuccess) return e;
+    }
+    if (!p.work[PRE_SQ]) return hipSuccess;
     const double es = src_dtype == DT_BF16 ? 2.0 : 4.0;
     {
         TraceScope tr(KC_SWEEP, KID_ORTHO, st, p.values * (es + (s.update ? 8.0 : 0.0)), 0.0);

@@ -123,7 +123,7 @@ def test_orthogonalize_refuses_lists(B):
     assert _ortho(B, [], count=0) == "BNR_OK"                          # nothing to do
     assert _ortho(B, [ONE], xt=3) == "BNR_ERR_DTYPE" and _ortho(B, [ONE], ot=-2) == "BNR_ERR_DTYPE"
     assert _ortho(B, [ONE], ws=None) == "BNR_ERR_WORKSPACE"
-    assert _ortho(B, [ONE], ws_bytes=1024) == "BNR_ERR_WORKSPACE"
+    assert _ortho(B, [ONE], ws_bytes=16) == "BNR_ERR_WORKSPACE"
     assert _ortho(B, [ONE], ws=A + 8) == "BNR_ERR_ALIGN"
     f, p = B._lib_fns["bnr_orthogonalize"], B.NSParams(5, 3.4445, -4.7750, 2.0315, 1e-7)
     assert B.STATUS[f(None, 1, F32, F32, ctypes.byref(p), A, 1 << 30, None)] == "BNR_ERR_NULL"
@@ -135,6 +135,10 @@ def test_orthogonalize_refuses_lists(B):
     wide = lambda p: (8, 16, A, 16, p, 40)  # noqa: E731
     assert _ortho(B, [wide(A + MB), wide(A + MB + 60)], ws=None) == "BNR_ERR_ALIAS"
     assert _ortho(B, [wide(A + MB + 64), wide(A + MB)], ws=None) == "BNR_ERR_WORKSPACE"
+    # over its own x, not over another's
+    assert _ortho(B, [(8, 16, A, 16, A, 16), ONE], ws=None) == "BNR_ERR_ALIAS"
+    assert _ortho(B, [(8, 16, A, 16, A, 16), (8, 16, A + MB, 16, A + MB + 32, 16)], ws=None) == "BNR_ERR_WORKSPACE"
+    assert _ortho(B, [ONE, (8, 16, A + MB + 32, 16, A + 2 * MB, 16)], ws=None) == "BNR_ERR_ALIAS"
     many = [(8, 16, A, 16, A + MB + 64 * 16 * i, 16) for i in range(1024)]
     assert _ortho(B, many, ws=None) == "BNR_ERR_WORKSPACE"
     assert _ortho(B, many[:-1] + [many[500]], ws=None) == "BNR_ERR_ALIAS"

@@ -62,7 +62,8 @@ def _close(name, got, ref, dtype, rel=REL):
 # lists whose tiles run whole and in pieces, in each tile size, and hang over the matrices' ends
 LARGE = [[(1024, 1024)] * 8, [(2048, 2048)], [(2048, 2048)] * 4, [(1024, 4096)] * 6, [(1300, 2900)] * 3, [(1023, 4093)],
          [(520, 2000), (2700, 1100), (130, 4000)], [(700, 700), (64, 300), (200, 1900), (1500, 129)], [(4096, 1000)],
-         [(3000, 2990)]]
+         [(3000, 2990)], [(64, 64), (700, 700), (20, 500)], [(60, 70), (3, 3), (128, 128), (30, 2000), (9, 9)],
+         [(128, 100)] * 300]
 
 
 @pytest.mark.parametrize("shapes", LARGE, ids=lambda s: "%dx%dx%d" % (len(s), *s[0]))
@@ -189,14 +190,14 @@ def test_list_equals_single_calls_in_place_and_again():
     """A matrix's result does not depend on the list around it, is the same on the next call, and may be written over
     the input."""
     B = _B()
-    shapes = [(1152, 32), (64, 128), (256, 128), (31, 7), (300, 300), (1, 9)] + [(96 + 8 * i, 128) for i in range(70)]
+    shapes = [(1152, 32), (64, 128), (256, 128), (31, 7), (300, 300), (1, 9), (700, 500)] + [(96 + 8 * i, 128) for i in range(70)]
     xs = [_rand(i, *s).float().cuda() for i, s in enumerate(shapes)]
     outs = [torch.empty_like(x) for x in xs]
     B.bnr_orthogonalize(xs, outs)
     again = [torch.empty_like(x) for x in xs]
     B.bnr_orthogonalize(xs, again)
     assert all(torch.equal(a, b) for a, b in zip(outs, again))
-    for i in (0, 1, 2, 3, 4, 5, 40, 75):
+    for i in (0, 1, 2, 3, 4, 5, 6, 40, 75):
         one = torch.empty_like(xs[i])
         B.bnr_orthogonalize(xs[i], one)
         _close("alone %d" % i, one, _d(outs[i]), torch.float32)
