@@ -1,8 +1,9 @@
 """Training-step drivers for the synthetic workloads, fused and unfused.
 
 Each driver owns its device buffers (allocated once), sequences C-ABI calls of
-``libbnr`` for one training step (forward + backward, no optimizer update) and
-exposes the results for parity checks.  ``fused=True`` runs the BN
+``libbnr`` for one training step (forward + backward) and exposes the results
+for parity checks.  ``FilterUpdate`` is the optimizer step of a driver's CONV
+filters, a separate call.  ``fused=True`` runs the BN
 fission/fusion path (Sec. 3.2 of the paper); ``fused=False`` runs the same math
 through ``bnr_reference_path`` (the unfused BN -> ReLU -> CONV chain with
 materialised intermediates, Sec. 3.2 "before" picture).
@@ -79,6 +80,27 @@ class _Unit:
                              dgamma=self.g.dgamma, dbeta=self.g.dbeta, dx=dx, dx_accumulate=accumulate)
 
 
+class FilterUpdate:
+    """Orthogonalised momentum updates of a driver's CONV filters (``driver.filters()``) from the weight gradients its
+    backward leaves: every filter [k, k, c_in, c_out] is a matrix [k k c_in, c_out], and one call updates all of them.
+
+    The updated weights are float32.  Where the driver's filters are bf16 they are kept here (``self.weights``) and
+    the update also writes the driver's bf16 ones; else they are the driver's own.  BN parameters, the first CONV and
+    the classifier are not matrices of this kind and are left to the caller."""
+
+    def __init__(self, driver, momentum=0.95, nesterov=True, weight_decay=0.0):
+        filters, grads = zip(*driver.filters())
+        bf16 = filters[0].dtype == torch.bfloat16
+        self.weights = [f.float() if bf16 else f for f in filters]
+        self.bufs = [torch.zeros_like(w) for w in self.weights]
+        self.kw = dict(momentum=momentum, nesterov=nesterov, weight_decay=weight_decay)
+        self.group = B.MuonGroup(self.weights, grads, self.bufs, copies=filters if bf16 else None)
+
+    def step(self, lr):
+        """lr: a number, or a float32 device tensor of one value (read when the step runs)."""
+        B.bnr_muon_update(self.group, lr, **self.kw)
+
+
 class SingleLayer:
     """BN-ReLU-CONV1x1 (fp32 by default): x [n,h,w,c_in] -> out [n,h,w,c_out],
     upstream gradient dy of out given."""
@@ -99,6 +121,9 @@ class SingleLayer:
         self.dz = torch.empty_like(self.x) if not fused else None
         self.fused = fused
         self.images = n
+
+    def filters(self):
+        return [(self.u.wt, self.u.dw)]
 
     def forward(self):
         u = self.u
@@ -151,6 +176,9 @@ class Bottleneck:
             self.dx2 = torch.empty_like(self.dy2)
         self.fused = fused
         self.images = n
+
+    def filters(self):
+        return [(u.wt, u.dw) for u in (self.u1, self.u2)]
 
     def forward(self):
         if self.fused:
@@ -298,6 +326,11 @@ class _DenseStage:
                 rob(st, self.run_mean[c_l:c_l + k], self.run_var[c_l:c_l + k])
                 wd = u2.bn.gamma.shape[0]
                 rob(u2.bn, torch.zeros(wd, **f32), torch.ones(wd, **f32))
+
+    def filters(self):
+        """(filter, weight gradient) of its CONVs in forward order."""
+        us = [u for _, _, u1, u2 in self.cpl for u in (u1, u2)] + ([self.ut] if self.ut is not None else [])
+        return [(u.wt, u.dw) for u in us]
 
     def shared(self, lo, hi):
         """Views of the shared per-channel statistics of channels [lo, hi)."""
@@ -562,6 +595,10 @@ class DenseNet:
         self.fused = fused
         self.images = n
 
+    def filters(self):
+        """(filter, weight gradient) of the dense blocks' and transitions' CONVs."""
+        return [f for st in self.stages for f in st.filters()]
+
     def forward(self):
         s0 = self.stages[0]
         n = self.n
@@ -673,6 +710,9 @@ class ResNetStack:
             self.dx3 = torch.empty_like(self.x0)
             self.dyw3 = torch.empty_like(self.dyw)
             self.dzw = torch.empty_like(self.dyw)
+
+    def filters(self):
+        return [f for b in self.blocks for f in ((b["w1"], b["dw1"]), (b["u2"].wt, b["u2"].dw), (b["u3"].wt, b["u3"].dw))]
 
     def forward(self):
         for i, b in enumerate(self.blocks):

@@ -1,0 +1,180 @@
+"""The layer norm, the CONVs and the orthogonalised update together, as a training step uses them.
+
+Tolerances are the library's for float32 compositions (max norm 1e-4, helpers.RTOL) and, for the updates, those of
+the update's own tests.
+"""
+import numpy as np
+import pytest
+import torch
+
+from helpers import RTOL, assert_close, host
+from paper_1807_01702_amd import synth
+
+pytestmark = pytest.mark.gpu
+
+COEF = (3.4445, -4.7750, 2.0315)
+EPS = 1e-5
+REL = 95 * 2.0 ** -21           # ||error|| / ||step|| of an orthogonalised step (float32 accuracy of five steps)
+
+
+def _ns64(u, steps=5):
+    x = u if u.shape[0] <= u.shape[1] else u.t()
+    x = x / (torch.linalg.norm(x) + 1e-7)
+    a, b, c = COEF
+    for _ in range(steps):
+        g = x @ x.t()
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x if u.shape[0] <= u.shape[1] else x.t()
+
+
+def _d(t):
+    return t.detach().double().cpu()
+
+
+def _scale(t):
+    return max(1.0, t.shape[-1] / (t.numel() // t.shape[-1])) ** 0.5
+
+
+def test_pre_norm_residual_blocks_forward_backward_update():
+    """Two residual blocks x + conv1x1(relu-free LN(x)) and a final layer norm on the pixels of small images: the
+    forward, every gradient and the filters' update against float64 autograd."""
+    from paper_1807_01702_amd import bnr as B
+    n, h, w, c, blocks = 2, 9, 7, 96, 2
+    m = n * h * w
+    g = torch.Generator().manual_seed(3)
+    r = lambda *s: torch.randn(s, generator=g).cuda()  # noqa: E731
+    x, dout = r(n, h, w, c), r(n, h, w, c)
+    ws = [r(1, 1, c, c) * 0.1 for _ in range(blocks)]
+    gam, bet = [1 + 0.2 * r(c) for _ in range(blocks + 1)], [0.2 * r(c) for _ in range(blocks + 1)]
+    lns = [B.LN(gam[i], bet[i], m, EPS) for i in range(blocks + 1)]
+    like = lambda: torch.empty_like(x)  # noqa: E731
+    ys, zs, sums = [like() for _ in range(blocks + 1)], [like() for _ in range(blocks)], [x] + [like() for _ in range(blocks)]
+    desc = B.desc_for(x, zs[0], 1, n, h, w)
+    # forward: every norm after the first adds the block's output to the stream
+    for i in range(blocks + 1):
+        if i == 0:
+            B.bnr_layernorm_fwd(x, lns[0], ys[0])
+        else:
+            B.bnr_layernorm_fwd(sums[i - 1], lns[i], ys[i], res=zs[i - 1], sum=sums[i])
+        if i < blocks:
+            B.bnr_conv_fwd(desc, ys[i], ws[i], zs[i])
+    # backward: the norm's input gradient joins the stream's, in place
+    dws, dg, db = [torch.empty_like(t) for t in ws], [torch.empty_like(t) for t in gam], [torch.empty_like(t) for t in bet]
+    stream, dy = like(), like()
+    B.bnr_layernorm_bwd(dout, sums[blocks], lns[blocks], stream, dg[blocks], db[blocks])
+    for i in reversed(range(blocks)):
+        B.bnr_bwd_fused(desc, ys[i], None, ws[i], B.grad_dense(stream), dws[i], dx=dy)
+        B.bnr_layernorm_bwd(dy, sums[i], lns[i], stream, dg[i], db[i], dsum=stream)
+    torch.cuda.synchronize()
+    # the same in float64
+    leaf = lambda t: _d(t).requires_grad_()  # noqa: E731
+    x64, w64 = leaf(x), [leaf(t) for t in ws]
+    g64, b64 = [leaf(t) for t in gam], [leaf(t) for t in bet]
+    s = x64
+    for i in range(blocks + 1):
+        y = torch.nn.functional.layer_norm(s, (c,), g64[i], b64[i], EPS)
+        if i < blocks:
+            s = s + y @ w64[i].reshape(c, c)
+    (y * _d(dout)).sum().backward()
+    tol = RTOL[False]
+    assert_close("y", host(ys[blocks]), y.detach().numpy(), tol)
+    assert_close("sum", host(sums[blocks]), s.detach().numpy(), tol)
+    assert_close("dx", host(stream), x64.grad.numpy(), tol)
+    for i in range(blocks + 1):
+        assert_close("dgamma%d" % i, host(dg[i]), g64[i].grad.numpy(), tol)
+        assert_close("dbeta%d" % i, host(db[i]), b64[i].grad.numpy(), tol)
+    for i in range(blocks):
+        assert_close("dw%d" % i, host(dws[i]), w64[i].grad.numpy(), tol)
+    before = [_d(t) for t in ws]
+    bufs = [torch.zeros_like(t) for t in ws]
+    B.bnr_muon_update(B.MuonGroup(ws, dws, bufs), 0.125, momentum=0.5, weight_decay=0.25)
+    for t, t0, gr in zip(ws, before, dws):
+        u = _d(gr).reshape(c, c) * 1.5                                  # buf = g, u = g + buf / 2
+        step = 0.125 * _ns64(u)
+        want = t0.reshape(c, c) * (1 - 0.125 * 0.25) - step
+        err = float((_d(t).reshape(c, c) - want).norm())
+        assert err <= REL * float(step.norm()) + 4 * 2.0 ** -24 * float(t0.norm() + step.norm()), err
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_filter_update_of_a_dense_block(bf16):
+    """A dense block's training step and the update of its filters, twice (momentum), then the forward with the
+    updated filters."""
+    from paper_1807_01702_amd import workloads as W
+    wl = W.DenseBlock(synth.dense_block(seed=0, n=2, h=16, w=16, bf16=bf16))
+    opt = W.FilterUpdate(wl, momentum=0.9, weight_decay=0.5)
+    filters = wl.filters()
+    assert len(filters) == 2 * len(wl.cpl) + 1
+    ref_w = [_d(t) for t in opt.weights]
+    ref_b = [torch.zeros_like(t) for t in ref_w]
+    u24 = 2.0 ** -24
+    lr, mom, wd = 0.25, float(np.float32(0.9)), 0.5
+    tol = [0.0] * len(filters)
+    for _ in range(2):
+        wl.step()
+        grads = [_d(dw) for _, dw in filters]
+        opt.step(lr)
+        torch.cuda.synchronize()
+        for i, ((f, _), t) in enumerate(zip(filters, opt.weights)):
+            ref_b[i] = mom * ref_b[i] + grads[i]
+            u = (grads[i] + mom * ref_b[i]).reshape(-1, f.shape[-1])
+            step = lr * _scale(f) * _ns64(u).reshape(f.shape)
+            ref_w[i] = ref_w[i] * (1 - lr * wd) - step
+            # the second step starts from the first one's rounded state
+            tol[i] += 2 * REL * float(step.norm()) + 4 * u24 * float(ref_w[i].norm() + step.norm())
+            assert float((_d(t) - ref_w[i]).norm()) <= tol[i], i
+            if bf16:
+                assert torch.equal(f, t.bfloat16())
+            else:
+                assert f.data_ptr() == t.data_ptr()
+    old = wl.pooled.clone()
+    wl.forward()
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(wl.pooled.float()).all()) and not torch.equal(old, wl.pooled)
+
+
+def test_filter_update_of_the_other_drivers():
+    """Every driver lists its filters with gradients of their shapes, and one call updates all of them."""
+    from paper_1807_01702_amd import workloads as W
+    drivers = [W.SingleLayer(synth.single_layer(seed=1)),
+               W.Bottleneck(synth.bottleneck(seed=2, n=1, h=8, w=8)),
+               W.ResNetStack(synth.resnet_stack(seed=3, n=1, h=8, w=8)),
+               W.DenseNet(synth.densenet(seed=4, n=2, hw=64, blocks=(2, 2), classes=10))]
+    for wl in drivers:
+        wl.step()
+        opt = W.FilterUpdate(wl)
+        before = [f.clone() for f, _ in wl.filters()]
+        opt.step(torch.full((1,), 0.1, device="cuda"))
+        torch.cuda.synchronize()
+        for (f, dw), f0, t in zip(wl.filters(), before, opt.weights):
+            assert f.shape == dw.shape == t.shape
+            assert bool(torch.isfinite(f.float()).all()) and not torch.equal(f, f0)
+            if f.dtype == torch.bfloat16:
+                assert torch.equal(f, t.bfloat16())
+
+
+def test_captured_training_step_with_update():
+    """A whole step with its update, captured once and replayed, equals the eager steps bit for bit."""
+    from paper_1807_01702_amd import workloads as W
+    d = synth.dense_block(seed=5, n=2, h=16, w=16)
+    eager, cap = W.DenseBlock(d), W.DenseBlock(d)
+    lr = torch.full((1,), 0.05, device="cuda")
+    oe, oc = W.FilterUpdate(eager), W.FilterUpdate(cap)
+    cap.step()                               # workspaces exist before the capture
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            cap.step()
+            oc.step(lr)
+    torch.cuda.current_stream().wait_stream(s)
+    for rate in (0.05, 0.02, 0.04):
+        lr.fill_(rate)
+        eager.step()
+        oe.step(lr)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(oe.weights + oe.bufs + [eager.pooled], oc.weights + oc.bufs + [cap.pooled]):
+            assert torch.equal(a, b)
