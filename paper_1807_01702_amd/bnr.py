@@ -692,28 +692,26 @@ def bnr_reference_bn_relu(backward, x, bn, y, z=None, gz=None, dy=None, dgamma=N
 # These calls run on the current stream of their tensors' device, which need not
 # be the current device, and take their workspace from torch's allocator per call:
 # calls on two streams share nothing, and a captured graph holds its own.
-class _on_device:
-    """Makes a tensor's device current for a call; yields that device's current stream."""
+def _device_of(*tensors):
+    """The index of the one GPU that all tensors (None: absent) are on."""
+    index = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError("tensors of two devices: %s and %s" % (tensors[0].device, t.device))
+    if index < 0:
+        raise ValueError("tensors of a GPU are wanted, got one of %s" % tensors[0].device)
+    return index
 
-    def __init__(self, *tensors):
-        tensors = [t for t in tensors if t is not None]
-        dev = tensors[0].device
-        if dev.type != "cuda":
-            raise ValueError("tensors of a GPU are wanted, got one of %s" % dev)
-        for t in tensors[1:]:
-            if t.device != dev:
-                raise ValueError("tensors of two devices: %s and %s" % (dev, t.device))
-        self.index = dev.index
 
-    def __enter__(self):
-        self.before = _current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return _stream()
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+def _run_on(index, fn, *args):
+    """fn(*args, stream) with the device current and its current stream; raises on a bad status."""
+    if _current_device() == index:
+        status = fn(*args, _stream())
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _stream())
+    if status:
+        _check(status)
 
 
 def _scratch(nbytes, device):
@@ -730,10 +728,16 @@ def _f32_array(t, n, name):
 
 
 def _rows(t, m, c, dtype, name):
+    """(data pointer, row stride) of a view of m rows; (None, 0) without one."""
     if t is None:
         return None, 0
-    p, tm, tc, ld = view(t)
-    if (tm, tc) != (m, c) or t.dtype != dtype:
+    if t.dim() == 2:                                     # the usual call, without the general walk
+        (tm, tc), (ld, unit), p = t.shape, t.stride(), t.data_ptr()
+        if unit != 1 and tc > 1:
+            raise ValueError("%s: a unit-stride channel dimension is wanted" % name)
+    else:
+        p, tm, tc, ld = view(t)
+    if tm != m or tc != c or t.dtype != dtype:
         raise ValueError("%s: [%d, %d] rows of %s are wanted, got [%d, %d] of %s" % (name, m, c, dtype, tm, tc, t.dtype))
     return p, ld if m > 1 else c
 
@@ -755,31 +759,33 @@ class LN:
 
 def bnr_layernorm_fwd(x, ln, y, res=None, sum=None):
     """y = layernorm(x), or, with res, sum = x + res and y = layernorm(sum) (views [.., c])."""
-    px, m, c, ldx = view(x)
-    py, ldy = _rows(y, m, c, x.dtype, "y")
-    pr, ldr = _rows(res, m, c, x.dtype, "res")
-    ps, lds = _rows(sum, m, c, x.dtype, "sum")
+    c, dt = x.shape[-1], x.dtype
+    m = x.numel() // c if c else 0
+    px, ldx = _rows(x, m, c, dt, "x")
+    py, ldy = _rows(y, m, c, dt, "y")
+    pr, ldr = _rows(res, m, c, dt, "res")
+    ps, lds = _rows(sum, m, c, dt, "sum")
     s = ln.struct(m, c)
-    with _on_device(x, y, ln.mean, ln.rstd, ln.gamma, ln.beta, res, sum) as stream:
-        _check(_lib_fns["bnr_layernorm_fwd"](m, c, dtype_code(x), px, ldx if m > 1 else c, pr, ldr, ps, lds,
-                                             ctypes.byref(s), py, ldy, stream))
+    _run_on(_device_of(x, y, ln.mean, ln.rstd, ln.gamma, ln.beta, res, sum), _lib_fns["bnr_layernorm_fwd"], m, c,
+            dtype_code(x), px, ldx, pr, ldr, ps, lds, ctypes.byref(s), py, ldy)
 
 
 def bnr_layernorm_bwd(dy, x, ln, dx, dgamma=None, dbeta=None, dsum=None):
     """dx (views [.., c]; + dsum), dgamma and dbeta ([c] float32, overwritten) of bnr_layernorm_fwd; x: what it
     normalised (its sum, where it had one)."""
-    px, m, c, ldx = view(x)
-    pd, ldd = _rows(dy, m, c, x.dtype, "dy")
-    po, ldo = _rows(dx, m, c, x.dtype, "dx")
-    pr, ldr = _rows(dsum, m, c, x.dtype, "dsum")
+    c, dt = x.shape[-1], x.dtype
+    m = x.numel() // c if c else 0
+    px, ldx = _rows(x, m, c, dt, "x")
+    pd, ldd = _rows(dy, m, c, dt, "dy")
+    po, ldo = _rows(dx, m, c, dt, "dx")
+    pr, ldr = _rows(dsum, m, c, dt, "dsum")
     s = ln.struct(m, c)
     pg, pb = _f32_array(dgamma, c, "dgamma"), _f32_array(dbeta, c, "dbeta")
-    with _on_device(x, dy, dx, ln.mean, ln.rstd, ln.gamma, dsum, dgamma, dbeta) as stream:
-        code = dtype_code(x)
-        nbytes = _lib_fns["bnr_layernorm_workspace_size"](m, c, code) if pg or pb else 0
-        ws = _scratch(nbytes, x.device) if nbytes else None
-        _check(_lib_fns["bnr_layernorm_bwd"](m, c, code, pd, ldd, px, ldx if m > 1 else c, ctypes.byref(s), pr, ldr,
-                                             po, ldo, pg, pb, _ptr(ws), nbytes, stream))
+    index, code = _device_of(x, dy, dx, ln.mean, ln.rstd, ln.gamma, dsum, dgamma, dbeta), dtype_code(x)
+    nbytes = _lib_fns["bnr_layernorm_workspace_size"](m, c, code) if pg or pb else 0
+    ws = _scratch(nbytes, x.device) if nbytes else None
+    _run_on(index, _lib_fns["bnr_layernorm_bwd"], m, c, code, pd, ldd, px, ldx, ctypes.byref(s), pr, ldr, po, ldo, pg,
+            pb, _ptr(ws), nbytes)
 
 
 NS_COEF = (3.4445, -4.7750, 2.0315)
@@ -806,12 +812,11 @@ def bnr_orthogonalize(xs, outs, steps=5, coef=NS_COEF, eps=1e-7):
         _, it.rows, it.cols, _ = view(x)
         it.x, it.x_ld = _matrix(x, (it.rows, it.cols), xs[0].dtype, "matrix")
         it.out, it.out_ld = _matrix(o, (it.rows, it.cols), outs[0].dtype, "output")
-    ns = NSParams(steps, *coef, eps)
-    with _on_device(*xs, *outs) as stream:
-        nbytes = _lib_fns["bnr_orthogonalize_workspace_size"](items, len(xs))
-        ws = _scratch(nbytes, xs[0].device)
-        _check(_lib_fns["bnr_orthogonalize"](items, len(xs), dtype_code(xs[0]), dtype_code(outs[0]), ctypes.byref(ns),
-                                             _ptr(ws), nbytes, stream))
+    ns, index = NSParams(steps, *coef, eps), _device_of(*xs, *outs)
+    nbytes = _lib_fns["bnr_orthogonalize_workspace_size"](items, len(xs))
+    ws = _scratch(nbytes, xs[0].device)
+    _run_on(index, _lib_fns["bnr_orthogonalize"], items, len(xs), dtype_code(xs[0]), dtype_code(outs[0]),
+            ctypes.byref(ns), _ptr(ws), nbytes)
 
 
 class MuonGroup:
@@ -837,7 +842,7 @@ class MuonGroup:
             it.scale = max(1.0, c / r) ** 0.5 if scales is None else scales[i]
         if n:
             self.w_code, self.g_code = dtype_code(ws[0]), dtype_code(gs[0])
-            self.on = _on_device(*(t for part in self.tensors if part is not None for t in part))
+            self.index = _device_of(*(t for part in self.tensors if part is not None for t in part))
             self.ws_bytes = _lib_fns["bnr_muon_workspace_size"](self.items, n)
 
 
@@ -854,7 +859,6 @@ def bnr_muon_update(group, lr, momentum=0.95, nesterov=True, weight_decay=0.0, s
         p.lr_dev = _f32_array(lr, 1, "lr")
     else:
         p.lr = lr
-    with group.on as stream:
-        ws = _scratch(group.ws_bytes, device)
-        _check(_lib_fns["bnr_muon_update"](group.items, group.count, group.w_code, group.g_code, ctypes.byref(p),
-                                           _ptr(ws), group.ws_bytes, stream))
+    ws = _scratch(group.ws_bytes, device)
+    _run_on(group.index, _lib_fns["bnr_muon_update"], group.items, group.count, group.w_code, group.g_code,
+            ctypes.byref(p), _ptr(ws), group.ws_bytes)

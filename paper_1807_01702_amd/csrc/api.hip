@@ -1750,7 +1750,7 @@ bnr_status bnr_layernorm_fwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
     return ok();
 }
 
-// workspace of the backward: partial rows | combine scratch | a stand-in for the one of dgamma, dbeta not asked for
+// workspace of the backward: the partial rows
 static size_t ln_part_bytes(int64_t m, int32_t c, bnr_dtype dtype)
 {
     const int64_t a = ln_bwd_groups(dt_of(dtype), m, c, false),
@@ -1761,7 +1761,7 @@ static size_t ln_part_bytes(int64_t m, int32_t c, bnr_dtype dtype)
 size_t bnr_layernorm_workspace_size(int64_t m, int32_t c, bnr_dtype dtype)
 {
     if (m <= 0 || m > ((int64_t)1 << 31) || c <= 0 || c > kLnMaxC || (dtype != BNR_F32 && dtype != BNR_BF16)) return 0;
-    return ln_part_bytes(m, c, dtype) + align_up(stats_red_bytes(c)) + align_up((size_t)c * 4);
+    return ln_part_bytes(m, c, dtype);
 }
 
 bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy, int32_t dy_ldc, const void *x,
@@ -1801,7 +1801,6 @@ bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
         return fail(BNR_ERR_ALIAS, "dgamma overlaps dbeta");
     const bool sums = dgamma || dbeta;
     if (sums) TRY(check_ws(ws, ws_bytes, bnr_layernorm_workspace_size(m, c, dtype)));
-    char *red = (char *)ws + (sums ? ln_part_bytes(m, c, dtype) : 0);
     LnParams p{};
     p.m = m; p.c = c;
     p.x = x; p.x_ldc = x_ldc;
@@ -1812,12 +1811,9 @@ bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
     p.part = sums ? (float *)ws : nullptr;
     hipStream_t st = (hipStream_t)stream;
     TRY_HIP(launch_ln_bwd(dt_of(dtype), p, vec, st), "layer norm backward");
-    if (sums) {
-        float *unused = (float *)(red + align_up(stats_red_bytes(c)));
-        TRY_HIP(launch_stats_finalize(p.part, ln_bwd_groups(dt_of(dtype), m, c, vec), c, m, FIN_BWD, 0.f, nullptr,
-                                      nullptr, nullptr, dbeta ? dbeta : unused, dgamma ? dgamma : unused, red, st),
-                "backward sums combine");
-    }
+    if (sums)
+        TRY_HIP(launch_ln_combine(p.part, ln_bwd_groups(dt_of(dtype), m, c, vec), c, dbeta, dgamma, st),
+                "layer norm sums combine");
     return ok();
 }
 

@@ -295,6 +295,7 @@ struct LnParams {
 int64_t ln_bwd_groups(int dtype, int64_t m, int c, bool vec);            // partial rows
 hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s);
 hipError_t launch_ln_bwd(int dtype, const LnParams &p, bool vec, hipStream_t s);
+hipError_t launch_ln_combine(const float *part, int64_t R, int c, float *dbeta, float *dgamma, hipStream_t s);
 
 // Newton-Schulz orthogonalisation of a list of matrices (newton_schulz.hip).
 struct NsIn {                     // one matrix as the caller gives it, row-major

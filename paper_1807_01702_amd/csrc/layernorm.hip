@@ -189,12 +189,18 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
 // Backward: workgroup b takes row sets b, b + grid, ...; each thread keeps the
 // sums of dy and dy xhat of its own channels in registers over all its rows
 // and the workgroup writes one partial row [2][c] at the end (float32 sums of
-// at most m / (grid GR) terms; the combine adds the partial rows in float64 in
-// a fixed order).  The next row set is loaded before the current one reduces.
+// at most m / (grid GR) terms; k_ln_combine adds the partial rows in float64 in
+// a fixed order).  The next row set is loaded before the current one reduces,
+// and gamma stays in registers, except in the widest rows (512 threads, up to 32
+// channels each), which do not hold both beside the sums (1024 threads of 16
+// channels and 128 registers spilled more): those read gamma again, and load
+// ahead only where a vector holds 8 values.  (Odd widths past 8192 still spill
+// about half of their sums.)
 template <typename T, int V, int TPR, int NV, int WG, bool RES>
 __global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
 {
     constexpr int GR = WG / TPR;
+    constexpr bool WIDE = TPR >= 512, AHEAD = !WIDE || V == 8, GAM = !WIDE;
     typedef LnVec<T, V> L;
     __shared__ float red[2][WG / 64 * 2];
     __shared__ float cols[GR > 1 ? 2 * WG * V : 1];
@@ -202,13 +208,13 @@ __global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
     const int nvec = p.c / V;
     const T *x = (const T *)p.x, *dy = (const T *)p.dy, *dsum = (const T *)p.res;
     T *dx = (T *)p.y;
-    float gam[NV][V], sb[NV][V], sg[NV][V];
+    float gam[GAM ? NV : 1][V], sb[NV][V], sg[NV][V];
     int col[NV];
     #pragma unroll
     for (int j = 0; j < NV; j++) {
         const int v = j * TPR + lane;
         col[j] = v < nvec ? v * V : -1;
-        ln_param<V>(p.gamma, (v < nvec ? v : nvec - 1) * V, 1.f, gam[j]);
+        if (GAM) ln_param<V>(p.gamma, (v < nvec ? v : nvec - 1) * V, 1.f, gam[GAM ? j : 0]);
         #pragma unroll
         for (int i = 0; i < V; i++) {
             sb[j][i] = 0.f;
@@ -219,7 +225,7 @@ __global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
     const int64_t step = (int64_t)gridDim.x * GR;
     const int64_t sets = (p.m + step - 1) / step;
     int64_t row = (int64_t)blockIdx.x * GR + grp;
-    typename L::raw rx[NV], rd[NV], rs[NV];
+    typename L::raw rx[NV], rd[NV], rs[RES ? NV : 1];
     float mean = 0.f, rstd = 0.f;
     auto load = [&](int64_t r) __attribute__((always_inline)) {
         if (r >= p.m) r = p.m - 1;                    // read and dropped
@@ -233,21 +239,25 @@ __global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
             if (RES) rs[j] = L::load(dsum + r * p.res_ldc + c);
         }
     };
-    load(row);
+    if (AHEAD) load(row);
     for (int64_t it = 0; it < sets; it++, row += step) {
-        float xh[NV][V], d[NV][V], e[RES ? NV : 1][V], s[2] = {0.f, 0.f};
+        if (!AHEAD) load(row);
+        float xh[NV][V], d[NV][V], s[2] = {0.f, 0.f};
+        typename L::raw e[RES ? NV : 1];
         const float rs0 = rstd, mu0 = mean;
         const bool live = row < p.m;
         #pragma unroll
         for (int j = 0; j < NV; j++) {
             L::unpack(rx[j], xh[j]);
             L::unpack(rd[j], d[j]);
-            if (RES) L::unpack(rs[j], e[j]);
+            if (RES) e[j] = rs[j];
         }
-        if (it + 1 < sets) load(row + step);
+        if (AHEAD && it + 1 < sets) load(row + step);
         #pragma unroll
         for (int j = 0; j < NV; j++)
-            if (col[j] >= 0)
+            if (col[j] >= 0) {
+                float g[V];
+                if (!GAM) ln_param<V>(p.gamma, col[j], 1.f, g);
                 #pragma unroll
                 for (int i = 0; i < V; i++) {
                     xh[j][i] = (xh[j][i] - mu0) * rs0;
@@ -255,21 +265,23 @@ __global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
                         sb[j][i] += d[j][i];
                         sg[j][i] += d[j][i] * xh[j][i];
                     }
-                    d[j][i] *= gam[j][i];
+                    d[j][i] *= GAM ? gam[GAM ? j : 0][i] : g[i];
                     s[0] += d[j][i];
                     s[1] += d[j][i] * xh[j][i];
                 }
+            }
         row_sums<TPR, 2>(s, red[it & 1]);
         if (live) {
             const float a = s[0] * inv_c, b = s[1] * inv_c;
             #pragma unroll
             for (int j = 0; j < NV; j++) {
                 if (col[j] < 0) continue;
-                float o[V];
+                float o[V], f[V];
+                if (RES) L::unpack(e[j], f);
                 #pragma unroll
                 for (int i = 0; i < V; i++) {
                     o[i] = rs0 * (d[j][i] - a - xh[j][i] * b);
-                    if (RES) o[i] += e[j][i];
+                    if (RES) o[i] += f[i];
                 }
                 L::store(dx + row * p.y_ldc + col[j], o);
             }
@@ -309,6 +321,42 @@ __global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
     }
 }
 
+// dbeta and dgamma (either may be NULL) from the partial rows [R][2 c], added in
+// float64 in a fixed order: a workgroup takes COLS of the 2 c columns with
+// 1024 / COLS row groups, eight rows in flight a thread, then adds the groups.
+// 64 columns are 256-byte reads of long rows; 16 columns keep enough workgroups
+// where rows are short.
+template <int COLS>
+__global__ __launch_bounds__(1024) void k_ln_combine(const float *__restrict__ part, int64_t R, int c, float *dbeta,
+                                                         float *dgamma)
+{
+    constexpr int GROUPS = 1024 / COLS, U = 8;
+    __shared__ double red[GROUPS][COLS + 1];
+    const int tx = threadIdx.x % COLS, ty = threadIdx.x / COLS;
+    const int64_t width = 2 * (int64_t)c, k = (int64_t)blockIdx.x * COLS + tx;
+    const float *src = part + (k < width ? k : width - 1);
+    double acc = 0.0;
+    for (int64_t r = ty; r < R; r += U * GROUPS) {
+        float v[U];
+        #pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int64_t rr = r + u * GROUPS;           // rows past the last are read again and left out
+            v[u] = src[(rr < R ? rr : R - 1) * width];
+        }
+        #pragma unroll
+        for (int u = 0; u < U; u++) acc += r + u * GROUPS < R ? (double)v[u] : 0.0;
+    }
+    red[ty][tx] = acc;
+    __syncthreads();
+    if (ty == 0 && k < width) {
+        double t = 0.0;
+        #pragma unroll
+        for (int g = 0; g < GROUPS; g++) t += red[g][tx];
+        float *out = k < c ? dbeta : dgamma;
+        if (out) out[k < c ? k : k - c] = (float)t;
+    }
+}
+
 // The row layout of a call: threads per row, loads per thread, and in the
 // backward pass the workgroup.
 struct LnPlan { bool vec; int tpr, nv, wg; };
@@ -333,28 +381,38 @@ LnPlan ln_plan(int dtype, int c, bool vec)
     return {true, 1024, n <= 2048 ? 2 : 4, 1024};
 }
 
-template <typename F>
+// The backward's: the rows of 1024 threads take 512 and twice the loads.
+LnPlan ln_bwd_plan(int dtype, int c, bool vec)
+{
+    LnPlan q = ln_plan(dtype, c, vec);
+    return q.tpr == 1024 ? LnPlan{q.vec, 512, 2 * q.nv, 512} : q;
+}
+
+template <bool BWD, typename F>
 hipError_t ln_dispatch(const LnPlan &q, int dtype, F &&go)
 {
     auto with = [&](auto tag, auto v, auto tpr, auto nv, auto wg) { return go(tag, v, tpr, nv, wg); };
 #define LN_I(N) std::integral_constant<int, N>{}
 #define LN_CASE(T, V, TPR, NV, WG) \
     if (q.tpr == TPR && q.nv == NV) return with((T *)nullptr, LN_I(V), LN_I(TPR), LN_I(NV), LN_I(WG))
+#define LN_WIDE(T, V, NV) \
+    if constexpr (BWD) { LN_CASE(T, V, 512, 2 * NV, 512); } else { LN_CASE(T, V, 1024, NV, 1024); }
 #define LN_VECTORS(T, V) \
     LN_CASE(T, V, 8, 1, 256);   LN_CASE(T, V, 16, 1, 256);  LN_CASE(T, V, 32, 1, 256);  LN_CASE(T, V, 64, 1, 256); \
     LN_CASE(T, V, 64, 2, 256);  LN_CASE(T, V, 256, 1, 512); LN_CASE(T, V, 256, 2, 512); LN_CASE(T, V, 256, 4, 512); \
-    LN_CASE(T, V, 1024, 2, 1024)
+    LN_WIDE(T, V, 2)
 #define LN_SCALARS(T) \
-    LN_CASE(T, 1, 64, 4, 256); LN_CASE(T, 1, 256, 8, 256); LN_CASE(T, 1, 1024, 8, 1024); LN_CASE(T, 1, 1024, 16, 1024)
+    LN_CASE(T, 1, 64, 4, 256); LN_CASE(T, 1, 256, 8, 256); LN_WIDE(T, 1, 8); LN_WIDE(T, 1, 16)
     if (dtype == DT_BF16) {
         if (q.vec) { LN_VECTORS(bf16_t, 8); }
         else { LN_SCALARS(bf16_t); }
     } else {
-        if (q.vec) { LN_VECTORS(float, 4); LN_CASE(float, 4, 1024, 4, 1024); }
+        if (q.vec) { LN_VECTORS(float, 4); LN_WIDE(float, 4, 4); }
         else { LN_SCALARS(float); }
     }
 #undef LN_SCALARS
 #undef LN_VECTORS
+#undef LN_WIDE
 #undef LN_CASE
 #undef LN_I
     return hipErrorInvalidValue;
@@ -367,9 +425,9 @@ hipError_t ln_dispatch(const LnPlan &q, int dtype, F &&go)
 // to the data (c = 4096: 512 rows are 16 MiB).
 int64_t ln_bwd_groups(int dtype, int64_t m, int c, bool vec)
 {
-    const LnPlan q = ln_plan(dtype, c, vec);
+    const LnPlan q = ln_bwd_plan(dtype, c, vec);
     const int64_t sets = ceil_div(m, q.wg / q.tpr);
-    const int64_t most = q.wg == 256 ? 1024 : (q.wg == 512 ? 512 : 256);
+    const int64_t most = q.wg == 256 ? 1024 : (q.tpr == 256 ? 512 : 256);
     return sets < most ? sets : most;
 }
 
@@ -378,7 +436,7 @@ hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s)
     const LnPlan q = ln_plan(dtype, p.c, vec);
     const double n = (double)p.m * p.c * (dtype == DT_BF16 ? 2 : 4);
     TraceScope tr(KC_SWEEP, KID_LAYERNORM, s, (p.res ? 4.0 : 2.0) * n + 8.0 * p.m + 8.0 * p.c, 0.0);
-    return ln_dispatch(q, dtype, [&](auto *tag, auto v, auto tpr, auto nv, auto) {
+    return ln_dispatch<false>(q, dtype, [&](auto *tag, auto v, auto tpr, auto nv, auto) {
         using T = std::remove_pointer_t<decltype(tag)>;
         constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, V = decltype(v)::value;
         constexpr int WG = TPR > kThreads ? TPR : kThreads, U = NV == 1 && TPR <= 64 ? 2 : 1;
@@ -389,13 +447,24 @@ hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s)
     });
 }
 
+hipError_t launch_ln_combine(const float *part, int64_t R, int c, float *dbeta, float *dgamma, hipStream_t s)
+{
+    TraceScope tr(KC_SMALL, KID_COMBINE, s, (double)R * 2 * c * 4 + 8.0 * c, 0.0);
+    const int64_t width = 2 * (int64_t)c;
+    if (c > 1024) hipLaunchKernelGGL(k_ln_combine<64>, dim3((unsigned)ceil_div(width, 64)), dim3(1024), 0, s, part, R, c,
+                                     dbeta, dgamma);
+    else hipLaunchKernelGGL(k_ln_combine<16>, dim3((unsigned)ceil_div(width, 16)), dim3(1024), 0, s, part, R, c,
+                            dbeta, dgamma);
+    return hipGetLastError();
+}
+
 hipError_t launch_ln_bwd(int dtype, const LnParams &p, bool vec, hipStream_t s)
 {
-    const LnPlan q = ln_plan(dtype, p.c, vec);
+    const LnPlan q = ln_bwd_plan(dtype, p.c, vec);
     const double n = (double)p.m * p.c * (dtype == DT_BF16 ? 2 : 4);
     const int64_t R = ln_bwd_groups(dtype, p.m, p.c, vec);
     TraceScope tr(KC_SWEEP, KID_LAYERNORM, s, (p.res ? 4.0 : 3.0) * n + 8.0 * p.m + 4.0 * p.c + 8.0 * R * p.c, 0.0);
-    return ln_dispatch(q, dtype, [&](auto *tag, auto v, auto tpr, auto nv, auto wg) {
+    return ln_dispatch<true>(q, dtype, [&](auto *tag, auto v, auto tpr, auto nv, auto wg) {
         using T = std::remove_pointer_t<decltype(tag)>;
         constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, V = decltype(v)::value;
         constexpr int WG = decltype(wg)::value;
