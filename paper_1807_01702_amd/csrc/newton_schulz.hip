@@ -50,9 +50,9 @@ constexpr int kSub = 64;                             // wide matrices are padded
 // Stages of a call and their work items: momentum and squares; the narrow
 // matrices' blocks and the sums of their partial Gram matrices; the wide ones'
 // conversion, symmetric product tiles and general product tiles, and the same in
-// large and in small tiles; the matrices of a single block, whole.
+// larger and smaller tiles; the matrices of a single block, whole.
 enum { PRE_SQ = 0, PRE_NARROW = 1, PRE_SUM = 2, PRE_PREP = 3, PRE_GRAM = 4, PRE_APPLY = 5, PRE_GRAM_L = 6, PRE_APPLY_L = 7,
-       PRE_GRAM_S = 8, PRE_APPLY_S = 9, PRE_TINY = 10, kPre = kNsStages };
+       PRE_GRAM_S = 8, PRE_APPLY_S = 9, PRE_TINY = 10, PRE_GRAM_T = 11, PRE_APPLY_T = 12, kPre = kNsStages };
 
 // one matrix of the list on the device: the caller's arguments and its place in the workspace
 struct NsDev {
@@ -72,6 +72,11 @@ struct NsSize {
     int work[kPre];                // work items per stage
     int64_t bytes;                 // workspace
 };
+// the stage that counts the symmetric tiles of a size; the general tiles' is the next
+__host__ __device__ constexpr int ns_gram_stage(int bt)
+{
+    return bt == 32 ? PRE_GRAM_T : (bt == 64 ? PRE_GRAM_S : (bt == 128 ? PRE_GRAM : PRE_GRAM_L));
+}
 constexpr int kMaxParts = 1024;    // partial sums of squares of a matrix
 constexpr int kNarrow = 128;       // short sides up to this take the narrow path
 constexpr int kBlock = 16384;      // values of a narrow matrix's block: [kBlock / P][P]
@@ -116,9 +121,9 @@ __host__ __device__ inline NsSize ns_size(int rows, int cols, int whole)
     z.P = up * 64;
     z.Q = uq * 64;
     z.work[PRE_PREP] = up * uq;
-    for (int l = 0; l < 3; l++) {                // tiles of 64, 128, 256
-        const int tp = (up + (1 << l) - 1) >> l, tq = (uq + (1 << l) - 1) >> l;
-        const int at = l == 0 ? PRE_GRAM_S : (l == 1 ? PRE_GRAM : PRE_GRAM_L);
+    for (int l = 0; l < 4; l++) {                // tiles of 32, 64, 128, 256
+        const int tp = l ? (up + (1 << l >> 1) - 1) >> (l - 1) : 2 * up, tq = l ? (uq + (1 << l >> 1) - 1) >> (l - 1) : 2 * uq;
+        const int at = ns_gram_stage(32 << l);
         z.work[at] = tp * (tp + 1) / 2;
         z.work[at + 1] = tp * tq;
     }
@@ -297,10 +302,19 @@ __device__ __forceinline__ void ns_pair(float v, h16 &hi, h16 &lo)
     hi = __builtin_bit_cast(h16, h);
     lo = __builtin_bit_cast(h16, l);
 }
-// four halves as two words
-__device__ __forceinline__ u32x2_t ns_words(const h16 *v)
+// the pairs of four values, hi and lo as two words each
+__device__ __forceinline__ void ns_pair4(const float *v, u32x2_t &hi, u32x2_t &lo)
 {
-    return u32x2_t{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16};
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    #pragma unroll
+    for (int k = 0; k < 2; k++) {
+        float a = v[2 * k], b = v[2 * k + 1];
+        asm("" : "+v"(a), "+v"(b));
+        const f16x2 h = __builtin_convertvector(f32x2_t{a, b}, f16x2);
+        const f16x2 l = __builtin_convertvector(f32x2_t{a - (float)h[0], b - (float)h[1]}, f16x2);
+        hi[k] = __builtin_bit_cast(uint32_t, h);
+        lo[k] = __builtin_bit_cast(uint32_t, l);
+    }
 }
 // element offset of (row, k) of a pair matrix with K columns: hi there, lo 32 further on
 __device__ __forceinline__ int64_t ns_at(int64_t row, int k, int K)
@@ -384,7 +398,7 @@ struct NsPlace { int it, ti, tj; };
 template <int BT, int MODE>
 __device__ __forceinline__ NsPlace ns_place(const NsTable &t, int count, int tile)
 {
-    const int *pre = t.pre[(BT == 64 ? PRE_GRAM_S : (BT == 128 ? PRE_GRAM : PRE_GRAM_L)) + !ns_sym(MODE)];
+    const int *pre = t.pre[ns_gram_stage(BT) + !ns_sym(MODE)];
     NsPlace pl;
     pl.it = ns_find(pre, count, tile);
     const int w = tile - pre[pl.it];
@@ -415,11 +429,10 @@ __device__ __forceinline__ void wave_sync()
 constexpr int kSubBytes = kSub * 256;
 __device__ __forceinline__ int sub_at(int j, int byte) { return j * 256 + ((byte >> 4 ^ (j & 15)) << 4) + (byte & 15); }
 
-// Results [MI][NI] of 16 x 16 blocks (a lane holds rows 4 g .. + 3 of column q)
-// into the sub-tile at block column nj0.  v(e, value, i, j) gives what is kept
-// of S times the product at (i, j) of the sub-tile.
+// Results [MI][NI] of 16 x 16 blocks (a lane holds rows 4 g .. + 3 of column q;
+// S^2 times the product) into the sub-tile from its block (mi0, nj0) on.
 template <int MODE, int MI, int NI>
-__device__ __forceinline__ void sub_put(lds_byte *sub, const f32x4 (&acc)[MI][NI], int nj0, const NsDev &d,
+__device__ __forceinline__ void sub_put(lds_byte *sub, const f32x4 (&acc)[MI][NI], int mi0, int nj0, const NsDev &d,
                                         const NsStep &s, int i0, int j0)
 {
     const int lane = threadIdx.x & 63, g = lane / 16, q = lane % 16;
@@ -427,7 +440,7 @@ __device__ __forceinline__ void sub_put(lds_byte *sub, const f32x4 (&acc)[MI][NI
     for (int nj = 0; nj < NI; nj++)
         #pragma unroll
         for (int mi = 0; mi < MI; mi++) {
-            const int i = mi * 16 + 4 * g, j = (nj0 + nj) * 16 + q;
+            const int i = (mi0 + mi) * 16 + 4 * g, j = (nj0 + nj) * 16 + q;
             float v[4];
             #pragma unroll
             for (int e = 0; e < 4; e++) v[e] = acc[mi][nj][e] * kInvS;
@@ -445,20 +458,19 @@ __device__ __forceinline__ void sub_put(lds_byte *sub, const f32x4 (&acc)[MI][NI
                 f32x4 o = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
                 lst(sub + sub_at(j, i * 4), o);
             } else {
-                h16 hi[4], lo[4];
-                #pragma unroll
-                for (int e = 0; e < 4; e++) ns_pair(v[e], hi[e], lo[e]);
+                u32x2_t hi, lo;
+                ns_pair4(v, hi, lo);
                 const int byte = (i >> 5) * 128 + (i & 31) * 2;
-                lst(sub + sub_at(j, byte), ns_words(hi));
-                lst(sub + sub_at(j, byte + 64), ns_words(lo));
+                lst(sub + sub_at(j, byte), hi);
+                lst(sub + sub_at(j, byte + 64), lo);
             }
         }
 }
 
-// The sub-tile to memory by waves first .. first + NW - 1 of the workgroup, w
-// this wave's number among them: rows of 256 bytes as they lie, and the other
-// orientation through transposing reads.  i0, j0: the sub-tile's place in the result.
-template <int MODE, int NW, typename W>
+// The SB x SB sub-tile to memory by NW waves, w this wave's number among them:
+// its rows as they lie, and the other orientation through transposing reads.
+// i0, j0: the sub-tile's place in the result.
+template <int MODE, int SB, int NW, typename W>
 __device__ __forceinline__ void sub_out(const lds_byte *sub, int w, const NsDev &d, const NsStep &s, int turn,
                                         bool mirror, int i0, int j0)
 {
@@ -466,8 +478,8 @@ __device__ __forceinline__ void sub_out(const lds_byte *sub, int w, const NsDev 
     if constexpr (MODE == NS_LAST) {
         const float lr = ns_rate(s);
         #pragma unroll 4
-        for (int k = w; k < kSub; k += NW) {     // one row of the caller's matrix a step
-            const int i = d.flip ? lane : k, j = d.flip ? k : lane;
+        for (int k = w; k < SB * SB / 64; k += NW) {     // along rows of the caller's matrix
+            const int r = k * (64 / SB) + lane / SB, c = lane % SB, i = d.flip ? c : r, j = d.flip ? r : c;
             const float o = lld<float>(sub + sub_at(j, i * 4));
             if (i0 + i < d.p && j0 + j < d.q)
                 ns_result<W>(d.in, s, lr, d.flip ? j0 + j : i0 + i, d.flip ? i0 + i : j0 + j, o);
@@ -476,16 +488,17 @@ __device__ __forceinline__ void sub_out(const lds_byte *sub, int w, const NsDev 
         h16 *straight = MODE == NS_GRAM ? d.g : (MODE == NS_SQUARE ? d.r : d.x);
         h16 *turned = MODE == NS_APPLY ? d.xt[turn ^ 1] : straight;
         const int ks = ns_sym(MODE) ? d.P : d.Q;
+        constexpr int CH = SB / 4;                       // 16-byte chunks of a row
         #pragma unroll
-        for (int k = w; k < 16; k += NW) {
-            const int j = k * 4 + lane / 16, c = lane % 16;
+        for (int k = w; k < SB * CH / 64; k += NW) {
+            const int j = k * (64 / CH) + lane / CH, c = lane % CH;
             gst(turned + ns_at(j0 + j, i0, d.P) + c * 8, lld<u32x4>(sub + sub_at(j, c * 16)));
         }
         if (!mirror) return;
         // 16 i x 32 j a step: a lane gets 8 consecutive j of one i
         #pragma unroll
-        for (int k = w; k < 16; k += NW) {
-            const int i = (k >> 2) * 16, jb = (k >> 1 & 1) * 32, part = k & 1;
+        for (int k = w; k < SB / 16 * (SB / 32) * 2; k += NW) {
+            const int part = k & 1, jb = (k >> 1) % (SB / 32) * 32, i = (k >> 1) / (SB / 32) * 16;
             const int byte = (i >> 5) * 128 + (i & 31) * 2 + part * 64 + 8 * (q % 4), j = jb + 8 * g + q / 4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sub + sub_at(j, byte)));
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sub + sub_at(j + 4, byte)));
@@ -615,10 +628,10 @@ __global__ __launch_bounds__(BT * 2) void k_ns_product(NsTable t, int count, NsS
         for (int i = 0; i < 4; i++)
             #pragma unroll
             for (int j = 0; j < NI; j++) part[i][j] = acc[h * 4 + i][j];
-        sub_put<MODE>(sub, part, 0, d, s, i0, j0);
+        sub_put<MODE>(sub, part, 0, 0, d, s, i0, j0);
         wave_sync();
         // both orientations already
-        sub_out<MODE, 1, W>(sub, 0, d, s, turn, !ns_sym(MODE) || ti != tj, i0, j0);
+        sub_out<MODE, kSub, 1, W>(sub, 0, d, s, turn, !ns_sym(MODE) || ti != tj, i0, j0);
         wave_sync();
     }
 }
@@ -648,47 +661,47 @@ __global__ __launch_bounds__(256) void k_ns_finish(NsTable t, int count, NsStep 
             const f32x4 v = gld<f32x4>(src + (int64_t)k * (BT * BT) + i * 256);
             acc[i][0][0] += v[0]; acc[i][0][1] += v[1]; acc[i][0][2] += v[2]; acc[i][0][3] += v[3];
         }
-    sub_put<MODE>((lds_byte *)sub, acc, wave, d, s, i0, j0);
+    sub_put<MODE>((lds_byte *)sub, acc, 0, wave, d, s, i0, j0);
     __syncthreads();
-    sub_out<MODE, 4, W>((lds_byte *)sub, wave, d, s, turn, !ns_sym(MODE) || pl.ti != pl.tj, i0, j0);
+    sub_out<MODE, kSub, 4, W>((lds_byte *)sub, wave, d, s, turn, !ns_sym(MODE) || pl.ti != pl.tj, i0, j0);
 }
 
-// Workgroup: a tile of 64 x 64 outputs whose k steps are split over its four
-// waves.  Nothing is shared between the waves, so the operands' fragments are
-// loaded straight into registers, four steps ahead, without LDS or barriers:
-// for few tiles, where the time of a stage is the round trip of its loads.  The
-// waves' sums are added through LDS in a fixed order.
-template <int MODE, typename W>
+// Workgroup: a tile of BT x BT outputs (64 or 32) whose k steps are split over
+// its four waves.  Nothing is shared between the waves, so the operands'
+// fragments are loaded straight into registers, AHEAD steps ahead, without LDS or
+// barriers: for few tiles, where the time of a stage is what one CU loads (30 to
+// 50 GB/s).  The waves' sums are added through LDS in a fixed order.
+template <int BT, int MODE, typename W>
 __global__ __launch_bounds__(256, 1) void k_ns_direct(NsTable t, int count, NsStep s, int turn)
 {
-    constexpr int AHEAD = 4;
-    __shared__ __align__(16) unsigned char lds[4 * kSubBytes];
-    const NsPlace pl = ns_place<64, MODE>(t, count, xcd_remap(blockIdx.x, gridDim.x));
+    constexpr int B = BT / 16, AHEAD = 16 / B;
+    __shared__ __align__(16) unsigned char lds[BT == 64 ? 4 * kSubBytes : kSubBytes];
+    const NsPlace pl = ns_place<BT, MODE>(t, count, xcd_remap(blockIdx.x, gridDim.x));
     const NsDev &d = t.items[pl.it];
     const int K = MODE == NS_GRAM ? d.Q : d.P;
     const h16 *pa = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.r);
     const h16 *pb = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.xt[turn]);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane % 16, fc = lane / 16;
-    const int i0 = pl.ti * 64, j0 = pl.tj * 64;
+    const int i0 = pl.ti * BT, j0 = pl.tj * BT;
     const int steps = K / 32, k0 = wave * steps / 4, n = (wave + 1) * steps / 4 - k0;
     const int64_t block = (int64_t)16 * 2 * K;
     const h16 *a = pa + (int64_t)(i0 + fr) * 2 * K + k0 * 64 + fc * 8, *b = pb + (int64_t)(j0 + fr) * 2 * K + k0 * 64 + fc * 8;
-    f16x8 f[AHEAD][16];                          // a hi, lo; b hi, lo of four blocks each
-    auto load = [&](f16x8 (&o)[16], int k) __attribute__((always_inline)) {
+    f16x8 f[AHEAD][4 * B];                       // a hi, lo; b hi, lo of B blocks each
+    auto load = [&](f16x8 (&o)[4 * B], int k) __attribute__((always_inline)) {
         #pragma unroll
-        for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < B; i++) {
             const h16 *p = a + i * block + k * 64, *q = b + i * block + k * 64;
             o[2 * i] = gld<f16x8>(p);
             o[2 * i + 1] = gld<f16x8>(p + 32);
-            o[8 + 2 * i] = gld<f16x8>(q);
-            o[9 + 2 * i] = gld<f16x8>(q + 32);
+            o[2 * B + 2 * i] = gld<f16x8>(q);
+            o[2 * B + 2 * i + 1] = gld<f16x8>(q + 32);
         }
     };
-    f32x4 acc[4][4];
+    f32x4 acc[B][B];
     #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int i = 0; i < B; i++)
         #pragma unroll
-        for (int j = 0; j < 4; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < B; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     #pragma unroll
     for (int u = 0; u < AHEAD; u++)
         if (u < n) load(f[u], u);
@@ -697,36 +710,38 @@ __global__ __launch_bounds__(256, 1) void k_ns_direct(NsTable t, int count, NsSt
         for (int u = 0; u < AHEAD; u++) {
             if (k + u < n)
                 #pragma unroll
-                for (int i = 0; i < 4; i++)
+                for (int i = 0; i < B; i++)
                     #pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[u][2 * i], f[u][9 + 2 * j], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[u][2 * i + 1], f[u][8 + 2 * j], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[u][2 * i], f[u][8 + 2 * j], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < B; j++) {
+                        const f16x8 &ah = f[u][2 * i], &al = f[u][2 * i + 1], &bh = f[u][2 * B + 2 * j], &bl = f[u][2 * B + 2 * j + 1];
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, acc[i][j], 0, 0, 0);
                     }
             if (k + u + AHEAD < n) load(f[u], k + u + AHEAD);
         }
-    // in the order of the fragments, [wave][block][lane]; wave w adds block column w
+    // in the order of the fragments, [wave][block][lane]; wave w adds the B B / 4 blocks from w B B / 4 on
+    constexpr int MINE = B * B / 4;
     f32x4 *red = reinterpret_cast<f32x4 *>(lds);
     #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int j = 0; j < B; j++)
         #pragma unroll
-        for (int j = 0; j < 4; j++) red[(wave * 16 + j * 4 + i) * 64 + lane] = acc[i][j];
+        for (int i = 0; i < B; i++) red[(wave * B * B + j * B + i) * 64 + lane] = acc[i][j];
     __syncthreads();
-    f32x4 sum[4][1];
+    f32x4 sum[MINE][1];
     #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        sum[i][0] = red[(wave * 4 + i) * 64 + lane];
+    for (int i = 0; i < MINE; i++) {
+        sum[i][0] = red[(wave * MINE + i) * 64 + lane];
         #pragma unroll
         for (int w = 1; w < 4; w++) {
-            const f32x4 v = red[(w * 16 + wave * 4 + i) * 64 + lane];
+            const f32x4 v = red[(w * B * B + wave * MINE + i) * 64 + lane];
             sum[i][0][0] += v[0]; sum[i][0][1] += v[1]; sum[i][0][2] += v[2]; sum[i][0][3] += v[3];
         }
     }
     __syncthreads();
-    sub_put<MODE>((lds_byte *)lds, sum, wave, d, s, i0, j0);
+    sub_put<MODE>((lds_byte *)lds, sum, wave * MINE % B, wave * MINE / B, d, s, i0, j0);
     __syncthreads();
-    sub_out<MODE, 4, W>((lds_byte *)lds, wave, d, s, turn, !ns_sym(MODE) || pl.ti != pl.tj, i0, j0);
+    sub_out<MODE, BT, 4, W>((lds_byte *)lds, wave, d, s, turn, !ns_sym(MODE) || pl.ti != pl.tj, i0, j0);
 }
 
 // ---- narrow matrices (short side up to 128) --------------------------------
@@ -800,11 +815,10 @@ __device__ __forceinline__ void nw_zero(f32x4 (&acc)[MI][NI])
 // four consecutive values of a pair row
 __device__ __forceinline__ void nw_store4(h16 *p, const float *v)
 {
-    h16 hi[4], lo[4];
-    #pragma unroll
-    for (int e = 0; e < 4; e++) ns_pair(v[e], hi[e], lo[e]);
-    *reinterpret_cast<u32x2_t *>(p) = ns_words(hi);
-    *reinterpret_cast<u32x2_t *>(p + 32) = ns_words(lo);
+    u32x2_t hi, lo;
+    ns_pair4(v, hi, lo);
+    *reinterpret_cast<u32x2_t *>(p) = hi;
+    *reinterpret_cast<u32x2_t *>(p + 32) = lo;
 }
 __device__ __forceinline__ void nw_load4(const h16 *p, float *v)
 {
@@ -816,8 +830,9 @@ __device__ __forceinline__ void nw_load4(const h16 *p, float *v)
 // The block's partial Gram matrix over `steps` k steps of 32 columns (S^2 times
 // it): the wave's tile in acc.  False for a wave without one (P = 32: four waves
 // have a tile).
-template <int P, int MI, int NI>
-__device__ __forceinline__ bool nw_gram(const h16 *xs, int steps, f32x4 (&acc)[MI][NI])
+// between(k) runs ahead of step k.
+template <int P, int MI, int NI, typename F>
+__device__ __forceinline__ bool nw_gram(const h16 *xs, int steps, f32x4 (&acc)[MI][NI], F &&between)
 {
     using N = Nw<P>;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -832,6 +847,7 @@ __device__ __forceinline__ bool nw_gram(const h16 *xs, int steps, f32x4 (&acc)[M
     };
     #pragma unroll 4
     for (int k = 0; k < steps; k++) {
+        between(k);
         f16x8 ah[MI], al[MI], bh[NI], bl[NI];
         #pragma unroll
         for (int i = 0; i < MI; i++) {
@@ -869,22 +885,29 @@ __device__ __forceinline__ void nw_tiles(const f32x4 (&acc)[MI][NI], F &&put)
         for (int j = 0; j < NI; j++) put(wn * N::TN + j * 16 + q, wm * N::TM + i * 16 + 4 * g, acc[i][j]);
 }
 
-// The block in LDS to the workspace, and its partial Gram matrix.
+// The block in LDS to the workspace, and its partial Gram matrix; the stores
+// (64 KiB, 2.5 us at what a CU writes) go out between the product's steps.
 template <int P>
 __device__ __forceinline__ void nw_leave(const NsDev &d, int block, const h16 *xs, float *part)
 {
     using N = Nw<P>;
+    constexpr int XL = kBlock * 4 / 16 / kNwThreads, STEPS = N::QB / 32, EACH = (XL + STEPS - 1) / STEPS;
     const int tid = threadIdx.x;
     h16 *out = d.xt[0] + (int64_t)block * kBlock * 2;
-    #pragma unroll
-    for (int l = 0; l < kBlock * 4 / 16 / kNwThreads; l++) {
+    auto store = [&](int l) __attribute__((always_inline)) {
         const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
         gst(out + (int64_t)v * 8, *reinterpret_cast<const u32x4 *>(xs + row * N::XP + c * 8));
-    }
+    };
     f32x4 acc[N::TM / 16][N::TN / 16];
     float *o = part + (int64_t)block * P * P;
-    if (nw_gram<P>(xs, N::QB / 32, acc))
-        nw_tiles<P>(acc, [&](int row, int col, const f32x4 &v) { gst(o + row * P + col, v); });
+    const bool has = nw_gram<P>(xs, STEPS, acc, [&](int k) __attribute__((always_inline)) {
+        #pragma unroll
+        for (int e = 0; e < EACH; e++)
+            if (k * EACH + e < XL) store(k * EACH + e);
+    });
+    if (has) nw_tiles<P>(acc, [&](int row, int col, const f32x4 &v) { gst(o + row * P + col, v); });
+    else
+        for (int l = 0; l < XL; l++) store(l);
 }
 
 // Stage 2 of a narrow matrix: X's block as pairs, and its partial Gram matrix.
@@ -1124,7 +1147,7 @@ __device__ __forceinline__ void nw_tiny(const NsDev &d, const NsStep &s, h16 *xs
     const int columns = (d.q + 31) / 32;
     for (int k = 0; k < s.steps; k++) {
         f32x4 gram[N::TM / 16][N::TN / 16];
-        if (nw_gram<P>(xs, columns, gram))
+        if (nw_gram<P>(xs, columns, gram, [](int) {}))
             nw_tiles<P>(gram, [&](int row, int col, const f32x4 &v) {
                 const float f[4] = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
                 nw_store4(gs + row * N::GP + nw_k(col), f);
@@ -1220,15 +1243,16 @@ int64_t cut_bytes(const NsCut &c) { return c.pieces > 1 ? (int64_t)(c.tiles - c.
 // the matrix, the first loads and leaving the results (16 bytes an element at 26
 // GB/s a CU), and a part per k step, which depends on whether the CU is shared;
 // for cut tiles the launch that adds the pieces (5 us + 0.27 us per MB).
-//   256 x 256 (8 steps): 64-tiles 8.9, 128-tiles 14.3, 256-tiles 23.8
-//   1024 x 1024 (32 steps): 20.9, 13.5 + 5.5, 22.7 + 5.6
-//   4096 x 4096, R X (128 steps): 973, 421, 321
+//   256 x 256 (8 steps): 32-tiles 5.9, 64-tiles 9.1, 128-tiles 14.3, 256-tiles 23.8
+//   512 x 512 (16 steps): 8.2, 13.6, 7.9 + 5.1, 18.5 + 5.6
+//   1024 x 1024 (32 steps): 30.7, 20.9, 12.0 + 6.5, 22.7 + 5.6
+//   4096 x 4096, R X (128 steps): -, 973, 421, 321
 double cut_time(const NsCut &c, int steps)
 {
     const int slots = ns_slots(c.bt), rest = c.tiles - c.whole;
-    if (c.bt == 64) {
+    if (c.bt <= 64) {
         const int rounds = (c.tiles + slots - 1) / slots;
-        return 5.5 + rounds * steps * (rounds > 1 ? 0.6 : 0.45);
+        return c.bt == 32 ? 4.0 + rounds * steps * (rounds > 1 ? 0.3 : 0.23) : 5.5 + rounds * steps * (rounds > 1 ? 0.6 : 0.45);
     }
     const double step = c.bt == 128 ? 1.56 : 2.38, alone = c.bt == 128 ? 0.75 : 1.6, leave = c.bt == 128 ? 10.0 : 16.0;
     const int units = rest * c.pieces;
@@ -1245,11 +1269,11 @@ NsCut ns_stage(const NsPlan &p, int sym, int steps)
 {
     NsCut best{};
     double least = 1e30;
-    for (int l = 0; l < 3; l++) {
-        const int bt = 64 << l, tiles = (int)p.work[(l == 0 ? PRE_GRAM_S : (l == 1 ? PRE_GRAM : PRE_GRAM_L)) + !sym];
-        const int rest = tiles % ns_slots(bt), most = l == 0 || !rest ? 1 : ns_slots(bt) / rest;
+    for (int bt = 32; bt <= 256; bt *= 2) {
+        const int tiles = (int)p.work[ns_gram_stage(bt) + !sym];
+        const int rest = tiles % ns_slots(bt), most = bt <= 64 || !rest ? 1 : ns_slots(bt) / rest;
         for (int pieces = 1; pieces <= most && (pieces == 1 || pieces * 4 <= steps); pieces += (pieces + 3) / 4) {
-            const NsCut c{bt, tiles, l == 0 ? tiles : tiles - rest, pieces, nullptr};
+            const NsCut c{bt, tiles, bt <= 64 ? tiles : tiles - rest, pieces, nullptr};
             const double t = cut_time(c, steps);
             if (t < least) {
                 least = t;
@@ -1338,7 +1362,8 @@ hipError_t ns_product(const NsPlan &p, const NsTable &t, const NsStep &s, int tu
     if (cut.bt == 128) return ns_product_bt<128, MODE, W>(p, t, s, turn, cut, st);
     if (cut.bt == 256) return ns_product_bt<256, MODE, W>(p, t, s, turn, cut, st);
     TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, ns_sym(MODE) ? 0.0 : p.flops);
-    hipLaunchKernelGGL((k_ns_direct<MODE, W>), dim3((unsigned)cut.tiles), dim3(256), 0, st, t, p.count, s, turn);
+    if (cut.bt == 64) hipLaunchKernelGGL((k_ns_direct<64, MODE, W>), dim3((unsigned)cut.tiles), dim3(256), 0, st, t, p.count, s, turn);
+    else hipLaunchKernelGGL((k_ns_direct<32, MODE, W>), dim3((unsigned)cut.tiles), dim3(256), 0, st, t, p.count, s, turn);
     return hipGetLastError();
 }
 

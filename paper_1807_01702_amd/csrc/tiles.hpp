@@ -222,7 +222,7 @@ constexpr int kLnMaxC = 16384;             // 16 channels a thread of a 1024-thr
 
 // ---- Newton-Schulz orthogonalisation ---------------------------------------
 constexpr int kNsSlots = 512;               // product workgroups the chip holds (2 a CU)
-constexpr int kNsStages = 11;               // stages with work items of their own
+constexpr int kNsStages = 13;               // stages with work items of their own
 constexpr int kNsChunk = 48;               // matrices per table launch (kernel arguments below 4 KiB)
 constexpr int kNsMaxCount = 1024;          // matrices of a call
 constexpr int kNsMaxShort = 16384, kNsMaxLong = 1 << 20;
