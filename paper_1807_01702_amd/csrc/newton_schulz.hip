@@ -820,12 +820,6 @@ __device__ __forceinline__ void nw_store4(h16 *p, const float *v)
     *reinterpret_cast<u32x2_t *>(p) = hi;
     *reinterpret_cast<u32x2_t *>(p + 32) = lo;
 }
-__device__ __forceinline__ void nw_load4(const h16 *p, float *v)
-{
-    const f16x4 hi = *reinterpret_cast<const f16x4 *>(p), lo = *reinterpret_cast<const f16x4 *>(p + 32);
-    #pragma unroll
-    for (int e = 0; e < 4; e++) v[e] = (float)hi[e] + (float)lo[e];
-}
 
 // The block's partial Gram matrix over `steps` k steps of 32 columns (S^2 times
 // it): the wave's tile in acc.  False for a wave without one (P = 32: four waves
@@ -898,16 +892,23 @@ __device__ __forceinline__ void nw_leave(const NsDev &d, int block, const h16 *x
         const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
         gst(out + (int64_t)v * 8, *reinterpret_cast<const u32x4 *>(xs + row * N::XP + c * 8));
     };
-    f32x4 acc[N::TM / 16][N::TN / 16];
+    constexpr int MI = N::TM / 16, NI = N::TN / 16;
+    f32x4 acc[MI][NI];
     float *o = part + (int64_t)block * P * P;
     const bool has = nw_gram<P>(xs, STEPS, acc, [&](int k) __attribute__((always_inline)) {
         #pragma unroll
         for (int e = 0; e < EACH; e++)
             if (k * EACH + e < XL) store(k * EACH + e);
     });
-    if (has) nw_tiles<P>(acc, [&](int row, int col, const f32x4 &v) { gst(o + row * P + col, v); });
-    else
+    if (has) {
+        // in the order of the fragments, [wave][block][lane]: the next step's waves take the same tiles
+        #pragma unroll
+        for (int i = 0; i < MI; i++)
+            #pragma unroll
+            for (int j = 0; j < NI; j++) gst(o + (((tid >> 6) * MI * NI + i * NI + j) * 64 + (tid & 63)) * 4, acc[i][j]);
+    } else {
         for (int l = 0; l < XL; l++) store(l);
+    }
 }
 
 // Stage 2 of a narrow matrix: X's block as pairs, and its partial Gram matrix.
@@ -946,31 +947,43 @@ __device__ __forceinline__ void nw_prepare(const NsDev &d, int block, const NsSt
     nw_leave<P>(d, block, xs, d.part[0]);
 }
 
-// R = a I + b G + c G G over G's place in LDS.  Starts after a barrier, ends with one.
-template <int P>
-__device__ __forceinline__ void nw_polynomial(const NsStep &s, h16 *gs)
+// G's pairs into LDS from the wave's tile of it (raw: S^2 times G, as the
+// product leaves it).
+template <int P, int MI, int NI>
+__device__ __forceinline__ void nw_put(h16 *gs, const f32x4 (&raw)[MI][NI])
+{
+    nw_tiles<P>(raw, [&](int row, int col, const f32x4 &v) {
+        const float f[4] = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
+        nw_store4(gs + row * Nw<P>::GP + nw_k(col), f);
+    });
+}
+
+// R = a I + b G + c G G over G's place in LDS; raw: this wave's tile of G as in
+// nw_put (has: it has one).  Starts after a barrier, ends with one.
+template <int P, int MI, int NI>
+__device__ __forceinline__ void nw_polynomial(const NsStep &s, h16 *gs, bool has, const f32x4 (&raw)[MI][NI])
 {
     using N = Nw<P>;
-    constexpr int MI = N::TM / 16, NI = N::TN / 16;
+    const int lane = threadIdx.x & 63, g = lane / 16, q = lane % 16;
     const int wave = threadIdx.x >> 6, wm = wave / N::WN, wn = wave % N::WN;
-    const bool has = wm * N::TM < P;
     f32x4 acc[MI][NI];
     nw_zero(acc);
     if (has) nw_product<MI, NI, P / 32>(gs + wm * N::TM * N::GP, N::GP, gs + wn * N::TN * N::GP, N::GP, acc);
-    float v[MI * NI][4];
-    int at = 0;
-    if (has)
-        nw_tiles<P>(acc, [&](int row, int col, const f32x4 &t) {
-            float gg[4];
-            nw_load4(gs + row * N::GP + nw_k(col), gg);
-            #pragma unroll
-            for (int e = 0; e < 4; e++)
-                v[at][e] = __builtin_fmaf(s.c, t[e] * kInvS, s.b * gg[e]) + (row == col + e ? s.a * kS : 0.f);
-            at++;
-        });
     __syncthreads();
-    at = 0;
-    if (has) nw_tiles<P>(acc, [&](int row, int col, const f32x4 &) { nw_store4(gs + row * N::GP + nw_k(col), v[at++]); });
+    if (has)
+        #pragma unroll
+        for (int i = 0; i < MI; i++)
+            #pragma unroll
+            for (int j = 0; j < NI; j++) {
+                const int row = wn * N::TN + j * 16, col = wm * N::TM + i * 16;
+                float v[4];
+                #pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = __builtin_fmaf(s.c, acc[i][j][e], s.b * raw[i][j][e]) * kInvS;
+                if (row == col)                  // a block of the diagonal
+                    #pragma unroll
+                    for (int e = 0; e < 4; e++) v[e] += q == 4 * g + e ? s.a * kS : 0.f;
+                nw_store4(gs + (row + q) * N::GP + nw_k(col + 4 * g), v);
+            }
     __syncthreads();
 }
 
@@ -1044,38 +1057,30 @@ __device__ __forceinline__ void nw_step(const NsDev &d, int block, const NsStep 
     const bool summed = ns_summed(d.blocks, P);
     const float *part = summed ? d.sum : d.part[turn];
     const int np = summed ? 1 : d.blocks;
-    constexpr int GV = P * P / 4, GL = (GV + kNwThreads - 1) / kNwThreads;
-    f32x4 gv[GL];
-    #pragma unroll
-    for (int l = 0; l < GL; l++) {
-        const int v = l * kNwThreads + tid;
-        gv[l] = gld<f32x4>(part + (int64_t)(v < GV ? v : 0) * 4);
+    constexpr int MI = N::TM / 16, NI = N::TN / 16;
+    const int lane = tid & 63, wave = tid >> 6;
+    const bool has = wave / N::WN * N::TM < P;
+    f32x4 raw[MI][NI];                           // this wave's tile of G, summed over the blocks
+    nw_zero(raw);
+    if (has) {
+        const float *from = part + (wave * MI * NI * 64 + lane) * 4;
+        for (int b = 0; b < np; b++)
+            #pragma unroll
+            for (int i = 0; i < MI; i++)
+                #pragma unroll
+                for (int j = 0; j < NI; j++) {
+                    const f32x4 w = gld<f32x4>(from + (int64_t)b * P * P + (i * NI + j) * 256);
+                    raw[i][j][0] += w[0]; raw[i][j][1] += w[1]; raw[i][j][2] += w[2]; raw[i][j][3] += w[3];
+                }
     }
-    for (int b = 1; b < np; b++)
-        #pragma unroll
-        for (int l = 0; l < GL; l++) {
-            const int v = l * kNwThreads + tid;
-            const f32x4 w = gld<f32x4>(part + (int64_t)b * P * P + (int64_t)(v < GV ? v : 0) * 4);
-            gv[l][0] += w[0]; gv[l][1] += w[1]; gv[l][2] += w[2]; gv[l][3] += w[3];
-        }
     #pragma unroll
     for (int l = 0; l < XL; l++) {
         const int v = l * kNwThreads + tid, row = v / (P / 4), c = v % (P / 4);
         *reinterpret_cast<u32x4 *>(xs + row * N::XP + c * 8) = xv[l];
     }
-    #pragma unroll
-    for (int l = 0; l < GL; l++) {
-        const int v = l * kNwThreads + tid;
-        if (v < GV) {
-            const int row = v / (P / 4), c = v % (P / 4) * 4;
-            float f[4];
-            #pragma unroll
-            for (int e = 0; e < 4; e++) f[e] = gv[l][e] * kInvS;
-            nw_store4(gs + row * N::GP + nw_k(c), f);
-        }
-    }
+    if (has) nw_put<P>(gs, raw);
     __syncthreads();
-    nw_polynomial<P>(s, gs);
+    nw_polynomial<P>(s, gs, has, raw);
     f32x4 acc[N::YM / 16][N::YN / 16];
     nw_apply<P>(xs, gs, acc);
     __syncthreads();
@@ -1147,13 +1152,10 @@ __device__ __forceinline__ void nw_tiny(const NsDev &d, const NsStep &s, h16 *xs
     const int columns = (d.q + 31) / 32;
     for (int k = 0; k < s.steps; k++) {
         f32x4 gram[N::TM / 16][N::TN / 16];
-        if (nw_gram<P>(xs, columns, gram, [](int) {}))
-            nw_tiles<P>(gram, [&](int row, int col, const f32x4 &v) {
-                const float f[4] = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
-                nw_store4(gs + row * N::GP + nw_k(col), f);
-            });
+        const bool has = nw_gram<P>(xs, columns, gram, [](int) {});
+        if (has) nw_put<P>(gs, gram);
         __syncthreads();
-        nw_polynomial<P>(s, gs);
+        nw_polynomial<P>(s, gs, has, gram);
         f32x4 acc[N::YM / 16][N::YN / 16];
         nw_apply<P>(xs, gs, acc);
         __syncthreads();
