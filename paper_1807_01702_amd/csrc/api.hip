@@ -1903,9 +1903,7 @@ static bnr_status check_ns_areas(int n, bool own, F &&area)
 
 static bnr_status check_ns_plan(const NsPlan &p)
 {
-    for (int64_t w : p.work)
-        if (w > (int64_t)1 << 30) return fail(BNR_ERR_UNSUPPORTED, "list too large for one call");
-    return BNR_OK;
+    return ns_plan_fits(p) ? BNR_OK : fail(BNR_ERR_UNSUPPORTED, "list too large for one call");
 }
 
 static NsIn ortho_in(const void *arg, int i)
@@ -1929,7 +1927,7 @@ static size_t ns_workspace(const T *items, int32_t count)
         if (check_ns_matrix(i, items[i].rows, items[i].cols) != BNR_OK) return 0;
         ns_plan_add(p, items[i].rows, items[i].cols);
     }
-    return ns_plan_bytes(p);
+    return ns_plan_fits(p) ? ns_plan_bytes(p) : 0;
 }
 
 extern "C" {

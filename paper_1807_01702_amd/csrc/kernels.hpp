@@ -322,6 +322,7 @@ struct NsPlan {
 };
 typedef NsIn (*NsFill)(const void *arg, int i);
 void ns_plan_add(NsPlan &p, int rows, int cols);
+bool ns_plan_fits(const NsPlan &p);              // running counts and grids stay in range
 size_t ns_plan_bytes(const NsPlan &p);
 hipError_t launch_ns(const NsPlan &p, NsFill fill, const void *arg, const NsStep &s, int src_dtype, int dst_dtype,
                      void *ws, hipStream_t st);

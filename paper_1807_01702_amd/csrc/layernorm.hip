@@ -96,7 +96,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *red)
     }
 }
 
-// U rows at a time per row group, GR row groups per workgroup.
+// U rows at a time per row group, GR row groups per workgroup; a workgroup takes
+// row sets b, b + grid, ... (one, unless there are more than a grid holds).
 template <typename T, int V, int TPR, int NV, int U, bool RES>
 __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnParams p)
 {
@@ -105,83 +106,85 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
     __shared__ float red[2][WG / 64 * U];
     const int lane = threadIdx.x % TPR, grp = threadIdx.x / TPR;
     const int nvec = p.c / V;
+    const float inv_c = 1.f / (float)p.c;
     const T *x = (const T *)p.x, *res = (const T *)p.res;
     T *sum = (T *)p.sum, *y = (T *)p.y;
-    const int64_t row0 = (int64_t)blockIdx.x * (GR * U) + grp;
-    typename L::raw rx[U][NV], rr[U][NV];
-    float f[U][NV][V], gam[NV][V], bet[NV][V], acc[U];
-    #pragma unroll
-    for (int u = 0; u < U; u++) {
-        // rows and vectors past the end read the last ones and are dropped
-        const int64_t row = row0 + u * GR < p.m ? row0 + u * GR : p.m - 1;
+    for (int64_t base = (int64_t)blockIdx.x * (GR * U); base < p.m; base += (int64_t)gridDim.x * (GR * U)) {
+        const int64_t row0 = base + grp;
+        typename L::raw rx[U][NV], rr[U][NV];
+        float f[U][NV][V], gam[NV][V], bet[NV][V], acc[U];
+        #pragma unroll
+        for (int u = 0; u < U; u++) {
+            // rows and vectors past the end read the last ones and are dropped
+            const int64_t row = row0 + u * GR < p.m ? row0 + u * GR : p.m - 1;
+            #pragma unroll
+            for (int j = 0; j < NV; j++) {
+                const int v = j * TPR + lane < nvec ? j * TPR + lane : nvec - 1;
+                rx[u][j] = L::load(x + row * p.x_ldc + (int64_t)v * V);
+                if (RES) rr[u][j] = L::load(res + row * p.res_ldc + (int64_t)v * V);
+            }
+        }
         #pragma unroll
         for (int j = 0; j < NV; j++) {
             const int v = j * TPR + lane < nvec ? j * TPR + lane : nvec - 1;
-            rx[u][j] = L::load(x + row * p.x_ldc + (int64_t)v * V);
-            if (RES) rr[u][j] = L::load(res + row * p.res_ldc + (int64_t)v * V);
-        }
-    }
-    #pragma unroll
-    for (int j = 0; j < NV; j++) {
-        const int v = j * TPR + lane < nvec ? j * TPR + lane : nvec - 1;
-        ln_param<V>(p.gamma, v * V, 1.f, gam[j]);
-        ln_param<V>(p.beta, v * V, 0.f, bet[j]);
-    }
-    #pragma unroll
-    for (int u = 0; u < U; u++) {
-        const int64_t row = row0 + u * GR;
-        acc[u] = 0.f;
-        #pragma unroll
-        for (int j = 0; j < NV; j++) {
-            const bool in = j * TPR + lane < nvec;
-            L::unpack(rx[u][j], f[u][j]);
-            if (RES) {
-                float r[V];
-                L::unpack(rr[u][j], r);
-                // what is normalised is the sum as it is stored
-                #pragma unroll
-                for (int i = 0; i < V; i++) f[u][j][i] = Elem<T>::round(f[u][j][i] + r[i]);
-                if (in && row < p.m) L::store(sum + row * p.sum_ldc + (int64_t)(j * TPR + lane) * V, f[u][j]);
-            }
-            if (in)
-                #pragma unroll
-                for (int i = 0; i < V; i++) acc[u] += f[u][j][i];
-        }
-    }
-    const float inv_c = 1.f / (float)p.c;
-    row_sums<TPR, U>(acc, red[0]);
-    float sq[U];
-    #pragma unroll
-    for (int u = 0; u < U; u++) {
-        acc[u] *= inv_c;
-        sq[u] = 0.f;
-        #pragma unroll
-        for (int j = 0; j < NV; j++)
-            if (j * TPR + lane < nvec)
-                #pragma unroll
-                for (int i = 0; i < V; i++) {
-                    f[u][j][i] -= acc[u];
-                    sq[u] += f[u][j][i] * f[u][j][i];
-                }
-    }
-    row_sums<TPR, U>(sq, red[1]);
-    #pragma unroll
-    for (int u = 0; u < U; u++) {
-        const int64_t row = row0 + u * GR;
-        if (row >= p.m) continue;
-        const float rstd = 1.f / sqrtf(sq[u] * inv_c + p.eps);
-        if (lane == 0) {
-            p.mean[row] = acc[u];
-            p.rstd[row] = rstd;
+            ln_param<V>(p.gamma, v * V, 1.f, gam[j]);
+            ln_param<V>(p.beta, v * V, 0.f, bet[j]);
         }
         #pragma unroll
-        for (int j = 0; j < NV; j++) {
-            const int v = j * TPR + lane;
-            if (v >= nvec) continue;
-            float o[V];
+        for (int u = 0; u < U; u++) {
+            const int64_t row = row0 + u * GR;
+            acc[u] = 0.f;
             #pragma unroll
-            for (int i = 0; i < V; i++) o[i] = f[u][j][i] * rstd * gam[j][i] + bet[j][i];
-            L::store(y + row * p.y_ldc + (int64_t)v * V, o);
+            for (int j = 0; j < NV; j++) {
+                const bool in = j * TPR + lane < nvec;
+                L::unpack(rx[u][j], f[u][j]);
+                if (RES) {
+                    float r[V];
+                    L::unpack(rr[u][j], r);
+                    // what is normalised is the sum as it is stored
+                    #pragma unroll
+                    for (int i = 0; i < V; i++) f[u][j][i] = Elem<T>::round(f[u][j][i] + r[i]);
+                    if (in && row < p.m) L::store(sum + row * p.sum_ldc + (int64_t)(j * TPR + lane) * V, f[u][j]);
+                }
+                if (in)
+                    #pragma unroll
+                    for (int i = 0; i < V; i++) acc[u] += f[u][j][i];
+            }
+        }
+        row_sums<TPR, U>(acc, red[0]);
+        float sq[U];
+        #pragma unroll
+        for (int u = 0; u < U; u++) {
+            acc[u] *= inv_c;
+            sq[u] = 0.f;
+            #pragma unroll
+            for (int j = 0; j < NV; j++)
+                if (j * TPR + lane < nvec)
+                    #pragma unroll
+                    for (int i = 0; i < V; i++) {
+                        f[u][j][i] -= acc[u];
+                        sq[u] += f[u][j][i] * f[u][j][i];
+                    }
+        }
+        row_sums<TPR, U>(sq, red[1]);
+        #pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int64_t row = row0 + u * GR;
+            if (row >= p.m) continue;
+            const float rstd = 1.f / sqrtf(sq[u] * inv_c + p.eps);
+            if (lane == 0) {
+                p.mean[row] = acc[u];
+                p.rstd[row] = rstd;
+            }
+            #pragma unroll
+            for (int j = 0; j < NV; j++) {
+                const int v = j * TPR + lane;
+                if (v >= nvec) continue;
+                float o[V];
+                #pragma unroll
+                for (int i = 0; i < V; i++) o[i] = f[u][j][i] * rstd * gam[j][i] + bet[j][i];
+                L::store(y + row * p.y_ldc + (int64_t)v * V, o);
+            }
         }
     }
 }
@@ -440,7 +443,8 @@ hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s)
         using T = std::remove_pointer_t<decltype(tag)>;
         constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, V = decltype(v)::value;
         constexpr int WG = TPR > kThreads ? TPR : kThreads, U = NV == 1 && TPR <= 64 ? 2 : 1;
-        const dim3 grid((unsigned)ceil_div(p.m, WG / TPR * U));
+        const int64_t sets = ceil_div(p.m, WG / TPR * U);
+        const dim3 grid((unsigned)(sets < kLnMaxGrid ? sets : kLnMaxGrid));
         if (p.res) hipLaunchKernelGGL((k_ln_fwd<T, V, TPR, NV, U, true>), grid, dim3(WG), 0, s, p);
         else hipLaunchKernelGGL((k_ln_fwd<T, V, TPR, NV, U, false>), grid, dim3(WG), 0, s, p);
         return hipGetLastError();

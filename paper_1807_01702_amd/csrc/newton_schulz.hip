@@ -138,6 +138,8 @@ struct NsChunk {                   // by value: the next matrices of the list
     NsIn in[kNsChunk];
 };
 
+static_assert(sizeof(NsChunk) + sizeof(NsTable) + sizeof(void *) <= 4096, "kernel arguments");
+
 // One wave, one matrix a lane; the places come from running sums across the lanes.
 __global__ __launch_bounds__(64) void k_ns_table(NsChunk c, NsTable t, char *base)
 {
@@ -1273,6 +1275,7 @@ NsCut ns_stage(const NsPlan &p, int sym, int steps)
     double least = 1e30;
     for (int bt = 32; bt <= 256; bt *= 2) {
         const int tiles = (int)p.work[ns_gram_stage(bt) + !sym];
+        if (tiles > kNsMaxGrid && bt < 256) continue;
         const int rest = tiles % ns_slots(bt), most = bt <= 64 || !rest ? 1 : ns_slots(bt) / rest;
         for (int pieces = 1; pieces <= most && (pieces == 1 || pieces * 4 <= steps); pieces += (pieces + 3) / 4) {
             const NsCut c{bt, tiles, bt <= 64 ? tiles : tiles - rest, pieces, nullptr};
@@ -1321,6 +1324,15 @@ void ns_plan_add(NsPlan &p, int rows, int cols)
     if (z.blocks) return;
     if (z.P > p.short_side) p.short_side = z.P;
     if (z.Q > p.long_side) p.long_side = z.Q;
+}
+
+bool ns_plan_fits(const NsPlan &p)
+{
+    for (int k = 0; k < kPre; k++) {
+        const bool choice = k == PRE_GRAM || k == PRE_APPLY || k >= PRE_GRAM_S;      // larger tiles can take it
+        if (p.work[k] > (choice && k != PRE_TINY ? (int64_t)1 << 30 : kNsMaxGrid)) return false;
+    }
+    return true;
 }
 
 size_t ns_plan_bytes(const NsPlan &p)

@@ -218,12 +218,14 @@ inline WgTrPlan wgrad_f32_plan(int64_t m, int n, int h, int w, int c_in, int c_o
 }
 
 // ---- layer normalisation ---------------------------------------------------
+constexpr int64_t kLnMaxGrid = 1 << 21;     // workgroups of up to 1024 threads (a grid holds fewer than 2^32)
 constexpr int kLnMaxC = 16384;             // 16 channels a thread of a 1024-thread workgroup
 
 // ---- Newton-Schulz orthogonalisation ---------------------------------------
 constexpr int kNsSlots = 512;               // product workgroups the chip holds (2 a CU)
 constexpr int kNsStages = 13;               // stages with work items of their own
-constexpr int kNsChunk = 48;               // matrices per table launch (kernel arguments below 4 KiB)
+constexpr int64_t kNsMaxGrid = 1 << 22;    // workgroups of a launch (a grid holds fewer than 2^32 threads)
+constexpr int kNsChunk = 60;               // matrices per table launch (kernel arguments below 4 KiB)
 constexpr int kNsMaxCount = 1024;          // matrices of a call
 constexpr int kNsMaxShort = 16384, kNsMaxLong = 1 << 20;
 

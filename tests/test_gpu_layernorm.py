@@ -362,3 +362,17 @@ def test_numpy_cross_check():
     # mean 4, squared differences 9 + 4 + 0 + 25 = 38, variance 9.5
     r = 1 / np.sqrt(9.5 + EPS)
     np.testing.assert_allclose(y.cpu().numpy()[0], [-3 * r + 0.5, -4 * r, 0.0, 20 * r - 1], rtol=1e-6, atol=1e-6)
+
+
+def test_more_rows_than_a_grid_holds():
+    """2^27 rows of 8, 64 a workgroup: more row sets than workgroups."""
+    B = _B()
+    m, c = (1 << 27) + 1001, 8
+    x = torch.empty(m, c, dtype=torch.bfloat16, device="cuda")
+    x.normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    y, ln = torch.empty_like(x), B.LN(None, None, m, EPS, device="cuda")
+    B.bnr_layernorm_fwd(x, ln, y)
+    for part in (slice(0, 1000), slice(m // 2, m // 2 + 1000), slice(m - 1000, m)):
+        z, l2 = torch.empty_like(x[part]), B.LN(None, None, 1000, EPS, device="cuda")
+        B.bnr_layernorm_fwd(x[part], l2, z)
+        assert torch.equal(y[part], z) and torch.equal(ln.mean[part], l2.mean) and torch.equal(ln.rstd[part], l2.rstd)
