@@ -16,9 +16,11 @@
 // smallest step is 2^-37 of the norm of X.  Three fp16 products run at 2.6 times
 // the rate of one float32 matrix product on this chip and carry the same error.
 //
-// Layout.  A pair matrix with K columns is [rows][K / 32][hi 32 | lo 32]: the 32
-// columns of one k step are one 128-byte line, so a tile row is one line per
-// step.  Every product is of the form C[i][j] = sum_k P[i][k] Q[j][k] with both
+// Layout.  A pair matrix lies in the order of the fragments that the matrix
+// instructions take (ns_at): a fragment is one KiB, whether it goes to registers
+// or, straight from memory, to LDS, and an LDS read of it has no bank conflicts.  (A CU
+// reads whole KiB at 105 to 124 GB/s from its L2, 16 rows of 64 bytes at 50.)
+// Every product is of the form C[i][j] = sum_k P[i][k] Q[j][k] with both
 // operands contiguous along k: G = X X^T as it is, G G because G is symmetric,
 // and R X from X's transpose, which each R X writes beside X for the next step.
 // Rows and columns are padded to whole tiles with zeros, which every product
@@ -318,10 +320,16 @@ __device__ __forceinline__ void ns_pair4(const float *v, u32x2_t &hi, u32x2_t &l
         lo[k] = __builtin_bit_cast(uint32_t, l);
     }
 }
-// element offset of (row, k) of a pair matrix with K columns: hi there, lo 32 further on
-__device__ __forceinline__ int64_t ns_at(int64_t row, int k, int K)
+// Element offset of (row, k) of a pair matrix with K columns: hi there, lo kLo
+// further on.  The order is the one in which the matrix instructions' fragments
+// are read: 16 rows x 32 columns of hi are one KiB, 8 columns of one row together,
+// 16 rows of them, four times that; then the lo ones; four such blocks make the 64
+// rows of one k step, then the next step follows.
+constexpr int kFrag = 512, kLo = kFrag, kBlk = 2 * kFrag, kStep = 4 * kBlk;      // halves
+__device__ __forceinline__ int64_t ns_at(int row, int k, int K)
 {
-    return row * 2 * K + (k >> 5) * 64 + (k & 31);
+    return ((int64_t)(row >> 6) * (K >> 5) + (k >> 5)) * kStep + ((row >> 4) & 3) * kBlk + ((k >> 3) & 3) * 128 +
+           (row & 15) * 8 + (k & 7);
 }
 
 // Stage 2: X and its transpose as pairs, from u / (||u||_F + eps); 64 x 64
@@ -350,17 +358,23 @@ __global__ __launch_bounds__(kThreads) void k_ns_prepare(NsTable t, int count, N
     const float scale = ns_factor<kThreads>(d, s.eps, red);              // (its barrier covers the tile)
     // as it is: [RP rows][K = CP]; turned: [CP rows][K = RP]
     h16 *straight = d.flip ? d.xt[0] : d.x, *turned = d.flip ? d.x : d.xt[0];
+    // a thread makes 8 columns of one row: lane, then 16-row block, then k step
     for (int v = tid; v < 64 * 8; v += kThreads) {
-        const int a = v / 8, k8 = v % 8 * 8;
-        __align__(16) h16 hi[8], lo[8];
-        for (int i = 0; i < 8; i++) ns_pair(tile[a][k8 + i] * scale, hi[i], lo[i]);
+        const int a = (v >> 6 & 3) * 16 + (v & 15), k8 = (v >> 8) * 32 + (v >> 4 & 3) * 8;
+        u32x2_t hi[2], lo[2];
+        float f[8];
+        for (int i = 0; i < 8; i++) f[i] = tile[a][k8 + i] * scale;
+        ns_pair4(f, hi[0], lo[0]);
+        ns_pair4(f + 4, hi[1], lo[1]);
         h16 *o = straight + ns_at(rb + a, cb + k8, CP);
-        gst(o, *reinterpret_cast<u32x4 *>(hi));
-        gst(o + 32, *reinterpret_cast<u32x4 *>(lo));
-        for (int i = 0; i < 8; i++) ns_pair(tile[k8 + i][a] * scale, hi[i], lo[i]);
+        gst(o, u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]});
+        gst(o + kLo, u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]});
+        for (int i = 0; i < 8; i++) f[i] = tile[k8 + i][a] * scale;
+        ns_pair4(f, hi[0], lo[0]);
+        ns_pair4(f + 4, hi[1], lo[1]);
         o = turned + ns_at(cb + a, rb + k8, RP);
-        gst(o, *reinterpret_cast<u32x4 *>(hi));
-        gst(o + 32, *reinterpret_cast<u32x4 *>(lo));
+        gst(o, u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]});
+        gst(o + kLo, u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]});
     }
 }
 
@@ -449,7 +463,7 @@ __device__ __forceinline__ void sub_put(lds_byte *sub, const f32x4 (&acc)[MI][NI
             if constexpr (MODE == NS_SQUARE) {
                 float gg[4];                     // G is symmetric: row j holds the four i together
                 const h16 *p = d.g + ns_at(j0 + j, i0 + i, d.P);
-                const f16x4 hi = gld<f16x4>(p), lo = gld<f16x4>(p + 32);
+                const f16x4 hi = gld<f16x4>(p), lo = gld<f16x4>(p + kLo);
                 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     gg[e] = (float)hi[e] + (float)lo[e];
@@ -490,22 +504,22 @@ __device__ __forceinline__ void sub_out(const lds_byte *sub, int w, const NsDev 
         h16 *straight = MODE == NS_GRAM ? d.g : (MODE == NS_SQUARE ? d.r : d.x);
         h16 *turned = MODE == NS_APPLY ? d.xt[turn ^ 1] : straight;
         const int ks = ns_sym(MODE) ? d.P : d.Q;
-        constexpr int CH = SB / 4;                       // 16-byte chunks of a row
+        // a fragment a step: 16 rows, 32 columns, hi or lo; a lane has 8 columns of row q
+        constexpr int FRAGS = SB / 16 * (SB / 32) * 2;
         #pragma unroll
-        for (int k = w; k < SB * CH / 64; k += NW) {
-            const int j = k * (64 / CH) + lane / CH, c = lane % CH;
-            gst(turned + ns_at(j0 + j, i0, d.P) + c * 8, lld<u32x4>(sub + sub_at(j, c * 16)));
+        for (int k = w; k < FRAGS; k += NW) {
+            const int part = k & 1, j = (k >> 1) / (SB / 32) * 16 + q, i = (k >> 1) % (SB / 32) * 32;
+            gst(turned + ns_at(j0 + j, i0 + i + 8 * g, d.P) + part * kLo, lld<u32x4>(sub + sub_at(j, i * 4 + part * 64 + g * 16)));
         }
         if (!mirror) return;
-        // 16 i x 32 j a step: a lane gets 8 consecutive j of one i
         #pragma unroll
-        for (int k = w; k < SB / 16 * (SB / 32) * 2; k += NW) {
+        for (int k = w; k < FRAGS; k += NW) {
             const int part = k & 1, jb = (k >> 1) % (SB / 32) * 32, i = (k >> 1) / (SB / 32) * 16;
             const int byte = (i >> 5) * 128 + (i & 31) * 2 + part * 64 + 8 * (q % 4), j = jb + 8 * g + q / 4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sub + sub_at(j, byte)));
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(sub + sub_at(j + 4, byte)));
             const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            gst(straight + ns_at(i0 + i + q, j0 + jb + 8 * g, ks) + part * 32, v);
+            gst(straight + ns_at(i0 + i + q, j0 + jb + 8 * g, ks) + part * kLo, v);
         }
     }
 }
@@ -515,15 +529,14 @@ __device__ __forceinline__ void sub_out(const lds_byte *sub, int w, const NsDev 
 // CU, for which a k step's operands are half of the lines per product and its
 // fragment reads three quarters (a tile may hang over the matrix by 128 rows or
 // columns: those rows are read again from inside and not written).  Two LDS
-// stages of 2 BT rows of 128 bytes (one k step of both operands); the 16-byte
-// chunks of a row are stored in the order chunk ^ (row % 8), so the 16 rows of a
-// fragment read lie in different banks.  The next step's lines are loaded
+// stages of BT / 4 fragments (one k step of both operands), each a KiB as it lies
+// in memory, hi and lo of 16 rows in turn.  The next step's fragments are loaded
 // straight into LDS while the current step multiplies.
 template <int BT, int MODE, typename W>
 __global__ __launch_bounds__(BT * 2) void k_ns_product(NsTable t, int count, NsStep s, int turn, NsCut cut)
 {
     constexpr int NT = BT * 2, WN = BT / 64, TM = BT / 2, TN = 64, MI = TM / 16, NI = TN / 16;
-    constexpr int kRow = 128, kStage = 2 * BT * kRow, kLoads = kStage / (NT * 16);
+    constexpr int kStage = BT / 4 * 1024, kLoads = kStage / (NT * 16);
     static_assert(kStage == NT / 128 * kSubBytes, "half of the waves' results fit a stage");
     __shared__ __align__(16) unsigned char lds0[kStage], lds1[kStage];
     int tile, piece = 0, pieces = 1;
@@ -543,35 +556,31 @@ __global__ __launch_bounds__(BT * 2) void k_ns_product(NsTable t, int count, NsS
     const h16 *pb = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.xt[turn]);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
-    // this thread's chunk of load l: row (l NT + tid) / 8 of the stage, position tid % 8
-    const int lrow = tid / 8, lchunk = (tid % 8) ^ (lrow % 8);
+    // fragment of this wave's load l: l (NT / 64) + wave of the stage
     const char *src[kLoads];
     #pragma unroll
     for (int l = 0; l < kLoads; l++) {
-        const int row = l * (NT / 8) + lrow;
-        const int end_a = P - 1, end_b = (ns_sym(MODE) ? P : Q) - 1;
-        const h16 *base = row < BT ? pa + (int64_t)min(ti * BT + row, end_a) * 2 * K
-                                   : pb + (int64_t)min(tj * BT + row - BT, end_b) * 2 * K;
-        src[l] = (const char *)base + lchunk * 16;
+        const int f = l * (NT / 64) + wave, row = f / 2 * 16;
+        const int end_a = P - 16, end_b = (ns_sym(MODE) ? P : Q) - 16;
+        const h16 *base = row < BT ? pa + ns_at(min(ti * BT + row, end_a), 0, K) : pb + ns_at(min(tj * BT + row - BT, end_b), 0, K);
+        src[l] = (const char *)(base + f % 2 * kLo + lane * 8);
     }
     auto load = [&](unsigned char *stage, int step) __attribute__((always_inline)) {
         #pragma unroll
         for (int l = 0; l < kLoads; l++)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(src[l] + (int64_t)step * kRow),
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(src[l] + (int64_t)step * (kStep * 2)),
                                              (__attribute__((address_space(3))) uint32_t *)(stage + (l * NT + wave * 64) * 16),
                                              16, 0, 0);
         __builtin_amdgcn_sched_barrier(0);       // (the scheduler would sink them to the barrier that waits for them)
     };
     const int wm = wave / WN, wn = wave % WN;
-    const int fr = lane % 16, fc = lane / 16;    // fragment row and k chunk of this lane
     f32x4 acc[MI][NI];
     #pragma unroll
     for (int i = 0; i < MI; i++)
         #pragma unroll
         for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     auto frag = [&](const unsigned char *stage, int row, int part) __attribute__((always_inline)) {
-        const int r = row + fr;
-        return *reinterpret_cast<const f16x8 *>(stage + r * kRow + ((part * 4 + fc) ^ (r % 8)) * 16);
+        return *reinterpret_cast<const f16x8 *>(stage + (row / 8 + part) * 1024 + lane * 16);
     };
     auto multiply = [&](const unsigned char *stage) __attribute__((always_inline)) {
         f16x8 ah[MI], al[MI], bh[NI], bl[NI];
@@ -683,20 +692,19 @@ __global__ __launch_bounds__(256, 1) void k_ns_direct(NsTable t, int count, NsSt
     const int K = MODE == NS_GRAM ? d.Q : d.P;
     const h16 *pa = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.r);
     const h16 *pb = MODE == NS_GRAM ? d.x : (MODE == NS_SQUARE ? d.g : d.xt[turn]);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane % 16, fc = lane / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int i0 = pl.ti * BT, j0 = pl.tj * BT;
     const int steps = K / 32, k0 = wave * steps / 4, n = (wave + 1) * steps / 4 - k0;
-    const int64_t block = (int64_t)16 * 2 * K;
-    const h16 *a = pa + (int64_t)(i0 + fr) * 2 * K + k0 * 64 + fc * 8, *b = pb + (int64_t)(j0 + fr) * 2 * K + k0 * 64 + fc * 8;
+    const h16 *a = pa + ns_at(i0, k0 * 32, K) + lane * 8, *b = pb + ns_at(j0, k0 * 32, K) + lane * 8;
     f16x8 f[AHEAD][4 * B];                       // a hi, lo; b hi, lo of B blocks each
     auto load = [&](f16x8 (&o)[4 * B], int k) __attribute__((always_inline)) {
         #pragma unroll
         for (int i = 0; i < B; i++) {
-            const h16 *p = a + i * block + k * 64, *q = b + i * block + k * 64;
+            const h16 *p = a + i * kBlk + (int64_t)k * kStep, *q = b + i * kBlk + (int64_t)k * kStep;
             o[2 * i] = gld<f16x8>(p);
-            o[2 * i + 1] = gld<f16x8>(p + 32);
+            o[2 * i + 1] = gld<f16x8>(p + kLo);
             o[2 * B + 2 * i] = gld<f16x8>(q);
-            o[2 * B + 2 * i + 1] = gld<f16x8>(q + 32);
+            o[2 * B + 2 * i + 1] = gld<f16x8>(q + kLo);
         }
     };
     f32x4 acc[B][B];
