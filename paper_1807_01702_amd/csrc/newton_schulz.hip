@@ -532,8 +532,11 @@ __device__ __forceinline__ void sub_out(const lds_byte *sub, int w, const NsDev 
 // stages of BT / 4 fragments (one k step of both operands), each a KiB as it lies
 // in memory, hi and lo of 16 rows in turn.  The next step's fragments are loaded
 // straight into LDS while the current step multiplies.
+// (For 128-tiles alone on their CUs, reading the next step's fragments from LDS
+// ahead of the products and memory four steps ahead through registers was no
+// faster: 256 tiles of 32 steps 44 us against 41.)
 template <int BT, int MODE, typename W>
-__global__ __launch_bounds__(BT * 2) void k_ns_product(NsTable t, int count, NsStep s, int turn, NsCut cut)
+__global__ __launch_bounds__(BT * 2, 2) void k_ns_product(NsTable t, int count, NsStep s, int turn, NsCut cut)
 {
     constexpr int NT = BT * 2, WN = BT / 64, TM = BT / 2, TN = 64, MI = TM / 16, NI = TN / 16;
     constexpr int kStage = BT / 4 * 1024, kLoads = kStage / (NT * 16);
@@ -582,26 +585,41 @@ __global__ __launch_bounds__(BT * 2) void k_ns_product(NsTable t, int count, NsS
     auto frag = [&](const unsigned char *stage, int row, int part) __attribute__((always_inline)) {
         return *reinterpret_cast<const f16x8 *>(stage + (row / 8 + part) * 1024 + lane * 16);
     };
-    auto multiply = [&](const unsigned char *stage) __attribute__((always_inline)) {
-        f16x8 ah[MI], al[MI], bh[NI], bl[NI];
+    struct Frags { f16x8 ah[MI], al[MI], bh[NI], bl[NI]; };
+    auto read = [&](Frags &f, const unsigned char *stage) __attribute__((always_inline)) {
         #pragma unroll
         for (int i = 0; i < MI; i++) {
-            ah[i] = frag(stage, wm * TM + i * 16, 0);
-            al[i] = frag(stage, wm * TM + i * 16, 1);
+            f.ah[i] = frag(stage, wm * TM + i * 16, 0);
+            f.al[i] = frag(stage, wm * TM + i * 16, 1);
         }
         #pragma unroll
         for (int j = 0; j < NI; j++) {
-            bh[j] = frag(stage, BT + wn * TN + j * 16, 0);
-            bl[j] = frag(stage, BT + wn * TN + j * 16, 1);
+            f.bh[j] = frag(stage, BT + wn * TN + j * 16, 0);
+            f.bl[j] = frag(stage, BT + wn * TN + j * 16, 1);
         }
-        #pragma unroll
-        for (int i = 0; i < MI; i++)
+    };
+    // the three products of a sum are far apart, except where the registers do not
+    // hold all fragments (256-tiles: spills, 140 -> 179 us)
+    auto multiply = [&](const Frags &f) __attribute__((always_inline)) {
+        if constexpr (BT == 128) {
             #pragma unroll
-            for (int j = 0; j < NI; j++) {
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
-            }
+            for (int term = 0; term < 3; term++)
+                #pragma unroll
+                for (int i = 0; i < MI; i++)
+                    #pragma unroll
+                    for (int j = 0; j < NI; j++)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(term == 1 ? f.al[i] : f.ah[i],
+                                                                           term == 0 ? f.bl[j] : f.bh[j], acc[i][j], 0, 0, 0);
+        } else {
+            #pragma unroll
+            for (int i = 0; i < MI; i++)
+                #pragma unroll
+                for (int j = 0; j < NI; j++) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.ah[i], f.bl[j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.al[i], f.bh[j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.ah[i], f.bh[j], acc[i][j], 0, 0, 0);
+                }
+        }
     };
     // steps in pairs (K is a multiple of 64); a piece may have none
     const int pairs = K / 64, k0 = piece * pairs / pieces * 2, k1 = (piece + 1) * pairs / pieces * 2;
@@ -609,11 +627,14 @@ __global__ __launch_bounds__(BT * 2) void k_ns_product(NsTable t, int count, NsS
         load(lds0, k0);
         __syncthreads();
         for (int k = k0; k < k1; k += 2) {
+            Frags f;
             load(lds1, k + 1);
-            multiply(lds0);
+            read(f, lds0);
+            multiply(f);
             __syncthreads();
             if (k + 2 < k1) load(lds0, k + 2);
-            multiply(lds1);
+            read(f, lds1);
+            multiply(f);
             __syncthreads();
         }
     }
@@ -1251,26 +1272,27 @@ constexpr int ns_slots(int bt) { return bt == 128 ? kNsSlots : kNsSlots / 2; }
 int64_t cut_bytes(const NsCut &c) { return c.pieces > 1 ? (int64_t)(c.tiles - c.whole) * c.pieces * c.bt * c.bt * 4 : 0; }
 
 // The time of a stage in us as measured (kernel traces of 256 x 256 to
-// 4096 x 4096, alone and in lists): per round of workgroups a part for finding
-// the matrix, the first loads and leaving the results (16 bytes an element at 26
-// GB/s a CU), and a part per k step, which depends on whether the CU is shared;
-// for cut tiles the launch that adds the pieces (5 us + 0.27 us per MB).
-//   256 x 256 (8 steps): 32-tiles 5.9, 64-tiles 9.1, 128-tiles 14.3, 256-tiles 23.8
-//   512 x 512 (16 steps): 8.2, 13.6, 7.9 + 5.1, 18.5 + 5.6
-//   1024 x 1024 (32 steps): 30.7, 20.9, 12.0 + 6.5, 22.7 + 5.6
-//   4096 x 4096, R X (128 steps): -, 973, 421, 321
+// 4096 x 4096, alone and in lists): the launch, and per round of workgroups a
+// part for finding the matrix, the first loads and leaving the results, and a
+// part per k step, which depends on whether the CUs are shared; for cut tiles the
+// launch that adds the pieces.  Measured, tiles of 32, 64, 128, 256:
+//   256 x 256, X X^T (8 steps)      4.7    6.8   13.3         12.8 + 4.0
+//   512 x 512 (16 steps)            6.0    8.8    8.6 + 4.6   13.3 + 5.2
+//   1024 x 1024 (32 steps)         17.2   12.0   12.1 + 6.4   20.0 + 6.5
+//   four 2048 x 2048, R X (64)      703    380    214          164
 double cut_time(const NsCut &c, int steps)
 {
     const int slots = ns_slots(c.bt), rest = c.tiles - c.whole;
     if (c.bt <= 64) {
         const int rounds = (c.tiles + slots - 1) / slots;
-        return c.bt == 32 ? 4.0 + rounds * steps * (rounds > 1 ? 0.3 : 0.23) : 5.5 + rounds * steps * (rounds > 1 ? 0.6 : 0.45);
+        return c.bt == 32 ? 2.5 + rounds * (1.3 + steps * (rounds > 1 ? 0.15 : 0.09))
+                          : 3.0 + rounds * (2.0 + steps * (rounds > 1 ? 0.31 : 0.19));
     }
-    const double step = c.bt == 128 ? 1.56 : 2.38, alone = c.bt == 128 ? 0.75 : 1.6, leave = c.bt == 128 ? 10.0 : 16.0;
+    const double step = c.bt == 128 ? 1.5 : 2.35, alone = c.bt == 128 ? 0.8 : 2.0, leave = c.bt == 128 ? 9.0 : 14.0;
     const int units = rest * c.pieces;
     double t = 2.0 + c.whole / slots * (leave + step * steps);
     if (units) t += leave + (steps + c.pieces - 1) / c.pieces * (units * 2 <= slots ? alone : step);
-    if (c.pieces > 1) t += 5.0 + cut_bytes(c) * 0.27e-6;
+    if (c.pieces > 1) t += 4.5 + cut_bytes(c) * 0.23e-6;
     return t;
 }
 
@@ -1368,8 +1390,8 @@ hipError_t ns_product_bt(const NsPlan &p, const NsTable &t, const NsStep &s, int
     const int rest = cut.tiles - cut.whole;
     {
         TraceScope tr(KC_CONV, KID_ORTHO, st, 0.0, ns_sym(MODE) ? 0.0 : p.flops);
-        hipLaunchKernelGGL((k_ns_product<BT, MODE, W>), dim3((unsigned)(cut.whole + rest * cut.pieces)), dim3(BT * 2), 0, st,
-                           t, p.count, s, turn, cut);
+        const int units = cut.whole + rest * cut.pieces;
+        hipLaunchKernelGGL((k_ns_product<BT, MODE, W>), dim3((unsigned)units), dim3(BT * 2), 0, st, t, p.count, s, turn, cut);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (cut.pieces == 1) return hipSuccess;
