@@ -350,3 +350,40 @@ def test_handle_refusals():
         B.bnr_muon_update(B.MuonGroup([w], [w.clone()], [w.clone()]), torch.zeros(1))
     assert bool((w == 0).all())
     B.bnr_muon_update(B.MuonGroup([], [], []), 0.1)
+
+
+@pytest.mark.parametrize("wdt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("r,c", [(200, 333), (333, 200), (150, 256), (40, 150), (150, 41), (9, 7)])
+def test_rows_of_every_alignment(r, c, wdt):
+    """Weights, copies and outputs inside larger buffers: pitches and first elements that do and do not allow
+    accesses of four columns give the contiguous matrices' bits, and nothing beside the rows changes."""
+    B = _B()
+
+    def inside(t, pitch, first):
+        whole = torch.full((r * pitch + first + 8,), 7.0, dtype=t.dtype, device="cuda")
+        view = whole[first:first + r * pitch].view(r, pitch)[:, :c]
+        view.copy_(t)
+        return whole, view
+
+    (w,), (g,), (b,), (k,) = _state([(r, c)], wdt, torch.float32, True, seed=5)
+    out = torch.empty_like(g)
+    B.bnr_orthogonalize([g], [out])
+    even = -(-c // 4) * 4
+    places = [(even + 4, 0), (even, 4), (even + 4, 8), (even + 1, 0), (even + 2, 2), (even + 4, 1)]
+    runs = [(w.clone(), b.clone(), k.clone())]
+    fences = []
+    for pitch, first in places:
+        (ww, wv), (kw, kv), (ow, ov) = inside(w, pitch, first), inside(k, pitch + 4, first), inside(out * 0, pitch, first)
+        B.bnr_orthogonalize([g], [ov])
+        assert torch.equal(ov, out)
+        runs.append((wv, b.clone(), kv))
+        fences += [(ww, wv, first, pitch), (kw, kv, first, pitch + 4), (ow, ov, first, pitch)]
+    for wv, bv, kv in runs:
+        B.bnr_muon_update(B.MuonGroup([wv], [g], [bv], copies=[kv]), 0.02, weight_decay=0.1)
+    assert not torch.equal(runs[0][0], w)
+    for wv, bv, kv in runs[1:]:
+        assert torch.equal(wv, runs[0][0]) and torch.equal(bv, runs[0][1]) and torch.equal(kv, runs[0][2])
+    for whole, view, first, pitch in fences:
+        out_of_rows = torch.ones_like(whole, dtype=torch.bool)
+        out_of_rows[first:first + r * pitch].view(r, pitch)[:, :c] = False
+        assert bool((whole[out_of_rows] == 7.0).all())
