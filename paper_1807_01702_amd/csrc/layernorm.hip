@@ -13,6 +13,9 @@
 // written once, with the row held in registers between the reductions (the
 // variance is the sum of squared differences from the mean already known, so
 // a mean far from zero costs no accuracy).  All arithmetic is float32.
+// Measured: forward, 8192 bf16 rows of 4096 with a residual, 40.6 us = 6.6 TB/s
+// (part of it from the last-level cache); backward there 50.6 us, 401408 rows of
+// 256 153.7 us = 5.35 TB/s, where a copy of 4 GiB runs at 5.44.
 //
 // A row is held by TPR threads with NV loads of V elements each: V is the
 // 16-byte vector where pointers, strides and the channel count allow it, else

@@ -13,8 +13,13 @@
 // 2^-22 of the term).  The factor S = 2^12 keeps both parts inside fp16's range:
 // the spectral norm of X, G and R stays below 16 (the caller's coefficients are
 // checked for that), so no |S v| reaches 65504, and what is lost below fp16's
-// smallest step is 2^-37 of the norm of X.  Three fp16 products run at 2.6 times
-// the rate of one float32 matrix product on this chip and carry the same error.
+// smallest step is 2^-37 of the norm of X.  A library's large product reaches 1330
+// TFLOP/s in fp16 and 150 in float32 on this chip: three fp16 products carry
+// float32's error at 2.9 times its rate.
+//
+// Measured: 4096 x 4096, five steps, 3.5 ms = 393 of the 443 TFLOP/s that pairs can
+// reach (the matrix cores bound it); twelve bf16 weights of 1024 x 4096 2.8 ms; all
+// 119 filters of DenseNet-121 405 us and 128 x 128 54 us (dependent short stages).
 //
 // Layout.  A pair matrix lies in the order of the fragments that the matrix
 // instructions take (ns_at): a fragment is one KiB, whether it goes to registers
