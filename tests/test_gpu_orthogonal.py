@@ -387,3 +387,17 @@ def test_rows_of_every_alignment(r, c, wdt):
         out_of_rows = torch.ones_like(whole, dtype=torch.bool)
         out_of_rows[first:first + r * pitch].view(r, pitch)[:, :c] = False
         assert bool((whole[out_of_rows] == 7.0).all())
+
+
+def test_one_input_for_several_outputs():
+    """The same matrix, and the same gradient, twice in a list: they are only read."""
+    B = _B()
+    for r, c in ((40, 60), (90, 700), (200, 300)):
+        x = _rand(7, r, c).float().cuda()
+        keep, outs = x.clone(), [torch.empty_like(x) for _ in range(3)]
+        B.bnr_orthogonalize([x, x, x], outs)
+        _close("%dx%d" % (r, c), outs[0], _ns64(_d(x)), torch.float32)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2]) and torch.equal(x, keep)
+        w = [torch.ones_like(x) for _ in range(2)]
+        B.bnr_muon_update(B.MuonGroup(w, [x, x], [torch.zeros_like(x) for _ in range(2)]), 0.1)
+        assert torch.equal(w[0], w[1]) and torch.equal(x, keep) and not torch.equal(w[0], torch.ones_like(x))
