@@ -85,12 +85,16 @@ __host__ __device__ constexpr int ns_gram_stage(int bt)
     return bt == 32 ? PRE_GRAM_T : (bt == 64 ? PRE_GRAM_S : (bt == 128 ? PRE_GRAM : PRE_GRAM_L));
 }
 constexpr int kMaxParts = 1024;    // partial sums of squares of a matrix
-constexpr int kNarrow = 128;       // short sides up to this take the narrow path
+// short sides up to this take the narrow path (128 x 4096 104 us, sixteen of 128 x
+// 1024 127; the wide path's 136 x 4096 157, sixteen of 136 x 1024 202)
+constexpr int kNarrow = 128;
 constexpr int kBlock = 16384;      // values of a narrow matrix's block: [kBlock / P][P]
-// Values of one narrow matrix's partial Gram matrices up to which every block
-// adds them itself; past it a launch of its own adds them once.
-constexpr int kSumValues = 2 * 128 * 128;
-__host__ __device__ inline bool ns_summed(int blocks, int P) { return blocks * (int64_t)(P * P) > kSumValues; }
+// Blocks of one narrow matrix up to which every block adds the partial Gram
+// matrices itself; past it a launch of its own adds them once (five steps, own
+// additions against launches: 128 x 512, 4 blocks, 94 us against 97, sixteen of
+// them 96 against 112; 128 x 1024, 8 blocks, 108 against 99; 64 x 2048, 8
+// blocks, 71 against 81; 32 x 8192, 16 blocks, 68 against 73).
+__host__ __device__ inline bool ns_summed(int blocks, int P) { return blocks > (P == 128 ? 4 : (P == 64 ? 8 : 32)); }
 
 // whole: a matrix of a single block runs as a launch of its own over all steps.
 __host__ __device__ inline NsSize ns_size(int rows, int cols, int whole)
@@ -1158,6 +1162,7 @@ __device__ __forceinline__ void nw_step(const NsDev &d, int block, const NsStep 
     nw_zero(raw);
     if (has) {
         const float *from = part + (wave * MI * NI * 64 + lane) * 4;
+        #pragma unroll (P == 128 ? 1 : 4)        // (a tile of 128's G is 32 registers: 98 us against 94 unrolled)
         for (int b = 0; b < np; b++)
             #pragma unroll
             for (int i = 0; i < MI; i++)

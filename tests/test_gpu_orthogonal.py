@@ -401,3 +401,18 @@ def test_one_input_for_several_outputs():
         w = [torch.ones_like(x) for _ in range(2)]
         B.bnr_muon_update(B.MuonGroup(w, [x, x], [torch.zeros_like(x) for _ in range(2)]), 0.1)
         assert torch.equal(w[0], w[1]) and torch.equal(x, keep) and not torch.equal(w[0], torch.ones_like(x))
+
+
+@pytest.mark.parametrize("r,c", [(128, 512), (128, 513), (64, 2048), (2049, 64), (32, 16384), (20, 16385), (32, 2047)])
+def test_narrow_blocks_around_the_sum(r, c):
+    """Short sides whose blocks add the partial Gram matrices themselves, up to the largest number, and one more."""
+    B = _B()
+    x = _rand(11, r, c).float().cuda()
+    out = torch.empty_like(x)
+    B.bnr_orthogonalize(x, out)
+    _close("alone", out, _ns64(_d(x)), torch.float32)
+    y = _rand(12, 16, 24).float().cuda()
+    outs = [torch.empty_like(x), torch.empty_like(y)]
+    B.bnr_orthogonalize([x, y], outs)
+    assert torch.equal(outs[0], out)
+    _close("beside", outs[1], _ns64(_d(y)), torch.float32)
