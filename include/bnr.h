@@ -604,9 +604,13 @@ bnr_status bnr_reference_bn_relu(int32_t backward, int64_t m, int32_t c, bnr_dty
  * c up to 16384, any stride >= c and element-aligned pointers (16-byte aligned
  * views and parameters whose c and strides are multiples of the 16-byte vector
  * are faster);
- * different channel slices of one buffer do not overlap each other.  A row of
- * one repeated value has rstd = 1/sqrt(eps) and y = beta; an infinity or NaN
- * makes its own row NaN and no other. */
+ * different channel slices of one buffer do not overlap each other.  The forward
+ * takes differences from the row's mean before it is rounded: a row of one
+ * repeated value has rstd = 1/sqrt(eps) and y = beta, and an offset costs a
+ * small spread no accuracy.  The mean is stored rounded to float32, and the
+ * backward's xhat carries that rounding (2^-24 |mean| rstd).  An infinity or NaN
+ * makes its own row NaN and no other; differences whose squares add up to more
+ * than float32 holds (3.4e38) give rstd = 0. */
 typedef struct {
     const float *gamma;    /* [c] scale, or NULL (1)                               */
     const float *beta;     /* [c] shift, or NULL (0); not read by the backward     */

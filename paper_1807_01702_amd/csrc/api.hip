@@ -1740,7 +1740,7 @@ bnr_status bnr_layernorm_fwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
         if (array_in_rows(g, c, y, y_ldc, m, c, es) || array_in_rows(g, c, sum, sum_ldc, m, c, es))
             return fail(BNR_ERR_ALIAS, "y / sum overlap ln.gamma / ln.beta");
     LnParams p{};
-    p.m = m; p.c = c; p.eps = ln->eps;
+    p.m = m; p.c = c; p.inv_c = 1.0 / c; p.eps = ln->eps;
     p.x = x; p.x_ldc = x_ldc;
     p.res = res; p.res_ldc = res_ldc;
     p.sum = sum; p.sum_ldc = sum_ldc;
@@ -1802,7 +1802,7 @@ bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
     const bool sums = dgamma || dbeta;
     if (sums) TRY(check_ws(ws, ws_bytes, bnr_layernorm_workspace_size(m, c, dtype)));
     LnParams p{};
-    p.m = m; p.c = c;
+    p.m = m; p.c = c; p.inv_c = 1.0 / c;
     p.x = x; p.x_ldc = x_ldc;
     p.res = dsum; p.res_ldc = dsum_ldc;
     p.dy = dy; p.dy_ldc = dy_ldc;

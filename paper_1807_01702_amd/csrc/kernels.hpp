@@ -277,6 +277,7 @@ struct LnParams {
     int64_t m;
     int c;
     float eps;                    // forward
+    double inv_c;                 // 1 / c
     const void *x;                // [m][c] view: forward input; backward: what the forward normalised
     int64_t x_ldc;
     const void *res;              // forward: added to x (NULL: none); backward: added to dx (NULL: none)

@@ -157,6 +157,64 @@ def test_forward_offsets_and_flat_rows():
     assert bool((y[0] == beta.bfloat16()).all())
 
 
+@pytest.mark.parametrize("c", [1, 7, 96, 201, 1001, 1024, 1536, 4096, 9000, 16384])
+def test_forward_rows_of_one_value(c):
+    """A row of one repeated value, whatever it is: the mean is the value, no difference is left, rstd is 1/sqrt(eps)
+    (two roundings: the root and the quotient) and y is beta, bit for bit; with and without a residual addition."""
+    B = _B()
+    vals = [3.7, 1000.1, 12345.678, 1e5, 1000000.1, -1e30, 3.4e38, 1e-30, 1e-40, 0.1, -0.0]
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.tensor([torch.tensor(v).to(dtype).float().item() for v in vals]).to(dtype)[:, None].repeat(1, c).cuda()
+        gamma, beta = _rand(40, c, mean=1.0).float().cuda(), _rand(41, c).float().cuda()
+        res = torch.full_like(x, 0.3)
+        for r, s in ((None, None), (res, torch.empty_like(x))):
+            ln, y = B.LN(gamma, beta, len(vals), EPS), torch.empty_like(x)
+            B.bnr_layernorm_fwd(x, ln, y, res=r, sum=s)
+            flat = x if r is None else s
+            fin = torch.isfinite(flat[:, 0])             # 3.4e38 is past bf16's largest value: an infinity there
+            assert int(fin.sum()) == len(vals) - (dtype == torch.bfloat16) and bool(torch.isnan(y[~fin]).all())
+            assert torch.equal(y[fin], beta.to(dtype).expand_as(y)[fin]), (dtype, r is None)
+            assert torch.equal(ln.mean[fin], flat[fin, 0].float()), (dtype, r is None)
+            want = 1.0 / np.sqrt(np.float64(np.float32(EPS)))
+            assert float((ln.rstd[fin].double() / want - 1).abs().max()) <= 2 * 2 * U
+
+
+@pytest.mark.parametrize("m,c", [(5, 96), (4, 1001), (3, 1536), (2, 4096), (2, 9000)])
+@pytest.mark.parametrize("offset,spread", [(1e4, 1.0), (1e6, 0.5), (-3e5, 0.1), (1e7, 2.0)])
+def test_forward_small_spread_on_a_large_offset(offset, spread, m, c):
+    """Differences from the mean keep their own precision.  A stored value less the mean's first part is exact where
+    the two are within a factor of two of each other and is rounded to 2^-24 of itself elsewhere; taking off the second
+    part rounds once, and that part, at most 2^-24 of the mean, is itself off by 2^-24.  So a difference is off by 2 U
+    of itself and 2 U^2 of the mean; the variance and y follow as in the general bound."""
+    B = _B()
+    x = (_rand(50 + c, m, c, std=spread) + offset).float().cuda()
+    gamma, beta = _rand(51, c, mean=1.0, std=0.3).float().cuda(), _rand(52, c).float().cuda()
+    ln, y = B.LN(gamma, beta, m, EPS), torch.empty_like(x)
+    B.bnr_layernorm_fwd(x, ln, y)
+    s = _d(x)
+    mean = s.mean(1, keepdim=True)
+    d = s - mean
+    rstd = 1.0 / torch.sqrt((d * d).mean(1, keepdim=True) + EPS)
+    want = _d(gamma) * d * rstd + _d(beta)
+    dm = 2 * U * U * mean.abs()
+    rel = 0.5 * ((K + 4) * U + (dm * rstd) ** 2) + 4 * U
+    _check("mean", ln.mean, mean[:, 0], U * mean[:, 0].abs())
+    _check("rstd", ln.rstd, rstd[:, 0], (rel * rstd)[:, 0])
+    _check("y", y, want, _d(gamma).abs() * rstd * (dm + d.abs() * (rel + 6 * U)) + 4 * U * (want.abs() + _d(beta).abs()))
+
+
+def test_forward_finite_rows_whose_sum_passes_float32():
+    """The row sum has room for any finite values; an infinity alone makes the mean infinite."""
+    B = _B()
+    x = torch.full((3, 100), 3e38, device="cuda")
+    x[0, ::2] = -3e38
+    x[2, 5] = float("inf")
+    ln, y = B.LN(None, None, 3, EPS, device="cuda"), torch.empty_like(x)
+    B.bnr_layernorm_fwd(x, ln, y)
+    assert float(ln.mean[0]) == 0.0 and float(ln.mean[1]) == float(x[1, 0]) and float(ln.mean[2]) == float("inf")
+    assert bool((y[1] == 0).all()) and bool(torch.isnan(y[2]).all())
+
+
 @pytest.mark.parametrize("m,c", [(6, 48), (5, 1001), (4, 1024), (3, 9000)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_non_finite_values_stay_in_their_row(m, c, dtype):
