@@ -727,6 +727,13 @@ def _f32_array(t, n, name):
     return t.data_ptr()
 
 
+def _int32(v, name):
+    # ctypes would drop the upper bits of a larger number
+    if not -0x80000000 <= v <= 0x7fffffff:
+        raise ValueError("%s: %d does not fit 32 bits" % (name, v))
+    return v
+
+
 def _rows(t, m, c, dtype, name):
     """(data pointer, row stride) of a view of m rows; (None, 0) without one."""
     if t is None:
@@ -739,7 +746,8 @@ def _rows(t, m, c, dtype, name):
         p, tm, tc, ld = view(t)
     if tm != m or tc != c or t.dtype != dtype:
         raise ValueError("%s: [%d, %d] rows of %s are wanted, got [%d, %d] of %s" % (name, m, c, dtype, tm, tc, t.dtype))
-    return p, ld if m > 1 else c
+    _int32(c, name)
+    return p, _int32(ld, name) if m > 1 else c
 
 
 class LN:
@@ -797,7 +805,8 @@ def _matrix(t, shape, dtype, name):
     p, r, c, ld = view(t)
     if (r, c) != shape or t.dtype != dtype:
         raise ValueError("%s: [%d, %d] of %s is wanted, got [%d, %d] of %s" % (name, *shape, dtype, r, c, t.dtype))
-    return p, ld if r > 1 else c
+    _int32(r, name), _int32(c, name)
+    return p, _int32(ld, name) if r > 1 else c
 
 
 def bnr_orthogonalize(xs, outs, steps=5, coef=NS_COEF, eps=1e-7):
@@ -809,10 +818,11 @@ def bnr_orthogonalize(xs, outs, steps=5, coef=NS_COEF, eps=1e-7):
         return
     items = (OrthoItem * len(xs))()
     for it, x, o in zip(items, xs, outs):
-        _, it.rows, it.cols, _ = view(x)
-        it.x, it.x_ld = _matrix(x, (it.rows, it.cols), xs[0].dtype, "matrix")
-        it.out, it.out_ld = _matrix(o, (it.rows, it.cols), outs[0].dtype, "output")
-    ns, index = NSParams(steps, *coef, eps), _device_of(*xs, *outs)
+        _, r, c, _ = view(x)
+        it.x, it.x_ld = _matrix(x, (r, c), xs[0].dtype, "matrix")
+        it.out, it.out_ld = _matrix(o, (r, c), outs[0].dtype, "output")
+        it.rows, it.cols = r, c
+    ns, index = NSParams(_int32(steps, "steps"), *coef, eps), _device_of(*xs, *outs)
     nbytes = _lib_fns["bnr_orthogonalize_workspace_size"](items, len(xs))
     ws = _scratch(nbytes, xs[0].device)
     _run_on(index, _lib_fns["bnr_orthogonalize"], items, len(xs), dtype_code(xs[0]), dtype_code(outs[0]),
@@ -833,8 +843,8 @@ class MuonGroup:
         self.count, self.items = n, (MuonItem * max(n, 1))()
         for i, it in enumerate(self.items[:n]):
             _, r, c, _ = view(ws[i])
-            it.rows, it.cols = r, c
             it.w, it.w_ld = _matrix(ws[i], (r, c), ws[0].dtype, "weight")
+            it.rows, it.cols = r, c
             it.g, it.g_ld = _matrix(gs[i], (r, c), gs[0].dtype, "gradient")
             it.buf, it.buf_ld = _matrix(bs[i], (r, c), torch.float32, "momentum")
             if cs is not None:
@@ -851,7 +861,7 @@ def bnr_muon_update(group, lr, momentum=0.95, nesterov=True, weight_decay=0.0, s
     is read when the step runs (a captured step follows it)."""
     if not group.count:
         return
-    p = MuonParams(0.0, None, momentum, 1 if nesterov else 0, weight_decay, NSParams(steps, *coef, eps))
+    p = MuonParams(0.0, None, momentum, 1 if nesterov else 0, weight_decay, NSParams(_int32(steps, "steps"), *coef, eps))
     device = group.tensors[0][0].device
     if isinstance(lr, torch.Tensor):
         if lr.device != device:

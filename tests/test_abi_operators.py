@@ -220,3 +220,28 @@ def test_binding_refuses_host_tensors_and_wrong_shapes(B):
         B.bnr_orthogonalize([x], [])
     with pytest.raises(ValueError, match="wanted"):
         B.bnr_orthogonalize([x, x.bfloat16()], [y, y])
+
+
+def test_binding_refuses_sizes_past_32_bits(B):
+    """Row strides, channels, rows and step counts that the C call's 32-bit arguments cannot hold: every one of these
+    would otherwise pass for the small number that its low bits make."""
+    import torch
+    big = 1 << 32
+    meta = lambda shape, stride, dt=torch.float32: torch.empty_strided(shape, stride, dtype=dt, device="meta")  # noqa: E731
+    ln = lambda m: B.LN(None, None, m, device="meta")  # noqa: E731
+    x, y = meta((2, 8), (8, 1)), meta((2, 8), (8, 1))
+    far = meta((2, 8), (big + 8, 1))
+    wide = meta((1, big + 8), (big + 8, 1))
+    tall = meta((big + 5, 2), (2, 1))
+    for call in (lambda: B.bnr_layernorm_fwd(far, ln(2), y), lambda: B.bnr_layernorm_fwd(x, ln(2), far),
+                 lambda: B.bnr_layernorm_fwd(x, ln(2), y, res=far, sum=y), lambda: B.bnr_layernorm_fwd(wide, ln(1), wide),
+                 lambda: B.bnr_layernorm_bwd(x, far, ln(2), y), lambda: B.bnr_layernorm_bwd(far, x, ln(2), y),
+                 lambda: B.bnr_layernorm_bwd(x, x, ln(2), y, dsum=far), lambda: B.bnr_layernorm_bwd(wide, wide, ln(1), wide),
+                 lambda: B.bnr_orthogonalize(far, y), lambda: B.bnr_orthogonalize(x, far),
+                 lambda: B.bnr_orthogonalize(tall, tall), lambda: B.bnr_orthogonalize(wide, wide),
+                 lambda: B.bnr_orthogonalize(x, y, steps=big + 5),
+                 lambda: B.MuonGroup([far], [x], [y]), lambda: B.MuonGroup([x], [far], [y]), lambda: B.MuonGroup([x], [y], [far]),
+                 lambda: B.MuonGroup([x], [x], [y], copies=[meta((2, 8), (big + 8, 1), torch.bfloat16)]),
+                 lambda: B.MuonGroup([tall], [tall], [tall])):
+        with pytest.raises(ValueError, match="does not fit 32 bits"):
+            call()
