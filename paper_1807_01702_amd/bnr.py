@@ -831,8 +831,9 @@ def bnr_orthogonalize(xs, outs, steps=5, coef=NS_COEF, eps=1e-7):
 
 class MuonGroup:
     """The weight matrices that one bnr_muon_update call updates, with their gradients, momentum buffers (float32),
-    and optionally bf16 copies and step factors (default: sqrt(max(1, outputs / inputs)) for [inputs, outputs]).
-    Leading dimensions collapse to rows.  The group holds the tensors; their values are read at every update."""
+    and optionally bf16 copies (an entry may be None) and step factors (default: sqrt(max(1, outputs / inputs)) for
+    [inputs, outputs]).  Leading dimensions collapse to rows.  The group holds the tensors; their values are read at
+    every update."""
 
     def __init__(self, weights, grads, bufs, copies=None, scales=None):
         self.tensors = (list(weights), list(grads), list(bufs), list(copies) if copies is not None else None)
@@ -847,7 +848,7 @@ class MuonGroup:
             it.rows, it.cols = r, c
             it.g, it.g_ld = _matrix(gs[i], (r, c), gs[0].dtype, "gradient")
             it.buf, it.buf_ld = _matrix(bs[i], (r, c), torch.float32, "momentum")
-            if cs is not None:
+            if cs is not None and cs[i] is not None:
                 it.copy, it.copy_ld = _matrix(cs[i], (r, c), torch.bfloat16, "copy")
             it.scale = max(1.0, c / r) ** 0.5 if scales is None else scales[i]
         if n:

@@ -416,3 +416,15 @@ def test_narrow_blocks_around_the_sum(r, c):
     B.bnr_orthogonalize([x, y], outs)
     assert torch.equal(outs[0], out)
     _close("beside", outs[1], _ns64(_d(y)), torch.float32)
+
+
+def test_copies_of_some_matrices():
+    """A list where only some matrices have a bf16 copy: the others' results are those of a list without copies."""
+    B = _B()
+    shapes = [(40, 60), (300, 200), (9, 7), (128, 600)]
+    ws, gs, bs, cs = _state(shapes, torch.float32, torch.float32, True)
+    plain = [w.clone() for w in ws], [b.clone() for b in bs]
+    B.bnr_muon_update(B.MuonGroup(plain[0], gs, plain[1]), 0.02)
+    B.bnr_muon_update(B.MuonGroup(ws, gs, bs, copies=[cs[0], None, None, cs[3]]), 0.02)
+    assert all(torch.equal(a, b) for a, b in zip(ws + bs, plain[0] + plain[1]))
+    assert torch.equal(cs[0], ws[0].bfloat16()) and torch.equal(cs[3], ws[3].bfloat16())
