@@ -208,8 +208,8 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
 // Backward: workgroup b takes row sets b, b + grid, ...; each thread keeps the
 // sums of dy and dy xhat of its own channels in registers over all its rows
 // and the workgroup writes one partial row [2][c] at the end (float32 sums of
-// at most m / (grid GR) terms; k_ln_combine adds the partial rows in float64 in
-// a fixed order).  The next row set is loaded before the current one reduces,
+// at most kLnChain terms; k_ln_combine adds the partial rows in float64 in a
+// fixed order).  The next row set is loaded before the current one reduces,
 // and gamma stays in registers, except in the widest rows (512 threads, up to 32
 // channels each), which do not hold both beside the sums (1024 threads of 16
 // channels and 128 registers spilled more): those read gamma again, and load
@@ -446,13 +446,17 @@ hipError_t ln_dispatch(const LnPlan &q, int dtype, F &&go)
 
 // Partial rows (= workgroups) of the backward: enough workgroups to fill the
 // chip, few enough that writing and adding the partial rows stays small next
-// to the data (c = 4096: 512 rows are 16 MiB).
+// to the data (c = 4096: 512 rows are 16 MiB), and so many that no thread adds
+// more than kLnChain rows in float32 (the partial rows are then at most 1/64 of
+// the data).
 int64_t ln_bwd_groups(int dtype, int64_t m, int c, bool vec)
 {
     const LnPlan q = ln_bwd_plan(dtype, c, vec);
     const int64_t sets = ceil_div(m, q.wg / q.tpr);
     const int64_t most = q.wg == 256 ? 1024 : (q.tpr == 256 ? 512 : 256);
-    return sets < most ? sets : most;
+    const int64_t enough = ceil_div(sets, kLnChain) > most ? ceil_div(sets, kLnChain) : most;
+    const int64_t groups = sets < enough ? sets : enough;
+    return groups < kLnMaxGrid ? groups : kLnMaxGrid;
 }
 
 hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s)

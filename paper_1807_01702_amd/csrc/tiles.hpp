@@ -219,6 +219,7 @@ inline WgTrPlan wgrad_f32_plan(int64_t m, int n, int h, int w, int c_in, int c_o
 
 // ---- layer normalisation ---------------------------------------------------
 constexpr int64_t kLnMaxGrid = 1 << 21;     // workgroups of up to 1024 threads (a grid holds fewer than 2^32)
+constexpr int kLnChain = 256;               // rows that a thread of the backward adds one after another
 constexpr int kLnMaxC = 16384;             // 16 channels a thread of a 1024-thread workgroup
 
 // ---- Newton-Schulz orthogonalisation ---------------------------------------

@@ -438,3 +438,24 @@ def test_more_rows_than_a_grid_holds():
         z, l2 = torch.empty_like(x[part]), B.LN(None, None, 1000, EPS, device="cuda")
         B.bnr_layernorm_fwd(x[part], l2, z)
         assert torch.equal(y[part], z) and torch.equal(ln.mean[part], l2.mean) and torch.equal(ln.rstd[part], l2.rstd)
+
+
+def test_backward_sums_over_very_many_rows():
+    """dbeta of 2^27 rows of one gradient value: 1 + 2^-13 - 2^-20 loses 2^-13 at every addition to a float32 sum
+    between 2^11 and 2^12, so one chain of 4096 rows a thread is 6e-5 off; a thread adds at most 256 rows and a
+    workgroup its 32 row groups in float32, and those sums are added in float64."""
+    B = _B()
+    m, c = 1 << 27, 8
+    v = 1.0 + 2.0 ** -13 - 2.0 ** -20
+    x = torch.empty(m, c, device="cuda")
+    x.normal_(generator=torch.Generator(device="cuda").manual_seed(2))
+    dy = torch.full_like(x, v)
+    ln, dx = B.LN(None, None, m, EPS, device="cuda"), torch.empty_like(x)
+    B.bnr_layernorm_fwd(x, ln, dx)
+    dgamma, dbeta = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    B.bnr_layernorm_bwd(dy, x, ln, dx, dgamma, dbeta)
+    n = 256 + 32 + 1                                     # additions in float32, and the result's rounding
+    assert float((dbeta.double() / (v * m) - 1).abs().max()) <= n * U
+    xhat = (x - ln.mean[:, None]) * ln.rstd[:, None]     # (its two roundings each add U of a term)
+    want, size = (xhat.double() * v).sum(0), xhat.abs().double().sum(0) * v
+    assert bool(((dgamma.double() - want).abs() <= (n + 4) * U * size).all())
