@@ -428,3 +428,137 @@ def test_copies_of_some_matrices():
     B.bnr_muon_update(B.MuonGroup(ws, gs, bs, copies=[cs[0], None, None, cs[3]]), 0.02)
     assert all(torch.equal(a, b) for a, b in zip(ws + bs, plain[0] + plain[1]))
     assert torch.equal(cs[0], ws[0].bfloat16()) and torch.equal(cs[3], ws[3].bfloat16())
+
+
+# Further choices of the tile rule for X X^T, its square and R X, so that every kernel and every way to cut is run:
+# tiles of 256 whole for all three (twelve of 1296 x 1489), R X in pieces only, of 128-tiles (1680 x 1256) and of
+# 256-tiles (2360 x 2160).
+@pytest.mark.parametrize("shapes", [[(1296, 1489)] * 12, [(1680, 1256)], [(2360, 2160)]], ids=lambda s: "%dx%dx%d" % (len(s), *s[0]))
+def test_whole_and_cut_large_tiles(shapes):
+    test_large_lists(shapes)
+
+
+# (shapes, how R X, whose last one leaves the result, is tiled)
+RESULTS = [([(1023, 4093)], "128 whole, ragged"), ([(4093, 1023)], "128 whole, turned"), ([(1680, 1256)], "128 in pieces"),
+           ([(2360, 2160)], "256 in pieces"), ([(1300, 2900)] * 3, "256 whole, ragged"), ([(1024, 4096)] * 6, "256, some in pieces"),
+           ([(3000, 2990)], "128, some in pieces"), ([(1000, 999)], "64"), ([(513, 300), (700, 260)], "32")]
+
+
+@pytest.mark.parametrize("shapes,how", RESULTS, ids=[h.replace(" ", "-") for _, h in RESULTS])
+def test_results_of_every_tile(shapes, how):
+    """bf16 results, and weight steps with float32 weights and bf16 copies and with bf16 weights, from every kernel
+    that leaves results.  The reference runs on the GPU in float64; longer sums as in test_large_lists."""
+    B = _B()
+    rel = REL * max(1.0, (max(max(s) for s in shapes) / 2048) ** 0.5)
+    xs = [_rand(i * 17 + r, r, c).bfloat16().cuda() for i, (r, c) in enumerate(shapes)]
+    outs = [torch.full_like(x, 5.0) for x in xs]
+    B.bnr_orthogonalize(xs, outs)
+    for x, o in zip(xs, outs):
+        ref = _ns64(x.double())
+        assert float((o.double() - ref).norm()) <= (rel + HALF[torch.bfloat16]) * float(ref.norm())
+    lr, mom, wd = 0.125, 0.5, 0.25
+    for wdt, gdt in ((torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)):
+        ws, gs, bs, cs = _state(shapes, wdt, gdt, True, seed=3)
+        before = [(w.double(), g.double(), b.double()) for w, g, b in zip(ws, gs, bs)]
+        scales = [0.5 + i for i in range(len(shapes))]
+        B.bnr_muon_update(B.MuonGroup(ws, gs, bs, copies=cs, scales=scales), lr, momentum=mom, weight_decay=wd)
+        for i, (w0, g0, b0) in enumerate(before):
+            w, b, step = _update64(w0, g0, b0, lr, mom, True, wd, scales[i])
+            u = 2.0 ** -24
+            assert bool(((bs[i].double() - b).abs() <= u * (b.abs() + (mom * b0).abs() + g0.abs())).all()), i
+            tol = rel * float(step.norm()) + 4 * u * float(w0.norm() + step.norm()) + HALF[wdt] * float(w.norm())
+            assert float((ws[i].double() - w).norm()) <= tol, (wdt, i)
+            assert torch.equal(cs[i], ws[i].bfloat16())
+
+
+@pytest.mark.parametrize("shapes", [[(200, 300), (129, 200), (300, 140), (513, 130), (150, 257)], [(1000, 999)] * 5,
+                                    [(1023, 4093), (1500, 700), (640, 1300), (900, 2000), (1100, 1030)],
+                                    [(1296, 1489)] * 12, [(2360, 2160)] * 5], ids=lambda s: "%dx%dx%d" % (len(s), *s[0]))
+def test_wide_zero_and_non_finite_matrices_of_a_list(shapes):
+    """As test_zero_and_non_finite_matrices_of_a_list for short sides past 128, where a tile that hangs over a matrix
+    reads its last rows again: a zero matrix gives zeros, a NaN in the last element and an infinity in the first make
+    their own matrices NaN, and every other matrix keeps its bits."""
+    B = _B()
+    xs = [_rand(i, *s).float().cuda() for i, s in enumerate(shapes)]
+    clean = [torch.empty_like(x) for x in xs]
+    B.bnr_orthogonalize(xs, clean)
+    xs[1] = torch.zeros_like(xs[1])
+    xs[2][-1, -1] = float("nan")
+    xs[3][0, 0] = float("-inf")
+    outs = [torch.full_like(x, 5.0) for x in xs]
+    B.bnr_orthogonalize(xs, outs)
+    assert bool((outs[1] == 0).all())
+    assert bool(torch.isnan(outs[2]).all()) and bool(torch.isnan(outs[3]).all())
+    for i in [0] + list(range(4, len(shapes))):
+        assert torch.equal(outs[i], clean[i]), i
+
+
+@pytest.mark.parametrize("r,c", [(200, 300), (1000, 999), (1023, 4093), (2360, 2160), (100, 3000)])
+def test_wide_scales_of_the_input(r, c):
+    """Powers of two in front of the matrix leave the bits as they are."""
+    B = _B()
+    x = _rand(7, r, c).float().cuda()
+    ref, out = torch.empty_like(x), torch.empty_like(x)
+    B.bnr_orthogonalize(x, ref, eps=0.0)
+    for k in (-90, -30, 60):
+        B.bnr_orthogonalize(x * 2.0 ** k, out, eps=0.0)
+        assert torch.equal(out, ref), k
+
+
+def _kinds(r, c, seed):
+    """Matrices whose singular values are far apart (float32, on the GPU)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    u = n(r, c)
+    yield "direction 30", u + 30 * n(r, 1) @ n(1, c)
+    yield "direction 1e4", u + 1e4 * n(r, 1) @ n(1, c)
+    yield "rows of 1 to 1e-4", u * 1e-4 ** torch.rand(r, 1, generator=g, device="cuda")
+    yield "rank 4", n(r, 4) @ n(4, c) + 1e-3 * u
+    p = min(r, c)
+    left, right = torch.linalg.qr(n(r, p))[0], torch.linalg.qr(n(c, p))[0]
+    yield "decay over five decades", (left * torch.logspace(0, -5, p, device="cuda")) @ right.t()
+
+
+@pytest.mark.parametrize("r,c", [(60, 90), (64, 576), (1152, 128), (300, 400), (512, 1024), (1023, 2047)])
+def test_matrices_of_low_effective_rank(r, c):
+    """A few directions hold almost all of the norm, so errors made beside them grow with the weak directions.  Step k
+    adds an error of at most (|a| + 2 |b| + 3 |c|) e ||X_k||_F (head of this file, e = 2^-21), and no later step
+    stretches a difference by more than its largest slope, p'(0) = a."""
+    B = _B()
+    a, b, cc = COEF
+    for name, u in _kinds(r, c, r + c):
+        out = torch.empty_like(u)
+        B.bnr_orthogonalize(u, out)
+        ud, tol = u.double(), 0.0
+        for k in range(5):
+            tol += (a - 2 * b + 3 * cc) * 2.0 ** -21 * float(_ns64(ud, k).norm()) * a ** (4 - k)
+        ref = _ns64(ud)
+        assert float((out.double() - ref).norm()) <= tol + HALF[torch.float32] * float(ref.norm()), name
+
+
+@pytest.mark.parametrize("r,c", [(40, 60), (100, 900), (900, 100), (300, 400), (700, 300)])
+def test_offsets_past_32_bits(r, c):
+    """Rows so far apart that the last ones start past 2^31 elements, for every argument, and 4 columns beside every
+    row: the contiguous matrices' bits, and nothing beside the rows changes."""
+    B = _B()
+    ld = -(-(1 << 31) // (r - 8)) // 8 * 8 + 8
+    n = (r - 1) * ld + c + 8
+    far = lambda dt: torch.as_strided(torch.empty(n, dtype=dt, device="cuda"), (r, c + 4), (ld, 1))  # noqa: E731
+
+    def put(t):
+        v = far(t.dtype)
+        v[:, :c] = t
+        v[:, c:] = 7.0
+        return v
+
+    assert (r - 1) * ld > 1 << 31
+    (w,), (g,), (b,), (k,) = _state([(r, c)], torch.float32, torch.float32, True, seed=9)
+    fw, fg, fb, fk = put(w), put(g), put(b), put(k)
+    B.bnr_muon_update(B.MuonGroup([fw[:, :c]], [fg[:, :c]], [fb[:, :c]], copies=[fk[:, :c]]), 0.02, weight_decay=0.1)
+    B.bnr_muon_update(B.MuonGroup([w], [g], [b], copies=[k]), 0.02, weight_decay=0.1)
+    for f, t in ((fw, w), (fg, g), (fb, b), (fk, k)):
+        assert torch.equal(f[:, :c], t) and bool((f[:, c:] == 7.0).all())
+    out = torch.empty_like(g)
+    B.bnr_orthogonalize(g, out)
+    B.bnr_orthogonalize(fg[:, :c], fw[:, :c])
+    assert torch.equal(fw[:, :c], out) and bool((fw[:, c:] == 7.0).all())

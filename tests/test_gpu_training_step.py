@@ -178,3 +178,24 @@ def test_captured_training_step_with_update():
         torch.cuda.synchronize()
         for a, b in zip(oe.weights + oe.bufs + [eager.pooled], oc.weights + oc.bufs + [cap.pooled]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_forward_and_backward_take_the_updated_filters(bf16):
+    """After an update a driver computes what a new driver given the updated filters computes, bit for bit: nothing of
+    the old filters is kept."""
+    from paper_1807_01702_amd import workloads as W
+    d = synth.dense_block(seed=6, n=2, h=16, w=16, bf16=bf16)
+    wl, new = W.DenseBlock(d), W.DenseBlock(d)
+    wl.step()
+    opt = W.FilterUpdate(wl)
+    opt.step(0.1)
+    for (f, _), (f2, _) in zip(wl.filters(), new.filters()):
+        assert not torch.equal(f, f2)
+        f2.copy_(f)
+    wl.step()
+    new.step()
+    torch.cuda.synchronize()
+    assert torch.equal(wl.pooled, new.pooled)
+    for (_, dw), (_, dw2) in zip(wl.filters(), new.filters()):
+        assert torch.equal(dw, dw2)
