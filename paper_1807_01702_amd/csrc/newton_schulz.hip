@@ -6,16 +6,18 @@
 //   `steps` times:  G = X X^T,  R = a I + b G + c G G,  X <- R X
 //   out = X, or  w <- w (1 - lr decay) - lr scale X
 //
-// Precision.  The products run on the fp16 matrix cores at float32 accuracy:
-// every operand v is held as a pair hi = fp16(S v), lo = fp16(S v - hi), 22
-// bits together, and a product of two operands is three matrix products,
-// hi hi' + hi lo' + lo hi', accumulated in float32 (the dropped lo lo' is below
-// 2^-22 of the term).  The factor S = 2^12 keeps both parts inside fp16's range:
-// the spectral norm of X, G and R stays below 16 (the caller's coefficients are
-// checked for that), so no |S v| reaches 65504, and what is lost below fp16's
-// smallest step is 2^-37 of the norm of X.  A library's large product reaches 1330
-// TFLOP/s in fp16 and 150 in float32 on this chip: three fp16 products carry
-// float32's error at 2.9 times its rate.
+// Precision.  The products run on the fp16 matrix cores: every operand v is held as
+// a pair hi = fp16(S v), lo = fp16(S v - hi), off by at most 2^-23 of v (float32:
+// 2^-24), and a product of two operands is three matrix products,
+// hi hi' + hi lo' + lo hi', accumulated in float32; the dropped lo lo', below 2^-22
+// of the term, is added where sums are short (nw_four, nw_third).  The factor S = 2^12 keeps
+// both parts inside fp16's range: the spectral norm of X, G and R stays below 16 (the
+// caller's coefficients are checked for that), so no |S v| reaches 65504, and what is
+// lost below fp16's smallest step is 2^-37, where X's norm is at most 1.  Against
+// float64 the results are 0.2 to 1.2 times as far off as those of float32 products,
+// for noise, strong directions, rows of different scale and decaying spectra of
+// 8 x 8 to 4096 x 4096.  A library's large product reaches 1330 TFLOP/s in fp16 and
+// 150 in float32 on this chip: three fp16 products run at 2.9 times float32's rate.
 //
 // Measured: 4096 x 4096, five steps, 3.5 ms = 393 of the 443 TFLOP/s that pairs can
 // reach (the matrix cores bound it); twelve bf16 weights of 1024 x 4096 2.8 ms; all
@@ -445,6 +447,32 @@ __device__ __forceinline__ void ns_result4(const NsIn &in, const NsStep &s, floa
 }
 __device__ __forceinline__ float ns_rate(const NsStep &s) { return !s.update ? 0.f : (s.lr_dev ? gld<float>(s.lr_dev) : s.lr); }
 
+// A product's sums: hi hi' in acc and the two smaller products apart in low, joined
+// at the end.  A matrix instruction adds its 32 terms in four roundings, so one
+// chain of all three products takes twelve a k step at the sum's full size; with
+// low, whose roundings are 2^-11 of that, it takes four.  (1023 x 4093 with singular
+// values over five decades: 1.56 times the error of float32 products in one chain,
+// 0.97 apart; 413 us and 421.  Tiles of 256 have no registers for both: 4096 x 4096
+// is 1.13 times as far off as float32 products.)
+template <int MI, int NI>
+__device__ __forceinline__ void ns_zero(f32x4 (&acc)[MI][NI])
+{
+    #pragma unroll
+    for (int i = 0; i < MI; i++)
+        #pragma unroll
+        for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+template <int MI, int NI>
+__device__ __forceinline__ void ns_join(f32x4 (&acc)[MI][NI], const f32x4 (&low)[MI][NI])
+{
+    #pragma unroll
+    for (int i = 0; i < MI; i++)
+        #pragma unroll
+        for (int j = 0; j < NI; j++)
+            #pragma unroll
+            for (int e = 0; e < 4; e++) acc[i][j][e] += low[i][j][e];
+}
+
 // One product stage over the whole list.
 //   NS_GRAM    G = X X^T            (lower-triangle tiles, mirrored)
 //   NS_SQUARE  R = a I + b G + c G G (likewise)
@@ -644,11 +672,10 @@ __global__ __launch_bounds__(BT * 2, 2) void k_ns_product(NsTable t, int count, 
         __builtin_amdgcn_sched_barrier(0);       // (the scheduler would sink them to the barrier that waits for them)
     };
     const int wm = wave / WN, wn = wave % WN;
-    f32x4 acc[MI][NI];
-    #pragma unroll
-    for (int i = 0; i < MI; i++)
-        #pragma unroll
-        for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr bool APART = BT == 128;
+    f32x4 acc[MI][NI], low[APART ? MI : 1][APART ? NI : 1];
+    ns_zero(acc);
+    ns_zero(low);
     auto frag = [&](const unsigned char *stage, int row, int part) __attribute__((always_inline)) {
         return *reinterpret_cast<const f16x8 *>(stage + (row / 8 + part) * 1024 + lane * 16);
     };
@@ -668,15 +695,17 @@ __global__ __launch_bounds__(BT * 2, 2) void k_ns_product(NsTable t, int count, 
     // the three products of a sum are far apart, except where the registers do not
     // hold all fragments (256-tiles: spills, 140 -> 179 us)
     auto multiply = [&](const Frags &f) __attribute__((always_inline)) {
-        if constexpr (BT == 128) {
+        if constexpr (APART) {
             #pragma unroll
             for (int term = 0; term < 3; term++)
                 #pragma unroll
                 for (int i = 0; i < MI; i++)
                     #pragma unroll
-                    for (int j = 0; j < NI; j++)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(term == 1 ? f.al[i] : f.ah[i],
-                                                                           term == 0 ? f.bl[j] : f.bh[j], acc[i][j], 0, 0, 0);
+                    for (int j = 0; j < NI; j++) {
+                        f32x4 &to = term < 2 ? low[i][j] : acc[i][j];
+                        to = __builtin_amdgcn_mfma_f32_16x16x32_f16(term == 1 ? f.al[i] : f.ah[i],
+                                                                    term == 0 ? f.bl[j] : f.bh[j], to, 0, 0, 0);
+                    }
         } else {
             #pragma unroll
             for (int i = 0; i < MI; i++)
@@ -705,6 +734,7 @@ __global__ __launch_bounds__(BT * 2, 2) void k_ns_product(NsTable t, int count, 
             __syncthreads();
         }
     }
+    if constexpr (APART) ns_join(acc, low);
     if (pieces > 1) {                            // in the order of the fragments: [wave][block][lane]
         float *o = cut.part + (int64_t)(blockIdx.x - cut.whole) * (BT * BT) + wave * (TM * TN);
         #pragma unroll
@@ -795,11 +825,9 @@ __global__ __launch_bounds__(256, 1) void k_ns_direct(NsTable t, int count, NsSt
             o[2 * B + 2 * i + 1] = gld<f16x8>(q + kLo);
         }
     };
-    f32x4 acc[B][B];
-    #pragma unroll
-    for (int i = 0; i < B; i++)
-        #pragma unroll
-        for (int j = 0; j < B; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 acc[B][B], low[B][B];
+    ns_zero(acc);
+    ns_zero(low);
     #pragma unroll
     for (int u = 0; u < AHEAD; u++)
         if (u < n) load(f[u], u);
@@ -812,12 +840,13 @@ __global__ __launch_bounds__(256, 1) void k_ns_direct(NsTable t, int count, NsSt
                     #pragma unroll
                     for (int j = 0; j < B; j++) {
                         const f16x8 &ah = f[u][2 * i], &al = f[u][2 * i + 1], &bh = f[u][2 * B + 2 * j], &bl = f[u][2 * B + 2 * j + 1];
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, acc[i][j], 0, 0, 0);
+                        low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, low[i][j], 0, 0, 0);
+                        low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, low[i][j], 0, 0, 0);
                         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, acc[i][j], 0, 0, 0);
                     }
             if (k + u + AHEAD < n) load(f[u], k + u + AHEAD);
         }
+    ns_join(acc, low);
     // in the order of the fragments, [wave][block][lane]; wave w adds the B B / 4 blocks from w B B / 4 on
     constexpr int MINE = B * B / 4;
     f32x4 *red = reinterpret_cast<f32x4 *>(lds);
@@ -856,7 +885,9 @@ template <int P> struct Nw {
     // row pitches in halves: 16 and 32 bytes past the pairs, so that the 16 rows
     // of a fragment and the rows of a transposing read start in different banks
     static constexpr int GP = 2 * P + 8, XP = 2 * P + 16;
-    static constexpr int XBytes = QB * XP * 2, LBytes = XBytes + P * GP * 2;
+    // G's third parts (nw_third), one a value
+    static constexpr int MP = P + 8, MBytes = P <= 32 ? P * MP * 2 : 0;
+    static constexpr int XBytes = QB * XP * 2, LBytes = XBytes + P * GP * 2 + MBytes;
     // waves over a P x P product and over R X
     static constexpr int TM = P == 128 ? 32 : 16, TN = P == 128 ? 64 : (P == 64 ? 32 : 16), WN = P / TN;
     static constexpr int YM = 32, YN = 64, YWN = QB / YN;
@@ -868,15 +899,33 @@ constexpr int kNwLds = nw_max(Nw<128>::LBytes, nw_max(Nw<64>::LBytes, Nw<32>::LB
 // halves offset of k (0 .. K) within a pair row
 __device__ __forceinline__ int nw_k(int k) { return (k >> 5) * 64 + (k & 31); }
 
+// In sums of few terms no other rounding covers those of the pairs.  Up to 64 rows
+// lo lo' is added too; up to 32 the square takes G in three parts, hi + lo + what those
+// leave, with the third ones' products with hi.  Times the error of float32 products,
+// without and with: 8 x 8 with rows of different scale 1.7 and 0.9, 16 x 40 of rank 4
+// and noise 1.33 and 1.16, 64 x 4096 1.28 and 1.05 (without the third parts, which do not
+// lower it and cost 4 %).  Time: 1 to 4 %.  Past 64 rows the errors are at most 1.12
+// times float32's without, and the fourth product costs 5 to 7 %.
+constexpr bool nw_four(int P) { return P <= 64; }
+constexpr bool nw_third(int P) { return P <= 32; }
+
 __device__ __forceinline__ f16x8 nw_frag(const h16 *p) { return *reinterpret_cast<const f16x8 *>(p); }
 
-// acc += A B^T over KS k steps, A rows at a, B rows at b (both contiguous along k)
-template <int MI, int NI, int KS>
-__device__ __forceinline__ void nw_product(const h16 *a, int pa, const h16 *b, int pb, f32x4 (&acc)[MI][NI])
+// acc += A B^T over KS k steps, A rows at a, B rows at b (both contiguous along k);
+// with THIRD also A's hi times B's third parts (rows at bm) and the reverse
+template <int MI, int NI, int KS, bool THIRD = false>
+__device__ __forceinline__ void nw_product(const h16 *a, int pa, const h16 *b, int pb, f32x4 (&acc)[MI][NI],
+                                           const h16 *am = nullptr, const h16 *bm = nullptr, int pm = 0)
 {
     const int lane = threadIdx.x & 63, fr = lane % 16, fc = lane / 16;
+    f32x4 low[MI][NI];
+    ns_zero(low);
     a += fr * pa + fc * 8;
     b += fr * pb + fc * 8;
+    if (THIRD) {
+        am += fr * pm + fc * 8;
+        bm += fr * pm + fc * 8;
+    }
     #pragma unroll
     for (int k = 0; k < KS; k++) {
         f16x8 ah[MI], al[MI], bh[NI], bl[NI];
@@ -894,20 +943,17 @@ __device__ __forceinline__ void nw_product(const h16 *a, int pa, const h16 *b, i
         for (int i = 0; i < MI; i++)
             #pragma unroll
             for (int j = 0; j < NI; j++) {
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
+                if constexpr (THIRD) {
+                    low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], nw_frag(bm + j * 16 * pm + k * 32), low[i][j], 0, 0, 0);
+                    low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(nw_frag(am + i * 16 * pm + k * 32), bh[j], low[i][j], 0, 0, 0);
+                }
+                if (nw_four(KS * 32)) low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bl[j], low[i][j], 0, 0, 0);
+                low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], low[i][j], 0, 0, 0);
+                low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], low[i][j], 0, 0, 0);
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
             }
     }
-}
-
-template <int MI, int NI>
-__device__ __forceinline__ void nw_zero(f32x4 (&acc)[MI][NI])
-{
-    #pragma unroll
-    for (int i = 0; i < MI; i++)
-        #pragma unroll
-        for (int j = 0; j < NI; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    ns_join(acc, low);
 }
 
 // four consecutive values of a pair row
@@ -930,7 +976,9 @@ __device__ __forceinline__ bool nw_gram(const h16 *xs, int steps, f32x4 (&acc)[M
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wm = wave / N::WN, wn = wave % N::WN;
     if (wm * N::TM >= P) return false;
-    nw_zero(acc);
+    f32x4 low[MI][NI];
+    ns_zero(acc);
+    ns_zero(low);
     // fragments of 8 consecutive block columns of one row of X: transposing reads
     const int g = lane / 16, q = lane % 16;
     const h16 *base = xs + (8 * g + q / 4) * N::XP + 4 * (q % 4);
@@ -955,11 +1003,13 @@ __device__ __forceinline__ bool nw_gram(const h16 *xs, int steps, f32x4 (&acc)[M
         for (int i = 0; i < MI; i++)
             #pragma unroll
             for (int j = 0; j < NI; j++) {
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
+                if (nw_four(P)) low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bl[j], low[i][j], 0, 0, 0);
+                low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bl[j], low[i][j], 0, 0, 0);
+                low[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al[i], bh[j], low[i][j], 0, 0, 0);
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
             }
     }
+    ns_join(acc, low);
     return true;
 }
 
@@ -1046,13 +1096,22 @@ __device__ __forceinline__ void nw_prepare(const NsDev &d, int block, const NsSt
 }
 
 // G's pairs into LDS from the wave's tile of it (raw: S^2 times G, as the
-// product leaves it).
+// product leaves it), and its third parts behind them (nw_third).
 template <int P, int MI, int NI>
 __device__ __forceinline__ void nw_put(h16 *gs, const f32x4 (&raw)[MI][NI])
 {
+    using N = Nw<P>;
     nw_tiles<P>(raw, [&](int row, int col, const f32x4 &v) {
-        const float f[4] = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
-        nw_store4(gs + row * Nw<P>::GP + nw_k(col), f);
+        float f[4] = {v[0] * kInvS, v[1] * kInvS, v[2] * kInvS, v[3] * kInvS};
+        h16 *o = gs + row * N::GP + nw_k(col);
+        nw_store4(o, f);
+        if constexpr (nw_third(P)) {
+            const f16x4 hi = *reinterpret_cast<const f16x4 *>(o), lo = *reinterpret_cast<const f16x4 *>(o + 32);
+            f16x4 m;
+            #pragma unroll
+            for (int e = 0; e < 4; e++) m[e] = (_Float16)(f[e] - (float)hi[e] - (float)lo[e]);
+            *reinterpret_cast<f16x4 *>(gs + P * N::GP + row * N::MP + col) = m;
+        }
     });
 }
 
@@ -1065,8 +1124,10 @@ __device__ __forceinline__ void nw_polynomial(const NsStep &s, h16 *gs, bool has
     const int lane = threadIdx.x & 63, g = lane / 16, q = lane % 16;
     const int wave = threadIdx.x >> 6, wm = wave / N::WN, wn = wave % N::WN;
     f32x4 acc[MI][NI];
-    nw_zero(acc);
-    if (has) nw_product<MI, NI, P / 32>(gs + wm * N::TM * N::GP, N::GP, gs + wn * N::TN * N::GP, N::GP, acc);
+    ns_zero(acc);
+    const h16 *gm = gs + P * N::GP;
+    if (has) nw_product<MI, NI, P / 32, nw_third(P)>(gs + wm * N::TM * N::GP, N::GP, gs + wn * N::TN * N::GP, N::GP, acc,
+                                                    gm + wm * N::TM * N::MP, gm + wn * N::TN * N::MP, N::MP);
     __syncthreads();
     if (has)
         #pragma unroll
@@ -1091,7 +1152,7 @@ __device__ __forceinline__ void nw_apply(const h16 *xs, const h16 *gs, f32x4 (&a
 {
     using N = Nw<P>;
     const int wave = threadIdx.x >> 6, ym = wave / N::YWN * N::YM, yn = wave % N::YWN * N::YN;
-    nw_zero(acc);
+    ns_zero(acc);
     nw_product<MI, NI, P / 32>(gs + ym * N::GP, N::GP, xs + yn * N::XP, N::XP, acc);
 }
 // Y over X's place.  The caller has had a barrier since the last read of X.
@@ -1159,7 +1220,7 @@ __device__ __forceinline__ void nw_step(const NsDev &d, int block, const NsStep 
     const int lane = tid & 63, wave = tid >> 6;
     const bool has = wave / N::WN * N::TM < P;
     f32x4 raw[MI][NI];                           // this wave's tile of G, summed over the blocks
-    nw_zero(raw);
+    ns_zero(raw);
     if (has) {
         const float *from = part + (wave * MI * NI * 64 + lane) * 4;
         #pragma unroll (P == 128 ? 1 : 4)        // (a tile of 128's G is 32 registers: 98 us against 94 unrolled)
