@@ -16,13 +16,14 @@
 // row of one repeated value differs from its mean by nothing; the rest is
 // float32.  The stored mean is rounded to float32, and the backward's xhat
 // carries that rounding, 2^-24 |mean| rstd.
-// Measured: forward, 8192 bf16 rows of 4096 with a residual, 40.6 us = 6.6 TB/s
-// (part of it from the last-level cache); backward there 50.6 us, 401408 rows of
-// 256 153.7 us = 5.35 TB/s, where a copy of 4 GiB runs at 5.44.
+// Measured: forward, 8192 bf16 rows of 4096 with a residual, 43.4 us = 6.2 TB/s
+// (part of it from the last-level cache); backward there 50.4 us, 401408 rows of
+// 256 154.5 us = 5.32 TB/s, where a copy of 4 GiB runs at 5.44.
 //
 // A row is held by TPR threads with NV loads of V elements each: V is the
 // 16-byte vector where pointers, strides and the channel count allow it, else
-// one element.  Rows of up to 64 TPR-lanes reduce with cross-lane shuffles and
+// one element.  (The 1024-thread forward of more than 8192 single elements spills 64
+// registers of its row.)  Rows of up to 64 TPR-lanes reduce with cross-lane shuffles and
 // need no barrier; longer rows take a workgroup of 256 or 1024 threads.
 #include "common.hpp"
 #include "kernels.hpp"
@@ -213,8 +214,8 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
 // and gamma stays in registers, except in the widest rows (512 threads, up to 32
 // channels each), which do not hold both beside the sums (1024 threads of 16
 // channels and 128 registers spilled more): those read gamma again, and load
-// ahead only where a vector holds 8 values.  (Odd widths past 8192 still spill
-// about half of their sums.)
+// ahead only where a vector holds 8 values.  (Widths past 8192 in single elements
+// still spill 130 to 163 registers, and 256 threads of 32 bf16 channels with dsum 15.)
 template <typename T, int V, int TPR, int NV, int WG, bool RES>
 __global__ __launch_bounds__(WG) void k_ln_bwd(LnParams p)
 {
@@ -379,10 +380,10 @@ __global__ __launch_bounds__(1024) void k_ln_combine(const float *__restrict__ p
 // The row layout of a call: threads per row, loads per thread, and in the
 // backward pass the workgroup.  As few threads as hold a row in a few loads each:
 // they reduce in fewer steps, and no lane idles (2^25 values, forward / backward in
-// us: 64 bf16 channels by 8 threads 27 / 41, by 32 threads 63 / 89; 1024 by 64
-// threads 27 / 43, by 256 41 / 53; 4096 by 256 28 / 49, by 1024 (512) 99 / 74; 201
-// float32 channels by 64 58 / 77, by 256 312 / 213; 1001 by 256 76 / 84, by 1024
-// (512) 385 / 251).
+// us: 64 bf16 channels by 8 threads 28 / 41, by 32 threads 71 / 90; 1024 by 64
+// threads 28 / 43, by 256 45 / 54; 4096 by 256 28 / 49, by 1024 (512) 106 / 74; 201
+// float32 channels by 64 62 / 77, by 256 335 / 213; 1001 by 256 81 / 84, by 1024
+// (512) 409 / 249).
 struct LnPlan { bool vec; int tpr, nv, wg; };
 
 LnPlan ln_plan(int dtype, int c, bool vec)

@@ -20,8 +20,8 @@
 // 150 in float32 on this chip: three fp16 products run at 2.9 times float32's rate.
 //
 // Measured: 4096 x 4096, five steps, 3.5 ms = 393 of the 443 TFLOP/s that pairs can
-// reach (the matrix cores bound it); twelve bf16 weights of 1024 x 4096 2.8 ms; all
-// 119 filters of DenseNet-121 405 us and 128 x 128 54 us (dependent short stages).
+// reach (the matrix cores bound it); twelve bf16 weights of 1024 x 4096 2.9 ms; all
+// 119 filters of DenseNet-121 412 us and 128 x 128 56 us (dependent short stages).
 //
 // Layout.  A pair matrix lies in the order of the fragments that the matrix
 // instructions take (ns_at): a fragment is one KiB, whether it goes to registers
@@ -87,15 +87,15 @@ __host__ __device__ constexpr int ns_gram_stage(int bt)
     return bt == 32 ? PRE_GRAM_T : (bt == 64 ? PRE_GRAM_S : (bt == 128 ? PRE_GRAM : PRE_GRAM_L));
 }
 constexpr int kMaxParts = 1024;    // partial sums of squares of a matrix
-// short sides up to this take the narrow path (128 x 4096 104 us, sixteen of 128 x
-// 1024 127; the wide path's 136 x 4096 157, sixteen of 136 x 1024 202)
+// short sides up to this take the narrow path (128 x 4096 106 us, sixteen of 128 x
+// 1024 128; the wide path's 136 x 4096 161, sixteen of 136 x 1024 214)
 constexpr int kNarrow = 128;
 constexpr int kBlock = 16384;      // values of a narrow matrix's block: [kBlock / P][P]
 // Blocks of one narrow matrix up to which every block adds the partial Gram
 // matrices itself; past it a launch of its own adds them once (five steps, own
-// additions against launches: 128 x 512, 4 blocks, 94 us against 97, sixteen of
-// them 96 against 112; 128 x 1024, 8 blocks, 108 against 99; 64 x 2048, 8
-// blocks, 71 against 81; 32 x 8192, 16 blocks, 68 against 73).
+// additions against launches: 128 x 512, 4 blocks, 95 us against 100, sixteen of
+// them 97 against 113; 128 x 1024, 8 blocks, 109 against 101; 64 x 2048, 8
+// blocks, 75 against 85; 32 x 8192, 16 blocks, 70 against 76).
 __host__ __device__ inline bool ns_summed(int blocks, int P) { return blocks > (P == 128 ? 4 : (P == 64 ? 8 : 32)); }
 
 // whole: a matrix of a single block runs as a launch of its own over all steps.
@@ -1401,7 +1401,8 @@ constexpr int ns_slots(int bt) { return bt == 128 ? kNsSlots : kNsSlots / 2; }
 int64_t cut_bytes(const NsCut &c) { return c.pieces > 1 ? (int64_t)(c.tiles - c.whole) * c.pieces * c.bt * c.bt * 4 : 0; }
 
 // The time of a stage in us as measured (kernel traces of 256 x 256 to
-// 4096 x 4096, alone and in lists): the launch, and per round of workgroups a
+// 4096 x 4096, alone and in lists; before the smaller products had sums of their
+// own, which add 0 to 3 %): the launch, and per round of workgroups a
 // part for finding the matrix, the first loads and leaving the results, and a
 // part per k step, which depends on whether the CUs are shared; for cut tiles the
 // launch that adds the pieces.  Measured, tiles of 32, 64, 128, 256:
