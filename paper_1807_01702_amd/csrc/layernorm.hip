@@ -110,10 +110,6 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
 {
     constexpr int WG = TPR > kThreads ? TPR : kThreads, GR = WG / TPR;
     typedef LnVec<T, V> L;
-    // A thread's own sum, up to 32 values: bf16 ones have 8 bits each, so float32 adds
-    // them without loss unless they are 2^11 apart, which no row of small spread holds.
-    // (float64 in their place: 96 bf16 channels 27.4 us for 23.2.)
-    typedef std::conditional_t<sizeof(T) == 2, float, double> A;
     __shared__ double red[WG / 64 * U];
     __shared__ float red_sq[WG / 64 * U];
     const int lane = threadIdx.x % TPR, grp = threadIdx.x / TPR;
@@ -145,7 +141,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
         #pragma unroll
         for (int u = 0; u < U; u++) {
             const int64_t row = row0 + u * GR;
-            A own = 0;
+            acc[u] = 0.0;
             #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const bool in = j * TPR + lane < nvec;
@@ -160,9 +156,8 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void k_ln_fwd(LnPa
                 }
                 if (in)
                     #pragma unroll
-                    for (int i = 0; i < V; i++) own += (A)f[u][j][i];
+                    for (int i = 0; i < V; i++) acc[u] += (double)f[u][j][i];
             }
-            acc[u] = (double)own;
         }
         row_sums<TPR, U>(acc, red);
         #pragma unroll

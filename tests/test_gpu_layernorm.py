@@ -459,3 +459,17 @@ def test_backward_sums_over_very_many_rows():
     xhat = (x - ln.mean[:, None]) * ln.rstd[:, None]     # (its two roundings each add U of a term)
     want, size = (xhat.double() * v).sum(0), xhat.abs().double().sum(0) * v
     assert bool(((dgamma.double() - want).abs() <= (n + 4) * U * size).all())
+
+
+@pytest.mark.parametrize("c", [8, 96, 201, 1024, 4096, 8192, 9001, 16384])
+def test_forward_rows_of_the_largest_values(c):
+    """Rows of a type's largest value and of its opposite: a few of them add up to more than float32 holds."""
+    B = _B()
+    for dtype in (torch.float32, torch.bfloat16):
+        big = torch.finfo(dtype).max
+        x = torch.full((2, c), big, dtype=dtype, device="cuda")
+        x[1] = -big
+        beta = _rand(60, c).float().cuda()
+        ln, y = B.LN(None, beta, 2, EPS), torch.empty_like(x)
+        B.bnr_layernorm_fwd(x, ln, y)
+        assert torch.equal(ln.mean, x[:, 0].float()) and torch.equal(y, beta.to(dtype).expand_as(y)), dtype
