@@ -17,8 +17,8 @@
 // float32.  The stored mean is rounded to float32, and the backward's xhat
 // carries that rounding, 2^-24 |mean| rstd.
 // Measured: forward, 8192 bf16 rows of 4096 with a residual, 43.4 us = 6.2 TB/s
-// (part of it from the last-level cache); backward there 50.4 us, 401408 rows of
-// 256 154.5 us = 5.32 TB/s, where a copy of 4 GiB runs at 5.44.
+// (part of it from the last-level cache); backward there 50.3 us, 401408 rows of
+// 256 154 to 158 us = 5.2 to 5.3 TB/s, where a copy of 4 GiB runs at 5.44.
 //
 // A row is held by TPR threads with NV loads of V elements each: V is the
 // 16-byte vector where pointers, strides and the channel count allow it, else
