@@ -8,7 +8,7 @@ classes, whose logits are never kept.
               another way)
 ``ce_fwd``    loss[0] the mean and loss[1 + i] the rows' softmax cross entropy of the
               logits h w^T + bias, and lse[1 + i] their log sum exp (lse[0]: the number
-              of rows that count)
+              of rows that count; loss and lse of the other rows, a batch's padding: 0)
 ``ce_bwd``    its gradients dh, dw (and dbias) from h, w, the labels and lse
 
 The generator is Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers:
@@ -198,7 +198,7 @@ def _ce_fwd(s):
     rows = lse - (1 - case["smoothing"]) * picked + case["z"] * lse * lse
     if case["smoothing"]:
         rows = rows - case["smoothing"] * logits.mean(1)
-    rows = torch.where(counts, rows, torch.zeros_like(rows))
+    rows, lse = torch.where(counts, rows, torch.zeros_like(rows)), torch.where(counts, lse, torch.zeros_like(lse))
     n = counts.sum()
     mean = rows.double().sum() / n
     return dict(loss=torch.cat((mean.float()[None], rows)), lse=torch.cat((n.float()[None], lse)))
@@ -254,12 +254,13 @@ def work(case):
     if case["op"] in ("drop_fwd", "drop_bwd"):
         # ten rounds of two products and six other operations for eight elements, two a kept one
         return {"bytes": m * c * es * (3 if case["add"] else 2), "flops": 12 * m * c}
-    v = case["v"]
-    values, bias = (m * c + v * c) * es, 4 * v if case["bias"] else 0
+    # rows that count, as drawn on average: the others need nothing read, and zeros written
+    v, rows = case["v"], m * (1 - case["ignored"])
+    values, bias = (rows * c + v * c) * es, 4 * v if case["bias"] else 0
     if case["op"] == "ce_fwd":                           # labels read, loss and lse written
-        return {"bytes": values + bias + 12 * m, "flops": 2 * m * c * v}
+        return {"bytes": values + bias + 12 * m, "flops": 2 * rows * c * v}
     # labels and lse read, a gradient written for each input; the logits are formed again: three products
-    return {"bytes": 2 * (values + bias) + 8 * m, "flops": 6 * m * c * v}
+    return {"bytes": 2 * (values + bias) + 8 * m + (m - rows) * c * es, "flops": 6 * rows * c * v}
 
 
 # -------------------------------------------------------------------- exact ----
@@ -310,6 +311,7 @@ def exact(case, seed):
     if case["op"] == "ce_bwd":
         grads = torch.autograd.grad(mean, (h, w, bias))
         return {k: t for k, t in zip(("dh", "dw", "dbias"), grads) if k != "dbias" or case["bias"]}
-    every = torch.zeros_like(total)
-    every[at] = rows
-    return dict(loss=torch.cat((mean[None], every)), lse=torch.cat((mean.new_full((1,), len(at)), total)))
+    loss, lse = total.new_zeros(1 + case["m"]), total.new_zeros(1 + case["m"])
+    loss[0], lse[0] = mean, len(at)
+    loss[1 + at], lse[1 + at] = rows, total[at]
+    return dict(loss=loss, lse=lse)
