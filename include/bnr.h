@@ -645,6 +645,40 @@ bnr_status bnr_layernorm_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *
                              int32_t x_ldc, const bnr_ln *ln, const void *dsum, int32_t dsum_ldc, void *dx,
                              int32_t dx_ldc, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream);
 
+/* -------------------------------------------------------------- dropout ---- */
+
+/* Dropout of rows [m][c] whose mask is not stored: whether element (row, ch)
+ * stays is a function of numbers that the caller keeps,
+ *   words = Philox4x32-10 (Salmon et al. 2011) of the counter
+ *           (ch / 8, row, site, step) with seed as its key (low word first),
+ *   bits  = half ch % 8 of the four words (low half of word 0 first),
+ *   kept where bits >= t, t = floor(65536 p + 1/2),
+ * and not of types, strides or launches: the backward forms the forward's mask
+ * again, and the same numbers give the same mask at any time.  site tells the
+ * dropouts of one network apart, step the training steps.  The probability is
+ * t / 65536, the kept values are scaled by its own 65536 / (65536 - t).
+ * Views as in the layer norm: any c, strides >= c, element-aligned pointers. */
+typedef struct {
+    double p;              /* probability that an element is dropped, in [0, 1]    */
+    uint64_t seed;
+    uint32_t site, step;
+    const uint32_t *step_dev;  /* device value in the place of step, read when the */
+                           /* call runs (a captured call follows it), or NULL      */
+} bnr_dropout;
+
+/* y = dropout(x) + res (res may be NULL: 0), rounded once.  What is dropped adds
+ * nothing, infinities and NaN included.  y may coincide exactly with x or res and
+ * may not overlap them otherwise.  1 <= m <= 2^31. */
+bnr_status bnr_dropout_fwd(int64_t m, int32_t c, bnr_dtype dtype, const void *x, int32_t x_ldc, const void *res,
+                           int32_t res_ldc, const bnr_dropout *d, void *y, int32_t y_ldc, void *stream);
+
+/* Its backward: dx = the forward's mask and scale on dy, + dsum, the gradient
+ * that reaches x by another way (may be NULL).  The gradient of res is dy.  dx may
+ * coincide exactly with dy or dsum and may not overlap them otherwise. */
+bnr_status bnr_dropout_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy, int32_t dy_ldc,
+                           const bnr_dropout *d, const void *dsum, int32_t dsum_ldc, void *dx, int32_t dx_ldc,
+                           void *stream);
+
 /* --------------------------------------- orthogonalised weight updates ---- */
 
 /* Newton-Schulz orthogonalisation of a matrix U [rows][cols]:
@@ -740,7 +774,7 @@ bnr_status bnr_hbm_copy(const void *src, void *dst, size_t bytes, void *stream);
  * 5 statistics sweep, 6 element-wise pass, 7 statistics combine, 8 weight
  * packing, 9 split-K sum, 10 pooling, 11 copy, 12 first CONV, 13 first-CONV
  * weight gradient, 14 max pooling, 15 classifier head, 16 layer norm,
- * 17 orthogonalised update); it returns the number of launches written.  Not
+ * 17 orthogonalised update, 18 dropout); it returns the number of launches written.  Not
  * meant for graph capture. */
 bnr_status bnr_trace_begin(int32_t kernel_classes, int32_t capacity);
 int32_t bnr_trace_end(double *ms, double *bytes, double *flops, int32_t *kernel_id, int32_t capacity);

@@ -67,6 +67,11 @@ class LNStruct(ctypes.Structure):
     _fields_ = [("gamma", c_vp), ("beta", c_vp), ("mean", c_vp), ("rstd", c_vp), ("eps", c_f)]
 
 
+class DropoutStruct(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("site", ctypes.c_uint32), ("step", ctypes.c_uint32),
+                ("step_dev", c_vp)]
+
+
 class NSParams(ctypes.Structure):
     _fields_ = [("steps", c_i32), ("a", c_f), ("b", c_f), ("c", c_f), ("eps", c_f)]
 
@@ -170,6 +175,10 @@ _lib_fns = dict(
     bnr_layernorm_workspace_size=_sig("bnr_layernorm_workspace_size", c_sz, c_i64, c_i32, ctypes.c_int),
     bnr_layernorm_bwd=_sig("bnr_layernorm_bwd", ctypes.c_int, c_i64, c_i32, ctypes.c_int, c_vp, c_i32, c_vp, c_i32,
                            _P(LNStruct), c_vp, c_i32, c_vp, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp),
+    bnr_dropout_fwd=_sig("bnr_dropout_fwd", ctypes.c_int, c_i64, c_i32, ctypes.c_int, c_vp, c_i32, c_vp, c_i32,
+                         _P(DropoutStruct), c_vp, c_i32, c_vp),
+    bnr_dropout_bwd=_sig("bnr_dropout_bwd", ctypes.c_int, c_i64, c_i32, ctypes.c_int, c_vp, c_i32, _P(DropoutStruct),
+                         c_vp, c_i32, c_vp, c_i32, c_vp),
     bnr_orthogonalize_workspace_size=_sig("bnr_orthogonalize_workspace_size", c_sz, _P(OrthoItem), c_i32),
     bnr_orthogonalize=_sig("bnr_orthogonalize", ctypes.c_int, _P(OrthoItem), c_i32, ctypes.c_int, ctypes.c_int,
                            _P(NSParams), c_vp, c_sz, c_vp),
@@ -183,7 +192,7 @@ _lib_fns = dict(
 
 KERNEL_IDS = {1: "conv1x1", 2: "conv3x3", 3: "wgrad1x1", 4: "wgrad3x3", 5: "stats_sweep", 6: "elementwise",
               7: "stats_combine", 8: "weight_pack", 9: "splitk_sum", 10: "pool", 11: "copy", 12: "stem_conv",
-              13: "stem_wgrad", 14: "maxpool", 15: "head", 16: "layernorm", 17: "ortho"}
+              13: "stem_wgrad", 14: "maxpool", 15: "head", 16: "layernorm", 17: "ortho", 18: "dropout"}
 
 
 class BnrError(RuntimeError):
@@ -794,6 +803,50 @@ def bnr_layernorm_bwd(dy, x, ln, dx, dgamma=None, dbeta=None, dsum=None):
     ws = _scratch(nbytes, x.device) if nbytes else None
     _run_on(index, _lib_fns["bnr_layernorm_bwd"], m, c, code, pd, ldd, px, ldx, ctypes.byref(s), pr, ldr, po, ldo, pg,
             pb, _ptr(ws), nbytes)
+
+
+class Dropout:
+    """One dropout: the probability p, the seed (64 bits), the site (which dropout of the network; 32 bits) and the
+    step (32 bits: a number, or an int32 tensor of one value that is read when a call runs, so that a captured step
+    follows it).  The backward forms the forward's mask from the same numbers."""
+
+    def __init__(self, p, seed, site=0, step=0):
+        if not (0 <= seed < 1 << 64 and 0 <= site < 1 << 32):
+            raise ValueError("a seed of 64 bits and a site of 32 are wanted")
+        self.p, self.seed, self.site, self.step = p, seed, site, step
+
+    def struct(self):
+        if not isinstance(self.step, torch.Tensor):
+            if not 0 <= self.step < 1 << 32:
+                raise ValueError("step: %d does not fit 32 bits" % self.step)
+            return DropoutStruct(self.p, self.seed, self.site, self.step, None), None
+        if self.step.dtype != torch.int32 or self.step.numel() != 1:
+            raise ValueError("step: an int32 tensor of one value is wanted")
+        return DropoutStruct(self.p, self.seed, self.site, 0, self.step.data_ptr()), self.step
+
+
+def bnr_dropout_fwd(x, drop, y, res=None):
+    """y = dropout(x) (+ res) (views [.., c])."""
+    c, dt = x.shape[-1], x.dtype
+    m = x.numel() // c if c else 0
+    px, ldx = _rows(x, m, c, dt, "x")
+    py, ldy = _rows(y, m, c, dt, "y")
+    pr, ldr = _rows(res, m, c, dt, "res")
+    s, step = drop.struct()
+    _run_on(_device_of(x, y, res, step), _lib_fns["bnr_dropout_fwd"], m, c, dtype_code(x), px, ldx, pr, ldr,
+            ctypes.byref(s), py, ldy)
+
+
+def bnr_dropout_bwd(dy, drop, dx, dsum=None):
+    """dx = the mask and scale of bnr_dropout_fwd on dy (+ dsum) (views [.., c])."""
+    c, dt = dy.shape[-1], dy.dtype
+    m = dy.numel() // c if c else 0
+    pd, ldd = _rows(dy, m, c, dt, "dy")
+    px, ldx = _rows(dx, m, c, dt, "dx")
+    pr, ldr = _rows(dsum, m, c, dt, "dsum")
+    s, step = drop.struct()
+    _run_on(_device_of(dy, dx, dsum, step), _lib_fns["bnr_dropout_bwd"], m, c, dtype_code(dy), pd, ldd,
+            ctypes.byref(s), pr, ldr, px, ldx)
 
 
 NS_COEF = (3.4445, -4.7750, 2.0315)

@@ -2026,3 +2026,56 @@ bnr_status bnr_muon_update(const bnr_muon_item *items, int32_t count, bnr_dtype 
 }
 
 }  // extern "C"
+
+// ------------------------------------------------------------- dropout ----
+static bnr_status dropout(int64_t m, int32_t c, bnr_dtype dtype, const void *x, int32_t x_ldc, const char *x_name,
+                          const void *add, int32_t add_ldc, const char *add_name, const bnr_dropout *d, void *y,
+                          int32_t y_ldc, const char *y_name, void *stream)
+{
+    TRY(check_dtype(dtype));
+    if (m <= 0 || m > ((int64_t)1 << 31)) return fail(BNR_ERR_SHAPE, "m = %lld out of range", (long long)m);
+    if (c <= 0) return fail(BNR_ERR_SHAPE, "channels %d must be positive", c);
+    if (dropout_groups(m, c) > INT32_MAX) return fail(BNR_ERR_UNSUPPORTED, "m %lld x %d channels too large for one call", (long long)m, c);
+    if (!d) return fail(BNR_ERR_NULL, "dropout is NULL");
+    if (!(d->p >= 0.0 && d->p <= 1.0)) return fail(BNR_ERR_SHAPE, "p must be in [0, 1]");
+    if (reinterpret_cast<uintptr_t>(d->step_dev) % 4) return fail(BNR_ERR_ALIGN, "step_dev is not 4-byte aligned");
+    TRY(check_ln_view(x, x_ldc, c, dtype, x_name));
+    TRY(check_ln_view(y, y_ldc, c, dtype, y_name));
+    const int es = esize(dtype);
+    if (ln_clash(y, y_ldc, x, x_ldc, m, c, es))
+        return fail(BNR_ERR_ALIAS, "%s overlaps %s without coinciding with it", y_name, x_name);
+    if (add) {
+        TRY(check_ln_view(add, add_ldc, c, dtype, add_name));
+        if (ln_clash(y, y_ldc, add, add_ldc, m, c, es))
+            return fail(BNR_ERR_ALIAS, "%s overlaps %s without coinciding with it", y_name, add_name);
+    }
+    if (d->step_dev && overlap(bytes_range(d->step_dev, 4), view_range(y, m, c, y_ldc, es)))
+        return fail(BNR_ERR_ALIAS, "step_dev lies in %s", y_name);
+    DropoutParams p{};
+    p.m = m; p.c = c;
+    p.x = x; p.x_ldc = x_ldc;
+    p.add = add; p.add_ldc = add_ldc;
+    p.y = y; p.y_ldc = y_ldc;
+    p.seed = d->seed; p.site = d->site; p.step = d->step; p.step_dev = d->step_dev;
+    p.limit = (uint32_t)(d->p * 65536.0 + 0.5);
+    p.scale = p.limit < 65536 ? (float)(65536.0 / (65536 - p.limit)) : 0.0f;
+    TRY_HIP(launch_dropout(dt_of(dtype), p, (hipStream_t)stream), "dropout");
+    return ok();
+}
+
+extern "C" {
+
+bnr_status bnr_dropout_fwd(int64_t m, int32_t c, bnr_dtype dtype, const void *x, int32_t x_ldc, const void *res,
+                           int32_t res_ldc, const bnr_dropout *d, void *y, int32_t y_ldc, void *stream)
+{
+    return dropout(m, c, dtype, x, x_ldc, "x", res, res_ldc, "res", d, y, y_ldc, "y", stream);
+}
+
+bnr_status bnr_dropout_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy, int32_t dy_ldc,
+                           const bnr_dropout *d, const void *dsum, int32_t dsum_ldc, void *dx, int32_t dx_ldc,
+                           void *stream)
+{
+    return dropout(m, c, dtype, dy, dy_ldc, "dy", dsum, dsum_ldc, "dsum", d, dx, dx_ldc, "dx", stream);
+}
+
+}  // extern "C"

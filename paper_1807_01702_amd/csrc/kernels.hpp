@@ -298,6 +298,27 @@ hipError_t launch_ln_fwd(int dtype, const LnParams &p, bool vec, hipStream_t s);
 hipError_t launch_ln_bwd(int dtype, const LnParams &p, bool vec, hipStream_t s);
 hipError_t launch_ln_combine(const float *part, int64_t R, int c, float *dbeta, float *dgamma, hipStream_t s);
 
+// Dropout of each row's channels, its mask formed from a counter (dropout.hip).
+struct DropoutParams {
+    int64_t m;
+    int c;
+    const void *x;                // [m][c] views
+    int64_t x_ldc;
+    const void *add;              // added behind (NULL: none)
+    int64_t add_ldc;
+    void *y;
+    int64_t y_ldc;
+    uint64_t seed;
+    uint32_t site, step;
+    const uint32_t *step_dev;     // in the place of step (NULL: step)
+    uint32_t limit;               // dropped where 16 bits are below
+    float scale;                  // of what is kept
+    uint32_t blocks, magic;       // blocks of eight channels a row, and its division
+    int shift;
+};
+int64_t dropout_groups(int64_t m, int c);
+hipError_t launch_dropout(int dtype, DropoutParams p, hipStream_t s);
+
 // Newton-Schulz orthogonalisation of a list of matrices (newton_schulz.hip).
 struct NsIn {                     // one matrix as the caller gives it, row-major
     const void *src;              // matrix to orthogonalise, or gradient
