@@ -679,6 +679,54 @@ bnr_status bnr_dropout_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy
                            const bnr_dropout *d, const void *dsum, int32_t dsum_ldc, void *dx, int32_t dx_ldc,
                            void *stream);
 
+/* ----------------------------- linear layer and softmax cross entropy ---- */
+
+/* The last linear layer and the softmax cross entropy over its classes (a large
+ * vocabulary, say), whose logits [m][classes] are never kept:
+ *   l = h w^T + bias,  lse[r] = log sum_v exp l[r][v],
+ *   loss[r] = lse - (1 - smoothing) l[r][label] - smoothing/classes sum_v l[r][v]
+ *             + z_loss lse^2.
+ * h [m][c] and w [classes][c] are row views in the storage type: a class's weights
+ * lie together, as in an embedding table (bnr_head_fwd's wfc lies across).  c and the
+ * strides are multiples of the 16-byte vector (strides up to 2^20), m is 1..2^24,
+ * classes any.  A row whose label is `ignore` (padding) does not count: its loss, lse
+ * and dh are zeros, and its features reach nothing, whatever they hold.  Any other
+ * label outside [0, classes) gives its row (and the mean) a NaN loss and NaN
+ * gradients.  A bias of -infinity takes its class out.  An infinity or NaN in a row
+ * of h makes its own loss NaN, and every row of dw. */
+typedef struct {
+    const float *bias;     /* [classes] or NULL (0)                                */
+    const int32_t *labels; /* [m]                                                  */
+    int32_t ignore;        /* the label of rows that do not count                  */
+    float smoothing;       /* in [0, 1)                                            */
+    float z_loss;          /* >= 0, finite                                         */
+    float *lse;            /* [1 + m]: lse[0] the number of rows that count,       */
+                           /* lse[1 + r]; written by the forward, read by the      */
+                           /* backward                                             */
+} bnr_ce;
+
+/* Workspace bytes enough for the forward (backward = 0) or the backward. */
+size_t bnr_linear_ce_workspace_size(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, int32_t backward);
+
+/* loss [1 + m]: loss[0] the mean over the rows that count (0 without any),
+ * loss[1 + r] the rows' losses; ce->lse likewise.  The same call gives the same bits. */
+bnr_status bnr_linear_ce_fwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, const void *h, int32_t h_ld,
+                             const void *w, int32_t w_ld, const bnr_ce *ce, float *loss, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/* Its gradients: with dloss [1 + m] the gradient of loss (NULL: that of the mean
+ * alone, {1, 0, ...}) and r[i] = dloss[0] / lse[0] + dloss[1 + i],
+ *   g = r (exp(l - lse) (1 + 2 z_loss lse) - (1 - smoothing) [v = label] - smoothing/classes),
+ *   dh = g w [m][c] (storage type),  dw = g^T h [classes][c] (dw_dtype),
+ *   dbias = column sums of g [classes] float32,
+ * all overwritten; each may be NULL.  The logits are formed again, the classes in
+ * pieces.  g is rounded to the storage type as the operand of the two products (dbias
+ * adds it unrounded); sums are float32.  The same call gives the same bits. */
+bnr_status bnr_linear_ce_bwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, const void *h, int32_t h_ld,
+                             const void *w, int32_t w_ld, const bnr_ce *ce, const float *dloss, void *dh, int32_t dh_ld,
+                             void *dw, int32_t dw_ld, bnr_dtype dw_dtype, float *dbias, void *ws, size_t ws_bytes,
+                             void *stream);
+
 /* --------------------------------------- orthogonalised weight updates ---- */
 
 /* Newton-Schulz orthogonalisation of a matrix U [rows][cols]:
@@ -774,7 +822,8 @@ bnr_status bnr_hbm_copy(const void *src, void *dst, size_t bytes, void *stream);
  * 5 statistics sweep, 6 element-wise pass, 7 statistics combine, 8 weight
  * packing, 9 split-K sum, 10 pooling, 11 copy, 12 first CONV, 13 first-CONV
  * weight gradient, 14 max pooling, 15 classifier head, 16 layer norm,
- * 17 orthogonalised update, 18 dropout); it returns the number of launches written.  Not
+ * 17 orthogonalised update, 18 dropout, 19 linear layer with cross entropy); it
+ * returns the number of launches written.  Not
  * meant for graph capture. */
 bnr_status bnr_trace_begin(int32_t kernel_classes, int32_t capacity);
 int32_t bnr_trace_end(double *ms, double *bytes, double *flops, int32_t *kernel_id, int32_t capacity);

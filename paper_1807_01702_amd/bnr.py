@@ -72,6 +72,10 @@ class DropoutStruct(ctypes.Structure):
                 ("step_dev", c_vp)]
 
 
+class CEStruct(ctypes.Structure):
+    _fields_ = [("bias", c_vp), ("labels", c_vp), ("ignore", c_i32), ("smoothing", c_f), ("z_loss", c_f), ("lse", c_vp)]
+
+
 class NSParams(ctypes.Structure):
     _fields_ = [("steps", c_i32), ("a", c_f), ("b", c_f), ("c", c_f), ("eps", c_f)]
 
@@ -179,6 +183,11 @@ _lib_fns = dict(
                          _P(DropoutStruct), c_vp, c_i32, c_vp),
     bnr_dropout_bwd=_sig("bnr_dropout_bwd", ctypes.c_int, c_i64, c_i32, ctypes.c_int, c_vp, c_i32, _P(DropoutStruct),
                          c_vp, c_i32, c_vp, c_i32, c_vp),
+    bnr_linear_ce_workspace_size=_sig("bnr_linear_ce_workspace_size", c_sz, c_i64, c_i32, c_i32, ctypes.c_int, c_i32),
+    bnr_linear_ce_fwd=_sig("bnr_linear_ce_fwd", ctypes.c_int, c_i64, c_i32, c_i32, ctypes.c_int, c_vp, c_i32, c_vp, c_i32,
+                           _P(CEStruct), c_vp, c_vp, c_sz, c_vp),
+    bnr_linear_ce_bwd=_sig("bnr_linear_ce_bwd", ctypes.c_int, c_i64, c_i32, c_i32, ctypes.c_int, c_vp, c_i32, c_vp, c_i32,
+                           _P(CEStruct), c_vp, c_vp, c_i32, c_vp, c_i32, ctypes.c_int, c_vp, c_vp, c_sz, c_vp),
     bnr_orthogonalize_workspace_size=_sig("bnr_orthogonalize_workspace_size", c_sz, _P(OrthoItem), c_i32),
     bnr_orthogonalize=_sig("bnr_orthogonalize", ctypes.c_int, _P(OrthoItem), c_i32, ctypes.c_int, ctypes.c_int,
                            _P(NSParams), c_vp, c_sz, c_vp),
@@ -192,7 +201,8 @@ _lib_fns = dict(
 
 KERNEL_IDS = {1: "conv1x1", 2: "conv3x3", 3: "wgrad1x1", 4: "wgrad3x3", 5: "stats_sweep", 6: "elementwise",
               7: "stats_combine", 8: "weight_pack", 9: "splitk_sum", 10: "pool", 11: "copy", 12: "stem_conv",
-              13: "stem_wgrad", 14: "maxpool", 15: "head", 16: "layernorm", 17: "ortho", 18: "dropout"}
+              13: "stem_wgrad", 14: "maxpool", 15: "head", 16: "layernorm", 17: "ortho", 18: "dropout",
+              19: "linear_ce"}
 
 
 class BnrError(RuntimeError):
@@ -847,6 +857,60 @@ def bnr_dropout_bwd(dy, drop, dx, dsum=None):
     s, step = drop.struct()
     _run_on(_device_of(dy, dx, dsum, step), _lib_fns["bnr_dropout_bwd"], m, c, dtype_code(dy), pd, ldd,
             ctypes.byref(s), pr, ldr, px, ldx)
+
+
+class CE:
+    """One softmax cross entropy behind a linear layer: the labels ([m] int32), the bias ([classes] float32 or None),
+    the label of rows that do not count, label smoothing, the factor of lse^2, and the rows' log sums lse ([1 + m]
+    float32, allocated unless given), which the forward writes and the backward reads."""
+
+    def __init__(self, labels, bias=None, ignore=-100, smoothing=0.0, z_loss=0.0, lse=None):
+        self.labels, self.bias, self.ignore, self.smoothing, self.z_loss = labels, bias, ignore, smoothing, z_loss
+        self.lse = lse if lse is not None else torch.empty(1 + labels.numel(), dtype=torch.float32, device=labels.device)
+
+    def struct(self, m, classes):
+        if self.labels.dtype != torch.int32 or self.labels.numel() != m or not self.labels.is_contiguous():
+            raise ValueError("labels: a contiguous int32 array of %d values is wanted" % m)
+        return CEStruct(_f32_array(self.bias, classes, "bias"), self.labels.data_ptr(), _int32(self.ignore, "ignore"),
+                        self.smoothing, self.z_loss, _f32_array(self.lse, 1 + m, "lse"))
+
+
+def _ce_sizes(h, w):
+    c, classes = h.shape[-1], w.shape[0]
+    if w.dim() != 2:
+        raise ValueError("w: [classes, c] is wanted")
+    return h.numel() // c if c else 0, c, classes
+
+
+def bnr_linear_ce_fwd(h, w, ce, loss):
+    """loss ([1 + m] float32: the mean over the rows that count, then the rows) and ce.lse of the softmax cross entropy
+    of h w^T + bias (h: a view [.., c]; w [classes, c])."""
+    m, c, classes = _ce_sizes(h, w)
+    ph, ldh = _rows(h, m, c, h.dtype, "h")
+    pw, ldw = _rows(w, classes, c, h.dtype, "w")
+    s, pl = ce.struct(m, classes), _f32_array(loss, 1 + m, "loss")
+    index, code = _device_of(h, w, ce.labels, ce.lse, ce.bias, loss), dtype_code(h)
+    nbytes = _lib_fns["bnr_linear_ce_workspace_size"](m, c, classes, code, 0)
+    ws = _scratch(nbytes, h.device)
+    _run_on(index, _lib_fns["bnr_linear_ce_fwd"], m, c, classes, code, ph, ldh, pw, ldw, ctypes.byref(s), pl, _ptr(ws),
+            nbytes)
+
+
+def bnr_linear_ce_bwd(h, w, ce, dh=None, dw=None, dbias=None, dloss=None):
+    """The gradients of bnr_linear_ce_fwd's loss (dloss: the gradient of all of loss, or None for that of the mean): dh
+    (a view like h), dw ([classes, c], float32 or bf16), dbias ([classes] float32); those given are overwritten."""
+    m, c, classes = _ce_sizes(h, w)
+    ph, ldh = _rows(h, m, c, h.dtype, "h")
+    pw, ldw = _rows(w, classes, c, h.dtype, "w")
+    pdh, lddh = _rows(dh, m, c, h.dtype, "dh")
+    pdw, lddw = _rows(dw, classes, c, dw.dtype if dw is not None else None, "dw")
+    s = ce.struct(m, classes)
+    pb, pd = _f32_array(dbias, classes, "dbias"), _f32_array(dloss, 1 + m, "dloss")
+    index, code = _device_of(h, w, ce.labels, ce.lse, ce.bias, dh, dw, dbias, dloss), dtype_code(h)
+    nbytes = _lib_fns["bnr_linear_ce_workspace_size"](m, c, classes, code, 1)
+    ws = _scratch(nbytes, h.device)
+    _run_on(index, _lib_fns["bnr_linear_ce_bwd"], m, c, classes, code, ph, ldh, pw, ldw, ctypes.byref(s), pd, pdh, lddh,
+            pdw, lddw, dtype_code(dw) if dw is not None else code, pb, _ptr(ws), nbytes)
 
 
 NS_COEF = (3.4445, -4.7750, 2.0315)

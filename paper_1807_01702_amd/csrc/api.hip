@@ -2079,3 +2079,134 @@ bnr_status bnr_dropout_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy
 }
 
 }  // extern "C"
+
+// ----------------------------------- linear layer and softmax cross entropy ----
+static bnr_status check_ce_rows(const void *p, int64_t rows, int32_t ld, int32_t c, bnr_dtype dtype, const char *name)
+{
+    TRY(check_ptr(p, name));
+    TRY(check_channels(c, ld, dtype, name));
+    if (ld > kCeMaxLd) return fail(BNR_ERR_UNSUPPORTED, "%s: stride %d exceeds %d", name, ld, kCeMaxLd);
+    return BNR_OK;
+}
+
+static bnr_status check_ce_sizes(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype)
+{
+    TRY(check_dtype(dtype));
+    if (m <= 0 || m > ((int64_t)1 << 24)) return fail(BNR_ERR_SHAPE, "m = %lld not in 1..2^24", (long long)m);
+    if (classes <= 0) return fail(BNR_ERR_SHAPE, "classes %d must be positive", classes);
+    if (c <= 0) return fail(BNR_ERR_SHAPE, "channels %d must be positive", c);
+    if (((m + 127) / 128) * ((classes + 127LL) / 128) > (1 << 30) || m * (int64_t)c > ((int64_t)1 << 40))
+        return fail(BNR_ERR_UNSUPPORTED, "%lld rows x %d classes, %d channels: too large for one call", (long long)m, classes, c);
+    return BNR_OK;
+}
+
+// the arguments that both directions read
+static bnr_status check_ce(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, const void *h, int32_t h_ld,
+                           const void *w, int32_t w_ld, const bnr_ce *ce)
+{
+    TRY(check_ce_sizes(m, c, classes, dtype));
+    TRY(check_ce_rows(h, m, h_ld, c, dtype, "h"));
+    TRY(check_ce_rows(w, classes, w_ld, c, dtype, "w"));
+    if (!ce) return fail(BNR_ERR_NULL, "ce is NULL");
+    if (!ce->labels) return fail(BNR_ERR_NULL, "ce.labels is NULL");
+    if (reinterpret_cast<uintptr_t>(ce->labels) % 4) return fail(BNR_ERR_ALIGN, "ce.labels is not 4-byte aligned");
+    if (ce->bias) TRY(check_fptr(ce->bias, "ce.bias"));
+    TRY(check_fptr(ce->lse, "ce.lse"));
+    if (!(ce->smoothing >= 0.0f && ce->smoothing < 1.0f)) return fail(BNR_ERR_SHAPE, "ce.smoothing must be in [0, 1)");
+    if (!(ce->z_loss >= 0.0f && ce->z_loss <= 3.4e38f)) return fail(BNR_ERR_SHAPE, "ce.z_loss must be finite and >= 0");
+    return BNR_OK;
+}
+
+static CeCall ce_call(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, const void *h, int32_t h_ld,
+                      const void *w, int32_t w_ld, const bnr_ce *ce)
+{
+    CeCall a{};
+    a.dtype = dt_of(dtype);
+    a.m = m; a.c = c; a.classes = classes;
+    a.h = h; a.h_ld = h_ld;
+    a.w = w; a.w_ld = w_ld;
+    if (ce) {
+        a.bias = ce->bias; a.labels = ce->labels; a.ignore = ce->ignore;
+        a.smoothing = ce->smoothing; a.z = ce->z_loss; a.lse = ce->lse;
+    }
+    return a;
+}
+
+extern "C" {
+
+size_t bnr_linear_ce_workspace_size(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, int32_t backward)
+{
+    if (check_ce_sizes(m, c, classes, dtype) != BNR_OK || c % vec_of(dtype)) return 0;
+    CeCall a = ce_call(m, c, classes, dtype, nullptr, c, nullptr, c, nullptr);
+    static float some;                           // every output asked for
+    a.smoothing = 0.5f;
+    if (!backward) return ce_fwd_bytes(a);
+    a.dh = a.dw = a.dbias = &some;
+    return ce_bwd_bytes(a);
+}
+
+bnr_status bnr_linear_ce_fwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, const void *h, int32_t h_ld,
+                             const void *w, int32_t w_ld, const bnr_ce *ce, float *loss, void *ws, size_t ws_bytes,
+                             void *stream)
+{
+    TRY(check_ce(m, c, classes, dtype, h, h_ld, w, w_ld, ce));
+    TRY(check_fptr(loss, "loss"));
+    const int es = esize(dtype);
+    const Range rl = bytes_range(loss, (1 + m) * 4), rs = bytes_range(ce->lse, (1 + m) * 4);
+    if (overlap(rl, rs)) return fail(BNR_ERR_ALIAS, "loss overlaps ce.lse");
+    for (const Range &o : {rl, rs})
+        if (overlap(o, view_range(h, m, c, h_ld, es)) || overlap(o, view_range(w, classes, c, w_ld, es)) ||
+            overlap(o, bytes_range(ce->labels, m * 4)) || (ce->bias && overlap(o, bytes_range(ce->bias, classes * (int64_t)4))))
+            return fail(BNR_ERR_ALIAS, "loss / ce.lse overlap an input");
+    CeCall a = ce_call(m, c, classes, dtype, h, h_ld, w, w_ld, ce);
+    a.loss = loss;
+    TRY(check_ws(ws, ws_bytes, ce_fwd_bytes(a)));
+    TRY_HIP(launch_ce_fwd(a, ws, (hipStream_t)stream), "linear cross entropy");
+    return ok();
+}
+
+bnr_status bnr_linear_ce_bwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, const void *h, int32_t h_ld,
+                             const void *w, int32_t w_ld, const bnr_ce *ce, const float *dloss, void *dh, int32_t dh_ld,
+                             void *dw, int32_t dw_ld, bnr_dtype dw_dtype, float *dbias, void *ws, size_t ws_bytes,
+                             void *stream)
+{
+    TRY(check_ce(m, c, classes, dtype, h, h_ld, w, w_ld, ce));
+    TRY(check_dtype(dw_dtype));
+    if (!dh && !dw && !dbias) return fail(BNR_ERR_NULL, "no gradient is asked for");
+    if (dloss) TRY(check_fptr(dloss, "dloss"));
+    const int es = esize(dtype);
+    struct Out { Range r; const char *name; } out[3];
+    int n = 0;
+    if (dh) {
+        TRY(check_ce_rows(dh, m, dh_ld, c, dtype, "dh"));
+        out[n++] = Out{view_range(dh, m, c, dh_ld, es), "dh"};
+    }
+    if (dw) {
+        TRY(check_ce_rows(dw, classes, dw_ld, c, dw_dtype, "dw"));
+        out[n++] = Out{view_range(dw, classes, c, dw_ld, esize(dw_dtype)), "dw"};
+    }
+    if (dbias) {
+        TRY(check_fptr(dbias, "dbias"));
+        out[n++] = Out{bytes_range(dbias, classes * (int64_t)4), "dbias"};
+    }
+    for (int i = 0; i < n; i++) {
+        for (int k = i + 1; k < n; k++)
+            if (overlap(out[i].r, out[k].r)) return fail(BNR_ERR_ALIAS, "%s overlaps %s", out[i].name, out[k].name);
+        const Range &o = out[i].r;
+        if (overlap(o, view_range(h, m, c, h_ld, es)) || overlap(o, view_range(w, classes, c, w_ld, es)) ||
+            overlap(o, bytes_range(ce->labels, m * 4)) || overlap(o, bytes_range(ce->lse, (1 + m) * 4)) ||
+            (ce->bias && overlap(o, bytes_range(ce->bias, classes * (int64_t)4))) ||
+            (dloss && overlap(o, bytes_range(dloss, (1 + m) * 4))))
+            return fail(BNR_ERR_ALIAS, "%s overlaps an input", out[i].name);
+    }
+    CeCall a = ce_call(m, c, classes, dtype, h, h_ld, w, w_ld, ce);
+    a.dloss = dloss;
+    a.dh = dh; a.dh_ld = dh_ld;
+    a.dw = dw; a.dw_ld = dw_ld; a.dw_dtype = dt_of(dw_dtype);
+    a.dbias = dbias;
+    TRY(check_ws(ws, ws_bytes, ce_bwd_bytes(a)));
+    TRY_HIP(launch_ce_bwd(a, ws, (hipStream_t)stream), "linear cross entropy backward");
+    return ok();
+}
+
+}  // extern "C"

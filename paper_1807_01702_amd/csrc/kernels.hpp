@@ -319,6 +319,90 @@ struct DropoutParams {
 int64_t dropout_groups(int64_t m, int c);
 hipError_t launch_dropout(int dtype, DropoutParams p, hipStream_t s);
 
+// Linear layer and softmax cross entropy without stored logits (linear_ce.hip).
+constexpr int kCeMaxLd = 1 << 20;  // row strides: 32-bit offsets within a tile
+struct CeCall {                    // one call (forward: loss; backward: the rest)
+    int dtype, dw_dtype;
+    int64_t m;
+    int c, classes, ignore;
+    const void *h, *w;
+    int64_t h_ld, w_ld;
+    const float *bias;             // NULL: none
+    const int32_t *labels;
+    float smoothing, z;
+    float *lse, *loss;             // [1 + m]
+    const float *dloss;            // [1 + m] or NULL
+    void *dh, *dw;                 // NULL: not wanted
+    int64_t dh_ld, dw_ld;
+    float *dbias;
+};
+struct CeRow { int row, label; float lse, scale; };   // a row that counts: its place, label, log sum, dloss / dlogit factor
+struct CeList {
+    int64_t m;
+    int classes, ignore, row_bytes;
+    const int32_t *labels;
+    int *count, *counts;           // rows that count, and per kCountRows rows (NULL: few)
+    CeRow *rows;
+    const void *h;
+    int64_t h_ld;                  // bytes
+    void *copy;                    // [count][c] dense
+    const float *lse, *dloss;      // backward
+    float *zero_loss, *zero_lse;   // forward: zeros for the rows that do not count
+    void *zero;                    // backward: likewise (NULL: none)
+    int64_t zero_ld;
+};
+enum { CE_STATS = 0, CE_GRAD = 1, CE_DH = 2, CE_DW = 3 };
+struct CeGemm {
+    const int *count;
+    const CeRow *rows;
+    const void *i, *j;             // operands
+    int64_t i_ld, j_ld;            // bytes
+    int64_t m;
+    int c, classes, first, parts;  // classes: of the piece, from `first` on
+    const float *bias;
+    float2 *stats;                 // CE_STATS: [column tile][m] maximum and sum of exponentials
+    float *sums, *picked;          // [column tile][m] sums of logits (NULL: none), [m] the labels' logits
+    float z, hit, flat;            // CE_GRAD
+    void *g;                       // [count][g_ld]
+    int64_t g_ld;
+    float *colsum;                 // [row tile][colsum_ld] (NULL: none)
+    int64_t colsum_ld;
+    void *out;                     // CE_DH, CE_DW: results, or parts of them
+    int64_t out_ld, part_stride;
+    int out_f32, add;
+};
+struct CeLoss {
+    const int *count;
+    const CeRow *rows;
+    const float2 *stats;
+    const float *sums, *picked;
+    int64_t m;
+    int tiles, groups, classes;
+    double hit, flat, z;
+    float *loss, *lse;
+    double *part;
+};
+struct CeSum {
+    const float *part;
+    int64_t part_stride, n;
+    int parts, c;
+    const CeRow *rows;             // results by the list (NULL: row by row, n of them)
+    const int *count;
+    void *out;
+    int64_t out_ld;
+};
+struct CeBias {
+    const int *count;
+    int tile, classes;
+    const float *colsum;
+    int64_t ld;
+    float *out;
+};
+size_t ce_fwd_bytes(const CeCall &a);
+size_t ce_bwd_bytes(const CeCall &a);
+hipError_t launch_ce_fwd(const CeCall &a, void *ws, hipStream_t s);
+hipError_t launch_ce_bwd(const CeCall &a, void *ws, hipStream_t s);
+
 // Newton-Schulz orthogonalisation of a list of matrices (newton_schulz.hip).
 struct NsIn {                     // one matrix as the caller gives it, row-major
     const void *src;              // matrix to orthogonalise, or gradient

@@ -1,0 +1,815 @@
+// linear_ce.hip -- the last linear layer and its softmax cross entropy over many
+// classes, whose logits are never kept, and its gradients.
+//
+//   l[i][v] = sum_k h[i][k] w[v][k] + bias[v],   lse[i] = log sum_v exp l[i][v]
+//   loss[i] = lse - (1 - s) l[i][label] - (s / V) sum_v l[i][v] + z lse^2
+//   g[i][v] = r[i] (exp(l - lse) (1 + 2 z lse) - (1 - s) [v = label] - s / V)
+//   dh = g w,  dw = g^T h,  dbias = column sums of g
+//
+// r[i] is the loss's gradient (1 / rows that count for the mean).  Rows of the
+// ignored label are left out of every product: the first launch (k_ce_list) copies
+// the rows that count together, so padding costs nothing and what stands in it
+// reaches nothing.
+//
+// Forward: one matrix product whose tiles never leave the registers as logits; a
+// tile's epilogue gives each row's maximum and sum of exponentials over its columns,
+// and k_ce_rows joins them.  Backward: the classes in pieces; a piece's logits are
+// formed again, g is written in the storage type (the operand type of the two
+// products that follow, as every stored gradient of this library), then the piece's
+// rows of dw and its share of dh are formed.  dh adds up over pieces in float32.
+//
+// Every product is k_ce_gemm: C[i][j] = sum_k I[i][k] J[j][k] with operands that lie
+// along k ("rows") or across it ("columns"); matrix instructions take the weights'
+// side as their rows, so that a lane holds four neighbouring results of one row.
+#include "common.hpp"
+#include "kernels.hpp"
+#include "mfma.hpp"
+#include "trace.hpp"
+
+#include <type_traits>
+
+namespace bnr {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+
+// exp(x) by the base-2 instruction; the product's rounding, which would cost |x| 2^-24
+// of the result, is put back.
+__device__ __forceinline__ float ce_exp(float x)
+{
+    const float t = x * kLog2e, e = __builtin_amdgcn_exp2f(t);
+    const float lo = __builtin_fmaf(x, kLog2e, -t);
+    return x > -100.f ? __builtin_fmaf(e, lo * 0.6931471805599453f, e) : e;   // (lo is NaN for -inf)
+}
+
+// ---- rows that count -------------------------------------------------------
+constexpr int kListRows = 16;              // rows a workgroup of k_ce_list takes
+constexpr int kCountRows = 4096;           // rows a workgroup of k_ce_count takes
+
+__device__ __forceinline__ int ce_counted(const int32_t *labels, int64_t from, int64_t to, int ignore, int tid)
+{
+    int n = 0;
+    #pragma unroll 8
+    for (int64_t i = from + tid; i < to; i += kThreads) n += labels[i] != ignore;
+    return n;
+}
+
+__device__ __forceinline__ int ce_group_sum(int n, int *red, int tid)
+{
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    if ((tid & 63) == 0) red[tid >> 6] = n;
+    __syncthreads();
+    n = 0;
+    for (int w = 0; w < kThreads / 64; w++) n += red[w];
+    return n;
+}
+
+__global__ __launch_bounds__(kThreads) void k_ce_count(CeList p)
+{
+    __shared__ int red[kThreads / 64];
+    const int64_t from = (int64_t)blockIdx.x * kCountRows;
+    const int n = ce_group_sum(ce_counted(p.labels, from, min(from + kCountRows, p.m), p.ignore, threadIdx.x), red, threadIdx.x);
+    if (threadIdx.x == 0) p.counts[blockIdx.x] = n;
+}
+
+// The list of rows that count, in order, with what the products' epilogues need of
+// each; their features copied together; zeros in the other rows' results.
+__global__ __launch_bounds__(kThreads) void k_ce_list(CeList p)
+{
+    __shared__ int red[kThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t first = (int64_t)blockIdx.x * kListRows;
+    int n = 0;
+    int64_t from = 0;
+    if (p.counts) {
+        const int whole = (int)(first / kCountRows);
+        for (int b = tid; b < whole; b += kThreads) n += p.counts[b];
+        from = (int64_t)whole * kCountRows;
+    }
+    n += ce_counted(p.labels, from, first, p.ignore, tid);
+    const int before = ce_group_sum(n, red, tid);
+    const int64_t row = first + lane;
+    const bool mine = lane < kListRows && row < p.m;
+    const int label = mine ? p.labels[row] : p.ignore;
+    const uint64_t here = __ballot(mine && label != p.ignore);
+    if (wave == 0 && mine) {
+        if (label != p.ignore) {
+            CeRow r;
+            r.row = (int)row;
+            r.label = label;
+            r.lse = r.scale = 0.f;
+            if (p.lse) {
+                r.lse = p.lse[1 + row];
+                r.scale = p.dloss ? p.dloss[0] / p.lse[0] + p.dloss[1 + row] : 1.0f / p.lse[0];
+                if ((uint32_t)label >= (uint32_t)p.classes) r.scale = NAN;
+            }
+            p.rows[before + __popcll(here & ((1ull << lane) - 1))] = r;
+        } else if (p.zero_loss) {
+            p.zero_loss[1 + row] = 0.f;
+            p.zero_lse[1 + row] = 0.f;
+        }
+    }
+    if (tid == 0 && first + kListRows >= p.m) *p.count = before + __popcll(here);
+    const int vecs = p.row_bytes / 16;
+    for (int k = wave; k < kListRows; k += kThreads / 64) {
+        if (first + k >= p.m) break;
+        if (here >> k & 1) {
+            const char *src = (const char *)p.h + (first + k) * p.h_ld;
+            char *dst = (char *)p.copy + (int64_t)(before + __popcll(here & ((1ull << k) - 1))) * p.row_bytes;
+            #pragma unroll 4
+            for (int i = lane; i < vecs; i += 64) stg16(dst + i * 16, ldg16(src + i * 16));
+        } else if (p.zero) {
+            char *dst = (char *)p.zero + (first + k) * p.zero_ld;
+            for (int i = lane; i < vecs; i += 64) stg16(dst + i * 16, zero16());
+        }
+    }
+}
+
+// ---- the product -----------------------------------------------------------
+// Operand tiles in LDS, 128 bytes for each of a stage's rows or columns:
+//   rows     B rows of 128 bytes along k, as 16-byte chunks in the order
+//            chunk ^ (row / 2 % 8), so that 16 rows of one chunk lie in different banks
+//   columns  the stage's k one after another, B values each; in bf16 the chunks of a
+//            k in the order chunk ^ 2 (k % 4 + 4 (k / 8 % 2)), for the transposing reads
+// The order is made by the addresses that the lanes load straight into LDS from.
+template <typename T, int B, int NT, bool COLS>
+struct CeLoad {
+    static constexpr int kLoads = B * 128 / (NT * 16), BK = 128 / sizeof(T);
+    uint32_t off[kLoads], at[kLoads];              // at: the chunk's place along k (rows)
+    __device__ __forceinline__ void init(int64_t ld, int tid)
+    {
+        #pragma unroll
+        for (int l = 0; l < kLoads; l++) {
+            const uint32_t byte = (l * NT + tid) * 16;
+            if constexpr (COLS) {
+                constexpr uint32_t kRow = B * sizeof(T);
+                const uint32_t k = byte / kRow, slot = byte % kRow / 16;
+                const uint32_t turn = sizeof(T) == 2 ? 2 * (k % 4 + 4 * (k / 8 % 2)) : 0;
+                off[l] = k * (uint32_t)ld + (slot ^ turn) * 16;
+                at[l] = 0;
+            } else {
+                const uint32_t row = byte / 128, slot = byte % 128 / 16;
+                at[l] = (slot ^ (row / 2 % 8)) * 16;
+                off[l] = row * (uint32_t)ld + at[l];
+            }
+        }
+    }
+    // stage `k0` of an operand whose tile starts at base, with `extent` rows (columns) left
+    __device__ __forceinline__ void load(unsigned char *lds, const char *base, int64_t ld, int extent, int k0, int k,
+                                         int wave) const
+    {
+        const int left = min(k - k0, BK), wide = min(extent, B);
+        const char *src = base + (COLS ? k0 * ld : k0 * (int64_t)sizeof(T));
+        // (c is a multiple of the 16-byte vector, and g's rows are whole vectors: a column tile's last vector is read whole)
+        const uint32_t bytes = COLS ? (left - 1) * (uint32_t)ld + (wide * sizeof(T) + 15) / 16 * 16
+                                    : (wide - 1) * (uint32_t)ld + left * sizeof(T);
+        const __amdgpu_buffer_rsrc_t r = buf_view(src, bytes);
+        #pragma unroll
+        for (int l = 0; l < kLoads; l++) {
+            uint32_t o = off[l];
+            if constexpr (!COLS) o = at[l] < left * sizeof(T) ? o : kBufOff;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + (l * NT + wave * 64) * 16),
+                                                     16, o, 0, 0, 0);
+        }
+    }
+};
+
+// Fragments of NB blocks of 16 rows (columns) from w0 on, of sub-step `sub` (64 bytes
+// along k).  Block b's lane value q stands for row 16 b + q, in float32 columns for
+// NB q + b (a lane's neighbouring values, one read).
+template <typename T, int B, int NB, bool COLS> struct CeFrags;
+template <int B, int NB> struct CeFrags<bf16_t, B, NB, false> {
+    uint32_t at;
+    __device__ __forceinline__ void init(int w0, int lane) { at = (w0 + lane % 16) * 128; }
+    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, bf16x8 *f) const
+    {
+        const unsigned char *p = lds + at + ((sub * 4 + lane / 16) ^ (lane % 16 / 2)) * 16;
+        #pragma unroll
+        for (int b = 0; b < NB; b++) f[b] = *reinterpret_cast<const bf16x8 *>(p + b * 2048);
+    }
+};
+template <int B, int NB> struct CeFrags<float, B, NB, false> {
+    uint32_t at;
+    __device__ __forceinline__ void init(int w0, int lane) { at = (w0 + lane % 16) * 128; }
+    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, f32x4 *f) const
+    {
+        const unsigned char *p = lds + at + ((sub * 4 + lane / 16) ^ (lane % 16 / 2)) * 16;
+        #pragma unroll
+        for (int b = 0; b < NB; b++) f[b] = *reinterpret_cast<const f32x4 *>(p + b * 2048);
+    }
+};
+template <int B, int NB> struct CeFrags<bf16_t, B, NB, true> {
+    static_assert(B >= 128, "the order of a k's chunks spans 256 bytes");
+    uint32_t at[NB];
+    __device__ __forceinline__ void init(int w0, int lane)
+    {
+        const uint32_t q = lane % 16, k = 8 * (lane / 16) + q / 4, turn = 2 * (k % 4 + 4 * (k / 8 % 2));
+        #pragma unroll
+        for (int b = 0; b < NB; b++) at[b] = k * (B * 2) + ((((w0 + 16 * b) / 8 + q % 4 / 2) ^ turn) * 16) + q % 2 * 8;
+    }
+    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, bf16x8 *f) const
+    {
+        #pragma unroll
+        for (int b = 0; b < NB; b++) f[b] = tr_frag((const bf16_t *)(lds + at[b] + sub * 32 * B * 2), B);
+    }
+};
+template <int B, int NB> struct CeFrags<float, B, NB, true> {
+    static_assert(NB == 4, "four blocks' values are one read");
+    uint32_t at;
+    __device__ __forceinline__ void init(int w0, int lane) { at = 4 * (lane / 16) * (B * 4) + (w0 + 4 * (lane % 16)) * 4; }
+    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, f32x4 *f) const
+    {
+        #pragma unroll
+        for (int t = 0; t < 4; t++) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(lds + at + (sub * 16 + t) * (B * 4));
+            #pragma unroll
+            for (int b = 0; b < NB; b++) f[b][t] = v[b];
+        }
+    }
+};
+
+__device__ __forceinline__ void ce_mma(f32x4 &c, bf16x8 a, bf16x8 b) { c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ void ce_mma(f32x4 &c, f32x4 a, f32x4 b)
+{
+    #pragma unroll
+    for (int t = 0; t < 4; t++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[t], b[t], c, 0, 0, 0);
+}
+
+// four neighbouring results
+__device__ __forceinline__ void ce_store4(float *p, const float *v) { *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void ce_store4(bf16_t *p, const float *v)
+{
+    *reinterpret_cast<u32x2_t *>(p) = u32x2_t{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
+}
+
+// A workgroup's tile: tiles of one k range first; eight row tiles take turns over the
+// column tiles, so that the workgroups of an XCD share both operands in its L2.
+struct CePlace { int ti, tj, part; };
+__device__ __forceinline__ bool ce_place(CePlace &pl, int nti, int ntj, int parts)
+{
+    const int tiles = nti * ntj, total = tiles * parts;
+    if ((int)blockIdx.x >= total) return false;
+    const int id = xcd_remap(blockIdx.x, total);
+    pl.part = id / tiles;
+    const int t = id - pl.part * tiles, per = 8 * ntj, first = t / per * 8, n = min(8, nti - first), r = t % per;
+    pl.ti = first + r % n;
+    pl.tj = r / n;
+    return true;
+}
+
+template <typename T, int BI, int BJ, int WI, int WJ, int MODE>
+__global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
+{
+    constexpr bool ICOLS = MODE == CE_DW, JCOLS = MODE == CE_DW || MODE == CE_DH;
+    constexpr int NT = WI * WJ * 64, TI = BI / WI, TJ = BJ / WJ, MI = TI / 16, NJ = TJ / 16, BK = 128 / sizeof(T);
+    constexpr int kStage = (BI + BJ) * 128;
+    typedef typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type frag;
+    __shared__ __align__(16) unsigned char lds0[kStage], lds1[kStage];
+    const int count = *p.count;
+    const int ni = MODE == CE_DW ? p.classes : count, nj = MODE == CE_DW || MODE == CE_DH ? p.c : p.classes;
+    const int K = MODE == CE_DW ? count : (MODE == CE_DH ? p.classes : p.c);
+    CePlace pl;
+    if (!ce_place(pl, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, p.parts)) return;
+    const int i0 = pl.ti * BI, j0 = pl.tj * BJ;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = wave / WJ, wj = wave % WJ, q = lane % 16, g = lane / 16;
+
+    const char *ibase = (const char *)p.i + (ICOLS ? (int64_t)i0 * sizeof(T) : i0 * p.i_ld);
+    const char *jbase = (const char *)p.j + (JCOLS ? (int64_t)j0 * sizeof(T) : j0 * p.j_ld);
+    CeLoad<T, BI, NT, ICOLS> li;
+    CeLoad<T, BJ, NT, JCOLS> lj;
+    li.init(p.i_ld, tid);
+    lj.init(p.j_ld, tid);
+    // g's rows are whole vectors of zeros past the classes: their last vector is read whole
+    const int Ki = MODE == CE_DH ? (K + 7) / 8 * 8 : K;
+    auto load = [&](unsigned char *stage, int k) __attribute__((always_inline)) {
+        li.load(stage, ibase, p.i_ld, ni - i0, k, Ki, wave);
+        lj.load(stage + BI * 128, jbase, p.j_ld, nj - j0, k, K, wave);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    CeFrags<T, BI, MI, ICOLS> ri;
+    CeFrags<T, BJ, NJ, JCOLS> rj;
+    ri.init(wi * TI, lane);
+    rj.init(wj * TJ, lane);
+    f32x4 acc[NJ][MI];
+    #pragma unroll
+    for (int b = 0; b < NJ; b++)
+        #pragma unroll
+        for (int a = 0; a < MI; a++) acc[b][a] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](const unsigned char *stage) __attribute__((always_inline)) {
+        #pragma unroll
+        for (int sub = 0; sub < 2; sub++) {
+            frag fi[MI], fj[NJ];
+            ri.read(stage, sub, lane, fi);
+            rj.read(stage + BI * 128, sub, lane, fj);
+            #pragma unroll
+            for (int a = 0; a < MI; a++)
+                #pragma unroll
+                for (int b = 0; b < NJ; b++) ce_mma(acc[b][a], fj[b], fi[a]);
+        }
+    };
+    const int steps = (K + BK - 1) / BK;
+    const int s0 = (int)((int64_t)pl.part * steps / p.parts), s1 = (int)((int64_t)(pl.part + 1) * steps / p.parts);
+    if (s0 < s1) {
+        load(lds0, s0 * BK);
+        __syncthreads();
+        for (int s = s0; s < s1; s += 2) {
+            if (s + 1 < s1) load(lds1, (s + 1) * BK);
+            multiply(lds0);
+            __syncthreads();
+            if (s + 1 >= s1) break;
+            if (s + 2 < s1) load(lds0, (s + 2) * BK);
+            multiply(lds1);
+            __syncthreads();
+        }
+    }
+
+    const int iw = i0 + wi * TI, jw = j0 + wj * TJ;
+    if constexpr (MODE == CE_STATS) {
+        // each row's maximum, sum of exponentials and sum over the tile's columns
+        float *red = reinterpret_cast<float *>(lds0);
+        #pragma unroll
+        for (int b = 0; b < NJ; b++)
+            #pragma unroll
+            for (int r = 0; r < 4; r++) {
+                const int j = jw + 16 * b + 4 * g + r;
+                const float add = j < nj ? (p.bias ? p.bias[j] : 0.f) : -INFINITY;
+                #pragma unroll
+                for (int a = 0; a < MI; a++) acc[b][a][r] += add;
+            }
+        #pragma unroll
+        for (int a = 0; a < MI; a++) {
+            const int i = iw + 16 * a + q, label = i < ni ? p.rows[i].label : -1;
+            float mx = -INFINITY, sum = 0.f, all = 0.f;
+            #pragma unroll
+            for (int b = 0; b < NJ; b++)
+                #pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    const int j = jw + 16 * b + 4 * g + r;
+                    mx = fmaxf(mx, acc[b][a][r]);
+                    all += j < nj ? acc[b][a][r] : 0.f;
+                    if (j == label && j < nj) p.picked[i] = acc[b][a][r];
+                }
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float base = mx == -INFINITY ? 0.f : mx;
+            #pragma unroll
+            for (int b = 0; b < NJ; b++)
+                #pragma unroll
+                for (int r = 0; r < 4; r++) sum += ce_exp(acc[b][a][r] - base);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            all += __shfl_xor(all, 16, 64);
+            all += __shfl_xor(all, 32, 64);
+            if (g == 0) {
+                float *o = red + (wj * BI + wi * TI + 16 * a + q) * 3;
+                o[0] = mx; o[1] = sum; o[2] = all;
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < BI; i += NT) {
+            if (i0 + i >= ni) break;
+            float mx = -INFINITY, sum = 0.f, all = 0.f;
+            #pragma unroll
+            for (int w = 0; w < WJ; w++) mx = fmaxf(mx, red[(w * BI + i) * 3]);
+            const float base = mx == -INFINITY ? 0.f : mx;
+            #pragma unroll
+            for (int w = 0; w < WJ; w++) {
+                sum += red[(w * BI + i) * 3 + 1] * ce_exp(red[(w * BI + i) * 3] - base);
+                all += red[(w * BI + i) * 3 + 2];
+            }
+            const int64_t o = (int64_t)pl.tj * p.m + i0 + i;
+            p.stats[o] = float2{mx, sum};
+            if (p.sums) p.sums[o] = all;
+        }
+    } else if constexpr (MODE == CE_GRAD) {
+        float *red = reinterpret_cast<float *>(lds0);
+        float col[NJ][4];
+        #pragma unroll
+        for (int b = 0; b < NJ; b++)
+            #pragma unroll
+            for (int r = 0; r < 4; r++) {
+                const int j = jw + 16 * b + 4 * g + r;
+                const float add = p.bias && j < nj ? p.bias[j] : 0.f;
+                col[b][r] = 0.f;
+                #pragma unroll
+                for (int a = 0; a < MI; a++) acc[b][a][r] += add;
+            }
+        #pragma unroll
+        for (int a = 0; a < MI; a++) {
+            const int i = iw + 16 * a + q;
+            if (i >= ni) continue;
+            const CeRow row = p.rows[i];
+            const int at = row.label - p.first;
+            const float grow = row.scale * (1.f + 2.f * p.z * row.lse), flat = row.scale * p.flat, hit = row.scale * p.hit;
+            T *o = (T *)p.g + (int64_t)i * p.g_ld;
+            #pragma unroll
+            for (int b = 0; b < NJ; b++) {
+                float v[4];
+                const int j = jw + 16 * b + 4 * g;
+                #pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    v[r] = __builtin_fmaf(ce_exp(acc[b][a][r] - row.lse), grow, -flat) - (j + r == at ? hit : 0.f);
+                    v[r] = j + r < nj ? v[r] : 0.f;
+                    col[b][r] += v[r];
+                }
+                if (j < p.g_ld) ce_store4(o + j, v);
+            }
+        }
+        if (p.colsum) {
+            #pragma unroll
+            for (int b = 0; b < NJ; b++)
+                #pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    float v = col[b][r];
+                    for (int o = 1; o < 16; o *= 2) v += __shfl_xor(v, o, 64);
+                    if (q == 0) red[wi * BJ + wj * TJ + 16 * b + 4 * g + r] = v;
+                }
+            __syncthreads();
+            for (int j = tid; j < BJ; j += NT) {
+                if (j0 + j >= nj) break;
+                float v = 0.f;
+                #pragma unroll
+                for (int w = 0; w < WI; w++) v += red[w * BJ + j];
+                p.colsum[(int64_t)pl.ti * p.colsum_ld + j0 + j] = v;
+            }
+        }
+    } else {
+        // the results themselves: i = 16 a + q and j = 16 b + 4 g + r, in float32 columns i = MI q + a, j = NJ (4 g + r) + b
+        constexpr bool IP = ICOLS && sizeof(T) == 4, JP = JCOLS && sizeof(T) == 4;
+        #pragma unroll
+        for (int a = 0; a < MI; a++) {
+            const int i = iw + (IP ? MI * q + a : 16 * a + q);
+            if (i >= ni) continue;
+            const int64_t row = p.part_stride || MODE == CE_DW ? i : p.rows[i].row;
+            #pragma unroll
+            for (int b = 0; b < NJ; b++) {
+                const int j = jw + (JP ? 16 * g + 4 * b : 16 * b + 4 * g);
+                if (j >= nj) continue;               // (c is a multiple of four)
+                float v[4];
+                #pragma unroll
+                for (int r = 0; r < 4; r++) v[r] = JP ? acc[r][a][b] : acc[b][a][r];
+                if (p.out_f32) {
+                    float *o = (float *)p.out + (int64_t)pl.part * p.part_stride + row * p.out_ld + j;
+                    if (p.add) {
+                        const f32x4 old = *reinterpret_cast<const f32x4 *>(o);
+                        #pragma unroll
+                        for (int r = 0; r < 4; r++) v[r] += old[r];
+                    }
+                    ce_store4(o, v);
+                } else {
+                    ce_store4((bf16_t *)p.out + row * p.out_ld + j, v);
+                }
+            }
+        }
+    }
+}
+
+// ---- rows' losses ------------------------------------------------------------
+constexpr int kLossRows = 16;              // rows a workgroup takes, 16 threads each
+
+__device__ __forceinline__ void ce_join(float &mx, double &sum, float mx2, double sum2)
+{
+    const float top = fmaxf(mx, mx2), base = top == -INFINITY ? 0.f : top;
+    sum = sum * ce_exp(mx - base) + sum2 * ce_exp(mx2 - base);
+    mx = top;
+}
+
+// The rows' losses and log sums from the tiles' maxima and sums (in float64), and the
+// sum of the workgroup's losses.
+__global__ __launch_bounds__(kThreads) void k_ce_rows(CeLoss p)
+{
+    __shared__ float rm[4][kLossRows];
+    __shared__ double rs[4][kLossRows], ra[4][kLossRows];
+    const int tid = threadIdx.x, r = tid % kLossRows, slice = tid / kLossRows, count = *p.count;
+    const int i = blockIdx.x * kLossRows + r;
+    if (blockIdx.x && (int)blockIdx.x * kLossRows >= count) return;
+    float mx = -INFINITY;
+    double sum = 0.0, all = 0.0;
+    if (i < count) {
+        #pragma unroll 4
+        for (int t = slice; t < p.tiles; t += kThreads / kLossRows) {
+            const float2 v = p.stats[(int64_t)t * p.m + i];
+            if (p.sums) all += (double)p.sums[(int64_t)t * p.m + i];
+            ce_join(mx, sum, v.x, (double)v.y);
+        }
+    }
+    for (int o = kLossRows; o < 64; o *= 2) {
+        ce_join(mx, sum, __shfl_xor(mx, o, 64), __shfl_xor(sum, o, 64));
+        all += __shfl_xor(all, o, 64);
+    }
+    if ((tid & 63) < kLossRows) { rm[tid >> 6][r] = mx; rs[tid >> 6][r] = sum; ra[tid >> 6][r] = all; }
+    __syncthreads();
+    if (tid >= kLossRows) return;
+    double loss = 0.0;
+    if (i < count) {
+        for (int w = 1; w < 4; w++) {
+            ce_join(mx, sum, rm[w][r], rs[w][r]);
+            all += ra[w][r];
+        }
+        const CeRow row = p.rows[i];
+        const double lse = (double)mx + log(sum);
+        loss = NAN;
+        if ((uint32_t)row.label < (uint32_t)p.classes) {
+            loss = lse - p.hit * (double)p.picked[i] + p.z * lse * lse;
+            if (p.sums) loss -= p.flat * all;
+        }
+        p.lse[1 + row.row] = (float)lse;
+        p.loss[1 + row.row] = (float)loss;
+    }
+    for (int o = 1; o < kLossRows; o *= 2) loss += __shfl_xor(loss, o, 64);
+    if (tid) return;
+    if (p.groups == 1) {
+        p.loss[0] = count ? (float)(loss / count) : 0.f;
+        p.lse[0] = (float)count;
+    } else {
+        p.part[blockIdx.x] = loss;
+    }
+}
+
+__global__ __launch_bounds__(1024) void k_ce_mean(CeLoss p)
+{
+    __shared__ double red[16];
+    const int tid = threadIdx.x, count = *p.count, groups = (count + kLossRows - 1) / kLossRows;
+    double v = 0.0;
+    for (int b = tid; b < groups; b += 1024) v += p.part[b];
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    if ((tid & 63) == 0) red[tid >> 6] = v;
+    __syncthreads();
+    if (tid) return;
+    v = 0.0;
+    for (int w = 0; w < 16; w++) v += red[w];
+    p.loss[0] = count ? (float)(v / count) : 0.f;
+    p.lse[0] = (float)count;
+}
+
+// ---- sums over parts -----------------------------------------------------------
+// out[row][j .. j + 3] = the sum of the parts' float32 results, in order.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_ce_sum(CeSum p)
+{
+    const int vecs = p.c / 4;
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, i = id / vecs;
+    const int j = (int)(id - i * vecs) * 4;
+    if (i >= (p.rows ? *p.count : p.n)) return;
+    const float *src = p.part + i * p.c + j;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    #pragma unroll 4
+    for (int s = 0; s < p.parts; s++) {
+        const f32x4 u = *reinterpret_cast<const f32x4 *>(src + s * p.part_stride);
+        #pragma unroll
+        for (int r = 0; r < 4; r++) v[r] += u[r];
+    }
+    const int64_t row = p.rows ? p.rows[i].row : i;
+    ce_store4((T *)p.out + row * p.out_ld + j, v);
+}
+
+__global__ __launch_bounds__(kThreads) void k_ce_bias(CeBias p)
+{
+    const int j = blockIdx.x * kThreads + threadIdx.x, tiles = (*p.count + p.tile - 1) / p.tile;
+    if (j >= p.classes) return;
+    double v = 0.0;
+    #pragma unroll 4
+    for (int t = 0; t < tiles; t++) v += (double)p.colsum[(int64_t)t * p.ld + j];
+    p.out[j] = (float)v;
+}
+
+// ---- how a call runs -------------------------------------------------------------
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
+
+// Tiles of 256 x 256 (one workgroup of eight waves a CU) where they fill the chip,
+// else of 128 x 128 (two workgroups of four waves a CU).
+inline int ce_tile(int dtype, int64_t ni, int64_t nj)
+{
+    return dtype == DT_BF16 && cdiv(ni, 256) * cdiv(nj, 256) >= 192 ? 256 : 128;
+}
+
+// k ranges a product is cut into where its tiles would leave the chip idle
+inline int ce_parts(int tile, int64_t ni, int64_t nj, int64_t steps)
+{
+    const int64_t slots = tile == 256 ? 256 : 512, tiles = cdiv(ni, tile) * cdiv(nj, tile);
+    const int64_t want = slots / tiles, most = steps / 4;
+    const int64_t n = want < most ? want : most;
+    return n < 1 ? 1 : (n > 64 ? 64 : (int)n);
+}
+
+template <typename T, int MODE>
+hipError_t go(const CeGemm &p, int tile, int64_t grid, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (tile == 256) {
+            hipLaunchKernelGGL((k_ce_gemm<T, 256, 256, 2, 4, MODE>), dim3((unsigned)grid), dim3(512), 0, s, p);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((k_ce_gemm<T, 128, 128, 2, 2, MODE>), dim3((unsigned)grid), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+template <int MODE>
+hipError_t gemm(const CeCall &a, const CeGemm &p, int tile, int64_t ni, int64_t nj, int64_t k, hipStream_t s)
+{
+    const double es = a.dtype == DT_BF16 ? 2 : 4;
+    TraceScope tr(KC_CONV, KID_LINEAR_CE, s, es * ((double)ni * k + (double)nj * k + (double)ni * nj), 2.0 * ni * nj * k);
+    const int64_t grid = cdiv(ni, tile) * cdiv(nj, tile) * p.parts;
+    return a.dtype == DT_BF16 ? go<bf16_t, MODE>(p, tile, grid, s) : go<float, MODE>(p, tile, grid, s);
+}
+
+// What both directions keep in the workspace: the count, the list and the rows' copy.
+struct CeHead {
+    int64_t counts, rows, copy, end;
+    explicit CeHead(const CeCall &a)
+    {
+        const int64_t es = a.dtype == DT_BF16 ? 2 : 4;
+        counts = 256;
+        rows = up256(counts + (a.m > 4 * kCountRows ? cdiv(a.m, kCountRows) * 4 : 0));
+        copy = up256(rows + a.m * (int64_t)sizeof(CeRow));
+        end = up256(copy + a.m * (int64_t)a.c * es);
+    }
+};
+
+hipError_t launch_list(const CeCall &a, const CeHead &w, char *ws, hipStream_t s)
+{
+    const int es = a.dtype == DT_BF16 ? 2 : 4;
+    CeList p{};
+    p.m = a.m; p.classes = a.classes; p.ignore = a.ignore;
+    p.labels = a.labels;
+    p.count = (int *)ws;
+    p.counts = a.m > 4 * kCountRows ? (int *)(ws + w.counts) : nullptr;
+    p.rows = (CeRow *)(ws + w.rows);
+    p.h = a.h; p.h_ld = a.h_ld * es;
+    p.copy = ws + w.copy; p.row_bytes = a.c * es;
+    if (a.loss) { p.zero_loss = a.loss; p.zero_lse = a.lse; }
+    else { p.lse = a.lse; p.dloss = a.dloss; p.zero = a.dh; p.zero_ld = a.dh_ld * es; }
+    TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 2.0 * a.m * p.row_bytes, 0.0);
+    if (p.counts) hipLaunchKernelGGL(k_ce_count, dim3((unsigned)cdiv(a.m, kCountRows)), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL(k_ce_list, dim3((unsigned)cdiv(a.m, kListRows)), dim3(kThreads), 0, s, p);
+    return hipGetLastError();
+}
+
+struct CeFwdPlan {
+    CeHead head;
+    int tile;
+    int64_t tiles, groups, stats, sums, picked, part, end;
+    explicit CeFwdPlan(const CeCall &a) : head(a)
+    {
+        tile = ce_tile(a.dtype, a.m, a.classes);
+        tiles = cdiv(a.classes, tile);
+        groups = cdiv(a.m, kLossRows);
+        stats = head.end;
+        sums = up256(stats + tiles * a.m * 8);
+        picked = up256(sums + (a.smoothing > 0.f ? tiles * a.m * 4 : 0));
+        part = up256(picked + a.m * 4);
+        end = up256(part + groups * 8);
+    }
+};
+
+// The widest piece of the classes whose g takes at most kPieceBytes.
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+constexpr int64_t kPieceWidth = kCeMaxLd;
+struct CeBwdPlan {
+    CeHead head;
+    int64_t pieces, width;                 // classes of a piece, a multiple of 256
+    int grad_tile, dh_tile, dw_tile, dh_parts, dw_parts;
+    int64_t g, dh, dw, colsum, end;
+    explicit CeBwdPlan(const CeCall &a) : head(a)
+    {
+        const int64_t es = a.dtype == DT_BF16 ? 2 : 4, bk = 128 / es;
+        int64_t most = kPieceBytes / (a.m * es) / 256 * 256;
+        most = most < 256 ? 256 : (most > kPieceWidth ? kPieceWidth : most);
+        pieces = cdiv(a.classes, most);
+        width = cdiv(cdiv(a.classes, pieces), 256) * 256;
+        pieces = cdiv(a.classes, width);
+        const int64_t wide = width < a.classes ? width : a.classes;
+        grad_tile = ce_tile(a.dtype, a.m, wide);
+        dh_tile = ce_tile(a.dtype, a.m, a.c);
+        dw_tile = ce_tile(a.dtype, wide, a.c);
+        dh_parts = ce_parts(dh_tile, a.m, a.c, cdiv(wide, bk));
+        dw_parts = ce_parts(dw_tile, wide, a.c, cdiv(a.m, bk));
+        g = head.end;
+        dh = up256(g + a.m * width * es);
+        dw = up256(dh + (a.dh && (pieces > 1 || dh_parts > 1) ? dh_parts * a.m * a.c * 4 : 0));
+        colsum = up256(dw + (a.dw && dw_parts > 1 ? dw_parts * wide * a.c * 4 : 0));
+        end = up256(colsum + (a.dbias ? cdiv(a.m, grad_tile) * a.classes * 4 : 0));
+    }
+};
+
+hipError_t sum_parts(const CeSum &p, int dtype, int64_t rows, hipStream_t s)
+{
+    TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, ((double)p.parts * 4 + (dtype == DT_BF16 ? 2 : 4)) * rows * p.c, 0.0);
+    const unsigned grid = (unsigned)cdiv(rows * (p.c / 4), kThreads);
+    if (dtype == DT_BF16) hipLaunchKernelGGL(k_ce_sum<bf16_t>, dim3(grid), dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL(k_ce_sum<float>, dim3(grid), dim3(kThreads), 0, s, p);
+    return hipGetLastError();
+}
+
+#define CE_TRY(e)                            \
+    do {                                     \
+        const hipError_t _e = (e);           \
+        if (_e != hipSuccess) return _e;     \
+    } while (0)
+
+}  // namespace
+
+size_t ce_fwd_bytes(const CeCall &a) { return (size_t)CeFwdPlan(a).end; }
+size_t ce_bwd_bytes(const CeCall &a) { return (size_t)CeBwdPlan(a).end; }
+
+hipError_t launch_ce_fwd(const CeCall &a, void *ws_, hipStream_t s)
+{
+    char *ws = (char *)ws_;
+    const CeFwdPlan w(a);
+    const int es = a.dtype == DT_BF16 ? 2 : 4;
+    CE_TRY(launch_list(a, w.head, ws, s));
+    CeGemm p{};
+    p.count = (const int *)ws; p.rows = (const CeRow *)(ws + w.head.rows);
+    p.c = a.c; p.classes = a.classes; p.m = a.m; p.parts = 1;
+    p.i = ws + w.head.copy; p.i_ld = (int64_t)a.c * es;
+    p.j = a.w; p.j_ld = a.w_ld * es;
+    p.bias = a.bias;
+    p.stats = (float2 *)(ws + w.stats);
+    p.sums = a.smoothing > 0.f ? (float *)(ws + w.sums) : nullptr;
+    p.picked = (float *)(ws + w.picked);
+    CE_TRY(gemm<CE_STATS>(a, p, w.tile, a.m, a.classes, a.c, s));
+    CeLoss l{};
+    l.count = p.count; l.rows = p.rows; l.stats = p.stats; l.sums = p.sums; l.picked = p.picked;
+    l.m = a.m; l.tiles = (int)w.tiles; l.groups = (int)w.groups; l.classes = a.classes;
+    l.hit = 1.0 - (double)a.smoothing; l.flat = (double)a.smoothing / a.classes; l.z = a.z;
+    l.loss = a.loss; l.lse = a.lse; l.part = (double *)(ws + w.part);
+    TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 8.0 * a.m * w.tiles, 0.0);
+    hipLaunchKernelGGL(k_ce_rows, dim3((unsigned)w.groups), dim3(kThreads), 0, s, l);
+    if (w.groups > 1) hipLaunchKernelGGL(k_ce_mean, dim3(1), dim3(1024), 0, s, l);
+    return hipGetLastError();
+}
+
+hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
+{
+    char *ws = (char *)ws_;
+    const CeBwdPlan w(a);
+    const int es = a.dtype == DT_BF16 ? 2 : 4;
+    CE_TRY(launch_list(a, w.head, ws, s));
+    CeGemm p{};
+    p.count = (const int *)ws; p.rows = (const CeRow *)(ws + w.head.rows);
+    p.c = a.c; p.m = a.m;
+    p.z = a.z; p.hit = 1.f - a.smoothing; p.flat = a.smoothing / (float)a.classes;
+    p.g = ws + w.g; p.g_ld = w.width;
+    p.colsum_ld = a.classes;
+    const char *copy = ws + w.head.copy;
+    const bool gather_dh = w.pieces > 1 || w.dh_parts > 1;
+    for (int64_t n = 0; n < w.pieces; n++) {
+        const int64_t first = n * w.width;
+        const int64_t wide = a.classes - first < w.width ? a.classes - first : w.width;
+        const char *weights = (const char *)a.w + first * a.w_ld * es;
+        p.classes = (int)wide; p.first = (int)first;
+        CeGemm q = p;
+        q.parts = 1;
+        q.i = copy; q.i_ld = (int64_t)a.c * es;
+        q.j = weights; q.j_ld = a.w_ld * es;
+        q.bias = a.bias ? a.bias + first : nullptr;
+        q.colsum = a.dbias ? (float *)(ws + w.colsum) + first : nullptr;
+        CE_TRY(gemm<CE_GRAD>(a, q, w.grad_tile, a.m, wide, a.c, s));
+        if (a.dw) {
+            q = p;
+            q.i = p.g; q.i_ld = w.width * es;
+            q.j = copy; q.j_ld = (int64_t)a.c * es;
+            q.parts = w.dw_parts;
+            q.out = (char *)a.dw + first * a.dw_ld * (a.dw_dtype == DT_BF16 ? 2 : 4);
+            q.out_ld = a.dw_ld; q.out_f32 = a.dw_dtype == DT_F32;
+            if (w.dw_parts > 1) { q.out = ws + w.dw; q.out_ld = a.c; q.out_f32 = 1; q.part_stride = wide * a.c; }
+            CE_TRY(gemm<CE_DW>(a, q, w.dw_tile, wide, a.c, a.m, s));
+            if (w.dw_parts > 1) {
+                CeSum t{};
+                t.part = (const float *)q.out; t.part_stride = q.part_stride; t.parts = w.dw_parts; t.c = a.c; t.n = wide;
+                t.out = (char *)a.dw + first * a.dw_ld * (a.dw_dtype == DT_BF16 ? 2 : 4); t.out_ld = a.dw_ld;
+                CE_TRY(sum_parts(t, a.dw_dtype, wide, s));
+            }
+        }
+        if (a.dh) {
+            q = p;
+            q.i = p.g; q.i_ld = w.width * es;
+            q.j = weights; q.j_ld = a.w_ld * es;
+            q.parts = w.dh_parts;
+            q.out = a.dh; q.out_ld = a.dh_ld; q.out_f32 = a.dtype == DT_F32;
+            if (gather_dh) { q.out = ws + w.dh; q.out_ld = a.c; q.out_f32 = 1; q.part_stride = a.m * a.c; q.add = n > 0; }
+            CE_TRY(gemm<CE_DH>(a, q, w.dh_tile, a.m, a.c, wide, s));
+        }
+    }
+    if (a.dh && gather_dh) {
+        CeSum t{};
+        t.part = (const float *)(ws + w.dh); t.part_stride = a.m * a.c; t.parts = w.dh_parts; t.c = a.c;
+        t.rows = p.rows; t.count = p.count;
+        t.out = a.dh; t.out_ld = a.dh_ld;
+        CE_TRY(sum_parts(t, a.dtype, a.m, s));
+    }
+    if (a.dbias) {
+        CeBias b{};
+        b.count = p.count; b.tile = w.grad_tile; b.classes = a.classes;
+        b.colsum = (const float *)(ws + w.colsum); b.ld = a.classes; b.out = a.dbias;
+        TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 4.0 * a.classes * (cdiv(a.m, w.grad_tile) + 1), 0.0);
+        hipLaunchKernelGGL(k_ce_bias, dim3((unsigned)cdiv(a.classes, kThreads)), dim3(kThreads), 0, s, b);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace bnr

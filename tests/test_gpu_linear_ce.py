@@ -1,0 +1,365 @@
+"""The linear layer with softmax cross entropy (bnr_linear_ce_fwd / bnr_linear_ce_bwd) against its definition in
+float64.
+
+Tolerances, element-wise, u = 2^-24 and H half a step of the storage type (bf16 2^-8, float32 2^-24):
+  logits  every product is rounded at most once and each of the c additions (and the bias's) once:
+          dl = (c + 8) u S with S = sum_k |h w| + |bias|
+  lse     the log of a sum whose terms are off by max dl absolutely in the exponent and by 8 u relatively (exponent's
+          product, exponential, its correction), added up in at most 64 float32 additions within a lane's and 4 across
+          lanes and waves, and in float64 after that: t = max_v dl + 100 u, and its own rounding u |lse|
+  loss    t + (1 - s) dl[label] + s mean dl + z (2 |lse| + t) t, and its rounding; the mean by the rows' mean
+  g       p (1 + 2 z lse) is off relatively by dl + t + u |lse| (the stored lse) + 16 u, and four roundings of the
+          terms; as an operand it is rounded once more: H |g|
+          Below float32's smallest normal number 2^-126 the exponential and a product's operand may be taken as 0: each
+          is then off by less than 2^-126 whatever its value (r and the terms' factors are at most 4 in size here),
+          TINY = 2^-123 in all
+  dh, dw  the operands' errors times the other operand's magnitudes, as many additions of u as terms (and 64 parts),
+          and the result's rounding; dbias likewise without H
+"""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+MARK = 777.0
+TINY = 2.0 ** -123
+IGNORE = -100
+
+
+def _B():
+    from paper_1807_01702_amd import bnr
+    return bnr
+
+
+def _rows(t, dtype, pad):
+    """t [m, c] as rows of a buffer of stride c + pad that holds NaN elsewhere."""
+    m, c = t.shape
+    buf = torch.full((m, c + pad), float("nan"), dtype=dtype, device="cuda")
+    buf[:, :c] = t.to(dtype)
+    return buf[:, :c]
+
+
+class Case:
+    def __init__(self, m, c, v, dtype, seed=0, bias=False, smoothing=0.0, z=0.0, ignored=0.0, pad=0, std=2.0):
+        g = torch.Generator(device="cuda").manual_seed(seed + 1000 * m + 10 * c + v)
+        n = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=torch.float32)  # noqa: E731
+        self.m, self.c, self.v, self.dtype, self.smoothing, self.z = m, c, v, dtype, smoothing, z
+        self.h, self.w = _rows(n(m, c), dtype, pad), _rows(n(v, c) * (std / c ** 0.5), dtype, pad)
+        self.labels = torch.randint(0, v, (m,), generator=g, device="cuda", dtype=torch.int32)
+        if ignored:
+            self.labels[torch.rand(m, generator=g, device="cuda") < ignored] = IGNORE
+        self.bias = n(v) * 0.3 if bias else None
+        self.ce = _B().CE(self.labels, bias=self.bias, ignore=IGNORE, smoothing=smoothing, z_loss=z)
+        self.loss = torch.full((1 + m,), MARK, device="cuda")
+
+    def forward(self):
+        _B().bnr_linear_ce_fwd(self.h, self.w, self.ce, self.loss)
+
+    def reference(self):
+        h, w = self.h.double(), self.w.double()
+        self.counts = self.labels != IGNORE
+        h = torch.where(self.counts[:, None], h, torch.zeros_like(h))       # what stands in padding reaches nothing
+        self.h64, self.w64 = h, w
+        b = torch.zeros(self.v, dtype=torch.float64, device="cuda") if self.bias is None else self.bias.double()
+        self.l = h @ w.t() + b
+        self.dl = (self.c + 8) * U * (h.abs() @ w.abs().t() + torch.where(b == -np.inf, torch.zeros_like(b), b.abs()))
+        self.lse = torch.logsumexp(self.l, 1)
+        self.t = self.dl.amax(1) + 100 * U
+        self.at = self.labels.clamp(0, self.v - 1).long()[:, None]
+        s = np.float64(np.float32(self.smoothing))
+        self.s, self.zz = s, np.float64(np.float32(self.z))
+        self.rows = self.lse - (1 - s) * self.l.gather(1, self.at)[:, 0] + self.zz * self.lse ** 2
+        if s:
+            self.rows = self.rows - s * self.l.mean(1)
+        tol = self.t + (1 - s) * self.dl.gather(1, self.at)[:, 0] + s * self.dl.mean(1) + \
+            self.zz * (2 * self.lse.abs() + self.t) * self.t
+        self.rows_tol = tol + 2 * U * self.rows.abs() + 1e-300
+
+    def check_forward(self):
+        self.reference()
+        n = int(self.counts.sum())
+        zero = torch.zeros_like(self.lse)
+        lse, rows = torch.where(self.counts, self.lse, zero), torch.where(self.counts, self.rows, zero)
+        _close("lse", self.ce.lse[1:], lse, torch.where(self.counts, self.t + U * lse.abs(), zero))
+        _close("loss", self.loss[1:], rows, torch.where(self.counts, self.rows_tol, zero))
+        assert float(self.ce.lse[0]) == n
+        mean = float(rows.sum() / n) if n else 0.0
+        tol = float(torch.where(self.counts, self.rows_tol, zero).sum() / n) if n else 0.0
+        assert abs(float(self.loss[0]) - mean) <= tol + U * abs(mean)
+
+    def backward(self, dloss=None, dw_dtype=None, want=("dh", "dw", "dbias"), pad=0):
+        m, c, v = self.m, self.c, self.v
+        full = lambda r, dt: torch.full((r, c + pad), MARK, dtype=dt, device="cuda")  # noqa: E731
+        self.bufs = dict(dh=full(m, self.dtype), dw=full(v, dw_dtype or self.dtype))
+        self.dh, self.dw = self.bufs["dh"][:, :c], self.bufs["dw"][:, :c]
+        self.dbias = torch.full((v,), MARK, device="cuda")
+        self.want = want
+        _B().bnr_linear_ce_bwd(self.h, self.w, self.ce, self.dh if "dh" in want else None,
+                               self.dw if "dw" in want else None, self.dbias if "dbias" in want else None, dloss=dloss)
+
+    def check_backward(self, dloss=None):
+        n = int(self.counts.sum())
+        r = torch.full((self.m,), 1.0 / n if n else 0.0, dtype=torch.float64, device="cuda")
+        if dloss is not None:
+            r = dloss[0].double() / max(n, 1) + dloss[1:].double()
+        r = torch.where(self.counts, r, torch.zeros_like(r))[:, None]
+        p = torch.exp(self.l - self.lse[:, None])
+        grow = 1 + 2 * self.zz * self.lse[:, None]
+        hot = torch.zeros_like(p).scatter_(1, self.at, 1.0)
+        g = r * (p * grow - (1 - self.s) * hot - self.s / self.v)
+        rel = self.dl + (self.t + U * self.lse.abs())[:, None] + 16 * U
+        size = r.abs() * (p * grow.abs() + (1 - self.s) * hot + self.s / self.v)
+        dg = r.abs() * p * grow.abs() * torch.expm1(rel) + 8 * U * size
+        as_operand = dg * (1 + HALF[self.dtype]) + HALF[self.dtype] * g.abs() + TINY
+        ga = g.abs() + as_operand
+        h, w = self.h64, self.w64
+        if "dh" in self.want:
+            tol = (as_operand + (self.v + 66) * U * ga) @ w.abs()
+            _close("dh", self.dh, g @ w, tol + HALF[self.dtype] * ((g @ w).abs() + tol))
+        if "dw" in self.want:
+            tol = (as_operand + (self.m + 66) * U * ga).t() @ h.abs()
+            ref = g.t() @ h
+            _close("dw", self.dw, ref, tol + HALF[self.dw.dtype] * (ref.abs() + tol))
+        if "dbias" in self.want:
+            tol = (dg + (self.m + 66) * U * (g.abs() + dg)).sum(0)
+            _close("dbias", self.dbias, g.sum(0), tol + U * g.sum(0).abs() + self.m * TINY)
+        for k in ("dh", "dw"):
+            rest = self.bufs[k][:, self.c:] if k in self.want else self.bufs[k]
+            assert bool((rest == MARK).all()), "wrote outside " + k
+
+
+def _close(name, got, ref, tol):
+    off = (got.double() - ref).abs()
+    bad = ~(off <= tol)
+    assert not bool(bad.any()), "%s: %d of %d values off, worst %.3g of the tolerance" % (
+        name, int(bad.sum()), bad.numel(), float((off / tol.clamp_min(1e-300)).max()))
+
+
+# rows, channels, classes: one of each, the ends of tiles and of a stage along k, few rows and many classes, many rows
+# and few classes, more tiles than the chip has units
+SIZES = [(1, 8, 1), (1, 64, 5), (2, 8, 2), (3, 8, 129), (17, 72, 1000), (64, 64, 64), (128, 64, 128), (129, 136, 257),
+         (300, 264, 513), (5, 1024, 3001), (16, 512, 4099), (33, 96, 2049), (1000, 64, 3), (2500, 32, 130), (70, 2048, 300)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,c,v", SIZES)
+def test_forward_and_backward(m, c, v, dtype):
+    for kw in (dict(), dict(bias=True, smoothing=0.1, z=1e-3, ignored=0.3, pad=8)):
+        k = Case(m, c, v, dtype, **kw)
+        k.forward()
+        k.check_forward()
+        k.backward(pad=kw.get("pad", 0))
+        k.check_backward()
+
+
+@pytest.mark.parametrize("dtype,m,c,v", [(torch.bfloat16, 3100, 2048, 4000), (torch.bfloat16, 3100, 4096, 520),
+                                         (torch.bfloat16, 520, 2056, 6200), (torch.float32, 1030, 520, 2060)])
+def test_large_tiles(dtype, m, c, v):
+    k = Case(m, c, v, dtype, bias=True, ignored=0.1)
+    k.forward()
+    k.check_forward()
+    k.backward()
+    k.check_backward()
+
+
+@pytest.mark.parametrize("dtype,m,v", [(torch.bfloat16, 2100, 140001), (torch.float32, 1100, 130001)])
+def test_pieces(dtype, m, v):
+    """Classes whose gradients pass a piece."""
+    k = Case(m, 64, v, dtype, bias=True, ignored=0.5)
+    k.forward()
+    k.check_forward()
+    k.backward()
+    k.check_backward()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("want", [("dh",), ("dw",), ("dbias",), ("dh", "dw")])
+def test_some_gradients(want, dtype):
+    k = Case(77, 136, 600, dtype, bias=True)
+    k.forward()
+    k.reference()
+    k.backward(want=want)
+    k.check_backward()
+    assert "dbias" in want or bool((k.dbias == MARK).all())
+
+
+@pytest.mark.parametrize("dw_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,c,v", [(200, 64, 300), (3000, 64, 100)])
+def test_weight_gradient_types_and_row_gradients(m, c, v, dtype, dw_dtype):
+    k = Case(m, c, v, dtype, ignored=0.2)
+    k.forward()
+    k.reference()
+    dloss = torch.randn(1 + m, device="cuda")
+    k.backward(dloss=dloss, dw_dtype=dw_dtype)
+    k.check_backward(dloss)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_padding_holds_anything(dtype):
+    """Rows that do not count hold NaN and infinities: nothing of them arrives anywhere."""
+    k = Case(100, 72, 301, dtype, ignored=0.4, smoothing=0.1)
+    pad = k.labels == IGNORE
+    k.h[pad] = float("nan")
+    k.h[torch.nonzero(pad)[0, 0]] = float("inf")
+    k.forward()
+    k.check_forward()
+    k.backward()
+    k.check_backward()
+    assert bool((k.dh[pad] == 0).all()) and bool((k.loss[1:][pad] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m", [1, 40, 300])
+def test_no_row_counts(m, dtype):
+    k = Case(m, 64, 300, dtype)
+    k.labels.fill_(IGNORE)
+    k.forward()
+    k.backward()
+    for t in (k.loss, k.ce.lse, k.dh, k.dw, k.dbias):
+        assert bool((t == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_labels_outside(dtype):
+    for bad in (-1, 301, 1 << 30, -(1 << 31)):
+        k = Case(40, 64, 301, dtype)
+        k.labels[7] = bad
+        k.forward()
+        k.backward()
+        assert bool(torch.isnan(k.loss[8])) and bool(torch.isnan(k.loss[0])) and bool(torch.isnan(k.dh[7]).all())
+        assert not bool(torch.isnan(torch.cat((k.loss[1:8], k.loss[9:]))).any())
+        assert not bool(torch.isnan(torch.cat((k.dh[:7], k.dh[8:]))).any())
+        assert bool(torch.isnan(k.dw).all()) and bool(torch.isnan(k.dbias).all())
+        assert bool(torch.isfinite(k.ce.lse).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_classes_taken_out(dtype):
+    """A bias of -infinity takes its class out; classes whose whole tile is out, too."""
+    k = Case(60, 64, 700, dtype, bias=True)
+    out = torch.zeros(700, dtype=torch.bool, device="cuda")
+    out[128:400] = True
+    out[::7] = True
+    keep = torch.nonzero(~out)[:, 0]
+    k.labels.copy_(keep[k.labels.long() % len(keep)].int())
+    k.bias[out] = float("-inf")
+    k.forward()
+    k.check_forward()
+    k.backward()
+    k.check_backward()
+    assert bool((k.dbias[out] == 0).all()) and bool((k.dw[out] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_row_of_infinities_is_its_own(dtype):
+    k = Case(50, 64, 300, dtype)
+    want = Case(50, 64, 300, dtype)
+    want.forward()
+    for value in (float("nan"), float("inf"), float("-inf")):
+        k.h[11] = value
+        k.forward()
+        assert bool(torch.isnan(k.loss[12])) and bool(torch.isnan(k.loss[0]))
+        assert torch.equal(torch.cat((k.loss[1:12], k.loss[13:])), torch.cat((want.loss[1:12], want.loss[13:])))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_large_logits(dtype):
+    """Logits of several hundred: exponentials that would overflow or vanish without the maximum."""
+    k = Case(64, 128, 900, dtype, std=200.0)
+    k.forward()
+    k.check_forward()
+    k.backward()
+    k.check_backward()
+
+
+def test_gradient_is_the_differences():
+    """Central differences of the float64 definition's mean loss along random directions against the gradients."""
+    k = Case(60, 64, 300, torch.float32, bias=True, smoothing=0.1, z=1e-2, ignored=0.2, std=1.0)
+    k.forward()
+    k.reference()
+    k.backward()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    d = [torch.randn(t.shape, generator=g, device="cuda", dtype=torch.float64) for t in (k.h64, k.w64, k.bias)]
+
+    def mean(e):
+        l = (k.h64 + e * d[0]) @ (k.w64 + e * d[1]).t() + k.bias.double() + e * d[2]
+        lse = torch.logsumexp(l, 1)
+        rows = lse - (1 - k.s) * l.gather(1, k.at)[:, 0] - k.s * l.mean(1) + k.zz * lse ** 2
+        return float(rows[k.counts].mean())
+
+    e = 1e-5
+    quotient = (mean(e) - mean(-e)) / (2 * e)
+    got = sum(float((t.double() * x).sum()) for t, x in zip((k.dh, k.dw, k.dbias), d))
+    # rounding 1e-16 |loss| / e, the third derivative's e^2 (its size bounded by the cube of a step's logit change),
+    # and the gradients' own relative 1e-5
+    change = float((k.h64 @ d[1].t() + d[0] @ k.w64.t()).abs().max()) + float(d[2].abs().max())
+    tol = 1e-15 * 10 / e + 8 * e * e * change ** 3 + 1e-5 * sum(float((t.double() * x).abs().sum()) for t, x in zip((k.dh, k.dw, k.dbias), d))
+    assert abs(quotient - got) <= tol, (quotient, got, tol)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_same_bits_streams_and_graph(dtype):
+    B = _B()
+    ks = [Case(333, 136, 2000, dtype, seed=s, bias=True, ignored=0.2) for s in (1, 2)]
+    for k in ks:
+        k.forward()
+        k.backward()
+        k.first = [t.clone() for t in (k.loss, k.ce.lse, k.dh, k.dw, k.dbias)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ks]
+    for _ in range(3):                                    # two calls at once
+        for k, s in zip(ks, streams):
+            with torch.cuda.stream(s):
+                B.bnr_linear_ce_fwd(k.h, k.w, k.ce, k.loss)
+                B.bnr_linear_ce_bwd(k.h, k.w, k.ce, k.dh, k.dw, k.dbias)
+    torch.cuda.synchronize()
+    for k in ks:
+        assert all(torch.equal(a, b) for a, b in zip((k.loss, k.ce.lse, k.dh, k.dw, k.dbias), k.first))
+    graphs = []
+    for k in ks:                                          # two graphs, replayed in turn, on changing labels
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.bnr_linear_ce_fwd(k.h, k.w, k.ce, k.loss)
+            B.bnr_linear_ce_bwd(k.h, k.w, k.ce, k.dh, k.dw, k.dbias)
+        graphs.append(g)
+    for turn in range(3):
+        for k in ks:
+            k.labels.copy_(torch.where(torch.rand(333, device="cuda") < 0.3 * turn, torch.full_like(k.labels, IGNORE),
+                                       torch.randint_like(k.labels, 0, 2000)))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for k in ks:
+            got = [t.clone() for t in (k.loss, k.ce.lse, k.dh, k.dw, k.dbias)]
+            B.bnr_linear_ce_fwd(k.h, k.w, k.ce, k.loss)
+            B.bnr_linear_ce_bwd(k.h, k.w, k.ce, k.dh, k.dw, k.dbias)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip((k.loss, k.ce.lse, k.dh, k.dw, k.dbias), got))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_rows(dtype):
+    """The list of rows past one level of counting."""
+    k = Case(40000, 8, 40, dtype, ignored=0.3)
+    k.forward()
+    k.check_forward()
+    k.backward()
+    k.check_backward()
+
+
+def test_offsets_past_32_bits():
+    """Weights past 4 GiB."""
+    m, c, v, ld = 20, 64, 5000, 1 << 19
+    buf = torch.empty(v, ld, dtype=torch.bfloat16, device="cuda")
+    k = Case(m, c, v, torch.bfloat16)
+    w = buf[:, ld - c:]
+    w.copy_(k.w)
+    k.w = w
+    k.forward()
+    k.check_forward()
+    k.backward()
+    k.check_backward()
