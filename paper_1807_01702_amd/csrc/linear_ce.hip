@@ -236,12 +236,26 @@ __device__ __forceinline__ void ce_mma(f32x4 &c, f32x4 a, f32x4 b)
     for (int t = 0; t < 4; t++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[t], b[t], c, 0, 0, 0);
 }
 
-// four neighbouring results
+// A wave's LDS accesses up to here are done before those that follow (its own area: no barrier).
+__device__ __forceinline__ void ce_wave_sync()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
+typedef __attribute__((address_space(3))) unsigned char lds_char;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+constexpr int kWaveOut = 64 * 64 * 4;      // bytes of LDS a wave turns its results in
+
+// neighbouring results
 __device__ __forceinline__ void ce_store4(float *p, const float *v) { *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]}; }
 __device__ __forceinline__ void ce_store4(bf16_t *p, const float *v)
 {
     *reinterpret_cast<u32x2_t *>(p) = u32x2_t{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
 }
+
+__device__ __forceinline__ void ce_store8(float *p, const float *v) { ce_store4(p, v); ce_store4(p + 4, v + 4); }
+__device__ __forceinline__ void ce_store8(bf16_t *p, const float *v) { stg16(p, Elem<bf16_t>::pack(v)); }
 
 // A workgroup's tile: tiles of one k range first; eight row tiles take turns over the
 // column tiles, so that the workgroups of an XCD share both operands in its L2.
@@ -273,7 +287,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
     if (!ce_place(pl, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, p.parts)) return;
     const int i0 = pl.ti * BI, j0 = pl.tj * BJ;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wi = wave / WJ, wj = wave % WJ, q = lane % 16, g = lane / 16;
+    const int wi = wave / WJ, wj = wave % WJ;
 
     const char *ibase = (const char *)p.i + (ICOLS ? (int64_t)i0 * sizeof(T) : i0 * p.i_ld);
     const char *jbase = (const char *)p.j + (JCOLS ? (int64_t)j0 * sizeof(T) : j0 * p.j_ld);
@@ -318,13 +332,16 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
             if (s + 1 < s1) load(lds1, (s + 1) * BK);
             multiply(lds0);
             __syncthreads();
-            if (s + 1 >= s1) break;
             if (s + 2 < s1) load(lds0, (s + 2) * BK);
-            multiply(lds1);
+            if (s + 1 < s1) multiply(lds1);
             __syncthreads();
         }
     }
 
+    // (the lane hidden from the compiler, which would form addresses ahead of the loop)
+    int late = lane;
+    asm volatile("" : "+v"(late));
+    const int q = late % 16, g = late / 16;
     const int iw = i0 + wi * TI, jw = j0 + wj * TJ;
     if constexpr (MODE == CE_STATS) {
         // each row's maximum, sum of exponentials and sum over the tile's columns
@@ -383,83 +400,100 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
             p.stats[o] = float2{mx, sum};
             if (p.sums) p.sums[o] = all;
         }
-    } else if constexpr (MODE == CE_GRAD) {
-        float *red = reinterpret_cast<float *>(lds0);
-        float col[NJ][4];
-        #pragma unroll
-        for (int b = 0; b < NJ; b++)
-            #pragma unroll
-            for (int r = 0; r < 4; r++) {
-                const int j = jw + 16 * b + 4 * g + r;
-                const float add = p.bias && j < nj ? p.bias[j] : 0.f;
-                col[b][r] = 0.f;
-                #pragma unroll
-                for (int a = 0; a < MI; a++) acc[b][a][r] += add;
-            }
-        #pragma unroll
-        for (int a = 0; a < MI; a++) {
-            const int i = iw + 16 * a + q;
-            if (i >= ni) continue;
-            const CeRow row = p.rows[i];
-            const int at = row.label - p.first;
-            const float grow = row.scale * (1.f + 2.f * p.z * row.lse), flat = row.scale * p.flat, hit = row.scale * p.hit;
-            T *o = (T *)p.g + (int64_t)i * p.g_ld;
-            #pragma unroll
-            for (int b = 0; b < NJ; b++) {
-                float v[4];
-                const int j = jw + 16 * b + 4 * g;
-                #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    v[r] = __builtin_fmaf(ce_exp(acc[b][a][r] - row.lse), grow, -flat) - (j + r == at ? hit : 0.f);
-                    v[r] = j + r < nj ? v[r] : 0.f;
-                    col[b][r] += v[r];
-                }
-                if (j < p.g_ld) ce_store4(o + j, v);
-            }
-        }
-        if (p.colsum) {
-            #pragma unroll
-            for (int b = 0; b < NJ; b++)
-                #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    float v = col[b][r];
-                    for (int o = 1; o < 16; o *= 2) v += __shfl_xor(v, o, 64);
-                    if (q == 0) red[wi * BJ + wj * TJ + 16 * b + 4 * g + r] = v;
-                }
-            __syncthreads();
-            for (int j = tid; j < BJ; j += NT) {
-                if (j0 + j >= nj) break;
-                float v = 0.f;
-                #pragma unroll
-                for (int w = 0; w < WI; w++) v += red[w * BJ + j];
-                p.colsum[(int64_t)pl.ti * p.colsum_ld + j0 + j] = v;
-            }
-        }
     } else {
-        // the results themselves: i = 16 a + q and j = 16 b + 4 g + r, in float32 columns i = MI q + a, j = NJ (4 g + r) + b
+        // The results through LDS, 64 x 64 of a wave at a time in its own 16 KiB (a row's
+        // 16-byte chunks in the order chunk ^ row % 16), so that a lane goes on with eight
+        // neighbouring columns: whole lines are stored, in a short loop over the rows.
+        // i = 16 a + q and j = 16 b + 4 g + r, in float32 columns i = MI q + a, j = NJ (4 g + r) + b.
         constexpr bool IP = ICOLS && sizeof(T) == 4, JP = JCOLS && sizeof(T) == 4;
-        #pragma unroll
-        for (int a = 0; a < MI; a++) {
-            const int i = iw + (IP ? MI * q + a : 16 * a + q);
-            if (i >= ni) continue;
-            const int64_t row = p.part_stride || MODE == CE_DW ? i : p.rows[i].row;
+        constexpr int kHalf = NT / 128;
+        static_assert(kStage == kHalf * kWaveOut && TJ == 64 && (!IP || TI == 64), "a wave's part of the stages");
+        lds_char *mine = (wave < kHalf ? (lds_char *)lds0 : (lds_char *)lds1) + wave % kHalf * kWaveOut;
+        const int lrow = late / 8, lcol = late % 8 * 8, j = jw + lcol;
+        float add[8], col[8];
+        if constexpr (MODE == CE_GRAD) {
             #pragma unroll
-            for (int b = 0; b < NJ; b++) {
-                const int j = jw + (JP ? 16 * g + 4 * b : 16 * b + 4 * g);
-                if (j >= nj) continue;               // (c is a multiple of four)
-                float v[4];
+            for (int e = 0; e < 8; e++) {
+                add[e] = p.bias && j + e < nj ? p.bias[j + e] : 0.f;
+                col[e] = 0.f;
+            }
+        }
+        #pragma unroll
+        for (int h = 0; h < TI / 64; h++) {
+            #pragma unroll
+            for (int a = 0; a < 4; a++)
                 #pragma unroll
-                for (int r = 0; r < 4; r++) v[r] = JP ? acc[r][a][b] : acc[b][a][r];
-                if (p.out_f32) {
-                    float *o = (float *)p.out + (int64_t)pl.part * p.part_stride + row * p.out_ld + j;
-                    if (p.add) {
-                        const f32x4 old = *reinterpret_cast<const f32x4 *>(o);
-                        #pragma unroll
-                        for (int r = 0; r < 4; r++) v[r] += old[r];
+                for (int b = 0; b < 4; b++) {
+                    const int row = IP ? 4 * q + a : 16 * a + q, chunk = JP ? 4 * g + b : 4 * b + g;
+                    const f32x4 v = JP ? f32x4{acc[0][4 * h + a][b], acc[1][4 * h + a][b], acc[2][4 * h + a][b], acc[3][4 * h + a][b]}
+                                       : acc[b][4 * h + a];
+                    *(lds_f32x4 *)(mine + row * 256 + ((chunk ^ (row % 16)) * 16)) = v;
+                }
+            ce_wave_sync();
+            #pragma unroll 2
+            for (int it = 0; it < 8; it++) {
+                const int row = it * 8 + lrow, i = iw + 64 * h + row;
+                float v[8];
+                #pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    const f32x4 u = *(const lds_f32x4 *)(mine + row * 256 + (((lcol / 4 + k) ^ (row % 16)) * 16));
+                    #pragma unroll
+                    for (int r = 0; r < 4; r++) v[4 * k + r] = u[r];
+                }
+                if (i >= ni) continue;
+                if constexpr (MODE == CE_GRAD) {
+                    const CeRow r = p.rows[i];
+                    const int at = r.label - p.first - j;
+                    const float grow = r.scale * (1.f + 2.f * p.z * r.lse), flat = r.scale * p.flat, hit = r.scale * p.hit;
+                    #pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        v[e] = __builtin_fmaf(ce_exp(v[e] + add[e] - r.lse), grow, -flat) - (e == at ? hit : 0.f);
+                        v[e] = j + e < nj ? v[e] : 0.f;
+                        col[e] += v[e];
                     }
-                    ce_store4(o, v);
-                } else {
-                    ce_store4((bf16_t *)p.out + row * p.out_ld + j, v);
+                    ce_store8((T *)p.g + (int64_t)i * p.g_ld + j, v);
+                } else if (j < nj) {                 // (the second half of a vector that c cuts, in float32: below)
+                    const int64_t row_out = p.part_stride || MODE == CE_DW ? i : p.rows[i].row;
+                    const bool whole = sizeof(T) == 2 || j + 4 < nj;
+                    if (p.out_f32) {
+                        float *o = (float *)p.out + (int64_t)pl.part * p.part_stride + row_out * p.out_ld + j;
+                        if (p.add) {
+                            #pragma unroll
+                            for (int k = 0; k < 2; k++) {
+                                if (k && !whole) break;
+                                const f32x4 old = *reinterpret_cast<const f32x4 *>(o + 4 * k);
+                                #pragma unroll
+                                for (int r = 0; r < 4; r++) v[4 * k + r] += old[r];
+                            }
+                        }
+                        ce_store4(o, v);
+                        if (whole) ce_store4(o + 4, v + 4);
+                    } else {
+                        bf16_t *o = (bf16_t *)p.out + row_out * p.out_ld + j;
+                        if (whole) ce_store8(o, v);
+                        else ce_store4(o, v);
+                    }
+                }
+            }
+            ce_wave_sync();
+        }
+        if constexpr (MODE == CE_GRAD) {
+            if (p.colsum) {
+                float *red = reinterpret_cast<float *>(lds0);
+                __syncthreads();
+                #pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    float v = col[e];
+                    for (int o = 8; o < 64; o *= 2) v += __shfl_xor(v, o, 64);
+                    if (lrow == 0) red[wi * BJ + wj * TJ + lcol + e] = v;
+                }
+                __syncthreads();
+                for (int c = tid; c < BJ; c += NT) {
+                    if (j0 + c >= nj) break;
+                    float v = 0.f;
+                    #pragma unroll
+                    for (int w = 0; w < WI; w++) v += red[w * BJ + c];
+                    p.colsum[(int64_t)pl.ti * p.colsum_ld + j0 + c] = v;
                 }
             }
         }
