@@ -136,67 +136,61 @@ __global__ __launch_bounds__(kThreads) void k_ce_list(CeList p)
 template <typename T, int B, int NT, bool COLS>
 struct CeLoad {
     static constexpr int kLoads = B * 128 / (NT * 16), BK = 128 / sizeof(T);
-    uint32_t off[kLoads], at[kLoads];              // at: the chunk's place along k (rows)
+    // a thread's loads lie kStep rows (k) apart, where the order repeats
+    static constexpr uint32_t kRow = COLS ? B * sizeof(T) : 128, kStep = NT * 16 / kRow;
+    static_assert(kStep % 16 == 0 || (COLS && sizeof(T) == 4), "the order repeats every 16 rows");
+    uint32_t off, at;                              // at: the chunk's place along k (rows)
     __device__ __forceinline__ void init(int64_t ld, int tid)
     {
-        #pragma unroll
-        for (int l = 0; l < kLoads; l++) {
-            const uint32_t byte = (l * NT + tid) * 16;
-            if constexpr (COLS) {
-                constexpr uint32_t kRow = B * sizeof(T);
-                const uint32_t k = byte / kRow, slot = byte % kRow / 16;
-                const uint32_t turn = sizeof(T) == 2 ? 2 * (k % 4 + 4 * (k / 8 % 2)) : 0;
-                off[l] = k * (uint32_t)ld + (slot ^ turn) * 16;
-                at[l] = 0;
-            } else {
-                const uint32_t row = byte / 128, slot = byte % 128 / 16;
-                at[l] = (slot ^ (row / 2 % 8)) * 16;
-                off[l] = row * (uint32_t)ld + at[l];
-            }
-        }
+        const uint32_t row = tid * 16 / kRow, slot = tid * 16 % kRow / 16;
+        const uint32_t turn = COLS ? (sizeof(T) == 2 ? 2 * (row % 4 + 4 * (row / 8 % 2)) : 0) : row / 2 % 8;
+        at = COLS ? 0 : (slot ^ turn) * 16;
+        off = row * (uint32_t)ld + (slot ^ turn) * 16;
     }
-    // stage `k0` of an operand whose tile starts at base, with `extent` rows (columns) left
-    __device__ __forceinline__ void load(unsigned char *lds, const char *base, int64_t ld, int extent, int k0, int k,
-                                         int wave) const
+    // stage `k0` of an operand whose tile starts at base, with `extent` rows (columns) left;
+    // past k no address is read and zeros arrive
+    struct Stage { const char *src; uint32_t bytes, o, step; };
+    __device__ __forceinline__ Stage stage(const char *base, int64_t ld, int extent, int k0, int k) const
     {
         const int left = min(k - k0, BK), wide = min(extent, B);
         const char *src = base + (COLS ? k0 * ld : k0 * (int64_t)sizeof(T));
         // (c is a multiple of the 16-byte vector, and g's rows are whole vectors: a column tile's last vector is read whole)
-        const uint32_t bytes = COLS ? (left - 1) * (uint32_t)ld + (wide * sizeof(T) + 15) / 16 * 16
-                                    : (wide - 1) * (uint32_t)ld + left * sizeof(T);
-        const __amdgpu_buffer_rsrc_t r = buf_view(src, bytes);
-        #pragma unroll
-        for (int l = 0; l < kLoads; l++) {
-            uint32_t o = off[l];
-            if constexpr (!COLS) o = at[l] < left * sizeof(T) ? o : kBufOff;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + (l * NT + wave * 64) * 16),
-                                                     16, o, 0, 0, 0);
-        }
+        const int bytes = COLS ? (left - 1) * (int)ld + (wide * (int)sizeof(T) + 15) / 16 * 16
+                               : (wide - 1) * (int)ld + left * (int)sizeof(T);
+        Stage s;
+        s.src = src;
+        s.bytes = __builtin_amdgcn_readfirstlane(left > 0 ? bytes : 0);
+        s.o = off;
+        if constexpr (!COLS) s.o = (int)at < left * (int)sizeof(T) ? off : kBufOff;
+        s.step = kStep * (uint32_t)ld;
+        return s;
+    }
+    __device__ __forceinline__ void load(const Stage &s, unsigned char *lds, int l, int wave) const
+    {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_view(s.src, s.bytes),
+                                                 (__attribute__((address_space(3))) void *)(lds + (l * NT + wave * 64) * 16),
+                                                 16, s.o + l * s.step, 0, 0, 0);
     }
 };
 
 // Fragments of NB blocks of 16 rows (columns) from w0 on, of sub-step `sub` (64 bytes
-// along k).  Block b's lane value q stands for row 16 b + q, in float32 columns for
+// along k), read in NB parts.  Block b's lane value q stands for row 16 b + q, in float32 columns for
 // NB q + b (a lane's neighbouring values, one read).
 template <typename T, int B, int NB, bool COLS> struct CeFrags;
 template <int B, int NB> struct CeFrags<bf16_t, B, NB, false> {
     uint32_t at;
     __device__ __forceinline__ void init(int w0, int lane) { at = (w0 + lane % 16) * 128; }
-    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, bf16x8 *f) const
+    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, bf16x8 *f, int part) const
     {
-        const unsigned char *p = lds + at + ((sub * 4 + lane / 16) ^ (lane % 16 / 2)) * 16;
-        #pragma unroll
-        for (int b = 0; b < NB; b++) f[b] = *reinterpret_cast<const bf16x8 *>(p + b * 2048);
+        f[part] = *reinterpret_cast<const bf16x8 *>(lds + at + ((sub * 4 + lane / 16) ^ (lane % 16 / 2)) * 16 + part * 2048);
     }
 };
 template <int B, int NB> struct CeFrags<float, B, NB, false> {
     uint32_t at;
     __device__ __forceinline__ void init(int w0, int lane) { at = (w0 + lane % 16) * 128; }
-    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, f32x4 *f) const
+    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, f32x4 *f, int part) const
     {
-        const unsigned char *p = lds + at + ((sub * 4 + lane / 16) ^ (lane % 16 / 2)) * 16;
-        #pragma unroll
-        for (int b = 0; b < NB; b++) f[b] = *reinterpret_cast<const f32x4 *>(p + b * 2048);
+        f[part] = *reinterpret_cast<const f32x4 *>(lds + at + ((sub * 4 + lane / 16) ^ (lane % 16 / 2)) * 16 + part * 2048);
     }
 };
 template <int B, int NB> struct CeFrags<bf16_t, B, NB, true> {
@@ -208,24 +202,20 @@ template <int B, int NB> struct CeFrags<bf16_t, B, NB, true> {
         #pragma unroll
         for (int b = 0; b < NB; b++) at[b] = k * (B * 2) + ((((w0 + 16 * b) / 8 + q % 4 / 2) ^ turn) * 16) + q % 2 * 8;
     }
-    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, bf16x8 *f) const
+    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, bf16x8 *f, int part) const
     {
-        #pragma unroll
-        for (int b = 0; b < NB; b++) f[b] = tr_frag((const bf16_t *)(lds + at[b] + sub * 32 * B * 2), B);
+        f[part] = tr_frag((const bf16_t *)(lds + at[part] + sub * 32 * B * 2), B);
     }
 };
 template <int B, int NB> struct CeFrags<float, B, NB, true> {
     static_assert(NB == 4, "four blocks' values are one read");
     uint32_t at;
     __device__ __forceinline__ void init(int w0, int lane) { at = 4 * (lane / 16) * (B * 4) + (w0 + 4 * (lane % 16)) * 4; }
-    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, f32x4 *f) const
+    __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, f32x4 *f, int part) const
     {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(lds + at + (sub * 16 + part) * (B * 4));
         #pragma unroll
-        for (int t = 0; t < 4; t++) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(lds + at + (sub * 16 + t) * (B * 4));
-            #pragma unroll
-            for (int b = 0; b < NB; b++) f[b][t] = v[b];
-        }
+        for (int b = 0; b < NB; b++) f[b][part] = v[b];
     }
 };
 
@@ -272,13 +262,93 @@ __device__ __forceinline__ bool ce_place(CePlace &pl, int nti, int ntj, int part
     return true;
 }
 
+// The sums acc of a wave: its blocks of a BI x BJ tile over the stages [s0, s1) along k.
+// Operand tiles start at i0 and j0, with ni, nj rows (columns) left and k_i, k_j values
+// along k.  Starts without, ends with a barrier.
+template <typename T, int BI, int BJ, int WI, int WJ, bool ICOLS, bool JCOLS>
+__device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 16], const char *i0, int64_t i_ld, int ni,
+                                           int k_i, const char *j0, int64_t j_ld, int nj, int k_j, int s0, int s1,
+                                           unsigned char *lds0, unsigned char *lds1)
+{
+    constexpr int NT = WI * WJ * 64, TI = BI / WI, TJ = BJ / WJ, MI = TI / 16, NJ = TJ / 16, BK = 128 / sizeof(T);
+    typedef typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type frag;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    typedef CeLoad<T, BI, NT, ICOLS> LoadI;
+    typedef CeLoad<T, BJ, NT, JCOLS> LoadJ;
+    LoadI li;
+    LoadJ lj;
+    li.init(i_ld, tid);
+    lj.init(j_ld, tid);
+    CeFrags<T, BI, MI, ICOLS> ri;
+    CeFrags<T, BJ, NJ, JCOLS> rj;
+    ri.init(wave / WJ * TI, lane);
+    rj.init(wave % WJ * TJ, lane);
+    #pragma unroll
+    for (int b = 0; b < NJ; b++)
+        #pragma unroll
+        for (int a = 0; a < MI; a++) acc[b][a] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int end = s1 * BK;
+    k_i = min(k_i, end);
+    k_j = min(k_j, end);
+    // A stage has two sub-steps.  Between two barriers a wave multiplies the second
+    // sub-step of the stage before, whose fragments it already holds, and the first of
+    // this one; meanwhile it reads this stage's fragments and the next stage is loaded
+    // into the LDS that the stage before has left.  Products, reads and loads alternate.
+    struct Frags { frag i[MI], j[NJ]; } f0, f1;
+    constexpr int kLi = LoadI::kLoads, kLj = LoadJ::kLoads;
+    auto load = [&](unsigned char *lds, const typename LoadI::Stage &a, const typename LoadJ::Stage &b, int from, int to)
+        __attribute__((always_inline)) {
+        #pragma unroll
+        for (int l = from; l < to; l++) {
+            if (l < kLi) li.load(a, lds, l, wave);
+            else lj.load(b, lds + BI * 128, l - kLi, wave);
+        }
+    };
+    auto read = [&](Frags &f, const unsigned char *lds, int sub, int part) __attribute__((always_inline)) {
+        if (part < NJ) rj.read(lds + BI * 128, sub, lane, f.j, part);
+        ri.read(lds, sub, lane, f.i, part);
+    };
+    auto multiply = [&](const Frags &f, int a) __attribute__((always_inline)) {
+        #pragma unroll
+        for (int b = 0; b < NJ; b++) ce_mma(acc[b][a], f.j[b], f.i[a]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto stage = [&](const unsigned char *now, unsigned char *other, int s, bool first) __attribute__((always_inline)) {
+        const typename LoadI::Stage sa = li.stage(i0, i_ld, ni, (s + 1) * BK, k_i);
+        const typename LoadJ::Stage sb = lj.stage(j0, j_ld, nj, (s + 1) * BK, k_j);
+        #pragma unroll
+        for (int a = 0; a < MI; a++) {
+            read(f0, now, 0, a);
+            load(other, sa, sb, a * (kLi + kLj) / MI, (a + 1) * (kLi + kLj) / MI);
+            if (!first) multiply(f1, a);
+        }
+        #pragma unroll
+        for (int a = 0; a < MI; a++) {
+            read(f1, now, 1, a);
+            multiply(f0, a);
+        }
+        __syncthreads();
+    };
+    if (s0 < s1) {
+        load(lds0, li.stage(i0, i_ld, ni, s0 * BK, k_i), lj.stage(j0, j_ld, nj, s0 * BK, k_j), 0, kLi + kLj);
+        __syncthreads();
+        stage(lds0, lds1, s0, true);
+        for (int s = s0 + 1; s < s1; s += 2) {
+            stage(lds1, lds0, s, false);
+            if (s + 1 < s1) stage(lds0, lds1, s + 1, false);
+        }
+        #pragma unroll
+        for (int a = 0; a < MI; a++) multiply(f1, a);
+    }
+    __syncthreads();
+}
+
 template <typename T, int BI, int BJ, int WI, int WJ, int MODE>
 __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
 {
     constexpr bool ICOLS = MODE == CE_DW, JCOLS = MODE == CE_DW || MODE == CE_DH;
     constexpr int NT = WI * WJ * 64, TI = BI / WI, TJ = BJ / WJ, MI = TI / 16, NJ = TJ / 16, BK = 128 / sizeof(T);
     constexpr int kStage = (BI + BJ) * 128;
-    typedef typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type frag;
     __shared__ __align__(16) unsigned char lds0[kStage], lds1[kStage];
     const int count = *p.count;
     const int ni = MODE == CE_DW ? p.classes : count, nj = MODE == CE_DW || MODE == CE_DH ? p.c : p.classes;
@@ -288,55 +358,14 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
     const int i0 = pl.ti * BI, j0 = pl.tj * BJ;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / WJ, wj = wave % WJ;
-
     const char *ibase = (const char *)p.i + (ICOLS ? (int64_t)i0 * sizeof(T) : i0 * p.i_ld);
     const char *jbase = (const char *)p.j + (JCOLS ? (int64_t)j0 * sizeof(T) : j0 * p.j_ld);
-    CeLoad<T, BI, NT, ICOLS> li;
-    CeLoad<T, BJ, NT, JCOLS> lj;
-    li.init(p.i_ld, tid);
-    lj.init(p.j_ld, tid);
-    // g's rows are whole vectors of zeros past the classes: their last vector is read whole
-    const int Ki = MODE == CE_DH ? (K + 7) / 8 * 8 : K;
-    auto load = [&](unsigned char *stage, int k) __attribute__((always_inline)) {
-        li.load(stage, ibase, p.i_ld, ni - i0, k, Ki, wave);
-        lj.load(stage + BI * 128, jbase, p.j_ld, nj - j0, k, K, wave);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    CeFrags<T, BI, MI, ICOLS> ri;
-    CeFrags<T, BJ, NJ, JCOLS> rj;
-    ri.init(wi * TI, lane);
-    rj.init(wj * TJ, lane);
-    f32x4 acc[NJ][MI];
-    #pragma unroll
-    for (int b = 0; b < NJ; b++)
-        #pragma unroll
-        for (int a = 0; a < MI; a++) acc[b][a] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto multiply = [&](const unsigned char *stage) __attribute__((always_inline)) {
-        #pragma unroll
-        for (int sub = 0; sub < 2; sub++) {
-            frag fi[MI], fj[NJ];
-            ri.read(stage, sub, lane, fi);
-            rj.read(stage + BI * 128, sub, lane, fj);
-            #pragma unroll
-            for (int a = 0; a < MI; a++)
-                #pragma unroll
-                for (int b = 0; b < NJ; b++) ce_mma(acc[b][a], fj[b], fi[a]);
-        }
-    };
     const int steps = (K + BK - 1) / BK;
     const int s0 = (int)((int64_t)pl.part * steps / p.parts), s1 = (int)((int64_t)(pl.part + 1) * steps / p.parts);
-    if (s0 < s1) {
-        load(lds0, s0 * BK);
-        __syncthreads();
-        for (int s = s0; s < s1; s += 2) {
-            if (s + 1 < s1) load(lds1, (s + 1) * BK);
-            multiply(lds0);
-            __syncthreads();
-            if (s + 2 < s1) load(lds0, (s + 2) * BK);
-            if (s + 1 < s1) multiply(lds1);
-            __syncthreads();
-        }
-    }
+    f32x4 acc[NJ][MI];
+    // (g's rows are whole vectors of zeros past the classes: their last vector is read whole)
+    ce_product<T, BI, BJ, WI, WJ, ICOLS, JCOLS>(acc, ibase, p.i_ld, ni - i0, MODE == CE_DH ? (K + 7) / 8 * 8 : K, jbase,
+                                                p.j_ld, nj - j0, K, s0, s1, lds0, lds1);
 
     // (the lane hidden from the compiler, which would form addresses ahead of the loop)
     int late = lane;
