@@ -336,12 +336,13 @@ struct CeCall {                    // one call (forward: loss; backward: the res
     int64_t dh_ld, dw_ld;
     float *dbias;
 };
-struct CeRow { int row, label; float lse, scale; };   // a row that counts: its place, label, log sum, dloss / dlogit factor
+struct CeRow { int row, label; float lse, scale; };   // a row that counts: its place, label, log sum, gradient / factor
 struct CeList {
     int64_t m;
     int classes, ignore, row_bytes;
     const int32_t *labels;
     int *count, *counts;           // rows that count, and per kCountRows rows (NULL: few)
+    float *factor;                 // backward: what the gradients' sums are multiplied by
     CeRow *rows;
     const void *h;
     int64_t h_ld;                  // bytes
@@ -354,7 +355,9 @@ struct CeList {
 enum { CE_STATS = 0, CE_GRAD = 1, CE_DH = 2, CE_DW = 3 };
 struct CeGemm {
     const int *count;
-    const CeRow *rows;
+    const CeRow *rows;             // NULL (CE_STATS of few rows): all m rows, by their labels
+    const int32_t *labels;
+    const float *factor;
     const void *i, *j;             // operands
     int64_t i_ld, j_ld;            // bytes
     int64_t m;
@@ -373,14 +376,16 @@ struct CeGemm {
 };
 struct CeLoss {
     const int *count;
-    const CeRow *rows;
+    const CeRow *rows;             // NULL: all m rows, by their labels
+    const int32_t *labels;
+    int ignore;
     const float2 *stats;
     const float *sums, *picked;
     int64_t m;
     int tiles, groups, classes;
     double hit, flat, z;
     float *loss, *lse;
-    double *part;
+    double2 *part;                 // per workgroup: losses and rows that count
 };
 struct CeSum {
     const float *part;
@@ -388,11 +393,13 @@ struct CeSum {
     int parts, c;
     const CeRow *rows;             // results by the list (NULL: row by row, n of them)
     const int *count;
+    const float *factor;
     void *out;
     int64_t out_ld;
 };
 struct CeBias {
     const int *count;
+    const float *factor;
     int tile, classes;
     const float *colsum;
     int64_t ld;

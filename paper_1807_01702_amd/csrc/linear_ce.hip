@@ -34,17 +34,12 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
 
-// exp(x) by the base-2 instruction; the product's rounding, which would cost |x| 2^-24
-// of the result, is put back.
-__device__ __forceinline__ float ce_exp(float x)
-{
-    const float t = x * kLog2e, e = __builtin_amdgcn_exp2f(t);
-    const float lo = __builtin_fmaf(x, kLog2e, -t);
-    return x > -100.f ? __builtin_fmaf(e, lo * 0.6931471805599453f, e) : e;   // (lo is NaN for -inf)
-}
+// exp(x) by the base-2 instruction: off by about |x| 2^-24 of itself, next to the
+// c 2^-24 sum |h w| that the logits are off by.
+__device__ __forceinline__ float ce_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // ---- rows that count -------------------------------------------------------
-constexpr int kListRows = 16;              // rows a workgroup of k_ce_list takes
+constexpr int kListRows = 4;               // rows a workgroup of k_ce_list takes, one a wave
 constexpr int kCountRows = 4096;           // rows a workgroup of k_ce_count takes
 
 __device__ __forceinline__ int ce_counted(const int32_t *labels, int64_t from, int64_t to, int ignore, int tid)
@@ -89,6 +84,17 @@ __global__ __launch_bounds__(kThreads) void k_ce_list(CeList p)
     }
     n += ce_counted(p.labels, from, first, p.ignore, tid);
     const int before = ce_group_sum(n, red, tid);
+    // The gradient of the mean, dloss[0] / n, multiplies every g.  Its significand is kept
+    // apart and multiplies the sums in float32: g's rounding to bf16 would otherwise shift
+    // the many values that are the same (-1 / n at the labels of a model that knows
+    // little yet) by the same error.
+    float mean = 0.f, factor = 1.f;
+    if (p.lse) {
+        mean = (p.dloss ? p.dloss[0] : 1.f) / p.lse[0];
+        const uint32_t bits = __float_as_uint(mean), exponent = bits >> 23 & 255;
+        if (exponent && exponent < 255) factor = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
+        if (tid == 0 && blockIdx.x == 0) *p.factor = factor;
+    }
     const int64_t row = first + lane;
     const bool mine = lane < kListRows && row < p.m;
     const int label = mine ? p.labels[row] : p.ignore;
@@ -101,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void k_ce_list(CeList p)
             r.lse = r.scale = 0.f;
             if (p.lse) {
                 r.lse = p.lse[1 + row];
-                r.scale = p.dloss ? p.dloss[0] / p.lse[0] + p.dloss[1 + row] : 1.0f / p.lse[0];
+                r.scale = (p.dloss ? mean + p.dloss[1 + row] : mean) / factor;
                 if ((uint32_t)label >= (uint32_t)p.classes) r.scale = NAN;
             }
             p.rows[before + __popcll(here & ((1ull << lane) - 1))] = r;
@@ -136,20 +142,21 @@ __global__ __launch_bounds__(kThreads) void k_ce_list(CeList p)
 template <typename T, int B, int NT, bool COLS>
 struct CeLoad {
     static constexpr int kLoads = B * 128 / (NT * 16), BK = 128 / sizeof(T);
-    // a thread's loads lie kStep rows (k) apart, where the order repeats
+    // a thread's loads lie kStep rows (k) apart; the order repeats every 16
     static constexpr uint32_t kRow = COLS ? B * sizeof(T) : 128, kStep = NT * 16 / kRow;
-    static_assert(kStep % 16 == 0 || (COLS && sizeof(T) == 4), "the order repeats every 16 rows");
-    uint32_t off, at;                              // at: the chunk's place along k (rows)
+    static_assert(kStep % (COLS ? 8 : 16) == 0, "two places at most");
+    uint32_t off, odd, at;                         // of even loads, of odd ones; at: the chunk's place along k (rows)
     __device__ __forceinline__ void init(int64_t ld, int tid)
     {
         const uint32_t row = tid * 16 / kRow, slot = tid * 16 % kRow / 16;
         const uint32_t turn = COLS ? (sizeof(T) == 2 ? 2 * (row % 4 + 4 * (row / 8 % 2)) : 0) : row / 2 % 8;
         at = COLS ? 0 : (slot ^ turn) * 16;
         off = row * (uint32_t)ld + (slot ^ turn) * 16;
+        odd = COLS && sizeof(T) == 2 && kStep % 16 ? row * (uint32_t)ld + (slot ^ turn ^ 8) * 16 : off;
     }
     // stage `k0` of an operand whose tile starts at base, with `extent` rows (columns) left;
     // past k no address is read and zeros arrive
-    struct Stage { const char *src; uint32_t bytes, o, step; };
+    struct Stage { const char *src; uint32_t bytes, o, odd, step; };
     __device__ __forceinline__ Stage stage(const char *base, int64_t ld, int extent, int k0, int k) const
     {
         const int left = min(k - k0, BK), wide = min(extent, B);
@@ -161,7 +168,8 @@ struct CeLoad {
         s.src = src;
         s.bytes = __builtin_amdgcn_readfirstlane(left > 0 ? bytes : 0);
         s.o = off;
-        if constexpr (!COLS) s.o = (int)at < left * (int)sizeof(T) ? off : kBufOff;
+        s.odd = odd;
+        if constexpr (!COLS) s.o = s.odd = (int)at < left * (int)sizeof(T) ? off : kBufOff;
         s.step = kStep * (uint32_t)ld;
         return s;
     }
@@ -169,7 +177,7 @@ struct CeLoad {
     {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_view(s.src, s.bytes),
                                                  (__attribute__((address_space(3))) void *)(lds + (l * NT + wave * 64) * 16),
-                                                 16, s.o + l * s.step, 0, 0, 0);
+                                                 16, (l % 2 ? s.odd : s.o) + l * s.step, 0, 0, 0);
     }
 };
 
@@ -226,6 +234,24 @@ __device__ __forceinline__ void ce_mma(f32x4 &c, f32x4 a, f32x4 b)
     for (int t = 0; t < 4; t++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[t], b[t], c, 0, 0, 0);
 }
 
+template <int N, int M> __device__ __forceinline__ void ce_zero(f32x4 (&v)[N][M])
+{
+    #pragma unroll
+    for (int b = 0; b < N; b++)
+        #pragma unroll
+        for (int a = 0; a < M; a++) v[b][a] = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+// total += part, part = 0
+template <int N, int M> __device__ __forceinline__ void ce_fold(f32x4 (&total)[N][M], f32x4 (&part)[N][M])
+{
+    #pragma unroll
+    for (int b = 0; b < N; b++)
+        #pragma unroll
+        for (int a = 0; a < M; a++)
+            #pragma unroll
+            for (int r = 0; r < 4; r++) { total[b][a][r] += part[b][a][r]; part[b][a][r] = 0.f; }
+}
+
 // A wave's LDS accesses up to here are done before those that follow (its own area: no barrier).
 __device__ __forceinline__ void ce_wave_sync()
 {
@@ -247,8 +273,9 @@ __device__ __forceinline__ void ce_store4(bf16_t *p, const float *v)
 __device__ __forceinline__ void ce_store8(float *p, const float *v) { ce_store4(p, v); ce_store4(p + 4, v + 4); }
 __device__ __forceinline__ void ce_store8(bf16_t *p, const float *v) { stg16(p, Elem<bf16_t>::pack(v)); }
 
-// A workgroup's tile: tiles of one k range first; eight row tiles take turns over the
-// column tiles, so that the workgroups of an XCD share both operands in its L2.
+// A workgroup's tile: tiles of one k range first; four row tiles take turns over the
+// column tiles, so that the 32 workgroups of an XCD share both operands in its L2
+// (8192 x 32768 x 4096, weight gradient: 1.58 ms with four, 1.67 with eight, 1.77 with 16).
 struct CePlace { int ti, tj, part; };
 __device__ __forceinline__ bool ce_place(CePlace &pl, int nti, int ntj, int parts)
 {
@@ -256,7 +283,7 @@ __device__ __forceinline__ bool ce_place(CePlace &pl, int nti, int ntj, int part
     if ((int)blockIdx.x >= total) return false;
     const int id = xcd_remap(blockIdx.x, total);
     pl.part = id / tiles;
-    const int t = id - pl.part * tiles, per = 8 * ntj, first = t / per * 8, n = min(8, nti - first), r = t % per;
+    const int t = id - pl.part * tiles, per = 4 * ntj, first = t / per * 4, n = min(4, nti - first), r = t % per;
     pl.ti = first + r % n;
     pl.tj = r / n;
     return true;
@@ -283,10 +310,13 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
     CeFrags<T, BJ, NJ, JCOLS> rj;
     ri.init(wave / WJ * TI, lane);
     rj.init(wave % WJ * TJ, lane);
-    #pragma unroll
-    for (int b = 0; b < NJ; b++)
-        #pragma unroll
-        for (int a = 0; a < MI; a++) acc[b][a] = f32x4{0.f, 0.f, 0.f, 0.f};
+    ce_zero(acc);
+    // float32 sums in two levels, 64 terms and then those: a chain of all terms, one
+    // rounding each, left the gradients of 128 x 1024 x 1000 7 times as far off float64
+    // as a library's product does
+    constexpr bool kFold = sizeof(T) == 4;
+    f32x4 total[kFold ? NJ : 1][kFold ? MI : 1];
+    if constexpr (kFold) ce_zero(total);
     const int end = s1 * BK;
     k_i = min(k_i, end);
     k_j = min(k_j, end);
@@ -295,7 +325,7 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
     // this one; meanwhile it reads this stage's fragments and the next stage is loaded
     // into the LDS that the stage before has left.  Products, reads and loads alternate.
     struct Frags { frag i[MI], j[NJ]; } f0, f1;
-    constexpr int kLi = LoadI::kLoads, kLj = LoadJ::kLoads;
+    constexpr int kLi = LoadI::kLoads, kLj = LoadJ::kLoads, kEach = (kLi + kLj) * 2 / MI;
     auto load = [&](unsigned char *lds, const typename LoadI::Stage &a, const typename LoadJ::Stage &b, int from, int to)
         __attribute__((always_inline)) {
         #pragma unroll
@@ -306,7 +336,7 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
     };
     auto read = [&](Frags &f, const unsigned char *lds, int sub, int part) __attribute__((always_inline)) {
         if (part < NJ) rj.read(lds + BI * 128, sub, lane, f.j, part);
-        ri.read(lds, sub, lane, f.i, part);
+        if (part < MI) ri.read(lds, sub, lane, f.i, part);
     };
     auto multiply = [&](const Frags &f, int a) __attribute__((always_inline)) {
         #pragma unroll
@@ -319,7 +349,7 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
         #pragma unroll
         for (int a = 0; a < MI; a++) {
             read(f0, now, 0, a);
-            load(other, sa, sb, a * (kLi + kLj) / MI, (a + 1) * (kLi + kLj) / MI);
+            load(other, sa, sb, min(a * kEach, kLi + kLj), min((a + 1) * kEach, kLi + kLj));
             if (!first) multiply(f1, a);
         }
         #pragma unroll
@@ -336,9 +366,17 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
         for (int s = s0 + 1; s < s1; s += 2) {
             stage(lds1, lds0, s, false);
             if (s + 1 < s1) stage(lds0, lds1, s + 1, false);
+            if constexpr (kFold) ce_fold(total, acc);
         }
         #pragma unroll
         for (int a = 0; a < MI; a++) multiply(f1, a);
+    }
+    if constexpr (kFold) {
+        ce_fold(total, acc);
+        #pragma unroll
+        for (int b = 0; b < NJ; b++)
+            #pragma unroll
+            for (int a = 0; a < MI; a++) acc[b][a] = total[b][a];
     }
     __syncthreads();
 }
@@ -362,6 +400,16 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
     const char *jbase = (const char *)p.j + (JCOLS ? (int64_t)j0 * sizeof(T) : j0 * p.j_ld);
     const int steps = (K + BK - 1) / BK;
     const int s0 = (int)((int64_t)pl.part * steps / p.parts), s1 = (int)((int64_t)(pl.part + 1) * steps / p.parts);
+    // what the epilogue needs of the tile's rows and columns, there before the products are done
+    __shared__ CeRow rows[MODE == CE_DW ? 1 : BI];
+    __shared__ float bias[MODE == CE_STATS || MODE == CE_GRAD ? BJ : 1];
+    if constexpr (MODE != CE_DW) {
+        for (int i = tid; i < BI; i += NT) rows[i] = i0 + i < ni ? p.rows[i0 + i] : CeRow{0, -1, 0.f, 0.f};
+    }
+    if constexpr (MODE == CE_STATS || MODE == CE_GRAD) {
+        for (int j = tid; j < BJ; j += NT)
+            bias[j] = j0 + j < nj ? (p.bias ? p.bias[j0 + j] : 0.f) : (MODE == CE_STATS ? -INFINITY : 0.f);
+    }
     f32x4 acc[NJ][MI];
     // (g's rows are whole vectors of zeros past the classes: their last vector is read whole)
     ce_product<T, BI, BJ, WI, WJ, ICOLS, JCOLS>(acc, ibase, p.i_ld, ni - i0, MODE == CE_DH ? (K + 7) / 8 * 8 : K, jbase,
@@ -375,28 +423,24 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
     if constexpr (MODE == CE_STATS) {
         // each row's maximum, sum of exponentials and sum over the tile's columns
         float *red = reinterpret_cast<float *>(lds0);
-        #pragma unroll
-        for (int b = 0; b < NJ; b++)
-            #pragma unroll
-            for (int r = 0; r < 4; r++) {
-                const int j = jw + 16 * b + 4 * g + r;
-                const float add = j < nj ? (p.bias ? p.bias[j] : 0.f) : -INFINITY;
-                #pragma unroll
-                for (int a = 0; a < MI; a++) acc[b][a][r] += add;
-            }
-        #pragma unroll
-        for (int a = 0; a < MI; a++) {
-            const int i = iw + 16 * a + q, label = i < ni ? p.rows[i].label : -1;
-            float mx = -INFINITY, sum = 0.f, all = 0.f;
+        if (p.bias || j0 + BJ > nj) {                // (classes past the last are -infinity)
             #pragma unroll
             for (int b = 0; b < NJ; b++)
                 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const int j = jw + 16 * b + 4 * g + r;
-                    mx = fmaxf(mx, acc[b][a][r]);
-                    all += j < nj ? acc[b][a][r] : 0.f;
-                    if (j == label && j < nj) p.picked[i] = acc[b][a][r];
+                    const float add = bias[wj * TJ + 16 * b + 4 * g + r];
+                    #pragma unroll
+                    for (int a = 0; a < MI; a++) acc[b][a][r] += add;
                 }
+        }
+        #pragma unroll
+        for (int a = 0; a < MI; a++) {
+            const int row = wi * TI + 16 * a + q, at = rows[row].label - jw;   // the label's column here
+            float mx = -INFINITY, sum = 0.f, all = 0.f;
+            #pragma unroll
+            for (int b = 0; b < NJ; b++)
+                #pragma unroll
+                for (int r = 0; r < 4; r++) mx = fmaxf(mx, acc[b][a][r]);
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
             const float base = mx == -INFINITY ? 0.f : mx;
@@ -406,10 +450,24 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
                 for (int r = 0; r < 4; r++) sum += ce_exp(acc[b][a][r] - base);
             sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
-            all += __shfl_xor(all, 16, 64);
-            all += __shfl_xor(all, 32, 64);
+            if (p.sums) {
+                #pragma unroll
+                for (int b = 0; b < NJ; b++)
+                    #pragma unroll
+                    for (int r = 0; r < 4; r++) all += jw + 16 * b + 4 * g + r < nj ? acc[b][a][r] : 0.f;
+                all += __shfl_xor(all, 16, 64);
+                all += __shfl_xor(all, 32, 64);
+            }
+            if (__any((uint32_t)at < TJ)) {
+                float hit = 0.f;
+                #pragma unroll
+                for (int b = 0; b < NJ; b++)
+                    #pragma unroll
+                    for (int r = 0; r < 4; r++) hit = at == 16 * b + 4 * g + r ? acc[b][a][r] : hit;
+                if ((uint32_t)at < TJ && at / 4 % 4 == g && jw + at < nj) p.picked[i0 + row] = hit;
+            }
             if (g == 0) {
-                float *o = red + (wj * BI + wi * TI + 16 * a + q) * 3;
+                float *o = red + (wj * BI + row) * 3;
                 o[0] = mx; o[1] = sum; o[2] = all;
             }
         }
@@ -436,16 +494,18 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
         // i = 16 a + q and j = 16 b + 4 g + r, in float32 columns i = MI q + a, j = NJ (4 g + r) + b.
         constexpr bool IP = ICOLS && sizeof(T) == 4, JP = JCOLS && sizeof(T) == 4;
         constexpr int kHalf = NT / 128;
-        static_assert(kStage == kHalf * kWaveOut && TJ == 64 && (!IP || TI == 64), "a wave's part of the stages");
+        static_assert(kStage >= kHalf * kWaveOut && (!IP || TI == 64) && (!JP || TJ == 64), "a wave's part of the stages");
         lds_char *mine = (wave < kHalf ? (lds_char *)lds0 : (lds_char *)lds1) + wave % kHalf * kWaveOut;
-        const int lrow = late / 8, lcol = late % 8 * 8, j = jw + lcol;
-        float add[8], col[8];
+        const int lrow = late / 8, lcol = late % 8 * 8;
+        // (parts are multiplied when they are added)
+        const float factor = MODE == CE_GRAD || p.part_stride ? 1.f : *p.factor;
+        #pragma unroll
+        for (int c = 0; c < TJ / 64; c++) {
+        const int j = jw + 64 * c + lcol;
+        float col[8];
         if constexpr (MODE == CE_GRAD) {
             #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                add[e] = p.bias && j + e < nj ? p.bias[j + e] : 0.f;
-                col[e] = 0.f;
-            }
+            for (int e = 0; e < 8; e++) col[e] = 0.f;
         }
         #pragma unroll
         for (int h = 0; h < TI / 64; h++) {
@@ -455,7 +515,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
                 for (int b = 0; b < 4; b++) {
                     const int row = IP ? 4 * q + a : 16 * a + q, chunk = JP ? 4 * g + b : 4 * b + g;
                     const f32x4 v = JP ? f32x4{acc[0][4 * h + a][b], acc[1][4 * h + a][b], acc[2][4 * h + a][b], acc[3][4 * h + a][b]}
-                                       : acc[b][4 * h + a];
+                                       : acc[4 * c + b][4 * h + a];
                     *(lds_f32x4 *)(mine + row * 256 + ((chunk ^ (row % 16)) * 16)) = v;
                 }
             ce_wave_sync();
@@ -471,19 +531,34 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
                 }
                 if (i >= ni) continue;
                 if constexpr (MODE == CE_GRAD) {
-                    const CeRow r = p.rows[i];
+                    const CeRow r = rows[i - i0];
                     const int at = r.label - p.first - j;
-                    const float grow = r.scale * (1.f + 2.f * p.z * r.lse), flat = r.scale * p.flat, hit = r.scale * p.hit;
+                    const float grow = r.scale * (1.f + 2.f * p.z * r.lse), flat = r.scale * p.flat;
+                    if (p.bias) {
+                        #pragma unroll
+                        for (int e = 0; e < 8; e++) v[e] += bias[j + e - j0];
+                    }
                     #pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        v[e] = __builtin_fmaf(ce_exp(v[e] + add[e] - r.lse), grow, -flat) - (e == at ? hit : 0.f);
-                        v[e] = j + e < nj ? v[e] : 0.f;
-                        col[e] += v[e];
+                    for (int e = 0; e < 8; e++) v[e] = __builtin_fmaf(ce_exp(v[e] - r.lse), grow, -flat);
+                    if ((uint32_t)at < 8) {
+                        const float hit = r.scale * p.hit;
+                        #pragma unroll
+                        for (int e = 0; e < 8; e++) v[e] -= e == at ? hit : 0.f;
+                    }
+                    if (j0 + BJ > nj) {
+                        #pragma unroll
+                        for (int e = 0; e < 8; e++) v[e] = j + e < nj ? v[e] : 0.f;
+                    }
+                    if (p.colsum) {
+                        #pragma unroll
+                        for (int e = 0; e < 8; e++) col[e] += v[e];
                     }
                     ce_store8((T *)p.g + (int64_t)i * p.g_ld + j, v);
                 } else if (j < nj) {                 // (the second half of a vector that c cuts, in float32: below)
-                    const int64_t row_out = p.part_stride || MODE == CE_DW ? i : p.rows[i].row;
+                    const int64_t row_out = MODE == CE_DW || p.part_stride ? i : rows[MODE == CE_DW ? 0 : i - i0].row;
                     const bool whole = sizeof(T) == 2 || j + 4 < nj;
+                    #pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] *= factor;
                     if (p.out_f32) {
                         float *o = (float *)p.out + (int64_t)pl.part * p.part_stride + row_out * p.out_ld + j;
                         if (p.add) {
@@ -507,24 +582,136 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
             ce_wave_sync();
         }
         if constexpr (MODE == CE_GRAD) {
-            if (p.colsum) {
-                float *red = reinterpret_cast<float *>(lds0);
-                __syncthreads();
+            if (p.colsum) {                          // the wave's rows; then the tile's, of all its waves
                 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    float v = col[e];
-                    for (int o = 8; o < 64; o *= 2) v += __shfl_xor(v, o, 64);
-                    if (lrow == 0) red[wi * BJ + wj * TJ + lcol + e] = v;
-                }
-                __syncthreads();
-                for (int c = tid; c < BJ; c += NT) {
-                    if (j0 + c >= nj) break;
-                    float v = 0.f;
-                    #pragma unroll
-                    for (int w = 0; w < WI; w++) v += red[w * BJ + c];
-                    p.colsum[(int64_t)pl.ti * p.colsum_ld + j0 + c] = v;
+                    for (int o = 8; o < 64; o *= 2) col[e] += __shfl_xor(col[e], o, 64);
+                    if (lrow == 0 && j + e < nj) p.colsum[(int64_t)(pl.ti * WI + wi) * p.colsum_ld + j + e] = col[e];
                 }
             }
+        }
+        }
+    }
+}
+
+// ---- few rows, or few tiles ---------------------------------------------------
+// Logits of 16 MI x 16 NJ by one workgroup, its four waves each a quarter of k.  Nothing
+// is shared, so the fragments are loaded straight into registers, kAhead steps ahead;
+// the waves' sums are added through LDS in order.  With few rows this is a stream of the
+// weights, with few tiles it spreads them over the chip.
+template <typename T, int MI, int NJ, int MODE>
+__global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
+{
+    constexpr int BI = 16 * MI, BJ = 16 * NJ, kAhead = 32 / (MI + NJ), kPitch = BJ + 4, BK = 64 / sizeof(T);
+    constexpr int kGroups = 4 * NJ, kLanes = 16 / MI;        // groups of four columns of a row, threads of a row
+    typedef typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type frag;
+    __shared__ __align__(16) float part[4][BI * kPitch];
+    const int ni = p.rows ? *p.count : (int)p.m, nj = p.classes;
+    CePlace pl;
+    if (!ce_place(pl, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, 1)) return;
+    const int i0 = pl.ti * BI, j0 = pl.tj * BJ;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane % 16, g = lane / 16;
+    const int width = p.c * (int)sizeof(T);
+    const __amdgpu_buffer_rsrc_t ri = buf_view((const char *)p.i + i0 * p.i_ld, (min(ni - i0, BI) - 1) * (int)p.i_ld + width);
+    const __amdgpu_buffer_rsrc_t rj = buf_view((const char *)p.j + j0 * p.j_ld, (min(nj - j0, BJ) - 1) * (int)p.j_ld + width);
+    const int steps = (p.c + BK - 1) / BK, s0 = wave * steps / 4, s1 = (wave + 1) * steps / 4;
+    frag fi[kAhead][MI], fj[kAhead][NJ];
+    auto load = [&](int d, int s) __attribute__((always_inline)) {
+        const uint32_t at = s * 64 + g * 16, in = s < s1 && (int)at < width ? at : kBufOff;
+        #pragma unroll
+        for (int b = 0; b < NJ; b++) fj[d][b] = __builtin_bit_cast(frag, bld16(rj, in + (16 * b + q) * (uint32_t)p.j_ld));
+        #pragma unroll
+        for (int a = 0; a < MI; a++) fi[d][a] = __builtin_bit_cast(frag, bld16(ri, in + (16 * a + q) * (uint32_t)p.i_ld));
+    };
+    f32x4 acc[NJ][MI], total[NJ][MI];
+    ce_zero(acc);
+    ce_zero(total);
+    #pragma unroll
+    for (int d = 0; d < kAhead; d++) load(d, s0 + d);
+    for (int s = s0; s < s1; s += kAhead) {
+        #pragma unroll
+        for (int d = 0; d < kAhead; d++) {
+            #pragma unroll
+            for (int a = 0; a < MI; a++)
+                #pragma unroll
+                for (int b = 0; b < NJ; b++) ce_mma(acc[b][a], fj[d][b], fi[d][a]);
+            load(d, s + kAhead + d);
+        }
+        if constexpr (sizeof(T) == 4) ce_fold(total, acc);
+    }
+    #pragma unroll
+    for (int a = 0; a < MI; a++)
+        #pragma unroll
+        for (int b = 0; b < NJ; b++)
+            *reinterpret_cast<f32x4 *>(&part[wave][(16 * a + q) * kPitch + 16 * b + 4 * g]) = sizeof(T) == 4 ? total[b][a] : acc[b][a];
+    __syncthreads();
+    // kLanes threads a row, group after group of its columns
+    const int row = tid / kLanes, i = i0 + row, li = tid % kLanes;
+    CeRow info = CeRow{0, -1, 0.f, 0.f};
+    if (i < ni) {
+        if (p.rows) info = p.rows[i];
+        else info.label = p.labels[i];
+    }
+    float mx = -INFINITY, sum = 0.f, all = 0.f, v[(kGroups + kLanes - 1) / kLanes][4];
+    #pragma unroll
+    for (int u = 0; u < (kGroups + kLanes - 1) / kLanes; u++) {
+        const int c = (u * kLanes + li) * 4;
+        #pragma unroll
+        for (int r = 0; r < 4; r++) v[u][r] = -INFINITY;
+        if (c >= BJ) continue;
+        const float *o = &part[0][row * kPitch + c];
+        #pragma unroll
+        for (int r = 0; r < 4; r++) {
+            float l = o[r];
+            #pragma unroll
+            for (int w = 1; w < 4; w++) l += o[w * BI * kPitch + r];
+            const int j = j0 + c + r;
+            if (p.bias && j < nj) l += p.bias[j];
+            v[u][r] = j < nj ? l : -INFINITY;
+            if constexpr (MODE == CE_STATS) {
+                mx = fmaxf(mx, v[u][r]);
+                all += j < nj ? l : 0.f;
+                if (j == info.label && j < nj && i < ni) p.picked[i] = l;
+            } else {
+                const float t = __builtin_fmaf(ce_exp(l - info.lse), info.scale * (1.f + 2.f * p.z * info.lse), -info.scale * p.flat) -
+                                (j + p.first == info.label ? info.scale * p.hit : 0.f);
+                v[u][r] = j < nj && i < ni ? t : 0.f;
+            }
+        }
+        if constexpr (MODE == CE_GRAD)
+            if (i < ni) ce_store4((T *)p.g + (int64_t)i * p.g_ld + j0 + c, v[u]);
+    }
+    if constexpr (MODE == CE_STATS) {
+        #pragma unroll
+        for (int o = 1; o < kLanes; o *= 2) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        const float base = mx == -INFINITY ? 0.f : mx;
+        #pragma unroll
+        for (int u = 0; u < (kGroups + kLanes - 1) / kLanes; u++)
+            #pragma unroll
+            for (int r = 0; r < 4; r++) sum += ce_exp(v[u][r] - base);
+        #pragma unroll
+        for (int o = 1; o < kLanes; o *= 2) {
+            sum += __shfl_xor(sum, o, 64);
+            all += __shfl_xor(all, o, 64);
+        }
+        if (li == 0 && i < ni) {
+            const int64_t o = (int64_t)pl.tj * p.m + i;
+            p.stats[o] = float2{mx, sum};
+            if (p.sums) p.sums[o] = all;
+        }
+    } else if (p.colsum) {
+        __syncthreads();
+        #pragma unroll
+        for (int u = 0; u < (kGroups + kLanes - 1) / kLanes; u++) {
+            const int c = (u * kLanes + li) * 4;
+            if (c < BJ) *reinterpret_cast<f32x4 *>(&part[0][row * kPitch + c]) = f32x4{v[u][0], v[u][1], v[u][2], v[u][3]};
+        }
+        __syncthreads();
+        if (tid < BJ && j0 + tid < nj) {
+            float t = 0.f;
+            #pragma unroll
+            for (int r = 0; r < BI; r++) t += part[0][r * kPitch + tid];
+            p.colsum[(int64_t)pl.ti * p.colsum_ld + j0 + tid] = t;
         }
     }
 }
@@ -540,71 +727,89 @@ __device__ __forceinline__ void ce_join(float &mx, double &sum, float mx2, doubl
 }
 
 // The rows' losses and log sums from the tiles' maxima and sums (in float64), and the
-// sum of the workgroup's losses.
-__global__ __launch_bounds__(kThreads) void k_ce_rows(CeLoss p)
+// sum of the workgroup's losses.  R rows a workgroup of NT threads.
+template <int R, int NT>
+__global__ __launch_bounds__(NT) void k_ce_rows(CeLoss p)
 {
-    __shared__ float rm[4][kLossRows];
-    __shared__ double rs[4][kLossRows], ra[4][kLossRows];
-    const int tid = threadIdx.x, r = tid % kLossRows, slice = tid / kLossRows, count = *p.count;
-    const int i = blockIdx.x * kLossRows + r;
-    if (blockIdx.x && (int)blockIdx.x * kLossRows >= count) return;
+    __shared__ float rm[NT / 64][R];
+    __shared__ double rs[NT / 64][R], ra[NT / 64][R];
+    const int tid = threadIdx.x, r = tid % R, slice = tid / R, count = p.rows ? *p.count : (int)p.m;
+    const int i = blockIdx.x * R + r;
+    if (blockIdx.x && (int)blockIdx.x * R >= count) return;
     float mx = -INFINITY;
     double sum = 0.0, all = 0.0;
     if (i < count) {
         #pragma unroll 4
-        for (int t = slice; t < p.tiles; t += kThreads / kLossRows) {
+        for (int t = slice; t < p.tiles; t += NT / R) {
             const float2 v = p.stats[(int64_t)t * p.m + i];
             if (p.sums) all += (double)p.sums[(int64_t)t * p.m + i];
             ce_join(mx, sum, v.x, (double)v.y);
         }
     }
-    for (int o = kLossRows; o < 64; o *= 2) {
+    #pragma unroll
+    for (int o = R; o < 64; o *= 2) {
         ce_join(mx, sum, __shfl_xor(mx, o, 64), __shfl_xor(sum, o, 64));
         all += __shfl_xor(all, o, 64);
     }
-    if ((tid & 63) < kLossRows) { rm[tid >> 6][r] = mx; rs[tid >> 6][r] = sum; ra[tid >> 6][r] = all; }
+    if ((tid & 63) < R) { rm[tid >> 6][r] = mx; rs[tid >> 6][r] = sum; ra[tid >> 6][r] = all; }
     __syncthreads();
-    if (tid >= kLossRows) return;
+    if (tid >= R) return;
     double loss = 0.0;
+    int counted = 0;
     if (i < count) {
-        for (int w = 1; w < 4; w++) {
+        for (int w = 1; w < NT / 64; w++) {
             ce_join(mx, sum, rm[w][r], rs[w][r]);
             all += ra[w][r];
         }
-        const CeRow row = p.rows[i];
-        const double lse = (double)mx + log(sum);
-        loss = NAN;
-        if ((uint32_t)row.label < (uint32_t)p.classes) {
-            loss = lse - p.hit * (double)p.picked[i] + p.z * lse * lse;
-            if (p.sums) loss -= p.flat * all;
+        const int row = p.rows ? p.rows[i].row : i, label = p.rows ? p.rows[i].label : p.labels[i];
+        double lse = 0.0;
+        counted = label != p.ignore;
+        if (counted) {
+            lse = (double)mx + log(sum);
+            loss = NAN;
+            if ((uint32_t)label < (uint32_t)p.classes) {
+                loss = lse - p.hit * (double)p.picked[i] + p.z * lse * lse;
+                if (p.sums) loss -= p.flat * all;
+            }
         }
-        p.lse[1 + row.row] = (float)lse;
-        p.loss[1 + row.row] = (float)loss;
+        p.lse[1 + row] = (float)lse;
+        p.loss[1 + row] = (float)loss;
     }
-    for (int o = 1; o < kLossRows; o *= 2) loss += __shfl_xor(loss, o, 64);
+    #pragma unroll
+    for (int o = 1; o < R; o *= 2) {
+        loss += __shfl_xor(loss, o, 64);
+        counted += __shfl_xor(counted, o, 64);
+    }
     if (tid) return;
     if (p.groups == 1) {
-        p.loss[0] = count ? (float)(loss / count) : 0.f;
-        p.lse[0] = (float)count;
+        p.loss[0] = counted ? (float)(loss / counted) : 0.f;
+        p.lse[0] = (float)counted;
     } else {
-        p.part[blockIdx.x] = loss;
+        p.part[blockIdx.x] = double2{loss, (double)counted};
     }
 }
 
 __global__ __launch_bounds__(1024) void k_ce_mean(CeLoss p)
 {
-    __shared__ double red[16];
-    const int tid = threadIdx.x, count = *p.count, groups = (count + kLossRows - 1) / kLossRows;
-    double v = 0.0;
-    for (int b = tid; b < groups; b += 1024) v += p.part[b];
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    if ((tid & 63) == 0) red[tid >> 6] = v;
+    __shared__ double red[16], red_n[16];
+    const int tid = threadIdx.x, count = p.rows ? *p.count : (int)p.m, groups = (count + kLossRows - 1) / kLossRows;
+    double v = 0.0, n = 0.0;
+    for (int b = tid; b < groups; b += 1024) {
+        const double2 u = p.part[b];
+        v += u.x;
+        n += u.y;
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+        v += __shfl_xor(v, o, 64);
+        n += __shfl_xor(n, o, 64);
+    }
+    if ((tid & 63) == 0) { red[tid >> 6] = v; red_n[tid >> 6] = n; }
     __syncthreads();
     if (tid) return;
-    v = 0.0;
-    for (int w = 0; w < 16; w++) v += red[w];
-    p.loss[0] = count ? (float)(v / count) : 0.f;
-    p.lse[0] = (float)count;
+    v = n = 0.0;
+    for (int w = 0; w < 16; w++) { v += red[w]; n += red_n[w]; }
+    p.loss[0] = n > 0.0 ? (float)(v / n) : 0.f;
+    p.lse[0] = (float)n;
 }
 
 // ---- sums over parts -----------------------------------------------------------
@@ -625,6 +830,9 @@ __global__ __launch_bounds__(kThreads) void k_ce_sum(CeSum p)
         for (int r = 0; r < 4; r++) v[r] += u[r];
     }
     const int64_t row = p.rows ? p.rows[i].row : i;
+    const float factor = *p.factor;
+    #pragma unroll
+    for (int r = 0; r < 4; r++) v[r] *= factor;
     ce_store4((T *)p.out + row * p.out_ld + j, v);
 }
 
@@ -635,49 +843,76 @@ __global__ __launch_bounds__(kThreads) void k_ce_bias(CeBias p)
     double v = 0.0;
     #pragma unroll 4
     for (int t = 0; t < tiles; t++) v += (double)p.colsum[(int64_t)t * p.ld + j];
-    p.out[j] = (float)v;
+    p.out[j] = (float)(v * *p.factor);
 }
 
 // ---- how a call runs -------------------------------------------------------------
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 
-// Tiles of 256 x 256 (one workgroup of eight waves a CU) where they fill the chip,
-// else of 128 x 128 (two workgroups of four waves a CU).
-inline int ce_tile(int dtype, int64_t ni, int64_t nj)
+// How a product's tiles run: 256 x 256 (one workgroup of eight waves a CU) where they
+// fill the chip, else 128 x 128 (two workgroups of four waves a CU); logits of few rows
+// or of too few tiles for that run as k_ce_small, 16 x i by 16 x j.
+struct CeTile { int bi, bj; bool small; };
+inline CeTile ce_tile(int dtype, int64_t ni, int64_t nj)
 {
-    return dtype == DT_BF16 && cdiv(ni, 256) * cdiv(nj, 256) >= 192 ? 256 : 128;
+    const int b = dtype == DT_BF16 && cdiv(ni, 256) * cdiv(nj, 256) >= 192 ? 256 : 128;
+    return CeTile{b, b, false};
+}
+inline CeTile ce_logit_tile(int dtype, int64_t m, int64_t classes)
+{
+    const CeTile t = ce_tile(dtype, m, classes);
+    if (m > 32 && cdiv(m, 128) * cdiv(classes, 128) >= 128) return t;
+    const int mi = m > 16 ? 2 : 1;
+    int nj = 4;
+    while (nj > 1 && cdiv(m, 16 * mi) * cdiv(classes, 16 * nj) < 512) nj /= 2;
+    return CeTile{16 * mi, 16 * nj, true};
 }
 
 // k ranges a product is cut into where its tiles would leave the chip idle
-inline int ce_parts(int tile, int64_t ni, int64_t nj, int64_t steps)
+inline int ce_parts(const CeTile &t, int64_t ni, int64_t nj, int64_t steps)
 {
-    const int64_t slots = tile == 256 ? 256 : 512, tiles = cdiv(ni, tile) * cdiv(nj, tile);
+    const int64_t slots = t.bi == 256 ? 256 : 512, tiles = cdiv(ni, t.bi) * cdiv(nj, t.bj);
     const int64_t want = slots / tiles, most = steps / 4;
     const int64_t n = want < most ? want : most;
     return n < 1 ? 1 : (n > 64 ? 64 : (int)n);
 }
 
 template <typename T, int MODE>
-hipError_t go(const CeGemm &p, int tile, int64_t grid, hipStream_t s)
+void go(const CeGemm &p, const CeTile &t, int64_t grid, hipStream_t s)
 {
-    if constexpr (sizeof(T) == 2) {
-        if (tile == 256) {
-            hipLaunchKernelGGL((k_ce_gemm<T, 256, 256, 2, 4, MODE>), dim3((unsigned)grid), dim3(512), 0, s, p);
-            return hipGetLastError();
+    const dim3 g((unsigned)grid);
+    if constexpr (MODE == CE_STATS || MODE == CE_GRAD) {
+        if (t.small) {
+            const auto at = [&](auto mi) {
+                constexpr int MI = decltype(mi)::value;
+                if (t.bj == 64) hipLaunchKernelGGL((k_ce_small<T, MI, 4, MODE>), g, dim3(kThreads), 0, s, p);
+                else if (t.bj == 32) hipLaunchKernelGGL((k_ce_small<T, MI, 2, MODE>), g, dim3(kThreads), 0, s, p);
+                else hipLaunchKernelGGL((k_ce_small<T, MI, 1, MODE>), g, dim3(kThreads), 0, s, p);
+            };
+            if (t.bi == 16) at(std::integral_constant<int, 1>{});
+            else at(std::integral_constant<int, 2>{});
+            return;
         }
     }
-    hipLaunchKernelGGL((k_ce_gemm<T, 128, 128, 2, 2, MODE>), dim3((unsigned)grid), dim3(256), 0, s, p);
-    return hipGetLastError();
+    if constexpr (sizeof(T) == 2) {
+        if (t.bi == 256) {
+            hipLaunchKernelGGL((k_ce_gemm<T, 256, 256, 2, 4, MODE>), g, dim3(512), 0, s, p);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((k_ce_gemm<T, 128, 128, 2, 2, MODE>), g, dim3(256), 0, s, p);
 }
 
 template <int MODE>
-hipError_t gemm(const CeCall &a, const CeGemm &p, int tile, int64_t ni, int64_t nj, int64_t k, hipStream_t s)
+hipError_t gemm(const CeCall &a, const CeGemm &p, const CeTile &t, int64_t ni, int64_t nj, int64_t k, hipStream_t s)
 {
     const double es = a.dtype == DT_BF16 ? 2 : 4;
     TraceScope tr(KC_CONV, KID_LINEAR_CE, s, es * ((double)ni * k + (double)nj * k + (double)ni * nj), 2.0 * ni * nj * k);
-    const int64_t grid = cdiv(ni, tile) * cdiv(nj, tile) * p.parts;
-    return a.dtype == DT_BF16 ? go<bf16_t, MODE>(p, tile, grid, s) : go<float, MODE>(p, tile, grid, s);
+    const int64_t grid = cdiv(ni, t.bi) * cdiv(nj, t.bj) * p.parts;
+    if (a.dtype == DT_BF16) go<bf16_t, MODE>(p, t, grid, s);
+    else go<float, MODE>(p, t, grid, s);
+    return hipGetLastError();
 }
 
 // What both directions keep in the workspace: the count, the list and the rows' copy.
@@ -700,6 +935,7 @@ hipError_t launch_list(const CeCall &a, const CeHead &w, char *ws, hipStream_t s
     p.m = a.m; p.classes = a.classes; p.ignore = a.ignore;
     p.labels = a.labels;
     p.count = (int *)ws;
+    p.factor = (float *)(ws + 8);
     p.counts = a.m > 4 * kCountRows ? (int *)(ws + w.counts) : nullptr;
     p.rows = (CeRow *)(ws + w.rows);
     p.h = a.h; p.h_ld = a.h_ld * es;
@@ -714,18 +950,18 @@ hipError_t launch_list(const CeCall &a, const CeHead &w, char *ws, hipStream_t s
 
 struct CeFwdPlan {
     CeHead head;
-    int tile;
+    CeTile tile;
     int64_t tiles, groups, stats, sums, picked, part, end;
     explicit CeFwdPlan(const CeCall &a) : head(a)
     {
-        tile = ce_tile(a.dtype, a.m, a.classes);
-        tiles = cdiv(a.classes, tile);
+        tile = ce_logit_tile(a.dtype, a.m, a.classes);
+        tiles = cdiv(a.classes, tile.bj);
         groups = cdiv(a.m, kLossRows);
-        stats = head.end;
+        stats = tile.small ? 0 : head.end;       // (few rows are taken as they are)
         sums = up256(stats + tiles * a.m * 8);
         picked = up256(sums + (a.smoothing > 0.f ? tiles * a.m * 4 : 0));
         part = up256(picked + a.m * 4);
-        end = up256(part + groups * 8);
+        end = up256(part + groups * 16);
     }
 };
 
@@ -735,7 +971,8 @@ constexpr int64_t kPieceWidth = kCeMaxLd;
 struct CeBwdPlan {
     CeHead head;
     int64_t pieces, width;                 // classes of a piece, a multiple of 256
-    int grad_tile, dh_tile, dw_tile, dh_parts, dw_parts;
+    CeTile grad_tile, dh_tile, dw_tile;
+    int grad_rows, dh_parts, dw_parts;     // grad_rows: of a partial row of dbias
     int64_t g, dh, dw, colsum, end;
     explicit CeBwdPlan(const CeCall &a) : head(a)
     {
@@ -746,7 +983,8 @@ struct CeBwdPlan {
         width = cdiv(cdiv(a.classes, pieces), 256) * 256;
         pieces = cdiv(a.classes, width);
         const int64_t wide = width < a.classes ? width : a.classes;
-        grad_tile = ce_tile(a.dtype, a.m, wide);
+        grad_tile = ce_logit_tile(a.dtype, a.m, wide);
+        grad_rows = grad_tile.small ? grad_tile.bi : grad_tile.bi / 2;
         dh_tile = ce_tile(a.dtype, a.m, a.c);
         dw_tile = ce_tile(a.dtype, wide, a.c);
         dh_parts = ce_parts(dh_tile, a.m, a.c, cdiv(wide, bk));
@@ -755,7 +993,7 @@ struct CeBwdPlan {
         dh = up256(g + a.m * width * es);
         dw = up256(dh + (a.dh && (pieces > 1 || dh_parts > 1) ? dh_parts * a.m * a.c * 4 : 0));
         colsum = up256(dw + (a.dw && dw_parts > 1 ? dw_parts * wide * a.c * 4 : 0));
-        end = up256(colsum + (a.dbias ? cdiv(a.m, grad_tile) * a.classes * 4 : 0));
+        end = up256(colsum + (a.dbias ? cdiv(a.m, grad_tile.bi) * (grad_tile.bi / grad_rows) * a.classes * 4 : 0));
     }
 };
 
@@ -784,11 +1022,16 @@ hipError_t launch_ce_fwd(const CeCall &a, void *ws_, hipStream_t s)
     char *ws = (char *)ws_;
     const CeFwdPlan w(a);
     const int es = a.dtype == DT_BF16 ? 2 : 4;
-    CE_TRY(launch_list(a, w.head, ws, s));
     CeGemm p{};
-    p.count = (const int *)ws; p.rows = (const CeRow *)(ws + w.head.rows);
     p.c = a.c; p.classes = a.classes; p.m = a.m; p.parts = 1;
-    p.i = ws + w.head.copy; p.i_ld = (int64_t)a.c * es;
+    if (w.tile.small) {
+        p.i = a.h; p.i_ld = a.h_ld * es;
+        p.labels = a.labels;
+    } else {
+        CE_TRY(launch_list(a, w.head, ws, s));
+        p.count = (const int *)ws; p.rows = (const CeRow *)(ws + w.head.rows);
+        p.i = ws + w.head.copy; p.i_ld = (int64_t)a.c * es;
+    }
     p.j = a.w; p.j_ld = a.w_ld * es;
     p.bias = a.bias;
     p.stats = (float2 *)(ws + w.stats);
@@ -796,12 +1039,16 @@ hipError_t launch_ce_fwd(const CeCall &a, void *ws_, hipStream_t s)
     p.picked = (float *)(ws + w.picked);
     CE_TRY(gemm<CE_STATS>(a, p, w.tile, a.m, a.classes, a.c, s));
     CeLoss l{};
-    l.count = p.count; l.rows = p.rows; l.stats = p.stats; l.sums = p.sums; l.picked = p.picked;
+    l.count = p.count; l.rows = p.rows; l.labels = a.labels; l.ignore = a.ignore;
+    l.stats = p.stats; l.sums = p.sums; l.picked = p.picked;
     l.m = a.m; l.tiles = (int)w.tiles; l.groups = (int)w.groups; l.classes = a.classes;
     l.hit = 1.0 - (double)a.smoothing; l.flat = (double)a.smoothing / a.classes; l.z = a.z;
-    l.loss = a.loss; l.lse = a.lse; l.part = (double *)(ws + w.part);
+    l.loss = a.loss; l.lse = a.lse; l.part = (double2 *)(ws + w.part);
     TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 8.0 * a.m * w.tiles, 0.0);
-    hipLaunchKernelGGL(k_ce_rows, dim3((unsigned)w.groups), dim3(kThreads), 0, s, l);
+    // (a single row takes all threads, and the tiles of up to 16 four times as many)
+    if (a.m == 1) hipLaunchKernelGGL((k_ce_rows<1, kThreads>), dim3(1), dim3(kThreads), 0, s, l);
+    else if (w.groups == 1) hipLaunchKernelGGL((k_ce_rows<kLossRows, 1024>), dim3(1), dim3(1024), 0, s, l);
+    else hipLaunchKernelGGL((k_ce_rows<kLossRows, kThreads>), dim3((unsigned)w.groups), dim3(kThreads), 0, s, l);
     if (w.groups > 1) hipLaunchKernelGGL(k_ce_mean, dim3(1), dim3(1024), 0, s, l);
     return hipGetLastError();
 }
@@ -813,7 +1060,7 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
     const int es = a.dtype == DT_BF16 ? 2 : 4;
     CE_TRY(launch_list(a, w.head, ws, s));
     CeGemm p{};
-    p.count = (const int *)ws; p.rows = (const CeRow *)(ws + w.head.rows);
+    p.count = (const int *)ws; p.rows = (const CeRow *)(ws + w.head.rows); p.factor = (const float *)(ws + 8);
     p.c = a.c; p.m = a.m;
     p.z = a.z; p.hit = 1.f - a.smoothing; p.flat = a.smoothing / (float)a.classes;
     p.g = ws + w.g; p.g_ld = w.width;
@@ -843,7 +1090,7 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
             CE_TRY(gemm<CE_DW>(a, q, w.dw_tile, wide, a.c, a.m, s));
             if (w.dw_parts > 1) {
                 CeSum t{};
-                t.part = (const float *)q.out; t.part_stride = q.part_stride; t.parts = w.dw_parts; t.c = a.c; t.n = wide;
+                t.part = (const float *)q.out; t.part_stride = q.part_stride; t.parts = w.dw_parts; t.c = a.c; t.n = wide; t.factor = p.factor;
                 t.out = (char *)a.dw + first * a.dw_ld * (a.dw_dtype == DT_BF16 ? 2 : 4); t.out_ld = a.dw_ld;
                 CE_TRY(sum_parts(t, a.dw_dtype, wide, s));
             }
@@ -861,15 +1108,15 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
     if (a.dh && gather_dh) {
         CeSum t{};
         t.part = (const float *)(ws + w.dh); t.part_stride = a.m * a.c; t.parts = w.dh_parts; t.c = a.c;
-        t.rows = p.rows; t.count = p.count;
+        t.rows = p.rows; t.count = p.count; t.factor = p.factor;
         t.out = a.dh; t.out_ld = a.dh_ld;
         CE_TRY(sum_parts(t, a.dtype, a.m, s));
     }
     if (a.dbias) {
         CeBias b{};
-        b.count = p.count; b.tile = w.grad_tile; b.classes = a.classes;
+        b.count = p.count; b.tile = w.grad_rows; b.factor = p.factor; b.classes = a.classes;
         b.colsum = (const float *)(ws + w.colsum); b.ld = a.classes; b.out = a.dbias;
-        TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 4.0 * a.classes * (cdiv(a.m, w.grad_tile) + 1), 0.0);
+        TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 4.0 * a.classes * (cdiv(a.m, w.grad_rows) + 1), 0.0);
         hipLaunchKernelGGL(k_ce_bias, dim3((unsigned)cdiv(a.classes, kThreads)), dim3(kThreads), 0, s, b);
     }
     return hipGetLastError();
