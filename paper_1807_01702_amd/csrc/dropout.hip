@@ -13,10 +13,12 @@
 // would take as long as the memory accesses of bf16 rows (quarter-rate products).
 // The scale is that of the rounded probability, so E[y] = x exactly.
 //
-// A thread takes eight channels of a row (one call of the generator), kDropWays of
-// them with their loads issued ahead of the generator.  Any stride and alignment:
-// the eight elements move as one 16-byte access (two in float32), which gfx950
-// allows at element alignment, and one by one at a row's ragged end.
+// A thread takes eight channels of a row: one call of the generator.  Any stride and
+// alignment: the eight elements move as one 16-byte access (two in float32), which
+// gfx950 allows at element alignment, and one by one at a row's ragged end.  Bound by
+// HBM: 8192 bf16 rows of 4096 with an addition 36.9 us = 5.5 TB/s (two, four and eight
+// blocks a thread, whose loads all come first: 39.0, 42.3 and 46.0 us), rows of 4095, none
+// of them aligned, 54 us.
 #include "common.hpp"
 #include "kernels.hpp"
 #include "trace.hpp"
@@ -24,8 +26,6 @@
 namespace bnr {
 
 namespace {
-
-constexpr int kDropWays = 4;
 
 __device__ __forceinline__ void philox4x32(uint32_t x[4], uint32_t k0, uint32_t k1)
 {
@@ -41,10 +41,10 @@ __device__ __forceinline__ void philox4x32(uint32_t x[4], uint32_t k0, uint32_t 
 // Eight elements of storage type T, as they lie in memory.
 template <typename T> struct Eight { T e[8]; };
 
-template <typename T> __device__ __forceinline__ Eight<T> load8(const T *p, int n)
+template <bool WHOLE, typename T> __device__ __forceinline__ Eight<T> load8(const T *p, int n)
 {
     Eight<T> v;
-    if (n == 8) {
+    if (WHOLE || n == 8) {
         __builtin_memcpy(&v, p, sizeof v);       // element-aligned: one 16-byte access each half KiB of a wave
     } else {
         #pragma unroll
@@ -52,9 +52,9 @@ template <typename T> __device__ __forceinline__ Eight<T> load8(const T *p, int 
     }
     return v;
 }
-template <typename T> __device__ __forceinline__ void store8(T *p, const Eight<T> &v, int n)
+template <bool WHOLE, typename T> __device__ __forceinline__ void store8(T *p, const Eight<T> &v, int n)
 {
-    if (n == 8) {
+    if (WHOLE || n == 8) {
         __builtin_memcpy(p, &v, sizeof v);
     } else {
         #pragma unroll
@@ -68,64 +68,59 @@ __device__ __forceinline__ float widen(bf16_t v) { return bf2f(v); }
 __device__ __forceinline__ void narrow(float v, float &o) { o = v; }
 __device__ __forceinline__ void narrow(float v, bf16_t &o) { o = f2bf(v); }
 
-// Work item i of a workgroup's kDropWays * kThreads: block (first + i) % blocks of row
-// (first + i) / blocks; the workgroup's own first item is divided once, the rest by a
-// product (i + a block number stays below 2^31).
-template <typename T, bool ADD>
+// Thread t of a workgroup: block (first + t) % blocks of row (first + t) / blocks; the
+// workgroup's own first item is divided once, the rest by a product (t + a block number
+// stays below 2^31).  WHOLE: rows of whole blocks (c a multiple of eight), without the
+// code of ragged ends.
+template <typename T, bool ADD, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutParams p)
 {
-    const uint64_t first = (uint64_t)blockIdx.x * (kDropWays * kThreads);
+    const uint64_t first = (uint64_t)blockIdx.x * kThreads;
     const uint64_t row0 = first / p.blocks;
     const uint32_t col0 = (uint32_t)(first - row0 * p.blocks);
     const uint32_t step = p.step_dev ? *p.step_dev : p.step;
     const uint32_t k0 = (uint32_t)p.seed, k1 = (uint32_t)(p.seed >> 32);
     const T *x = (const T *)p.x, *add = (const T *)p.add;
     T *y = (T *)p.y;
-    Eight<T> vx[kDropWays], va[kDropWays];
-    uint32_t row[kDropWays], blk[kDropWays];
-    int n[kDropWays];
+    const uint32_t t = col0 + threadIdx.x, q = (uint32_t)(((uint64_t)t * p.magic) >> p.shift);
+    const uint64_t r = row0 + q;
+    const uint32_t blk = t - q * p.blocks, row = (uint32_t)r;
+    if (r >= (uint64_t)p.m) return;
+    const int n = WHOLE ? 8 : min(8, p.c - (int)blk * 8);
+    const Eight<T> vx = load8<WHOLE>(x + (int64_t)row * p.x_ldc + blk * 8, n);
+    Eight<T> va;
+    if constexpr (ADD) va = load8<WHOLE>(add + (int64_t)row * p.add_ldc + blk * 8, n);
+    uint32_t w[4] = {blk, row, p.site, step};
+    philox4x32(w, k0, k1);
+    Eight<T> o;
     #pragma unroll
-    for (int u = 0; u < kDropWays; u++) {
-        const uint32_t t = col0 + u * kThreads + threadIdx.x;
-        const uint32_t q = (uint32_t)(((uint64_t)t * p.magic) >> p.shift);
-        const uint64_t r = row0 + q;
-        blk[u] = t - q * p.blocks;
-        row[u] = (uint32_t)r;
-        n[u] = r < (uint64_t)p.m ? min(8, p.c - (int)blk[u] * 8) : 0;
-        if (n[u] > 0) {
-            vx[u] = load8(x + (int64_t)row[u] * p.x_ldc + blk[u] * 8, n[u]);
-            if constexpr (ADD) va[u] = load8(add + (int64_t)row[u] * p.add_ldc + blk[u] * 8, n[u]);
-        }
+    for (int i = 0; i < 8; i++) {
+        const uint32_t bits = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
+        const float a = ADD ? widen(va.e[i]) : 0.f, v = widen(vx.e[i]);
+        // (a dropped infinity or NaN adds nothing)
+        narrow(bits >= p.limit ? (ADD ? __builtin_fmaf(v, p.scale, a) : v * p.scale) : a, o.e[i]);
     }
-    #pragma unroll
-    for (int u = 0; u < kDropWays; u++) {
-        if (n[u] <= 0) continue;
-        uint32_t w[4] = {blk[u], row[u], p.site, step};
-        philox4x32(w, k0, k1);
-        Eight<T> o;
-        #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const uint32_t bits = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
-            const float a = ADD ? widen(va[u].e[i]) : 0.f, v = widen(vx[u].e[i]);
-            // (a dropped infinity or NaN adds nothing)
-            narrow(bits >= p.limit ? (ADD ? __builtin_fmaf(v, p.scale, a) : v * p.scale) : a, o.e[i]);
-        }
-        store8(y + (int64_t)row[u] * p.y_ldc + blk[u] * 8, o, n[u]);
-    }
+    store8<WHOLE>(y + (int64_t)row * p.y_ldc + blk * 8, o, n);
 }
 
 template <typename T>
 void go(const DropoutParams &p, unsigned grid, hipStream_t s)
 {
-    if (p.add) hipLaunchKernelGGL((k_dropout<T, true>), dim3(grid), dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((k_dropout<T, false>), dim3(grid), dim3(kThreads), 0, s, p);
+    const dim3 g(grid), b(kThreads);
+    if (p.c % 8 == 0) {
+        if (p.add) hipLaunchKernelGGL((k_dropout<T, true, true>), g, b, 0, s, p);
+        else hipLaunchKernelGGL((k_dropout<T, false, true>), g, b, 0, s, p);
+    } else {
+        if (p.add) hipLaunchKernelGGL((k_dropout<T, true, false>), g, b, 0, s, p);
+        else hipLaunchKernelGGL((k_dropout<T, false, false>), g, b, 0, s, p);
+    }
 }
 
 }  // namespace
 
 int64_t dropout_groups(int64_t m, int c)
 {
-    const int64_t per = kDropWays * kThreads, blocks = (c + 7LL) / 8;
+    const int64_t per = kThreads, blocks = (c + 7LL) / 8;
     return m > INT64_MAX / 2 / blocks ? INT64_MAX : (m * blocks + per - 1) / per;
 }
 

@@ -366,8 +366,10 @@ struct CeGemm {
     float2 *stats;                 // CE_STATS: [column tile][m] maximum and sum of exponentials
     float *sums, *picked;          // [column tile][m] sums of logits (NULL: none), [m] the labels' logits
     float z, hit, flat;            // CE_GRAD
-    void *g;                       // [count][g_ld]
+    void *g;                       // [count][g_ld]; few bf16 rows: [2 count][g_ld], rounded and what that left
     int64_t g_ld;
+    void *gt;                      // few bf16 rows: [classes][gt_rows][16 rows, rounded, then their rest] (NULL: many rows)
+    int gt_rows;
     float *colsum;                 // [row tile][colsum_ld] (NULL: none)
     int64_t colsum_ld;
     void *out;                     // CE_DH, CE_DW: results, or parts of them
@@ -390,7 +392,7 @@ struct CeLoss {
 struct CeSum {
     const float *part;
     int64_t part_stride, n;
-    int parts, c;
+    int parts, c, twice;           // twice: a second set of rows, added
     const CeRow *rows;             // results by the list (NULL: row by row, n of them)
     const int *count;
     const float *factor;

@@ -144,7 +144,7 @@ struct CeLoad {
     static constexpr int kLoads = B * 128 / (NT * 16), BK = 128 / sizeof(T);
     // a thread's loads lie kStep rows (k) apart; the order repeats every 16
     static constexpr uint32_t kRow = COLS ? B * sizeof(T) : 128, kStep = NT * 16 / kRow;
-    static_assert(kStep % (COLS ? 8 : 16) == 0, "two places at most");
+    static_assert(kStep % (COLS ? (sizeof(T) == 2 ? 8 : 1) : 16) == 0, "two places at most");
     uint32_t off, odd, at;                         // of even loads, of odd ones; at: the chunk's place along k (rows)
     __device__ __forceinline__ void init(int64_t ld, int tid)
     {
@@ -325,7 +325,8 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
     // this one; meanwhile it reads this stage's fragments and the next stage is loaded
     // into the LDS that the stage before has left.  Products, reads and loads alternate.
     struct Frags { frag i[MI], j[NJ]; } f0, f1;
-    constexpr int kLi = LoadI::kLoads, kLj = LoadJ::kLoads, kEach = (kLi + kLj) * 2 / MI;
+    constexpr int kLi = LoadI::kLoads, kLj = LoadJ::kLoads, kParts = MI > NJ ? MI : NJ,
+                  kEach = MI > 2 ? (kLi + kLj) * 2 / MI : kLi + kLj;
     auto load = [&](unsigned char *lds, const typename LoadI::Stage &a, const typename LoadJ::Stage &b, int from, int to)
         __attribute__((always_inline)) {
         #pragma unroll
@@ -348,13 +349,15 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
         const typename LoadJ::Stage sb = lj.stage(j0, j_ld, nj, (s + 1) * BK, k_j);
         #pragma unroll
         for (int a = 0; a < MI; a++) {
-            read(f0, now, 0, a);
+            #pragma unroll
+            for (int b = a; b < (a + 1 < MI ? a + 1 : kParts); b++) read(f0, now, 0, b);
             load(other, sa, sb, min(a * kEach, kLi + kLj), min((a + 1) * kEach, kLi + kLj));
             if (!first) multiply(f1, a);
         }
         #pragma unroll
         for (int a = 0; a < MI; a++) {
-            read(f1, now, 1, a);
+            #pragma unroll
+            for (int b = a; b < (a + 1 < MI ? a + 1 : kParts); b++) read(f1, now, 1, b);
             multiply(f0, a);
         }
         __syncthreads();
@@ -389,7 +392,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
     constexpr int kStage = (BI + BJ) * 128;
     __shared__ __align__(16) unsigned char lds0[kStage], lds1[kStage];
     const int count = *p.count;
-    const int ni = MODE == CE_DW ? p.classes : count, nj = MODE == CE_DW || MODE == CE_DH ? p.c : p.classes;
+    const int ni = MODE == CE_DW ? p.classes : (MODE == CE_DH && p.gt ? 2 * count : count), nj = MODE == CE_DW || MODE == CE_DH ? p.c : p.classes;
     const int K = MODE == CE_DW ? count : (MODE == CE_DH ? p.classes : p.c);
     CePlace pl;
     if (!ce_place(pl, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, p.parts)) return;
@@ -404,7 +407,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
     __shared__ CeRow rows[MODE == CE_DW ? 1 : BI];
     __shared__ float bias[MODE == CE_STATS || MODE == CE_GRAD ? BJ : 1];
     if constexpr (MODE != CE_DW) {
-        for (int i = tid; i < BI; i += NT) rows[i] = i0 + i < ni ? p.rows[i0 + i] : CeRow{0, -1, 0.f, 0.f};
+        for (int i = tid; i < BI; i += NT) rows[i] = i0 + i < count ? p.rows[i0 + i] : CeRow{0, -1, 0.f, 0.f};
     }
     if constexpr (MODE == CE_STATS || MODE == CE_GRAD) {
         for (int j = tid; j < BJ; j += NT)
@@ -494,6 +497,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
         // i = 16 a + q and j = 16 b + 4 g + r, in float32 columns i = MI q + a, j = NJ (4 g + r) + b.
         constexpr bool IP = ICOLS && sizeof(T) == 4, JP = JCOLS && sizeof(T) == 4;
         constexpr int kHalf = NT / 128;
+        constexpr int kSub = TI < 64 ? TI : 64;
         static_assert(kStage >= kHalf * kWaveOut && (!IP || TI == 64) && (!JP || TJ == 64), "a wave's part of the stages");
         lds_char *mine = (wave < kHalf ? (lds_char *)lds0 : (lds_char *)lds1) + wave % kHalf * kWaveOut;
         const int lrow = late / 8, lcol = late % 8 * 8;
@@ -508,9 +512,9 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
             for (int e = 0; e < 8; e++) col[e] = 0.f;
         }
         #pragma unroll
-        for (int h = 0; h < TI / 64; h++) {
+        for (int h = 0; h < TI / kSub; h++) {
             #pragma unroll
-            for (int a = 0; a < 4; a++)
+            for (int a = 0; a < kSub / 16; a++)
                 #pragma unroll
                 for (int b = 0; b < 4; b++) {
                     const int row = IP ? 4 * q + a : 16 * a + q, chunk = JP ? 4 * g + b : 4 * b + g;
@@ -520,8 +524,8 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
                 }
             ce_wave_sync();
             #pragma unroll 2
-            for (int it = 0; it < 8; it++) {
-                const int row = it * 8 + lrow, i = iw + 64 * h + row;
+            for (int it = 0; it < kSub / 8; it++) {
+                const int row = it * 8 + lrow, i = iw + kSub * h + row;
                 float v[8];
                 #pragma unroll
                 for (int k = 0; k < 2; k++) {
@@ -678,8 +682,18 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
                 v[u][r] = j < nj && i < ni ? t : 0.f;
             }
         }
-        if constexpr (MODE == CE_GRAD)
-            if (i < ni) ce_store4((T *)p.g + (int64_t)i * p.g_ld + j0 + c, v[u]);
+        if constexpr (MODE == CE_GRAD) {
+            if (i < ni) {
+                T *to = (T *)p.g + (int64_t)i * p.g_ld + j0 + c;
+                ce_store4(to, v[u]);
+                if (sizeof(T) == 2 && p.gt) {            // what the rounding left, as rows of their own
+                    float rest[4];
+                    #pragma unroll
+                    for (int r = 0; r < 4; r++) rest[r] = v[u][r] - bf2f(f2bf(v[u][r]));
+                    ce_store4(to + ni * p.g_ld, rest);
+                }
+            }
+        }
     }
     if constexpr (MODE == CE_STATS) {
         #pragma unroll
@@ -699,7 +713,7 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
             p.stats[o] = float2{mx, sum};
             if (p.sums) p.sums[o] = all;
         }
-    } else if (p.colsum) {
+    } else if (p.colsum || p.gt) {
         __syncthreads();
         #pragma unroll
         for (int u = 0; u < (kGroups + kLanes - 1) / kLanes; u++) {
@@ -707,12 +721,96 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
             if (c < BJ) *reinterpret_cast<f32x4 *>(&part[0][row * kPitch + c]) = f32x4{v[u][0], v[u][1], v[u][2], v[u][3]};
         }
         __syncthreads();
-        if (tid < BJ && j0 + tid < nj) {
+        if (sizeof(T) == 2 && p.gt) {                    // a class's 16 rows together, then what they left
+            for (int e = tid; e < BJ * 4 * MI; e += kThreads) {
+                const int col = e / (4 * MI), a = e / 4 % MI, quarter = e % 4;
+                float f[8];
+                #pragma unroll
+                for (int r = 0; r < 8; r++) {
+                    const float t = part[0][(16 * a + quarter % 2 * 8 + r) * kPitch + col];
+                    f[r] = quarter < 2 ? t : t - bf2f(f2bf(t));
+                }
+                stg16((char *)p.gt + ((int64_t)(j0 + col) * p.gt_rows + pl.ti * MI + a) * 64 + quarter * 16, Elem<bf16_t>::pack(f));
+            }
+        }
+        if (p.colsum && tid < BJ && j0 + tid < nj) {
             float t = 0.f;
             #pragma unroll
             for (int r = 0; r < BI; r++) t += part[0][r * kPitch + tid];
             p.colsum[(int64_t)pl.ti * p.colsum_ld + j0 + tid] = t;
         }
+    }
+}
+
+// The weights' gradient of few bf16 rows, a stream of results: a wave keeps the features
+// of 64 columns (16 rows a matrix instruction) and walks over the classes.  g comes with
+// 16 rows of a class together, rounded, and then what the rounding left: the same
+// instruction adds both, so dw has no error of g's rounding.  Block b's row 4 g + r stands
+// for column 32 (b / 2) + 8 g + 4 (b % 2) + r, so that a lane stores eight neighbours.
+template <typename W, int KB>
+__global__ __launch_bounds__(kThreads) void k_ce_outer(CeGemm p, int chunk)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane % 16, g = lane / 16, count = *p.count;
+    const int blocks = (p.c + 255) / 256, j0 = (int)(blockIdx.x % blocks) * 256 + wave * 64;
+    const int v0 = (int)(blockIdx.x / blocks) * chunk, v1 = min(v0 + chunk, p.classes);
+    if (j0 >= p.c) return;
+    const bf16_t *h = (const bf16_t *)p.i;
+    bf16x8 f[KB][4];
+    #pragma unroll
+    for (int k = 0; k < KB; k++)
+        #pragma unroll
+        for (int b = 0; b < 4; b++) {
+            const int j = j0 + 32 * (b / 2) + 8 * (q / 4) + 4 * (b % 2) + q % 4;
+            #pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const int row = 16 * k + (8 * g + e) % 16;
+                const bool in = row < count && j < p.c;
+                const bf16_t u = h[in ? (int64_t)row * p.c + j : 0];
+                f[k][b][e] = __builtin_bit_cast(__bf16, in ? u : (bf16_t)0);
+            }
+        }
+    const float factor = *p.factor;
+    const char *gt = (const char *)p.gt + (int64_t)q * p.gt_rows * 64 + g * 16;
+    // kSteps steps of 16 classes at a time, loaded a turn ahead (one step ahead: 80 us for
+    // 65536 classes of 2048, the time of a load each)
+    constexpr int kSteps = 8 / KB;
+    bf16x8 now[kSteps][KB], next[kSteps][KB];
+    auto load = [&](int v, bf16x8 (&to)[kSteps][KB]) __attribute__((always_inline)) {
+        #pragma unroll
+        for (int u = 0; u < kSteps; u++) {
+            const int at = v + 16 * u < v1 ? v + 16 * u : v0;
+            #pragma unroll
+            for (int k = 0; k < KB; k++)         // (past the rows that count g is not written)
+                to[u][k] = __builtin_bit_cast(bf16x8, k * 16 < count ? ldg16(gt + ((int64_t)at * p.gt_rows + k) * 64) : zero16());
+        }
+    };
+    load(v0, now);
+    for (int v = v0; v < v1; v += 16 * kSteps) {
+        load(v + 16 * kSteps, next);
+        #pragma unroll
+        for (int u = 0; u < kSteps; u++) {
+            f32x4 acc[4];
+            #pragma unroll
+            for (int b = 0; b < 4; b++) {
+                acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                #pragma unroll
+                for (int k = 0; k < KB; k++) ce_mma(acc[b], f[k][b], now[u][k]);
+            }
+            if (v + 16 * u + q < v1) {
+                W *o = (W *)p.out + (int64_t)(v + 16 * u + q) * p.out_ld + j0 + 8 * g;
+                #pragma unroll
+                for (int s = 0; s < 2; s++) {
+                    float r[8];
+                    #pragma unroll
+                    for (int e = 0; e < 8; e++) r[e] = acc[2 * s + e / 4][e % 4] * factor;
+                    if (j0 + 32 * s + 8 * g < p.c) ce_store8(o + 32 * s, r);
+                }
+            }
+        }
+        #pragma unroll
+        for (int u = 0; u < kSteps; u++)
+            #pragma unroll
+            for (int k = 0; k < KB; k++) now[u][k] = next[u][k];
     }
 }
 
@@ -814,21 +912,39 @@ __global__ __launch_bounds__(1024) void k_ce_mean(CeLoss p)
 
 // ---- sums over parts -----------------------------------------------------------
 // out[row][j .. j + 3] = the sum of the parts' float32 results, in order.
-template <typename T>
+// SL threads share a vector's parts (few results of many parts), joined in order.
+template <typename T, int SL>
 __global__ __launch_bounds__(kThreads) void k_ce_sum(CeSum p)
 {
-    const int vecs = p.c / 4;
-    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, i = id / vecs;
+    __shared__ float red[SL > 1 ? SL : 1][SL > 1 ? kThreads / SL : 1][4];
+    const int vecs = p.c / 4, tid = threadIdx.x, slice = tid / (kThreads / SL), at = tid % (kThreads / SL);
+    const int64_t id = (int64_t)blockIdx.x * (kThreads / SL) + at, i = id / vecs;
     const int j = (int)(id - i * vecs) * 4;
-    if (i >= (p.rows ? *p.count : p.n)) return;
-    const float *src = p.part + i * p.c + j;
+    const int64_t n = p.rows ? *p.count : p.n;
+    const bool mine = i < n;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    #pragma unroll 4
-    for (int s = 0; s < p.parts; s++) {
-        const f32x4 u = *reinterpret_cast<const f32x4 *>(src + s * p.part_stride);
-        #pragma unroll
-        for (int r = 0; r < 4; r++) v[r] += u[r];
+    if (mine) {
+        for (int t = 0; t <= p.twice; t++) {     // (few bf16 rows: those of what g's rounding left)
+            const float *src = p.part + (i + t * n) * p.c + j;
+            #pragma unroll 4
+            for (int s = slice; s < p.parts; s += SL) {
+                const f32x4 u = *reinterpret_cast<const f32x4 *>(src + s * p.part_stride);
+                #pragma unroll
+                for (int r = 0; r < 4; r++) v[r] += u[r];
+            }
+        }
     }
+    if constexpr (SL > 1) {
+        #pragma unroll
+        for (int r = 0; r < 4; r++) red[slice][at][r] = v[r];
+        __syncthreads();
+        if (slice) return;
+        #pragma unroll
+        for (int s = 1; s < SL; s++)
+            #pragma unroll
+            for (int r = 0; r < 4; r++) v[r] += red[s][at][r];
+    }
+    if (!mine) return;
     const int64_t row = p.rows ? p.rows[i].row : i;
     const float factor = *p.factor;
     #pragma unroll
@@ -853,6 +969,10 @@ inline int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 // How a product's tiles run: 256 x 256 (one workgroup of eight waves a CU) where they
 // fill the chip, else 128 x 128 (two workgroups of four waves a CU); logits of few rows
 // or of too few tiles for that run as k_ce_small, 16 x i by 16 x j.
+// Up to kFewRows bf16 rows g is kept in two parts, rounded and the rest, in separate rows
+// (their products cost next to nothing beside reading the weights): with few rows the
+// rounding of one label's g is no longer one of many.
+constexpr int kFewRows = 64;
 struct CeTile { int bi, bj; bool small; };
 inline CeTile ce_tile(int dtype, int64_t ni, int64_t nj)
 {
@@ -862,7 +982,7 @@ inline CeTile ce_tile(int dtype, int64_t ni, int64_t nj)
 inline CeTile ce_logit_tile(int dtype, int64_t m, int64_t classes)
 {
     const CeTile t = ce_tile(dtype, m, classes);
-    if (m > 32 && cdiv(m, 128) * cdiv(classes, 128) >= 128) return t;
+    if (m > kFewRows && cdiv(m, 128) * cdiv(classes, 128) >= 128) return t;
     const int mi = m > 16 ? 2 : 1;
     int nj = 4;
     while (nj > 1 && cdiv(m, 16 * mi) * cdiv(classes, 16 * nj) < 512) nj /= 2;
@@ -870,10 +990,10 @@ inline CeTile ce_logit_tile(int dtype, int64_t m, int64_t classes)
 }
 
 // k ranges a product is cut into where its tiles would leave the chip idle
-inline int ce_parts(const CeTile &t, int64_t ni, int64_t nj, int64_t steps)
+inline int ce_parts(const CeTile &t, int64_t ni, int64_t nj, int64_t steps, int least)
 {
     const int64_t slots = t.bi == 256 ? 256 : 512, tiles = cdiv(ni, t.bi) * cdiv(nj, t.bj);
-    const int64_t want = slots / tiles, most = steps / 4;
+    const int64_t want = slots / tiles, most = steps / least;   // least: stages of a range
     const int64_t n = want < most ? want : most;
     return n < 1 ? 1 : (n > 64 ? 64 : (int)n);
 }
@@ -892,6 +1012,13 @@ void go(const CeGemm &p, const CeTile &t, int64_t grid, hipStream_t s)
             };
             if (t.bi == 16) at(std::integral_constant<int, 1>{});
             else at(std::integral_constant<int, 2>{});
+            return;
+        }
+    }
+    if constexpr (MODE == CE_DH) {
+        if (t.bi == 32) {
+            if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_ce_gemm<T, 32, 256, 1, 4, MODE>), g, dim3(256), 0, s, p);
+            else hipLaunchKernelGGL((k_ce_gemm<T, 32, 128, 1, 2, MODE>), g, dim3(128), 0, s, p);
             return;
         }
     }
@@ -969,11 +1096,13 @@ struct CeFwdPlan {
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 constexpr int64_t kPieceWidth = kCeMaxLd;
 struct CeBwdPlan {
+    bool gather() const { return pieces > 1 || dh_parts > 1 || few; }      // dh leaves the products as parts
     CeHead head;
     int64_t pieces, width;                 // classes of a piece, a multiple of 256
     CeTile grad_tile, dh_tile, dw_tile;
     int grad_rows, dh_parts, dw_parts;     // grad_rows: of a partial row of dbias
-    int64_t g, dh, dw, colsum, end;
+    int few;                               // groups of 16 rows of g's second form (0: many rows)
+    int64_t g, gt, dh, dw, colsum, end;
     explicit CeBwdPlan(const CeCall &a) : head(a)
     {
         const int64_t es = a.dtype == DT_BF16 ? 2 : 4, bk = 128 / es;
@@ -985,13 +1114,17 @@ struct CeBwdPlan {
         const int64_t wide = width < a.classes ? width : a.classes;
         grad_tile = ce_logit_tile(a.dtype, a.m, wide);
         grad_rows = grad_tile.small ? grad_tile.bi : grad_tile.bi / 2;
-        dh_tile = ce_tile(a.dtype, a.m, a.c);
-        dw_tile = ce_tile(a.dtype, wide, a.c);
-        dh_parts = ce_parts(dh_tile, a.m, a.c, cdiv(wide, bk));
-        dw_parts = ce_parts(dw_tile, wide, a.c, cdiv(a.m, bk));
+        few = a.dtype == DT_BF16 && a.m <= kFewRows ? (a.m <= 16 ? 1 : (a.m <= 32 ? 2 : 4)) : 0;   // (tiles of k_ce_small: 32 rows past 16)
+        const int64_t rows = few ? 2 * a.m : a.m;
+        // few rows: dh streams the weights past them, dw writes more than it multiplies
+        dh_tile = rows <= 32 ? CeTile{32, a.dtype == DT_BF16 ? 256 : 128, false} : ce_tile(a.dtype, rows, a.c);
+        dw_tile = a.m <= 128 ? CeTile{128, 128, false} : ce_tile(a.dtype, wide, a.c);
+        dh_parts = ce_parts(dh_tile, rows, a.c, cdiv(wide, bk), 2);
+        dw_parts = few ? 1 : ce_parts(dw_tile, wide, a.c, cdiv(a.m, bk), 4);
         g = head.end;
-        dh = up256(g + a.m * width * es);
-        dw = up256(dh + (a.dh && (pieces > 1 || dh_parts > 1) ? dh_parts * a.m * a.c * 4 : 0));
+        gt = up256(g + rows * width * es);
+        dh = up256(gt + few * width * 64);
+        dw = up256(dh + (a.dh && gather() ? dh_parts * rows * a.c * 4 : 0));
         colsum = up256(dw + (a.dw && dw_parts > 1 ? dw_parts * wide * a.c * 4 : 0));
         end = up256(colsum + (a.dbias ? cdiv(a.m, grad_tile.bi) * (grad_tile.bi / grad_rows) * a.classes * 4 : 0));
     }
@@ -1000,9 +1133,36 @@ struct CeBwdPlan {
 hipError_t sum_parts(const CeSum &p, int dtype, int64_t rows, hipStream_t s)
 {
     TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, ((double)p.parts * 4 + (dtype == DT_BF16 ? 2 : 4)) * rows * p.c, 0.0);
-    const unsigned grid = (unsigned)cdiv(rows * (p.c / 4), kThreads);
-    if (dtype == DT_BF16) hipLaunchKernelGGL(k_ce_sum<bf16_t>, dim3(grid), dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL(k_ce_sum<float>, dim3(grid), dim3(kThreads), 0, s, p);
+    const int64_t vecs = rows * (p.c / 4);
+    const bool shared = vecs < 512 * kThreads && p.parts >= 8;   // (16 x 2048 of 64 parts: 13 us one thread a vector)
+    const dim3 grid((unsigned)cdiv(vecs, shared ? kThreads / 8 : kThreads)), block(kThreads);
+    if (dtype == DT_BF16) {
+        if (shared) hipLaunchKernelGGL((k_ce_sum<bf16_t, 8>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((k_ce_sum<bf16_t, 1>), grid, block, 0, s, p);
+    } else {
+        if (shared) hipLaunchKernelGGL((k_ce_sum<float, 8>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((k_ce_sum<float, 1>), grid, block, 0, s, p);
+    }
+    return hipGetLastError();
+}
+
+// classes in ranges that give the chip four workgroups a CU
+hipError_t launch_outer(const CeCall &a, const CeGemm &p, int few, hipStream_t s)
+{
+    const int64_t blocks = cdiv(a.c, 256), ranges = cdiv(1024, blocks);
+    const int chunk = (int)(cdiv(cdiv(p.classes, ranges), 16) * 16);
+    const dim3 grid((unsigned)(blocks * cdiv(p.classes, chunk)));
+    TraceScope tr(KC_CONV, KID_LINEAR_CE, s, (double)p.classes * a.c * (a.dw_dtype == DT_BF16 ? 2 : 4), 2.0 * a.m * p.classes * a.c);
+    const auto at = [&](auto w, auto kb) {
+        hipLaunchKernelGGL((k_ce_outer<decltype(w), decltype(kb)::value>), grid, dim3(kThreads), 0, s, p, chunk);
+    };
+    const auto of = [&](auto w) {
+        if (few == 1) at(w, std::integral_constant<int, 1>{});
+        else if (few == 2) at(w, std::integral_constant<int, 2>{});
+        else at(w, std::integral_constant<int, 4>{});
+    };
+    if (a.dw_dtype == DT_BF16) of(bf16_t{});
+    else of(float{});
     return hipGetLastError();
 }
 
@@ -1066,7 +1226,9 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
     p.g = ws + w.g; p.g_ld = w.width;
     p.colsum_ld = a.classes;
     const char *copy = ws + w.head.copy;
-    const bool gather_dh = w.pieces > 1 || w.dh_parts > 1;
+    const bool gather_dh = w.gather();
+    const int64_t dh_rows = w.few ? 2 * a.m : a.m;
+    if (w.few) { p.gt = ws + w.gt; p.gt_rows = w.few; }
     for (int64_t n = 0; n < w.pieces; n++) {
         const int64_t first = n * w.width;
         const int64_t wide = a.classes - first < w.width ? a.classes - first : w.width;
@@ -1079,6 +1241,15 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
         q.bias = a.bias ? a.bias + first : nullptr;
         q.colsum = a.dbias ? (float *)(ws + w.colsum) + first : nullptr;
         CE_TRY(gemm<CE_GRAD>(a, q, w.grad_tile, a.m, wide, a.c, s));
+        if (a.dh) {
+            q = p;
+            q.i = p.g; q.i_ld = w.width * es;
+            q.j = weights; q.j_ld = a.w_ld * es;
+            q.parts = w.dh_parts;
+            q.out = a.dh; q.out_ld = a.dh_ld; q.out_f32 = a.dtype == DT_F32;
+            if (gather_dh) { q.out = ws + w.dh; q.out_ld = a.c; q.out_f32 = 1; q.part_stride = dh_rows * a.c; q.add = n > 0; }
+            CE_TRY(gemm<CE_DH>(a, q, w.dh_tile, dh_rows, a.c, wide, s));
+        }
         if (a.dw) {
             q = p;
             q.i = p.g; q.i_ld = w.width * es;
@@ -1086,6 +1257,10 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
             q.parts = w.dw_parts;
             q.out = (char *)a.dw + first * a.dw_ld * (a.dw_dtype == DT_BF16 ? 2 : 4);
             q.out_ld = a.dw_ld; q.out_f32 = a.dw_dtype == DT_F32;
+            if (w.few) {
+                q.i = copy;
+                CE_TRY(launch_outer(a, q, w.few, s));
+            } else {
             if (w.dw_parts > 1) { q.out = ws + w.dw; q.out_ld = a.c; q.out_f32 = 1; q.part_stride = wide * a.c; }
             CE_TRY(gemm<CE_DW>(a, q, w.dw_tile, wide, a.c, a.m, s));
             if (w.dw_parts > 1) {
@@ -1094,20 +1269,12 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
                 t.out = (char *)a.dw + first * a.dw_ld * (a.dw_dtype == DT_BF16 ? 2 : 4); t.out_ld = a.dw_ld;
                 CE_TRY(sum_parts(t, a.dw_dtype, wide, s));
             }
-        }
-        if (a.dh) {
-            q = p;
-            q.i = p.g; q.i_ld = w.width * es;
-            q.j = weights; q.j_ld = a.w_ld * es;
-            q.parts = w.dh_parts;
-            q.out = a.dh; q.out_ld = a.dh_ld; q.out_f32 = a.dtype == DT_F32;
-            if (gather_dh) { q.out = ws + w.dh; q.out_ld = a.c; q.out_f32 = 1; q.part_stride = a.m * a.c; q.add = n > 0; }
-            CE_TRY(gemm<CE_DH>(a, q, w.dh_tile, a.m, a.c, wide, s));
+            }
         }
     }
     if (a.dh && gather_dh) {
         CeSum t{};
-        t.part = (const float *)(ws + w.dh); t.part_stride = a.m * a.c; t.parts = w.dh_parts; t.c = a.c;
+        t.part = (const float *)(ws + w.dh); t.part_stride = dh_rows * a.c; t.twice = w.few ? 1 : 0; t.parts = w.dh_parts; t.c = a.c;
         t.rows = p.rows; t.count = p.count; t.factor = p.factor;
         t.out = a.dh; t.out_ld = a.dh_ld;
         CE_TRY(sum_parts(t, a.dtype, a.m, s));
