@@ -144,3 +144,14 @@ def densenet(seed=0, n=128, hw=224, c_img=3, c_stem=64, growth=32, width=128, bl
                      w=normal(seed, "head.w", (c_l, classes), std=float(1.0 / np.sqrt(c_l)), bf16=bf16),
                      b=normal(seed, "head.b", (classes,), 0.1))
     return d
+
+
+def token_head(seed=0, m=4096, c=1024, classes=32768, p=0.1, ignored=0.1, bf16=True):
+    """The end of a network over m tokens: the last layer's output and the residual stream, dropout's probability and
+    seed, the layer norm's parameters, the classes' weights (N(0, 1/C)) and labels, `ignored` of which are padding."""
+    bn = bn_params(seed, "norm", c)
+    labels = _gen(seed, "labels").integers(0, classes, size=m).astype(np.int32)
+    labels[_gen(seed, "padding").uniform(size=m) < ignored] = -100
+    return dict(x=normal(seed, "x", (m, c), bf16=bf16), res=normal(seed, "res", (m, c), bf16=bf16), gamma=bn["gamma"],
+                beta=bn["beta"], w=normal(seed, "w", (classes, c), std=float(1.0 / np.sqrt(c)), bf16=bf16), labels=labels,
+                p=p, seed=seed, eps=EPS, bf16=bf16)

@@ -22,6 +22,9 @@ Workloads (shapes of the paper's DenseNet-121 / ResNet-50 training):
                       (pointer passing, as the paper's reference does for
                       Split); Split's backward is the accumulation of every
                       reader's input gradient into that buffer's gradient.
+* ``TokenHead``    -- the end of a network over tokens: dropout and residual
+                      addition, layer norm, linear layer with softmax cross
+                      entropy over many classes.
 """
 import numpy as np
 import torch
@@ -759,6 +762,46 @@ class ResNetStack:
                 B.bnr_bwd_fused(b["desc1"], b["xin"], None, b["w1"], B.grad_dense(self.dyw3), b["dw1"],
                                 dx=self.gbuf, dx_accumulate=True)
             g = self.gbuf
+
+    def step(self):
+        self.forward()
+        self.backward()
+
+
+class TokenHead:
+    """The end of a network over m tokens: s = dropout(x) + res, h = layer norm of s, and the softmax cross entropy of
+    h w^T over the classes.  Neither the dropout's mask nor the logits are stored.  Backward: dw, dh, the norm's input
+    gradient ds (which is res's gradient) and dx, with the mask formed again.  ``turn`` ([1] int32 on the device) is
+    the dropout's step: a captured step takes a new mask wherever the caller advances it."""
+
+    def __init__(self, data, device="cuda", site=0):
+        bf16 = data["bf16"]
+        dev = torch.device(device)
+        self.x, self.res = _t(data["x"], dev, bf16), _t(data["res"], dev, bf16)
+        self.w = _t(data["w"], dev, bf16)
+        m, c = self.x.shape
+        self.tokens = m
+        self.turn = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.drop = B.Dropout(data["p"], data["seed"], site=site, step=self.turn)
+        self.ln = B.LN(_f32(data["gamma"], dev), _f32(data["beta"], dev), m, data["eps"])
+        self.ce = B.CE(torch.from_numpy(data["labels"]).to(dev))
+        self.loss = torch.empty(1 + m, dtype=torch.float32, device=dev)
+        self.s, self.h, self.dh, self.ds, self.dx = (torch.empty_like(self.x) for _ in range(5))
+        self.dw = torch.empty_like(self.w)
+        self.g = _Grads(c, dev)
+
+    def filters(self):
+        return [(self.w, self.dw)]
+
+    def forward(self):
+        B.bnr_dropout_fwd(self.x, self.drop, self.s, res=self.res)
+        B.bnr_layernorm_fwd(self.s, self.ln, self.h)
+        B.bnr_linear_ce_fwd(self.h, self.w, self.ce, self.loss)
+
+    def backward(self):
+        B.bnr_linear_ce_bwd(self.h, self.w, self.ce, self.dh, self.dw)
+        B.bnr_layernorm_bwd(self.dh, self.s, self.ln, self.ds, self.g.dgamma, self.g.dbeta)
+        B.bnr_dropout_bwd(self.ds, self.drop, self.dx)
 
     def step(self):
         self.forward()
