@@ -602,11 +602,13 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
 // Logits of 16 MI x 16 NJ by one workgroup, its four waves each a quarter of k.  Nothing
 // is shared, so the fragments are loaded straight into registers, kAhead steps ahead;
 // the waves' sums are added through LDS in order.  With few rows this is a stream of the
-// weights, with few tiles it spreads them over the chip.
+// weights, with few tiles it spreads them over the chip.  Sums in two levels, four steps
+// and then those: where few classes make the model sure of its labels, g is a difference
+// of numbers near 1 and shows every rounding of the logits.
 template <typename T, int MI, int NJ, int MODE>
 __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
 {
-    constexpr int BI = 16 * MI, BJ = 16 * NJ, kAhead = 32 / (MI + NJ), kPitch = BJ + 4, BK = 64 / sizeof(T);
+    constexpr int BI = 16 * MI, BJ = 16 * NJ, kAhead = 20 / (MI + NJ), kPitch = BJ + 4, BK = 64 / sizeof(T);
     constexpr int kGroups = 4 * NJ, kLanes = 16 / MI;        // groups of four columns of a row, threads of a row
     typedef typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type frag;
     __shared__ __align__(16) float part[4][BI * kPitch];
@@ -627,6 +629,22 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
         #pragma unroll
         for (int a = 0; a < MI; a++) fi[d][a] = __builtin_bit_cast(frag, bld16(ri, in + (16 * a + q) * (uint32_t)p.i_ld));
     };
+    // kLanes threads a row, group after group of its columns: what they will need of them
+    constexpr int kTurns = (kGroups + kLanes - 1) / kLanes;
+    const int row = tid / kLanes, i = i0 + row, li = tid % kLanes;
+    CeRow info = CeRow{0, -1, 0.f, 0.f};
+    if (i < ni) {
+        if (p.rows) info = p.rows[i];
+        else info.label = p.labels[i];
+    }
+    float bias[kTurns][4];
+    #pragma unroll
+    for (int u = 0; u < kTurns; u++)
+        #pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const int j = j0 + (u * kLanes + li) * 4 + r;
+            bias[u][r] = p.bias ? p.bias[min(j, nj - 1)] : 0.f;
+        }
     f32x4 acc[NJ][MI], total[NJ][MI];
     ce_zero(acc);
     ce_zero(total);
@@ -640,25 +658,18 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
                 #pragma unroll
                 for (int b = 0; b < NJ; b++) ce_mma(acc[b][a], fj[d][b], fi[d][a]);
             load(d, s + kAhead + d);
+            if (d % 4 == 3 || d == kAhead - 1) ce_fold(total, acc);
         }
-        if constexpr (sizeof(T) == 4) ce_fold(total, acc);
     }
     #pragma unroll
     for (int a = 0; a < MI; a++)
         #pragma unroll
         for (int b = 0; b < NJ; b++)
-            *reinterpret_cast<f32x4 *>(&part[wave][(16 * a + q) * kPitch + 16 * b + 4 * g]) = sizeof(T) == 4 ? total[b][a] : acc[b][a];
+            *reinterpret_cast<f32x4 *>(&part[wave][(16 * a + q) * kPitch + 16 * b + 4 * g]) = total[b][a];
     __syncthreads();
-    // kLanes threads a row, group after group of its columns
-    const int row = tid / kLanes, i = i0 + row, li = tid % kLanes;
-    CeRow info = CeRow{0, -1, 0.f, 0.f};
-    if (i < ni) {
-        if (p.rows) info = p.rows[i];
-        else info.label = p.labels[i];
-    }
-    float mx = -INFINITY, sum = 0.f, all = 0.f, v[(kGroups + kLanes - 1) / kLanes][4];
+    float mx = -INFINITY, sum = 0.f, all = 0.f, v[kTurns][4];
     #pragma unroll
-    for (int u = 0; u < (kGroups + kLanes - 1) / kLanes; u++) {
+    for (int u = 0; u < kTurns; u++) {
         const int c = (u * kLanes + li) * 4;
         #pragma unroll
         for (int r = 0; r < 4; r++) v[u][r] = -INFINITY;
@@ -670,7 +681,7 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
             #pragma unroll
             for (int w = 1; w < 4; w++) l += o[w * BI * kPitch + r];
             const int j = j0 + c + r;
-            if (p.bias && j < nj) l += p.bias[j];
+            l += bias[u][r];
             v[u][r] = j < nj ? l : -INFINITY;
             if constexpr (MODE == CE_STATS) {
                 mx = fmaxf(mx, v[u][r]);
@@ -700,7 +711,7 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
         for (int o = 1; o < kLanes; o *= 2) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
         const float base = mx == -INFINITY ? 0.f : mx;
         #pragma unroll
-        for (int u = 0; u < (kGroups + kLanes - 1) / kLanes; u++)
+        for (int u = 0; u < kTurns; u++)
             #pragma unroll
             for (int r = 0; r < 4; r++) sum += ce_exp(v[u][r] - base);
         #pragma unroll
@@ -716,7 +727,7 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
     } else if (p.colsum || p.gt) {
         __syncthreads();
         #pragma unroll
-        for (int u = 0; u < (kGroups + kLanes - 1) / kLanes; u++) {
+        for (int u = 0; u < kTurns; u++) {
             const int c = (u * kLanes + li) * 4;
             if (c < BJ) *reinterpret_cast<f32x4 *>(&part[0][row * kPitch + c]) = f32x4{v[u][0], v[u][1], v[u][2], v[u][3]};
         }
@@ -985,7 +996,7 @@ inline CeTile ce_logit_tile(int dtype, int64_t m, int64_t classes)
     if (m > kFewRows && cdiv(m, 128) * cdiv(classes, 128) >= 128) return t;
     const int mi = m > 16 ? 2 : 1;
     int nj = 4;
-    while (nj > 1 && cdiv(m, 16 * mi) * cdiv(classes, 16 * nj) < 512) nj /= 2;
+    while (nj > 1 && cdiv(m, 16 * mi) * cdiv(classes, 16 * nj) < 192) nj /= 2;
     return CeTile{16 * mi, 16 * nj, true};
 }
 
@@ -1205,9 +1216,9 @@ hipError_t launch_ce_fwd(const CeCall &a, void *ws_, hipStream_t s)
     l.hit = 1.0 - (double)a.smoothing; l.flat = (double)a.smoothing / a.classes; l.z = a.z;
     l.loss = a.loss; l.lse = a.lse; l.part = (double2 *)(ws + w.part);
     TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 8.0 * a.m * w.tiles, 0.0);
-    // (a single row takes all threads, and the tiles of up to 16 four times as many)
+    // (a single row takes all threads, and many tiles take 64 threads a row instead of 16)
     if (a.m == 1) hipLaunchKernelGGL((k_ce_rows<1, kThreads>), dim3(1), dim3(kThreads), 0, s, l);
-    else if (w.groups == 1) hipLaunchKernelGGL((k_ce_rows<kLossRows, 1024>), dim3(1), dim3(1024), 0, s, l);
+    else if (w.tiles >= 64) hipLaunchKernelGGL((k_ce_rows<kLossRows, 1024>), dim3((unsigned)w.groups), dim3(1024), 0, s, l);
     else hipLaunchKernelGGL((k_ce_rows<kLossRows, kThreads>), dim3((unsigned)w.groups), dim3(kThreads), 0, s, l);
     if (w.groups > 1) hipLaunchKernelGGL(k_ce_mean, dim3(1), dim3(1024), 0, s, l);
     return hipGetLastError();
