@@ -277,11 +277,11 @@ __device__ __forceinline__ void ce_store8(bf16_t *p, const float *v) { stg16(p, 
 // column tiles, so that the 32 workgroups of an XCD share both operands in its L2
 // (8192 x 32768 x 4096, weight gradient: 1.58 ms with four, 1.67 with eight, 1.77 with 16).
 struct CePlace { int ti, tj, part; };
-__device__ __forceinline__ bool ce_place(CePlace &pl, int nti, int ntj, int parts)
+__device__ __forceinline__ bool ce_place(CePlace &pl, int block, int nti, int ntj, int parts)
 {
     const int tiles = nti * ntj, total = tiles * parts;
-    if ((int)blockIdx.x >= total) return false;
-    const int id = xcd_remap(blockIdx.x, total);
+    if (block >= total) return false;
+    const int id = xcd_remap(block, total);
     pl.part = id / tiles;
     const int t = id - pl.part * tiles, per = 4 * ntj, first = t / per * 4, n = min(4, nti - first), r = t % per;
     pl.ti = first + r % n;
@@ -384,18 +384,26 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
     __syncthreads();
 }
 
+// LDS of a workgroup: two stages, and what the epilogue needs of the tile's rows and columns
+#define CE_LDS(BI, BJ)                                                                  \
+    __shared__ __align__(16) unsigned char lds0[(BI + BJ) * 128], lds1[(BI + BJ) * 128]; \
+    __shared__ CeRow rows[BI];                                                          \
+    __shared__ float bias[BJ]
+
+// One tile of a product, by workgroup `block` of its grid.
 template <typename T, int BI, int BJ, int WI, int WJ, int MODE>
-__global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
+__device__ __forceinline__ void ce_tile_of(const CeGemm &p, int block, unsigned char *lds0, unsigned char *lds1, CeRow *rows,
+                                           float *bias)
 {
+#ifdef __HIP_DEVICE_COMPILE__              // (the host pass cannot instantiate the matrix instructions twice)
     constexpr bool ICOLS = MODE == CE_DW, JCOLS = MODE == CE_DW || MODE == CE_DH;
     constexpr int NT = WI * WJ * 64, TI = BI / WI, TJ = BJ / WJ, MI = TI / 16, NJ = TJ / 16, BK = 128 / sizeof(T);
     constexpr int kStage = (BI + BJ) * 128;
-    __shared__ __align__(16) unsigned char lds0[kStage], lds1[kStage];
     const int count = *p.count;
     const int ni = MODE == CE_DW ? p.classes : (MODE == CE_DH && p.gt ? 2 * count : count), nj = MODE == CE_DW || MODE == CE_DH ? p.c : p.classes;
     const int K = MODE == CE_DW ? count : (MODE == CE_DH ? p.classes : p.c);
     CePlace pl;
-    if (!ce_place(pl, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, p.parts)) return;
+    if (!ce_place(pl, block, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, p.parts)) return;
     const int i0 = pl.ti * BI, j0 = pl.tj * BJ;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / WJ, wj = wave % WJ;
@@ -403,9 +411,7 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
     const char *jbase = (const char *)p.j + (JCOLS ? (int64_t)j0 * sizeof(T) : j0 * p.j_ld);
     const int steps = (K + BK - 1) / BK;
     const int s0 = (int)((int64_t)pl.part * steps / p.parts), s1 = (int)((int64_t)(pl.part + 1) * steps / p.parts);
-    // what the epilogue needs of the tile's rows and columns, there before the products are done
-    __shared__ CeRow rows[MODE == CE_DW ? 1 : BI];
-    __shared__ float bias[MODE == CE_STATS || MODE == CE_GRAD ? BJ : 1];
+    // (there before the products are done)
     if constexpr (MODE != CE_DW) {
         for (int i = tid; i < BI; i += NT) rows[i] = i0 + i < count ? p.rows[i0 + i] : CeRow{0, -1, 0.f, 0.f};
     }
@@ -596,6 +602,25 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
         }
         }
     }
+#endif
+}
+
+template <typename T, int BI, int BJ, int WI, int WJ, int MODE>
+__global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
+{
+    CE_LDS(BI, BJ);
+    ce_tile_of<T, BI, BJ, WI, WJ, MODE>(p, blockIdx.x, lds0, lds1, rows, bias);
+}
+
+// dh and dw of a piece, which do not need each other, in one launch: dh's longer tiles
+// first (`first` workgroups, a multiple of the eight XCDs), and dw's fill the chip as
+// they end.
+template <typename T, int BI, int BJ, int WI, int WJ>
+__global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_pair(CeGemm dh, CeGemm dw, int first)
+{
+    CE_LDS(BI, BJ);
+    if ((int)blockIdx.x < first) ce_tile_of<T, BI, BJ, WI, WJ, CE_DH>(dh, blockIdx.x, lds0, lds1, rows, bias);
+    else ce_tile_of<T, BI, BJ, WI, WJ, CE_DW>(dw, blockIdx.x - first, lds0, lds1, rows, bias);
 }
 
 // ---- few rows, or few tiles ---------------------------------------------------
@@ -614,7 +639,7 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
     __shared__ __align__(16) float part[4][BI * kPitch];
     const int ni = p.rows ? *p.count : (int)p.m, nj = p.classes;
     CePlace pl;
-    if (!ce_place(pl, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, 1)) return;
+    if (!ce_place(pl, blockIdx.x, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, 1)) return;
     const int i0 = pl.ti * BI, j0 = pl.tj * BJ;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane % 16, g = lane / 16;
     const int width = p.c * (int)sizeof(T);
@@ -1053,6 +1078,19 @@ hipError_t gemm(const CeCall &a, const CeGemm &p, const CeTile &t, int64_t ni, i
     return hipGetLastError();
 }
 
+// both products of g (dh has dh_rows results a column, dw `wide`)
+hipError_t pair(const CeCall &a, const CeGemm &dh, const CeGemm &dw, const CeTile &t, int64_t dh_rows, int64_t wide, hipStream_t s)
+{
+    const double es = a.dtype == DT_BF16 ? 2 : 4;
+    TraceScope tr(KC_CONV, KID_LINEAR_CE, s, es * ((double)a.m * wide + (2.0 * a.m + 2.0 * wide) * a.c), 4.0 * a.m * wide * a.c);
+    const int64_t cols = cdiv(a.c, t.bj), first = cdiv(cdiv(dh_rows, t.bi) * cols * dh.parts, 8) * 8;
+    const dim3 g((unsigned)(first + cdiv(wide, t.bi) * cols * dw.parts));
+    if (a.dtype != DT_BF16) hipLaunchKernelGGL((k_ce_pair<float, 128, 128, 2, 2>), g, dim3(256), 0, s, dh, dw, (int)first);
+    else if (t.bi == 256) hipLaunchKernelGGL((k_ce_pair<bf16_t, 256, 256, 2, 4>), g, dim3(512), 0, s, dh, dw, (int)first);
+    else hipLaunchKernelGGL((k_ce_pair<bf16_t, 128, 128, 2, 2>), g, dim3(256), 0, s, dh, dw, (int)first);
+    return hipGetLastError();
+}
+
 // What both directions keep in the workspace: the count, the list and the rows' copy.
 struct CeHead {
     int64_t counts, rows, copy, end;
@@ -1252,36 +1290,38 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
         q.bias = a.bias ? a.bias + first : nullptr;
         q.colsum = a.dbias ? (float *)(ws + w.colsum) + first : nullptr;
         CE_TRY(gemm<CE_GRAD>(a, q, w.grad_tile, a.m, wide, a.c, s));
-        if (a.dh) {
-            q = p;
-            q.i = p.g; q.i_ld = w.width * es;
-            q.j = weights; q.j_ld = a.w_ld * es;
-            q.parts = w.dh_parts;
-            q.out = a.dh; q.out_ld = a.dh_ld; q.out_f32 = a.dtype == DT_F32;
-            if (gather_dh) { q.out = ws + w.dh; q.out_ld = a.c; q.out_f32 = 1; q.part_stride = dh_rows * a.c; q.add = n > 0; }
-            CE_TRY(gemm<CE_DH>(a, q, w.dh_tile, dh_rows, a.c, wide, s));
+        CeGemm dh = p, dw = p;
+        dh.i = dw.i = p.g; dh.i_ld = dw.i_ld = w.width * es;
+        dh.j = weights; dh.j_ld = a.w_ld * es;
+        dh.parts = w.dh_parts;
+        dh.out = a.dh; dh.out_ld = a.dh_ld; dh.out_f32 = a.dtype == DT_F32;
+        if (gather_dh) {
+            dh.out = ws + w.dh; dh.out_ld = a.c; dh.out_f32 = 1;
+            dh.part_stride = dh_rows * a.c; dh.add = n > 0;
         }
-        if (a.dw) {
-            q = p;
-            q.i = p.g; q.i_ld = w.width * es;
-            q.j = copy; q.j_ld = (int64_t)a.c * es;
-            q.parts = w.dw_parts;
-            q.out = (char *)a.dw + first * a.dw_ld * (a.dw_dtype == DT_BF16 ? 2 : 4);
-            q.out_ld = a.dw_ld; q.out_f32 = a.dw_dtype == DT_F32;
-            if (w.few) {
-                q.i = copy;
-                CE_TRY(launch_outer(a, q, w.few, s));
-            } else {
-            if (w.dw_parts > 1) { q.out = ws + w.dw; q.out_ld = a.c; q.out_f32 = 1; q.part_stride = wide * a.c; }
-            CE_TRY(gemm<CE_DW>(a, q, w.dw_tile, wide, a.c, a.m, s));
-            if (w.dw_parts > 1) {
-                CeSum t{};
-                t.part = (const float *)q.out; t.part_stride = q.part_stride; t.parts = w.dw_parts; t.c = a.c; t.n = wide; t.factor = p.factor;
-                t.out = (char *)a.dw + first * a.dw_ld * (a.dw_dtype == DT_BF16 ? 2 : 4); t.out_ld = a.dw_ld;
-                CE_TRY(sum_parts(t, a.dw_dtype, wide, s));
-            }
+        dw.j = copy; dw.j_ld = (int64_t)a.c * es;
+        dw.parts = w.dw_parts;
+        dw.out = (char *)a.dw + first * a.dw_ld * (a.dw_dtype == DT_BF16 ? 2 : 4);
+        dw.out_ld = a.dw_ld; dw.out_f32 = a.dw_dtype == DT_F32;
+        CeSum t{};
+        t.parts = w.dw_parts; t.c = a.c; t.n = wide; t.factor = p.factor;
+        t.out = dw.out; t.out_ld = a.dw_ld;
+        if (w.dw_parts > 1) {
+            dw.out = ws + w.dw; dw.out_ld = a.c; dw.out_f32 = 1; dw.part_stride = wide * a.c;
+            t.part = (const float *)dw.out; t.part_stride = dw.part_stride;
+        }
+        if (a.dh && a.dw && !w.few && w.dh_tile.bi == w.dw_tile.bi) {
+            CE_TRY(pair(a, dh, dw, w.dh_tile, dh_rows, wide, s));
+        } else {
+            if (a.dh) CE_TRY(gemm<CE_DH>(a, dh, w.dh_tile, dh_rows, a.c, wide, s));
+            if (a.dw && w.few) {
+                dw.i = copy;
+                CE_TRY(launch_outer(a, dw, w.few, s));
+            } else if (a.dw) {
+                CE_TRY(gemm<CE_DW>(a, dw, w.dw_tile, wide, a.c, a.m, s));
             }
         }
+        if (a.dw && w.dw_parts > 1) CE_TRY(sum_parts(t, a.dw_dtype, wide, s));
     }
     if (a.dh && gather_dh) {
         CeSum t{};
