@@ -689,7 +689,7 @@ bnr_status bnr_dropout_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy
  * h [m][c] and w [classes][c] are row views in the storage type: a class's weights
  * lie together, as in an embedding table (bnr_head_fwd's wfc lies across).  c and the
  * strides are multiples of the 16-byte vector (strides up to 2^20), m is 1..2^24,
- * classes any.  A row whose label is `ignore` (padding) does not count: its loss, lse
+ * classes 1..2^30.  A row whose label is `ignore` (padding) does not count: its loss, lse
  * and dh are zeros, and its features reach nothing, whatever they hold.  Any other
  * label outside [0, classes) gives its row (and the mean) a NaN loss and NaN
  * gradients.  A bias of -infinity takes its class out.  An infinity or NaN in a row
@@ -721,7 +721,9 @@ bnr_status bnr_linear_ce_fwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dt
  *   dbias = column sums of g [classes] float32,
  * all overwritten; each may be NULL.  The logits are formed again, the classes in
  * pieces.  g is rounded to the storage type as the operand of the two products (dbias
- * adds it unrounded); sums are float32.  The same call gives the same bits. */
+ * adds it unrounded; up to 64 bf16 rows keep what the rounding left as well), with the
+ * significand of dloss[0] / lse[0] outside it; sums are float32.  The same call gives the
+ * same bits. */
 bnr_status bnr_linear_ce_bwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, const void *h, int32_t h_ld,
                              const void *w, int32_t w_ld, const bnr_ce *ce, const float *dloss, void *dh, int32_t dh_ld,
                              void *dw, int32_t dw_ld, bnr_dtype dw_dtype, float *dbias, void *ws, size_t ws_bytes,
@@ -823,8 +825,7 @@ bnr_status bnr_hbm_copy(const void *src, void *dst, size_t bytes, void *stream);
  * packing, 9 split-K sum, 10 pooling, 11 copy, 12 first CONV, 13 first-CONV
  * weight gradient, 14 max pooling, 15 classifier head, 16 layer norm,
  * 17 orthogonalised update, 18 dropout, 19 linear layer with cross entropy); it
- * returns the number of launches written.  Not
- * meant for graph capture. */
+ * returns the number of launches written.  Not meant for graph capture. */
 bnr_status bnr_trace_begin(int32_t kernel_classes, int32_t capacity);
 int32_t bnr_trace_end(double *ms, double *bytes, double *flops, int32_t *kernel_id, int32_t capacity);
 

@@ -2095,7 +2095,7 @@ static bnr_status check_ce_sizes(int64_t m, int32_t c, int32_t classes, bnr_dtyp
     if (m <= 0 || m > ((int64_t)1 << 24)) return fail(BNR_ERR_SHAPE, "m = %lld not in 1..2^24", (long long)m);
     if (classes <= 0) return fail(BNR_ERR_SHAPE, "classes %d must be positive", classes);
     if (c <= 0) return fail(BNR_ERR_SHAPE, "channels %d must be positive", c);
-    if (((m + 127) / 128) * ((classes + 127LL) / 128) > (1 << 30) || m * (int64_t)c > ((int64_t)1 << 40))
+    if (classes > (1 << 30) || ((m + 127) / 128) * ((classes + 127LL) / 128) > (1 << 30) || m * (int64_t)c > ((int64_t)1 << 40))
         return fail(BNR_ERR_UNSUPPORTED, "%lld rows x %d classes, %d channels: too large for one call", (long long)m, classes, c);
     return BNR_OK;
 }
@@ -2138,10 +2138,11 @@ size_t bnr_linear_ce_workspace_size(int64_t m, int32_t c, int32_t classes, bnr_d
 {
     if (check_ce_sizes(m, c, classes, dtype) != BNR_OK || c % vec_of(dtype)) return 0;
     CeCall a = ce_call(m, c, classes, dtype, nullptr, c, nullptr, c, nullptr);
-    static float some;                           // every output asked for
+    float some;                                  // every output asked for (none is touched)
     a.smoothing = 0.5f;
     if (!backward) return ce_fwd_bytes(a);
-    a.dh = a.dw = a.dbias = &some;
+    a.dbias = &some;
+    a.dh = a.dw = &some;
     return ce_bwd_bytes(a);
 }
 
@@ -2193,7 +2194,9 @@ bnr_status bnr_linear_ce_bwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dt
         for (int k = i + 1; k < n; k++)
             if (overlap(out[i].r, out[k].r)) return fail(BNR_ERR_ALIAS, "%s overlaps %s", out[i].name, out[k].name);
         const Range &o = out[i].r;
-        if (overlap(o, view_range(h, m, c, h_ld, es)) || overlap(o, view_range(w, classes, c, w_ld, es)) ||
+        // (different channel slices of rows of one stride do not overlap)
+        const bool on_h = out[i].name[1] == 'h' ? rows_overlap(dh, dh_ld, h, h_ld, m, c, es) : overlap(o, view_range(h, m, c, h_ld, es));
+        if (on_h || overlap(o, view_range(w, classes, c, w_ld, es)) ||
             overlap(o, bytes_range(ce->labels, m * 4)) || overlap(o, bytes_range(ce->lse, (1 + m) * 4)) ||
             (ce->bias && overlap(o, bytes_range(ce->bias, classes * (int64_t)4))) ||
             (dloss && overlap(o, bytes_range(dloss, (1 + m) * 4))))

@@ -1168,6 +1168,9 @@ struct CeBwdPlan {
         // few rows: dh streams the weights past them, dw writes more than it multiplies
         dh_tile = rows <= 32 ? CeTile{32, a.dtype == DT_BF16 ? 256 : 128, false} : ce_tile(a.dtype, rows, a.c);
         dw_tile = a.m <= 128 ? CeTile{128, 128, false} : ce_tile(a.dtype, wide, a.c);
+        // one launch for both: a dw of few stages in the smaller tiles, else a dh in the larger
+        // (1001 x 776 x 40961: 246 us and 266; 5037 x 792 x 101207: 2958 and 2917, apart 3460)
+        if (dw_tile.bi == 256 && dh_tile.bi == 128) (a.m < 1024 ? dw_tile : dh_tile) = a.m < 1024 ? dh_tile : dw_tile;
         dh_parts = ce_parts(dh_tile, rows, a.c, cdiv(wide, bk), 2);
         dw_parts = few ? 1 : ce_parts(dw_tile, wide, a.c, cdiv(a.m, bk), 4);
         g = head.end;

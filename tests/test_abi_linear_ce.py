@@ -22,6 +22,7 @@ BASE = dict(m=10, c=64, classes=100, dtype=BF16, h=A, h_ld=64, w=A + MB, w_ld=64
 BAD = [
     (dict(m=0), "BNR_ERR_SHAPE"), (dict(m=-2), "BNR_ERR_SHAPE"), (dict(m=(1 << 24) + 1), "BNR_ERR_SHAPE"),
     (dict(c=0), "BNR_ERR_SHAPE"), (dict(classes=0), "BNR_ERR_SHAPE"), (dict(classes=-5), "BNR_ERR_SHAPE"),
+    (dict(classes=(1 << 30) + 1), "BNR_ERR_UNSUPPORTED"),
     (dict(dtype=2), "BNR_ERR_DTYPE"), (dict(m=1 << 24, classes=1 << 30), "BNR_ERR_UNSUPPORTED"),
     (dict(m=1 << 24, c=(1 << 16) + 8, h_ld=1 << 17, w_ld=1 << 17), "BNR_ERR_UNSUPPORTED"),
     (dict(h=None), "BNR_ERR_NULL"), (dict(w=None), "BNR_ERR_NULL"), (dict(ce=False), "BNR_ERR_NULL"),
@@ -80,6 +81,13 @@ def test_forward_refuses(B, kw, status):
 ])
 def test_backward_refuses(B, kw, status):
     assert _bwd(B, **kw) == status, B._lib_fns["bnr_last_error"]()
+
+
+def test_slices_of_one_buffer_are_apart(B):
+    """dh may be another channel slice of h's buffer (here the call goes on to the next refusal), not one that shares
+    channels."""
+    assert _bwd(B, h_ld=192, dh=A + 128, dh_ld=192, ws=None) == "BNR_ERR_WORKSPACE"
+    assert _bwd(B, h_ld=192, dh=A + 64, dh_ld=192, ws=None) == "BNR_ERR_ALIAS"
 
 
 def test_workspace_size(B):
