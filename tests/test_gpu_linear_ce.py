@@ -100,7 +100,7 @@ class Case:
         _B().bnr_linear_ce_bwd(self.h, self.w, self.ce, self.dh if "dh" in want else None,
                                self.dw if "dw" in want else None, self.dbias if "dbias" in want else None, dloss=dloss)
 
-    def check_backward(self, dloss=None):
+    def check_backward(self, dloss=None, sure=False):
         n = int(self.counts.sum())
         r = torch.full((self.m,), 1.0 / n if n else 0.0, dtype=torch.float64, device="cuda")
         if dloss is not None:
@@ -113,6 +113,10 @@ class Case:
         rel = self.dl + (self.t + U * self.lse.abs())[:, None] + 16 * U
         size = r.abs() * (p * grow.abs() + (1 - self.s) * hot + self.s / self.v)
         dg = r.abs() * p * grow.abs() * torch.expm1(rel) + 8 * U * size
+        if sure:                                             # (p - 1) grow = -(the others' p) grow, each right as above,
+            others = torch.where(hot > 0, torch.zeros_like(p), p * grow.abs())   # up to 64 float32 additions, U of the result
+            near = (others * (torch.expm1(rel) + 64 * U)).sum(1, keepdim=True) + 8 * U * others.sum(1, keepdim=True) + 1e-15
+            dg = torch.where(hot > 0, r.abs() * near, dg)
         as_operand = dg * (1 + HALF[self.dtype]) + HALF[self.dtype] * g.abs() + TINY
         ga = g.abs() + as_operand
         h, w = self.h64, self.w64
@@ -272,6 +276,35 @@ def test_large_logits(dtype):
     k = Case(64, 128, 900, dtype, std=200.0)
     k.forward()
     k.check_forward()
+    k.backward()
+    k.check_backward()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,c,v", [(1, 280, 6), (2, 128, 1), (5, 128, 3), (16, 512, 200), (20, 136, 40), (61, 256, 7),
+                                   (100, 256, 300), (40, 520, 500), (300, 128, 17)])
+def test_rows_sure_of_their_label(m, c, v, dtype):
+    """Few classes and features that lean far towards their label's weights: 1 - p of about v 1e-6, which the roundings
+    of the label's logit and of lse (1e-6 of 14) would bury; some labels many times."""
+    k = Case(m, c, v, dtype, bias=True, std=1.0, ignored=0.2 if m > 20 else 0.0)
+    at = k.labels.clamp(0, v - 1).long()
+    k.h.copy_((k.h.double() + 14.0 * k.w.double()[at]).to(dtype))
+    k.forward()
+    k.check_forward()
+    p = torch.exp(k.l - k.lse[:, None]).gather(1, k.at)[k.counts]
+    assert bool((p > 0.6).all())
+    k.backward()
+    k.check_backward(sure=True)
+
+
+def test_an_lse_of_other_logits_is_taken_as_it_is():
+    """exp(l - lse) of an lse that no softmax of these logits has: the entry stays what the formula says."""
+    k = Case(20, 128, 5, torch.float32, std=1.0)
+    k.h.copy_(k.h + 6.0 * k.w[k.labels.long()])
+    k.forward()
+    k.reference()
+    k.ce.lse[1:] += 0.25
+    k.lse = k.lse + 0.25
     k.backward()
     k.check_backward()
 
