@@ -876,9 +876,9 @@ class CE:
 
 
 def _ce_sizes(h, w):
+    if w.dim() != 2 or h.dim() < 1:
+        raise ValueError("a view h [.., c] and w [classes, c] are wanted")
     c, classes = h.shape[-1], w.shape[0]
-    if w.dim() != 2:
-        raise ValueError("w: [classes, c] is wanted")
     return h.numel() // c if c else 0, c, classes
 
 

@@ -925,6 +925,8 @@ __global__ __launch_bounds__(kThreads) void k_ce_outer(CeGemm p, int chunk)
 
 // ---- rows' losses ------------------------------------------------------------
 constexpr int kLossRows = 16;              // rows a workgroup takes, 16 threads each
+// or 8 threads each: one workgroup, no launch for the mean (128 x 1024 x 1000 float32 18.7 us -> 16.3)
+constexpr int kLossWide = 128;
 
 __device__ __forceinline__ void ce_join(float &mx, double &sum, float mx2, double sum2)
 {
@@ -934,13 +936,16 @@ __device__ __forceinline__ void ce_join(float &mx, double &sum, float mx2, doubl
 }
 
 // The rows' losses and log sums from the tiles' maxima and sums (in float64), and the
-// sum of the workgroup's losses.  R rows a workgroup of NT threads.
+// sum of the workgroup's losses.  R rows a workgroup of NT threads; a row's threads leave
+// their part in kParts places (a wave each, or a thread each from 64 rows on).
 template <int R, int NT>
 __global__ __launch_bounds__(NT) void k_ce_rows(CeLoss p)
 {
-    __shared__ float rm[NT / 64][R];
-    __shared__ double rs[NT / 64][R], ra[NT / 64][R];
-    const int tid = threadIdx.x, r = tid % R, slice = tid / R, count = p.rows ? *p.count : (int)p.m;
+    constexpr int kParts = R < 64 ? NT / 64 : NT / R, kWaves = R < 64 ? 1 : R / 64;
+    __shared__ float rm[kParts][R];
+    __shared__ double rs[kParts][R], ra[kParts][R], red[kWaves];
+    __shared__ int red_n[kWaves];
+    const int tid = threadIdx.x, r = tid % R, slice = tid / R, place = R < 64 ? tid >> 6 : slice, count = p.rows ? *p.count : (int)p.m;
     const int i = blockIdx.x * R + r;
     if (blockIdx.x && (int)blockIdx.x * R >= count) return;
     float mx = -INFINITY;
@@ -958,13 +963,13 @@ __global__ __launch_bounds__(NT) void k_ce_rows(CeLoss p)
         ce_join(mx, sum, __shfl_xor(mx, o, 64), __shfl_xor(sum, o, 64));
         all += __shfl_xor(all, o, 64);
     }
-    if ((tid & 63) < R) { rm[tid >> 6][r] = mx; rs[tid >> 6][r] = sum; ra[tid >> 6][r] = all; }
+    if ((tid & 63) < R) { rm[place][r] = mx; rs[place][r] = sum; ra[place][r] = all; }
     __syncthreads();
-    if (tid >= R) return;
+    if (R < 64 && tid >= R) return;
     double loss = 0.0;
     int counted = 0;
-    if (i < count) {
-        for (int w = 1; w < NT / 64; w++) {
+    if (i < count && tid < R) {
+        for (int w = 1; w < kParts; w++) {
             ce_join(mx, sum, rm[w][r], rs[w][r]);
             all += ra[w][r];
         }
@@ -983,9 +988,15 @@ __global__ __launch_bounds__(NT) void k_ce_rows(CeLoss p)
         p.loss[1 + row] = (float)loss;
     }
     #pragma unroll
-    for (int o = 1; o < R; o *= 2) {
+    for (int o = 1; o < (R < 64 ? R : 64); o *= 2) {
         loss += __shfl_xor(loss, o, 64);
         counted += __shfl_xor(counted, o, 64);
+    }
+    if constexpr (kWaves > 1) {
+        if (tid < R && (tid & 63) == 0) { red[tid >> 6] = loss; red_n[tid >> 6] = counted; }
+        __syncthreads();
+        if (tid) return;
+        for (int w = 1; w < kWaves; w++) { loss += red[w]; counted += red_n[w]; }
     }
     if (tid) return;
     if (p.groups == 1) {
@@ -1020,11 +1031,25 @@ __global__ __launch_bounds__(1024) void k_ce_mean(CeLoss p)
 }
 
 // ---- sums over parts -----------------------------------------------------------
-// out[row][j .. j + 3] = the sum of the parts' float32 results, in order.
-// SL threads share a vector's parts (few results of many parts), joined in order.
-template <typename T, int SL>
-__global__ __launch_bounds__(kThreads) void k_ce_sum(CeSum p)
+__device__ __forceinline__ void ce_bias(const CeBias &p, int block)
 {
+    const int j = block * kThreads + threadIdx.x, tiles = (*p.count + p.tile - 1) / p.tile;
+    if (j >= p.classes) return;
+    double v = 0.0;
+    #pragma unroll 4
+    for (int t = 0; t < tiles; t++) v += (double)p.colsum[(int64_t)t * p.ld + j];
+    p.out[j] = (float)(v * *p.factor);
+}
+__global__ __launch_bounds__(kThreads) void k_ce_bias(CeBias p) { ce_bias(p, blockIdx.x); }
+
+// out[row][j .. j + 3] = the sum of the parts' float32 results, in order.
+// SL threads share a vector's parts (few results of many parts), joined in order.  The
+// workgroups behind the first `first` add up dbias: a launch less (128 x 1024 x 1000 float32
+// 38.3 us -> 36.4).
+template <typename T, int SL>
+__global__ __launch_bounds__(kThreads) void k_ce_sum(CeSum p, CeBias bias, int first)
+{
+    if ((int)blockIdx.x >= first) return ce_bias(bias, blockIdx.x - first);
     __shared__ float red[SL > 1 ? SL : 1][SL > 1 ? kThreads / SL : 1][4];
     const int vecs = p.c / 4, tid = threadIdx.x, slice = tid / (kThreads / SL), at = tid % (kThreads / SL);
     const int64_t id = (int64_t)blockIdx.x * (kThreads / SL) + at, i = id / vecs;
@@ -1059,16 +1084,6 @@ __global__ __launch_bounds__(kThreads) void k_ce_sum(CeSum p)
     #pragma unroll
     for (int r = 0; r < 4; r++) v[r] *= factor;
     ce_store4((T *)p.out + row * p.out_ld + j, v);
-}
-
-__global__ __launch_bounds__(kThreads) void k_ce_bias(CeBias p)
-{
-    const int j = blockIdx.x * kThreads + threadIdx.x, tiles = (*p.count + p.tile - 1) / p.tile;
-    if (j >= p.classes) return;
-    double v = 0.0;
-    #pragma unroll 4
-    for (int t = 0; t < tiles; t++) v += (double)p.colsum[(int64_t)t * p.ld + j];
-    p.out[j] = (float)(v * *p.factor);
 }
 
 // ---- how a call runs -------------------------------------------------------------
@@ -1214,12 +1229,13 @@ hipError_t launch_list(const CeCall &a, const CeHead &w, char *ws, hipStream_t s
 struct CeFwdPlan {
     CeHead head;
     CeTile tile;
-    int64_t tiles, groups, stats, sums, picked, part, end;
+    int64_t tiles, loss_rows, groups, stats, sums, picked, part, end;
     explicit CeFwdPlan(const CeCall &a) : head(a)
     {
         tile = ce_logit_tile(a.dtype, a.m, a.classes);
         tiles = cdiv(a.classes, tile.bj);
-        groups = cdiv(a.m, kLossRows);
+        loss_rows = a.m > kLossRows && a.m <= kLossWide && tiles < 64 ? kLossWide : kLossRows;
+        groups = cdiv(a.m, loss_rows);
         stats = tile.small ? 0 : head.end;       // (few rows are taken as they are)
         sums = up256(stats + tiles * a.m * 8);
         picked = up256(sums + (a.smoothing > 0.f ? tiles * a.m * 4 : 0));
@@ -1272,18 +1288,20 @@ struct CeBwdPlan {
     }
 };
 
-hipError_t sum_parts(const CeSum &p, int dtype, int64_t rows, hipStream_t s)
+// (with dbias's workgroups behind it where `bias` asks for them)
+hipError_t sum_parts(const CeSum &p, const CeBias &bias, int dtype, int64_t rows, hipStream_t s)
 {
     TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, ((double)p.parts * 4 + (dtype == DT_BF16 ? 2 : 4)) * rows * p.c, 0.0);
     const int64_t vecs = rows * (p.c / 4);
     const bool shared = vecs < 512 * kThreads && p.parts >= 8;   // (16 x 2048 of 64 parts: 13 us one thread a vector)
-    const dim3 grid((unsigned)cdiv(vecs, shared ? kThreads / 8 : kThreads)), block(kThreads);
+    const int first = (int)cdiv(vecs, shared ? kThreads / 8 : kThreads);
+    const dim3 grid((unsigned)(first + (bias.out ? cdiv(bias.classes, kThreads) : 0))), block(kThreads);
     if (dtype == DT_BF16) {
-        if (shared) hipLaunchKernelGGL((k_ce_sum<bf16_t, 8>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((k_ce_sum<bf16_t, 1>), grid, block, 0, s, p);
+        if (shared) hipLaunchKernelGGL((k_ce_sum<bf16_t, 8>), grid, block, 0, s, p, bias, first);
+        else hipLaunchKernelGGL((k_ce_sum<bf16_t, 1>), grid, block, 0, s, p, bias, first);
     } else {
-        if (shared) hipLaunchKernelGGL((k_ce_sum<float, 8>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((k_ce_sum<float, 1>), grid, block, 0, s, p);
+        if (shared) hipLaunchKernelGGL((k_ce_sum<float, 8>), grid, block, 0, s, p, bias, first);
+        else hipLaunchKernelGGL((k_ce_sum<float, 1>), grid, block, 0, s, p, bias, first);
     }
     return hipGetLastError();
 }
@@ -1349,6 +1367,7 @@ hipError_t launch_ce_fwd(const CeCall &a, void *ws_, hipStream_t s)
     TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 8.0 * a.m * w.tiles, 0.0);
     // (a single row takes all threads, and many tiles take 64 threads a row instead of 16)
     if (a.m == 1) hipLaunchKernelGGL((k_ce_rows<1, kThreads>), dim3(1), dim3(kThreads), 0, s, l);
+    else if (w.loss_rows == kLossWide) hipLaunchKernelGGL((k_ce_rows<kLossWide, 1024>), dim3(1), dim3(1024), 0, s, l);
     else if (w.tiles >= 64) hipLaunchKernelGGL((k_ce_rows<kLossRows, 1024>), dim3((unsigned)w.groups), dim3(1024), 0, s, l);
     else hipLaunchKernelGGL((k_ce_rows<kLossRows, kThreads>), dim3((unsigned)w.groups), dim3(kThreads), 0, s, l);
     if (w.groups > 1) hipLaunchKernelGGL(k_ce_mean, dim3(1), dim3(1024), 0, s, l);
@@ -1416,19 +1435,18 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
                 CE_TRY(gemm<CE_DW>(a, dw, w.dw_tile, wide, a.c, a.m, s));
             }
         }
-        if (a.dw && w.dw_parts > 1) CE_TRY(sum_parts(t, a.dw_dtype, wide, s));
+        if (a.dw && w.dw_parts > 1) CE_TRY(sum_parts(t, CeBias{}, a.dw_dtype, wide, s));
     }
+    CeBias b{};
+    b.count = p.count; b.tile = w.grad_rows; b.factor = p.factor; b.classes = a.classes;
+    b.colsum = (const float *)(ws + w.colsum); b.ld = a.classes; b.out = a.dbias;
     if (a.dh && gather_dh) {
         CeSum t{};
         t.part = (const float *)(ws + w.dh); t.part_stride = dh_rows * a.c; t.twice = w.few ? 1 : 0; t.parts = w.dh_parts; t.c = a.c;
         t.rows = p.rows; t.count = p.count; t.factor = p.factor;
         t.out = a.dh; t.out_ld = a.dh_ld;
-        CE_TRY(sum_parts(t, a.dtype, a.m, s));
-    }
-    if (a.dbias) {
-        CeBias b{};
-        b.count = p.count; b.tile = w.grad_rows; b.factor = p.factor; b.classes = a.classes;
-        b.colsum = (const float *)(ws + w.colsum); b.ld = a.classes; b.out = a.dbias;
+        CE_TRY(sum_parts(t, b, a.dtype, a.m, s));
+    } else if (a.dbias) {
         TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 4.0 * a.classes * (cdiv(a.m, w.grad_rows) + 1), 0.0);
         hipLaunchKernelGGL(k_ce_bias, dim3((unsigned)cdiv(a.classes, kThreads)), dim3(kThreads), 0, s, b);
     }
