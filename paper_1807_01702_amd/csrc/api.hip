@@ -2095,7 +2095,7 @@ static bnr_status check_ce_sizes(int64_t m, int32_t c, int32_t classes, bnr_dtyp
     if (m <= 0 || m > ((int64_t)1 << 24)) return fail(BNR_ERR_SHAPE, "m = %lld not in 1..2^24", (long long)m);
     if (classes <= 0) return fail(BNR_ERR_SHAPE, "classes %d must be positive", classes);
     if (c <= 0) return fail(BNR_ERR_SHAPE, "channels %d must be positive", c);
-    if (classes > (1 << 30) || ((m + 127) / 128) * ((classes + 127LL) / 128) > (1 << 30) || m * (int64_t)c > ((int64_t)1 << 40))
+    if (classes > (1 << 30) || ((m + 127) / 128) * ((classes + 127LL) / 128) > (1 << 29) || m * (int64_t)c > ((int64_t)1 << 40))
         return fail(BNR_ERR_UNSUPPORTED, "%lld rows x %d classes, %d channels: too large for one call", (long long)m, classes, c);
     return BNR_OK;
 }

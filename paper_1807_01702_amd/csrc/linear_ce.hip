@@ -222,12 +222,13 @@ template <int B, int NB> struct CeFrags<bf16_t, B, NB, true> {
     }
 };
 template <int B, int NB> struct CeFrags<float, B, NB, true> {
-    static_assert(NB == 4, "four blocks' values are one read");
+    static_assert(NB == 4 || NB == 2, "the blocks' values are one read");
+    typedef __attribute__((ext_vector_type(NB))) float vec;
     uint32_t at;
-    __device__ __forceinline__ void init(int w0, int lane) { at = 4 * (lane / 16) * (B * 4) + (w0 + 4 * (lane % 16)) * 4; }
+    __device__ __forceinline__ void init(int w0, int lane) { at = 4 * (lane / 16) * (B * 4) + (w0 + NB * (lane % 16)) * 4; }
     __device__ __forceinline__ void read(const unsigned char *lds, int sub, int lane, f32x4 *f, int part) const
     {
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(lds + at + (sub * 16 + part) * (B * 4));
+        const vec v = *reinterpret_cast<const vec *>(lds + at + (sub * 16 + part) * (B * 4));
         #pragma unroll
         for (int b = 0; b < NB; b++) f[b][part] = v[b];
     }
@@ -267,7 +268,6 @@ __device__ __forceinline__ void ce_wave_sync()
 
 typedef __attribute__((address_space(3))) unsigned char lds_char;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-constexpr int kWaveOut = 64 * 64 * 4;      // bytes of LDS a wave turns its results in
 
 // neighbouring results
 __device__ __forceinline__ void ce_store4(float *p, const float *v) { *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]}; }
@@ -331,7 +331,8 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
     // this one; meanwhile it reads this stage's fragments and the next stage is loaded
     // into the LDS that the stage before has left.  Products, reads and loads alternate.
     struct Frags { frag i[MI], j[NJ]; } f0, f1;
-    constexpr int kLi = LoadI::kLoads, kLj = LoadJ::kLoads, kParts = MI > NJ ? MI : NJ,
+    constexpr int kPi = ICOLS && sizeof(T) == 4 ? 4 : MI, kPj = JCOLS && sizeof(T) == 4 ? 4 : NJ;     // reads of a sub-step
+    constexpr int kLi = LoadI::kLoads, kLj = LoadJ::kLoads, kParts = kPi > kPj ? kPi : kPj,
                   kEach = MI > 2 ? (kLi + kLj) * 2 / MI : kLi + kLj;
     auto load = [&](unsigned char *lds, const typename LoadI::Stage &a, const typename LoadJ::Stage &b, int from, int to)
         __attribute__((always_inline)) {
@@ -342,8 +343,8 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
         }
     };
     auto read = [&](Frags &f, const unsigned char *lds, int sub, int part) __attribute__((always_inline)) {
-        if (part < NJ) rj.read(lds + BI * 128, sub, lane, f.j, part);
-        if (part < MI) ri.read(lds, sub, lane, f.i, part);
+        if (part < kPj) rj.read(lds + BI * 128, sub, lane, f.j, part);
+        if (part < kPi) ri.read(lds, sub, lane, f.i, part);
     };
     auto multiply = [&](const Frags &f, int a) __attribute__((always_inline)) {
         #pragma unroll
@@ -509,8 +510,8 @@ __device__ __forceinline__ void ce_tile_of(const CeGemm &p, int block, unsigned 
         // i = 16 a + q and j = 16 b + 4 g + r, in float32 columns i = MI q + a, j = NJ (4 g + r) + b.
         constexpr bool IP = ICOLS && sizeof(T) == 4, JP = JCOLS && sizeof(T) == 4;
         constexpr int kHalf = NT / 128;
-        constexpr int kSub = TI < 64 ? TI : 64;
-        static_assert(kStage >= kHalf * kWaveOut && (!IP || TI == 64) && (!JP || TJ == 64), "a wave's part of the stages");
+        constexpr int kSub = TI < 64 ? TI : 64, kWaveOut = kSub * 64 * 4;
+        static_assert(kStage >= kHalf * kWaveOut && (!IP || TI == kSub) && (!JP || TJ == 64), "a wave's part of the stages");
         lds_char *mine = (wave < kHalf ? (lds_char *)lds0 : (lds_char *)lds1) + wave % kHalf * kWaveOut;
         const int lrow = late / 8, lcol = late % 8 * 8;
         // (parts are multiplied when they are added)
@@ -529,7 +530,7 @@ __device__ __forceinline__ void ce_tile_of(const CeGemm &p, int block, unsigned 
             for (int a = 0; a < kSub / 16; a++)
                 #pragma unroll
                 for (int b = 0; b < 4; b++) {
-                    const int row = IP ? 4 * q + a : 16 * a + q, chunk = JP ? 4 * g + b : 4 * b + g;
+                    const int row = IP ? MI * q + a : 16 * a + q, chunk = JP ? 4 * g + b : 4 * b + g;
                     const f32x4 v = JP ? f32x4{acc[0][4 * h + a][b], acc[1][4 * h + a][b], acc[2][4 * h + a][b], acc[3][4 * h + a][b]}
                                        : acc[4 * c + b][4 * h + a];
                     *(lds_f32x4 *)(mine + row * 256 + ((chunk ^ (row % 16)) * 16)) = v;
@@ -1090,9 +1091,11 @@ __global__ __launch_bounds__(kThreads) void k_ce_sum(CeSum p, CeBias bias, int f
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 
-// How a product's tiles run: 256 x 256 (one workgroup of eight waves a CU) where they
-// fill the chip, else 128 x 128 (two workgroups of four waves a CU); logits of few rows
-// or of too few tiles for that run as k_ce_small, 16 x i by 16 x j.
+// How a product's tiles run: bf16 in 256 x 256 (one workgroup of eight waves a CU) where
+// they fill the chip, else in 128 x 128 (two workgroups of four waves a CU), float32 in 64 x
+// 128 (three of four; against two of 128 x 128: 128 x 1024 x 1000 backward 32.9 us and 36.5,
+// 4907 x 1832 x 7449 1.61 ms and 1.72, 299 x 976 x 102340 forward 519 us and 637); logits of
+// few rows or of too few tiles for that run as k_ce_small, 16 x i by 16 x j.
 // Up to kFewRows bf16 rows g is kept in two parts, rounded and the rest, in separate rows
 // (their products cost next to nothing beside reading the weights): with few rows the
 // rounding of one label's g is no longer one of many.
@@ -1104,7 +1107,8 @@ constexpr int kFewClasses = 512;
 struct CeTile { int bi, bj; bool small; };
 inline CeTile ce_tile(int dtype, int64_t ni, int64_t nj)
 {
-    const int b = dtype == DT_BF16 && cdiv(ni, 256) * cdiv(nj, 256) >= 192 ? 256 : 128;
+    if (dtype == DT_F32) return CeTile{64, 128, false};
+    const int b = cdiv(ni, 256) * cdiv(nj, 256) >= 192 ? 256 : 128;
     return CeTile{b, b, false};
 }
 inline CeTile ce_logit_tile(int dtype, int64_t m, int64_t classes)
@@ -1156,7 +1160,7 @@ void go(const CeGemm &p, const CeTile &t, int64_t grid, hipStream_t s)
             return;
         }
     }
-    hipLaunchKernelGGL((k_ce_gemm<T, 128, 128, 2, 2, MODE>), g, dim3(256), 0, s, p);
+    hipLaunchKernelGGL((k_ce_gemm<T, sizeof(T) == 2 ? 128 : 64, 128, 2, 2, MODE>), g, dim3(256), 0, s, p);
 }
 
 template <int MODE>
@@ -1187,7 +1191,7 @@ hipError_t pair(const CeCall &a, const CeGemm &dh, const CeGemm &dw, const CeTil
     TraceScope tr(KC_CONV, KID_LINEAR_CE, s, es * ((double)a.m * wide + (2.0 * a.m + 2.0 * wide) * a.c), 4.0 * a.m * wide * a.c);
     const int64_t cols = cdiv(a.c, t.bj), first = cdiv(cdiv(dh_rows, t.bi) * cols * dh.parts, 8) * 8;
     const dim3 g((unsigned)(first + cdiv(wide, t.bi) * cols * dw.parts));
-    if (a.dtype != DT_BF16) hipLaunchKernelGGL((k_ce_pair<float, 128, 128, 2, 2>), g, dim3(256), 0, s, dh, dw, (int)first);
+    if (a.dtype != DT_BF16) hipLaunchKernelGGL((k_ce_pair<float, 64, 128, 2, 2>), g, dim3(256), 0, s, dh, dw, (int)first);
     else if (t.bi == 256) hipLaunchKernelGGL((k_ce_pair<bf16_t, 256, 256, 2, 4>), g, dim3(512), 0, s, dh, dw, (int)first);
     else hipLaunchKernelGGL((k_ce_pair<bf16_t, 128, 128, 2, 2>), g, dim3(256), 0, s, dh, dw, (int)first);
     return hipGetLastError();
@@ -1272,7 +1276,7 @@ struct CeBwdPlan {
         const int64_t rows = few ? 2 * a.m : a.m;
         // few rows: dh streams the weights past them, dw writes more than it multiplies
         dh_tile = rows <= 32 ? CeTile{32, a.dtype == DT_BF16 ? 256 : 128, false} : ce_tile(a.dtype, rows, a.c);
-        dw_tile = a.m <= 128 ? CeTile{128, 128, false} : ce_tile(a.dtype, wide, a.c);
+        dw_tile = a.dtype == DT_BF16 && a.m <= 128 ? CeTile{128, 128, false} : ce_tile(a.dtype, wide, a.c);
         // one launch for both: a dw of few stages in the smaller tiles, else a dh in the larger
         // (1001 x 776 x 40961: 246 us and 266; 5037 x 792 x 101207: 2958 and 2917, apart 3460)
         if (dw_tile.bi == 256 && dh_tile.bi == 128) (a.m < 1024 ? dw_tile : dh_tile) = a.m < 1024 ? dh_tile : dw_tile;
