@@ -169,6 +169,31 @@ def test_large_tiles(dtype, m, c, v):
     k.check_backward()
 
 
+@pytest.mark.parametrize("m,c,v", [(1, 4, 3), (9, 12, 700), (33, 140, 600), (70, 516, 130), (257, 36, 2000), (1500, 140, 1700)])
+def test_odd_vectors_of_float32(m, c, v):
+    """Rows of an odd number of 16-byte vectors: results that leave in eights end in a four."""
+    for kw in (dict(), dict(bias=True, ignored=0.3, pad=4)):
+        k = Case(m, c, v, torch.float32, **kw)
+        k.forward()
+        k.check_forward()
+        k.backward(pad=kw.get("pad", 0))
+        k.check_backward()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,v", [(20, 7), (128, 300), (300, 700)])
+def test_rows_of_padding_alone(m, v, dtype):
+    """No row counts: a mean of 0 and gradients of zeros, whatever stands there."""
+    k = Case(m, 64, v, dtype, bias=True)
+    k.labels.fill_(IGNORE)
+    k.h[m // 2] = float("nan")
+    k.forward()
+    k.check_forward()
+    k.backward()
+    for t in (k.loss, k.ce.lse, k.dh, k.dw, k.dbias):
+        assert bool((t == 0).all())
+
+
 @pytest.mark.parametrize("dtype,m,v", [(torch.bfloat16, 2100, 140001), (torch.float32, 1100, 130001)])
 def test_pieces(dtype, m, v):
     """Classes whose gradients pass a piece."""
