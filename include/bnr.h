@@ -668,7 +668,8 @@ typedef struct {
 
 /* y = dropout(x) + res (res may be NULL: 0), rounded once.  What is dropped adds
  * nothing, infinities and NaN included.  y may coincide exactly with x or res and
- * may not overlap them otherwise.  1 <= m <= 2^31. */
+ * may not overlap them otherwise.  1 <= m <= 2^31, m ceil(c / 8) < 2^39
+ * (BNR_ERR_UNSUPPORTED). */
 bnr_status bnr_dropout_fwd(int64_t m, int32_t c, bnr_dtype dtype, const void *x, int32_t x_ldc, const void *res,
                            int32_t res_ldc, const bnr_dropout *d, void *y, int32_t y_ldc, void *stream);
 

@@ -13,6 +13,16 @@ struct alignas(16) vec16 { uint32_t u[4]; };
 
 constexpr int kThreads = 256;   // every kernel runs 256-thread workgroups (4 waves of 64)
 
+// Grids of any number of workgroups of up to 1024 threads: a dimension of a grid holds fewer
+// than 2^32 threads, so workgroups past kGridX go on in rows of the second dimension, whose
+// last may pass `groups` (a kernel leaves those out itself).
+constexpr int kGridX = 1 << 21;
+inline dim3 wide_grid(int64_t groups)
+{
+    return groups <= kGridX ? dim3((unsigned)groups) : dim3(kGridX, (unsigned)((groups + kGridX - 1) / kGridX));
+}
+__device__ __forceinline__ int64_t wide_block() { return (int64_t)blockIdx.y * kGridX + blockIdx.x; }
+
 __device__ __forceinline__ float bf2f(bf16_t h) { return __uint_as_float((uint32_t)h << 16); }
 // float -> bf16, round to nearest even (v_cvt_pk_bf16_f32 on gfx950).
 __device__ __forceinline__ bf16_t f2bf(float f) {

@@ -75,7 +75,7 @@ __device__ __forceinline__ void narrow(float v, bf16_t &o) { o = f2bf(v); }
 template <typename T, bool ADD, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_dropout(DropoutParams p)
 {
-    const uint64_t first = (uint64_t)blockIdx.x * kThreads;
+    const uint64_t first = (uint64_t)wide_block() * kThreads;
     const uint64_t row0 = first / p.blocks;
     const uint32_t col0 = (uint32_t)(first - row0 * p.blocks);
     const uint32_t step = p.step_dev ? *p.step_dev : p.step;
@@ -104,9 +104,9 @@ __global__ __launch_bounds__(kThreads) void k_dropout(DropoutParams p)
 }
 
 template <typename T>
-void go(const DropoutParams &p, unsigned grid, hipStream_t s)
+void go(const DropoutParams &p, dim3 g, hipStream_t s)
 {
-    const dim3 g(grid), b(kThreads);
+    const dim3 b(kThreads);
     if (p.c % 8 == 0) {
         if (p.add) hipLaunchKernelGGL((k_dropout<T, true, true>), g, b, 0, s, p);
         else hipLaunchKernelGGL((k_dropout<T, false, true>), g, b, 0, s, p);
@@ -133,7 +133,7 @@ hipError_t launch_dropout(int dtype, DropoutParams p, hipStream_t s)
     p.magic = (uint32_t)(((1ull << p.shift) + p.blocks - 1) / p.blocks);
     const double es = dtype == DT_BF16 ? 2 : 4, n = (double)p.m * p.c * es;
     TraceScope tr(KC_SWEEP, KID_DROPOUT, s, (p.add ? 3.0 : 2.0) * n, 0.0);
-    const unsigned grid = (unsigned)dropout_groups(p.m, p.c);
+    const dim3 grid = wide_grid(dropout_groups(p.m, p.c));
     if (dtype == DT_BF16) go<bf16_t>(p, grid, s);
     else go<float>(p, grid, s);
     return hipGetLastError();

@@ -59,3 +59,13 @@ def test_dropout_binding_refuses(B):
     for step in (-1, 1 << 32, torch.zeros(1), torch.zeros(2, dtype=torch.int32)):
         with pytest.raises(ValueError):
             B.Dropout(0.1, 1, step=step).struct()
+
+
+@pytest.mark.parametrize("name", ["bnr_dropout_fwd", "bnr_dropout_bwd"])
+def test_largest_call(B, name):
+    """2^39 blocks of eight channels are the first too many."""
+    d = B.DropoutStruct(0.1, 1, 2, 3, None)
+    mid = (None, 0, ctypes.byref(d)) if name == "bnr_dropout_fwd" else (ctypes.byref(d), None, 0)
+    for m, c, ldc in ((1 << 31, 2041, 2048), (1 << 31, 2048, 2048), (1 << 28, 1 << 14, 1 << 14)):
+        got = B._lib_fns[name](m, c, BF16, A, ldc, *mid, A + (1 << 53), ldc, None)
+        assert B.STATUS[got] == "BNR_ERR_UNSUPPORTED"

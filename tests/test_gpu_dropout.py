@@ -206,3 +206,32 @@ def test_offsets_past_32_bits():
     drop = B.Dropout(0.4, 21)
     B.bnr_dropout_fwd(x, drop, y)
     _check(y, _np(x), drop, 0, torch.float32)
+
+
+def test_more_threads_than_a_dimension_of_a_grid_holds():
+    """2^31 - 5 rows of three blocks: past 2^32 threads (73 GB, in place), checked in windows of rows."""
+    B = _B()
+    m, c, p, seed, site, step = (1 << 31) - 5, 17, 0.3, 0x123456789ABCDEF, 6, 11
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 2 * m * c + (4 << 30):
+        pytest.skip("74 GB of device memory are wanted")
+    x = torch.empty(m, c, dtype=torch.bfloat16, device="cuda")
+    n = 1000
+    # the ends, the rows about the end of the grid's first dimension (2^29 threads), about 2^32 threads
+    starts = [0, (1 << 29) // 3 - n // 2, (1 << 30) - 7, (1 << 32) // 3 - n // 2, m - n]
+    before = []
+    for s in starts:
+        x[s:s + n] = torch.randn(n, c, device="cuda").bfloat16()
+        before.append(_np(x[s:s + n]))
+    B.bnr_dropout_fwd(x, B.Dropout(p, seed, site=site, step=step), x)
+    for s, was in zip(starts, before):
+        col, row = np.meshgrid(np.arange(3), s + np.arange(n))
+        words = D.philox4x32((col, row, site, step), (seed & 0xFFFFFFFF, seed >> 32))
+        words = np.stack([np.broadcast_to(w, col.shape) for w in words], 2).astype(np.int64)
+        bits = np.stack((words & 0xFFFF, words >> 16), 3).reshape(n, 24)[:, :c]
+        t = D.limit(p)
+        ref = np.where(bits >= t, was * (65536 / (65536 - t)), 0.0)
+        off, tol = np.abs(_np(x[s:s + n]) - ref), (2 * U + HALF[torch.bfloat16]) * np.abs(ref) * (1 + U)
+        assert bool((off <= tol).all()), "rows from %d" % s
+    del x
+    torch.cuda.empty_cache()
