@@ -690,7 +690,8 @@ bnr_status bnr_dropout_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy
  * h [m][c] and w [classes][c] are row views in the storage type: a class's weights
  * lie together, as in an embedding table (bnr_head_fwd's wfc lies across).  c and the
  * strides are multiples of the 16-byte vector (strides up to 2^20), m is 1..2^24,
- * classes 1..2^30.  A row whose label is `ignore` (padding) does not count: its loss, lse
+ * classes 1..2^30, with ceil(m / 128) ceil(classes / 128) up to 2^29 and m c up to 2^40
+ * (BNR_ERR_UNSUPPORTED).  A row whose label is `ignore` (padding) does not count: its loss, lse
  * and dh are zeros, and its features reach nothing, whatever they hold.  Any other
  * label outside [0, classes) gives its row (and the mean) a NaN loss and NaN
  * gradients.  A bias of -infinity takes its class out.  An infinity or NaN in a row

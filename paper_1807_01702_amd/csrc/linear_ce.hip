@@ -616,7 +616,7 @@ template <typename T, int BI, int BJ, int WI, int WJ, int MODE>
 __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
 {
     CE_LDS(BI, BJ);
-    ce_tile_of<T, BI, BJ, WI, WJ, MODE>(p, blockIdx.x, lds0, lds1, rows, bias);
+    ce_tile_of<T, BI, BJ, WI, WJ, MODE>(p, (int)wide_block(), lds0, lds1, rows, bias);
 }
 
 // dh and dw of a piece, which do not need each other, in one launch: dh's longer tiles
@@ -626,8 +626,9 @@ template <typename T, int BI, int BJ, int WI, int WJ>
 __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_pair(CeGemm dh, CeGemm dw, int first)
 {
     CE_LDS(BI, BJ);
-    if ((int)blockIdx.x < first) ce_tile_of<T, BI, BJ, WI, WJ, CE_DH>(dh, blockIdx.x, lds0, lds1, rows, bias);
-    else ce_tile_of<T, BI, BJ, WI, WJ, CE_DW>(dw, blockIdx.x - first, lds0, lds1, rows, bias);
+    const int block = (int)wide_block();
+    if (block < first) ce_tile_of<T, BI, BJ, WI, WJ, CE_DH>(dh, block, lds0, lds1, rows, bias);
+    else ce_tile_of<T, BI, BJ, WI, WJ, CE_DW>(dw, block - first, lds0, lds1, rows, bias);
 }
 
 // ---- few rows, or few tiles ---------------------------------------------------
@@ -646,7 +647,7 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
     __shared__ __align__(16) float part[4][BI * kPitch];
     const int ni = p.rows ? *p.count : (int)p.m, nj = p.classes;
     CePlace pl;
-    if (!ce_place(pl, blockIdx.x, (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, 1)) return;
+    if (!ce_place(pl, (int)wide_block(), (ni + BI - 1) / BI, (nj + BJ - 1) / BJ, 1)) return;
     const int i0 = pl.ti * BI, j0 = pl.tj * BJ;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane % 16, g = lane / 16;
     const int width = p.c * (int)sizeof(T);
@@ -1050,10 +1051,14 @@ __global__ __launch_bounds__(kThreads) void k_ce_bias(CeBias p) { ce_bias(p, blo
 template <typename T, int SL>
 __global__ __launch_bounds__(kThreads) void k_ce_sum(CeSum p, CeBias bias, int first)
 {
-    if ((int)blockIdx.x >= first) return ce_bias(bias, blockIdx.x - first);
+    const int64_t block = wide_block();
+    if (block >= first) {
+        if (bias.out) ce_bias(bias, (int)(block - first));
+        return;
+    }
     __shared__ float red[SL > 1 ? SL : 1][SL > 1 ? kThreads / SL : 1][4];
     const int vecs = p.c / 4, tid = threadIdx.x, slice = tid / (kThreads / SL), at = tid % (kThreads / SL);
-    const int64_t id = (int64_t)blockIdx.x * (kThreads / SL) + at, i = id / vecs;
+    const int64_t id = block * (kThreads / SL) + at, i = id / vecs;
     const int j = (int)(id - i * vecs) * 4;
     const int64_t n = p.rows ? *p.count : p.n;
     const bool mine = i < n;
@@ -1133,7 +1138,7 @@ inline int ce_parts(const CeTile &t, int64_t ni, int64_t nj, int64_t steps, int 
 template <typename T, int MODE>
 void go(const CeGemm &p, const CeTile &t, int64_t grid, hipStream_t s)
 {
-    const dim3 g((unsigned)grid);
+    const dim3 g = wide_grid(grid);
     if constexpr (MODE == CE_STATS || MODE == CE_GRAD) {
         if (t.small) {
             const auto at = [&](auto mi) {
@@ -1190,7 +1195,7 @@ hipError_t pair(const CeCall &a, const CeGemm &dh, const CeGemm &dw, const CeTil
     const double es = a.dtype == DT_BF16 ? 2 : 4;
     TraceScope tr(KC_CONV, KID_LINEAR_CE, s, es * ((double)a.m * wide + (2.0 * a.m + 2.0 * wide) * a.c), 4.0 * a.m * wide * a.c);
     const int64_t cols = cdiv(a.c, t.bj), first = cdiv(cdiv(dh_rows, t.bi) * cols * dh.parts, 8) * 8;
-    const dim3 g((unsigned)(first + cdiv(wide, t.bi) * cols * dw.parts));
+    const dim3 g = wide_grid(first + cdiv(wide, t.bi) * cols * dw.parts);
     if (a.dtype != DT_BF16) hipLaunchKernelGGL((k_ce_pair<float, 64, 128, 2, 2>), g, dim3(256), 0, s, dh, dw, (int)first);
     else if (t.bi == 256) hipLaunchKernelGGL((k_ce_pair<bf16_t, 256, 256, 2, 4>), g, dim3(512), 0, s, dh, dw, (int)first);
     else hipLaunchKernelGGL((k_ce_pair<bf16_t, 128, 128, 2, 2>), g, dim3(256), 0, s, dh, dw, (int)first);
@@ -1299,7 +1304,7 @@ hipError_t sum_parts(const CeSum &p, const CeBias &bias, int dtype, int64_t rows
     const int64_t vecs = rows * (p.c / 4);
     const bool shared = vecs < 512 * kThreads && p.parts >= 8;   // (16 x 2048 of 64 parts: 13 us one thread a vector)
     const int first = (int)cdiv(vecs, shared ? kThreads / 8 : kThreads);
-    const dim3 grid((unsigned)(first + (bias.out ? cdiv(bias.classes, kThreads) : 0))), block(kThreads);
+    const dim3 grid = wide_grid(first + (bias.out ? cdiv(bias.classes, kThreads) : 0)), block(kThreads);
     if (dtype == DT_BF16) {
         if (shared) hipLaunchKernelGGL((k_ce_sum<bf16_t, 8>), grid, block, 0, s, p, bias, first);
         else hipLaunchKernelGGL((k_ce_sum<bf16_t, 1>), grid, block, 0, s, p, bias, first);

@@ -421,3 +421,89 @@ def test_offsets_past_32_bits():
     k.check_forward()
     k.backward()
     k.check_backward()
+
+
+def _room(nbytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < nbytes + (4 << 30):
+        pytest.skip("%.0f GB of device memory are wanted" % (nbytes / 1e9))
+
+
+def test_forward_of_more_threads_than_a_dimension_of_a_grid_holds():
+    """2^20 rows of 131072 classes in float32: 2^24 tiles of 256 threads (16 GB), some rows checked."""
+    _room(16 << 30)
+    m, v = 1 << 20, 131072
+    k = Case(m, 4, v, torch.float32, smoothing=0.1, z=1e-3, ignored=0.1)
+    k.forward()
+    at = torch.cat([torch.arange(s, s + 100, device="cuda") for s in (0, (1 << 17) - 50, (1 << 19) - 50, m - 100)])
+    loss, lse, n = k.loss[1:][at], k.ce.lse[1:][at], int((k.labels != IGNORE).sum())
+    assert float(k.ce.lse[0]) == n and bool(torch.isfinite(k.loss).all())
+    k.h, k.labels = k.h[at], k.labels[at]
+    k.reference()
+    zero = torch.zeros_like(k.lse)
+    _close("lse", lse, torch.where(k.counts, k.lse, zero), torch.where(k.counts, k.t + U * k.lse.abs(), zero))
+    _close("loss", loss, torch.where(k.counts, k.rows, zero), torch.where(k.counts, k.rows_tol, zero))
+    torch.cuda.empty_cache()
+
+
+def test_few_rows_of_more_threads_than_a_dimension_of_a_grid_holds():
+    """33 rows of 2^29 + 5 classes: 2^24 + 2 tiles of 256 threads (11 GB)."""
+    _room(16 << 30)
+    m, c, v = 33, 8, (1 << 29) + 5
+    w = torch.empty(v, c, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(7)
+    step = 1 << 23
+    for s in range(0, v, step):
+        w[s:s + step] = torch.randn(min(step, v - s), c, generator=g, device="cuda").bfloat16()
+    h = torch.randn(m, c, generator=g, device="cuda").bfloat16()
+    labels = torch.randint(0, v, (m,), generator=g, device="cuda", dtype=torch.int32)
+    labels[3], labels[32] = v - 1, v - 6                  # the last tile, and the one before it
+    ce, loss = _B().CE(labels), torch.empty(1 + m, device="cuda")
+    _B().bnr_linear_ce_fwd(h, w, ce, loss)
+    top = torch.full((m,), -float("inf"), dtype=torch.float64, device="cuda")
+    dl = torch.zeros_like(top)
+    for s in range(0, v, step):
+        l = h.double() @ w[s:s + step].double().t()
+        dl = torch.maximum(dl, (c + 8) * U * (h.double().abs() @ w[s:s + step].double().abs().t()).amax(1))
+        top = torch.logaddexp(top, torch.logsumexp(l, 1))
+    picked = (h.double() * w[labels.long()].double()).sum(1)
+    t = dl + 100 * U
+    _close("lse", ce.lse[1:], top, t + U * top.abs())
+    _close("loss", loss[1:], top - picked, t + dl + 2 * U * (top - picked).abs())
+    assert float(ce.lse[0]) == m
+    del w
+    torch.cuda.empty_cache()
+
+
+def test_gradient_of_rows_of_more_threads_than_a_dimension_of_a_grid_holds():
+    """2^24 rows of 1024 channels whose dh adds up over two pieces: 2^32 threads add the parts (180 GB)."""
+    m, c, v = 1 << 24, 1024, 300
+    _room(170 << 30)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    h, dh = (torch.empty(m, c, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    step = 1 << 20
+    for s in range(0, m, step):
+        h[s:s + step] = torch.randn(step, c, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(v, c, generator=g, device="cuda") * (1.0 / 32)).bfloat16()
+    labels = torch.randint(0, v, (m,), generator=g, device="cuda", dtype=torch.int32)
+    labels[torch.rand(m, generator=g, device="cuda") < 0.1] = IGNORE
+    labels[m - 1] = 299
+    lse = torch.full((1 + m,), float(np.log(v) + 0.5), device="cuda")        # any log sum: the formula's g of it
+    n = int((labels != IGNORE).sum())
+    lse[0] = n
+    _B().bnr_linear_ce_bwd(h, w, _B().CE(labels, ignore=IGNORE, lse=lse), dh)
+    for s in (0, (1 << 21) - 200, m // 2 - 200, m - 400):
+        hh, ww, y = h[s:s + 400].double(), w.double(), labels[s:s + 400].long()
+        counts = (y != IGNORE)[:, None]
+        l = hh @ ww.t()
+        p = torch.exp(l - float(lse[1]))
+        hot = torch.zeros_like(p).scatter_(1, y.clamp_min(0)[:, None], 1.0)
+        r = counts / n
+        gg = r * (p - hot)
+        dg = r * p * torch.expm1((c + 8) * U * (hh.abs() @ ww.abs().t()) + 20 * U) + 8 * U * r * (p + hot)
+        half = HALF[torch.bfloat16]
+        operand = dg * (1 + half) + half * gg.abs() + TINY
+        tol = (operand + (v + 66) * U * (gg.abs() + operand)) @ ww.abs()
+        _close("dh from row %d" % s, dh[s:s + 400], gg @ ww, tol + half * ((gg @ ww).abs() + tol))
+    del h, dh
+    torch.cuda.empty_cache()
