@@ -724,10 +724,12 @@ bnr_status bnr_linear_ce_fwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dt
  * all overwritten; each may be NULL.  The logits are formed again, the classes in
  * pieces.  g is rounded to the storage type as the operand of the two products (dbias
  * adds it unrounded; up to 64 bf16 rows keep what the rounding left as well), with the
- * significand of dloss[0] / lse[0] outside it; sums are float32.  With up to 512 classes (and
- * few tiles of logits) a label's entry beyond p = 1/2 is formed from the sum of the others'
- * p, so that rows sure of their label keep their digits.  The same call gives the same
- * bits. */
+ * significand of dloss[0] / lse[0] outside it; sums are float32.
+ * A label's entry beyond p = 1/2 is formed from the sum of the others' p, so that rows sure
+ * of their label keep their digits.  With more than 512 classes it is p - 1 as computed, off
+ * by about 1e-6 absolutely (the roundings of l and lse), for more than 64 bf16 rows, with
+ * smoothing from 1/64 on, and where the classes take several pieces: from about 2^26 float32
+ * or 2^27 bf16 logits on, and past 2^20 classes.  The same call gives the same bits. */
 bnr_status bnr_linear_ce_bwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dtype, const void *h, int32_t h_ld,
                              const void *w, int32_t w_ld, const bnr_ce *ce, const float *dloss, void *dh, int32_t dh_ld,
                              void *dw, int32_t dw_ld, bnr_dtype dw_dtype, float *dbias, void *ws, size_t ws_bytes,

@@ -372,7 +372,7 @@ struct CeGemm {
     int gt_rows;
     float *colsum;                 // [row tile][colsum_ld] (NULL: none)
     int64_t colsum_ld;
-    float2 *own;                   // k_ce_small: [column tile][m] label's probability and the others' sum (NULL: not kept)
+    float *others, *prob;          // CE_GRAD: [column part][m] sums of the others' probabilities (NULL: not kept), [m] the label's
     void *out;                     // CE_DH, CE_DW: results, or parts of them
     int64_t out_ld, part_stride;
     int out_f32, add;

@@ -46,6 +46,7 @@ __device__ __forceinline__ float ce_g(float e, const CeRow &r, const CeGemm &p, 
 
 // ---- rows that count -------------------------------------------------------
 constexpr int kListRows = 4;               // rows a workgroup of k_ce_list takes, one a wave
+constexpr int kOwnRows = 128;              // rows a workgroup of k_ce_own takes at most
 constexpr int kCountRows = 4096;           // rows a workgroup of k_ce_count takes
 
 __device__ __forceinline__ int ce_counted(const int32_t *labels, int64_t from, int64_t to, int ignore, int tid)
@@ -269,6 +270,19 @@ __device__ __forceinline__ void ce_wave_sync()
 typedef __attribute__((address_space(3))) unsigned char lds_char;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
+// The sum over eight neighbouring lanes, in every one of them: neighbours, pairs, and the
+// mirrored half row (no LDS).
+template <int CTRL> __device__ __forceinline__ float ce_lane(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float ce_sum8(float v)
+{
+    v += ce_lane<0xB1>(v);                           // quad_perm 1 0 3 2
+    v += ce_lane<0x4E>(v);                           // quad_perm 2 3 0 1
+    return v + ce_lane<0x141>(v);                    // row_half_mirror
+}
+
 // neighbouring results
 __device__ __forceinline__ void ce_store4(float *p, const float *v) { *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]}; }
 __device__ __forceinline__ void ce_store4(bf16_t *p, const float *v)
@@ -395,12 +409,12 @@ __device__ __forceinline__ void ce_product(f32x4 (&acc)[BJ / WJ / 16][BI / WI / 
 #define CE_LDS(BI, BJ)                                                                  \
     __shared__ __align__(16) unsigned char lds0[(BI + BJ) * 128], lds1[(BI + BJ) * 128]; \
     __shared__ CeRow rows[BI];                                                          \
-    __shared__ float bias[BJ]
+    __shared__ float bias[BJ], others[WJ * BI]
 
 // One tile of a product, by workgroup `block` of its grid.
 template <typename T, int BI, int BJ, int WI, int WJ, int MODE>
 __device__ __forceinline__ void ce_tile_of(const CeGemm &p, int block, unsigned char *lds0, unsigned char *lds1, CeRow *rows,
-                                           float *bias)
+                                           float *bias, float *others)
 {
 #ifdef __HIP_DEVICE_COMPILE__              // (the host pass cannot instantiate the matrix instructions twice)
     constexpr bool ICOLS = MODE == CE_DW, JCOLS = MODE == CE_DW || MODE == CE_DH;
@@ -556,7 +570,28 @@ __device__ __forceinline__ void ce_tile_of(const CeGemm &p, int block, unsigned 
                         for (int e = 0; e < 8; e++) v[e] += bias[j + e - j0];
                     }
                     #pragma unroll
-                    for (int e = 0; e < 8; e++) v[e] = __builtin_fmaf(ce_exp(v[e] - r.lse), grow, -flat);
+                    for (int e = 0; e < 8; e++) v[e] = ce_exp(v[e] - r.lse);
+                    if (p.others) {                  // (eight lanes share a row's 64 columns)
+                        if (j0 + BJ > nj) {
+                            #pragma unroll
+                            for (int e = 0; e < 8; e++) v[e] = j + e < nj ? v[e] : 0.f;
+                        }
+                        float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+                        if ((uint32_t)at < 8) {
+                            float prob = 0.f;
+                            sum = 0.f;
+                            #pragma unroll
+                            for (int e = 0; e < 8; e++) {
+                                sum += e == at ? 0.f : v[e];
+                                prob = e == at ? v[e] : prob;
+                            }
+                            if (j + at < nj) p.prob[i] = prob;
+                        }
+                        sum = ce_sum8(sum);
+                        if (lcol == 0) others[wj * BI + i - i0] = sum;
+                    }
+                    #pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] = __builtin_fmaf(v[e], grow, -flat);
                     if ((uint32_t)at < 8) {
                         const float hit = r.scale * p.hit;
                         #pragma unroll
@@ -599,6 +634,7 @@ __device__ __forceinline__ void ce_tile_of(const CeGemm &p, int block, unsigned 
             ce_wave_sync();
         }
         if constexpr (MODE == CE_GRAD) {
+            static_assert(MODE != CE_GRAD || TJ == 64, "a row's others of a wave");
             if (p.colsum) {                          // the wave's rows; then the tile's, of all its waves
                 #pragma unroll
                 for (int e = 0; e < 8; e++) {
@@ -608,6 +644,17 @@ __device__ __forceinline__ void ce_tile_of(const CeGemm &p, int block, unsigned 
             }
         }
         }
+        if constexpr (MODE == CE_GRAD) {
+            if (p.others) {                          // the tile's columns
+                __syncthreads();
+                for (int i = tid; i < min(BI, ni - i0); i += NT) {
+                    float sum = others[i];
+                    #pragma unroll
+                    for (int w = 1; w < WJ; w++) sum += others[w * BI + i];
+                    p.others[(int64_t)pl.tj * p.m + i0 + i] = sum;
+                }
+            }
+        }
     }
 #endif
 }
@@ -616,7 +663,7 @@ template <typename T, int BI, int BJ, int WI, int WJ, int MODE>
 __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_gemm(CeGemm p)
 {
     CE_LDS(BI, BJ);
-    ce_tile_of<T, BI, BJ, WI, WJ, MODE>(p, (int)wide_block(), lds0, lds1, rows, bias);
+    ce_tile_of<T, BI, BJ, WI, WJ, MODE>(p, (int)wide_block(), lds0, lds1, rows, bias, others);
 }
 
 // dh and dw of a piece, which do not need each other, in one launch: dh's longer tiles
@@ -627,8 +674,8 @@ __global__ __launch_bounds__(WI * WJ * 64, 2) void k_ce_pair(CeGemm dh, CeGemm d
 {
     CE_LDS(BI, BJ);
     const int block = (int)wide_block();
-    if (block < first) ce_tile_of<T, BI, BJ, WI, WJ, CE_DH>(dh, block, lds0, lds1, rows, bias);
-    else ce_tile_of<T, BI, BJ, WI, WJ, CE_DW>(dw, block - first, lds0, lds1, rows, bias);
+    if (block < first) ce_tile_of<T, BI, BJ, WI, WJ, CE_DH>(dh, block, lds0, lds1, rows, bias, others);
+    else ce_tile_of<T, BI, BJ, WI, WJ, CE_DW>(dw, block - first, lds0, lds1, rows, bias, others);
 }
 
 // ---- few rows, or few tiles ---------------------------------------------------
@@ -701,7 +748,7 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
             *reinterpret_cast<f32x4 *>(&part[wave][(16 * a + q) * kPitch + 16 * b + 4 * g]) = total[b][a];
     __syncthreads();
     float mx = -INFINITY, sum = 0.f, all = 0.f, v[kTurns][4];
-    float2 own = float2{0.f, 0.f};                   // CE_GRAD: the label's probability, the other classes' sum
+    float others = 0.f;                              // CE_GRAD: the sum of the classes' probabilities without the label's
     #pragma unroll
     for (int u = 0; u < kTurns; u++) {
         const int c = (u * kLanes + li) * 4;
@@ -724,7 +771,8 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
             } else {
                 const float e = ce_exp(l - info.lse);
                 v[u][r] = j < nj && i < ni ? ce_g(e, info, p, j + p.first == info.label) : 0.f;
-                if (j < nj) (j + p.first == info.label ? own.x : own.y) += e;
+                if (j < nj && j + p.first != info.label) others += e;
+                else if (j < nj && i < ni && p.others) p.prob[i] = e;
             }
         }
         if constexpr (MODE == CE_GRAD) {
@@ -758,13 +806,10 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
             p.stats[o] = float2{mx, sum};
             if (p.sums) p.sums[o] = all;
         }
-    } else if (p.own) {
+    } else if (p.others) {
         #pragma unroll
-        for (int o = 1; o < kLanes; o *= 2) {
-            own.x += __shfl_xor(own.x, o, 64);
-            own.y += __shfl_xor(own.y, o, 64);
-        }
-        if (li == 0 && i < ni) p.own[(int64_t)pl.tj * p.m + i] = own;
+        for (int o = 1; o < kLanes; o *= 2) others += __shfl_xor(others, o, 64);
+        if (li == 0 && i < ni) p.others[(int64_t)pl.tj * p.m + i] = others;
     }
     if (MODE == CE_GRAD && (p.colsum || p.gt)) {
         __syncthreads();
@@ -795,37 +840,54 @@ __global__ __launch_bounds__(kThreads) void k_ce_small(CeGemm p)
     }
 }
 
-// Of few classes, the labels' own entries of g once more.  Where a row is sure of its
-// label, p - 1 is what the roundings of l and lse left of it: 1e-6 of an lse of 8, a
-// thousandth of a g of 1e-3.  The others' probabilities are each right relative to
-// themselves and their sum is 1 - p, so beyond p = 1/2 the entry is formed from that sum
-// (while the two agree: an lse that is not these logits' stays as it was given).  A row a
-// thread, a row tile of k_ce_small a workgroup (one wave), so dbias's partial sums are
-// mended by the first row of each label, in the rows' order.
+// The labels' own entries of g once more.  Where a row is sure of its label, p - 1 is what
+// the roundings of l and lse left of it: 1e-6 of an lse of 8, a thousandth of a g of 1e-3.
+// The others' probabilities are each right relative to themselves and their sum is 1 - p, so
+// beyond p = 1/2 the entry is formed from that sum (while the two agree: an lse that is not
+// these logits' stays as it was given).  A workgroup takes the rows of one of dbias's partial
+// sums, each in NT / tile slices of the column parts; the partial sums are mended by the first
+// row of each label, in the rows' order.
 // 64 x 2192 of 6 classes in float32: dh off by 3.3e-7 of its norm, without it by 1.8e-6, and
-// a row of 1488 of 3 classes with p = 0.9995 by 1.5e-6 and 2.2e-3.  3 us a call (18.6 us ->
-// 21.5, 61 x 72 of 7 classes).
-template <typename T>
-__global__ __launch_bounds__(64) void k_ce_own(CeGemm p, int tile, int tiles)
+// a row of 1488 of 3 classes with p = 0.9995 by 1.5e-6 and 2.2e-3.
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void k_ce_own(CeGemm p, int tile, int parts)
 {
-    const int ni = *p.count, r = threadIdx.x, i = blockIdx.x * tile + r;
-    if ((int)blockIdx.x * tile >= ni) return;
+    __shared__ double sums[NT];
+    __shared__ int labels[kOwnRows], before[NT];
+    __shared__ float changes[kOwnRows];
+    const int tid = threadIdx.x, first = blockIdx.x * tile, r = tid % tile, slice = tid / tile, slices = NT / tile, i = first + r;
+    const int64_t at = min((int64_t)i, p.m - 1);     // (the loads do not wait for the count: what lies behind it is left unused)
+    const int ni = *p.count;
+    double others = 0.0;
+    for (int t = slice; t < parts; t += 8 * slices) {
+        float part[8];
+        #pragma unroll
+        for (int u = 0; u < 8; u++) part[u] = p.others[min(t + u * slices, parts - 1) * p.m + at];
+        #pragma unroll
+        for (int u = 0; u < 8; u++) others += t + u * slices < parts ? part[u] : 0.f;
+    }
+    CeRow info = CeRow{0, -1, 0.f, 0.f};
+    float prob = 0.f, old = 0.f;
+    if (tid < tile) {
+        info = p.rows[at];
+        prob = p.prob[at];
+    }
+    if (first >= ni) return;
+    // (a label outside the classes has left no probability)
+    const bool known = tid < tile && i < ni && (uint32_t)info.label < (uint32_t)p.classes;
+    float *sum_to = p.colsum + (int64_t)blockIdx.x * p.colsum_ld + (known ? info.label : 0);
+    if (known && p.colsum) old = *sum_to;
+    sums[tid] = others;
+    __syncthreads();
     int label = -1;
-    float change = 0.f;
-    if (r < tile && i < ni) {
-        const CeRow info = p.rows[i];
-        double prob = 0.0, others = 0.0;
-        #pragma unroll 8
-        for (int t = 0; t < tiles; t++) {
-            const float2 o = p.own[(int64_t)t * p.m + i];
-            prob += o.x;
-            others += o.y;
-        }
-        if ((uint32_t)info.label < (uint32_t)p.classes && prob > 0.5 && fabs(prob + others - 1.0) < 1e-3) {
+    if (tid < tile) {
+        float change = 0.f;
+        for (int s = 1; s < slices; s++) others += sums[s * tile + r];
+        if (known && prob > 0.5f && fabs(prob + others - 1.0) < 1e-3) {
             label = info.label;
             const double grow = 1.0 + 2.0 * p.z * info.lse;
             const float v = (float)(info.scale * (grow * (1.0 - others) - p.hit - p.flat));
-            change = v - ce_g((float)prob, info, p, true);
+            change = v - ce_g(prob, info, p, true);
             T *to = (T *)p.g + (int64_t)i * p.g_ld + label;
             if constexpr (sizeof(T) == 2) {
                 *to = f2bf(v);
@@ -840,17 +902,28 @@ __global__ __launch_bounds__(64) void k_ce_own(CeGemm p, int tile, int tiles)
                 *to = v;
             }
         }
+        labels[r] = label;
+        changes[r] = change;
     }
-    if (!p.colsum) return;
+    if (!p.colsum || !__syncthreads_or(label >= 0)) return;
+    // the rows of each row's label, in as many slices
+    const int mine = labels[r], per = (tile + slices - 1) / slices;
     double sum = 0.0;
-    bool first = label >= 0;
-    for (int k = 0; k < tile; k++) {
-        const float c = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, change), k));
-        if (__builtin_amdgcn_readlane(label, k) != label) continue;
-        sum += c;
-        first = first && k >= r;
+    bool earlier = false;
+    for (int k = slice * per; k < min(slice * per + per, tile); k++) {
+        const bool same = labels[k] == mine;
+        sum += same ? changes[k] : 0.f;
+        earlier = earlier || (same && k < r);
     }
-    if (first) p.colsum[(int64_t)blockIdx.x * p.colsum_ld + label] += (float)sum;
+    sums[tid] = sum;
+    before[tid] = earlier;
+    __syncthreads();
+    if (label < 0) return;
+    for (int s = 1; s < slices; s++) {
+        sum += sums[s * tile + r];
+        earlier = earlier || before[s * tile + r];
+    }
+    if (!earlier) *sum_to = old + (float)sum;
 }
 
 // The weights' gradient of few bf16 rows, a stream of results: a wave keeps the features
@@ -1105,9 +1178,16 @@ inline int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 // (their products cost next to nothing beside reading the weights): with few rows the
 // rounding of one label's g is no longer one of many.
 constexpr int kFewRows = 64;
-// Up to kFewClasses classes the labels' entries are formed a second time (k_ce_own: one
-// launch more).  With more, a row that is sure has this many small probabilities to be sure
-// of, and its g is seldom small enough to show the roundings.
+// The labels' entries of g are formed a second time (k_ce_own) where one piece holds all
+// classes (kFewClasses always fit), so that the others' sum is whole before the products.  Not
+// so beyond kFewClasses
+//   with smoothing from kOwnSmoothing on: the entry is at least s then, which hides the
+//     roundings (128 x 1024 x 1000 float32, s = 0.1: 32.7 us, with the launch 39.3), and
+//   in bf16 past kFewRows: g is rounded to 8 bits, beside which the roundings of l and lse show
+//     from 1 - p = 5e-4 down (1001 x 776 x 40961: 233 us, with sums and launch 247).
+// It costs 128 x 1024 x 513 float32 3 to 5 us of 28, 1000 x 512 x 4000 3 of 129, 16 x 2048 x
+// 65536 bf16 5 of 198, 20001 x 256 x 3 float32 6 of 90.
+constexpr float kOwnSmoothing = 1.f / 64;
 constexpr int kFewClasses = 512;
 struct CeTile { int bi, bj; bool small; };
 inline CeTile ce_tile(int dtype, int64_t ni, int64_t nj)
@@ -1179,13 +1259,18 @@ hipError_t gemm(const CeCall &a, const CeGemm &p, const CeTile &t, int64_t ni, i
     return hipGetLastError();
 }
 
-hipError_t launch_own(const CeCall &a, const CeGemm &p, const CeTile &t, hipStream_t s)
+// tile: rows of a partial row of dbias; parts: column parts of the others' sums
+hipError_t launch_own(const CeCall &a, const CeGemm &p, int tile, int parts, hipStream_t s)
 {
-    const int tiles = (int)cdiv(a.classes, t.bj);
-    TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 8.0 * a.m * tiles, 0.0);
-    const dim3 g((unsigned)cdiv(a.m, t.bi));
-    if (a.dtype == DT_BF16) hipLaunchKernelGGL(k_ce_own<bf16_t>, g, dim3(64), 0, s, p, t.bi, tiles);
-    else hipLaunchKernelGGL(k_ce_own<float>, g, dim3(64), 0, s, p, t.bi, tiles);
+    TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 4.0 * a.m * (parts + 8), 0.0);
+    const dim3 g((unsigned)cdiv(a.m, tile));
+    const auto at = [&](auto nt) {
+        constexpr int NT = decltype(nt)::value;
+        if (a.dtype == DT_BF16) hipLaunchKernelGGL((k_ce_own<bf16_t, NT>), g, dim3(NT), 0, s, p, tile, parts);
+        else hipLaunchKernelGGL((k_ce_own<float, NT>), g, dim3(NT), 0, s, p, tile, parts);
+    };
+    if (parts >= 64) at(std::integral_constant<int, 1024>{});
+    else at(std::integral_constant<int, kThreads>{});
     return hipGetLastError();
 }
 
@@ -1253,7 +1338,7 @@ struct CeFwdPlan {
     }
 };
 
-// The widest piece of the classes whose g takes at most kPieceBytes (8192 x 4096 x 131072:
+// The widest piece of the classes whose g takes at most kPieceBytes, or kFewClasses of them (8192 x 4096 x 131072:
 // 18.8 ms with 256 MiB and with 512, 18.5 with 1 GiB).
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 constexpr int64_t kPieceWidth = kCeMaxLd;
@@ -1264,13 +1349,13 @@ struct CeBwdPlan {
     CeTile grad_tile, dh_tile, dw_tile;
     int grad_rows, dh_parts, dw_parts;     // grad_rows: of a partial row of dbias
     int few;                               // groups of 16 rows of g's second form (0: many rows)
-    int64_t g, gt, dh, dw, colsum, own, end;
-    bool again() const { return own < end; }
+    int own_parts;                         // column parts of the others' sums (0: the labels' entries stay as they are)
+    int64_t g, gt, dh, dw, colsum, others, prob, end;
     explicit CeBwdPlan(const CeCall &a) : head(a)
     {
         const int64_t es = a.dtype == DT_BF16 ? 2 : 4, bk = 128 / es;
         int64_t most = kPieceBytes / (a.m * es) / 256 * 256;
-        most = most < 256 ? 256 : (most > kPieceWidth ? kPieceWidth : most);
+        most = most < kFewClasses ? kFewClasses : (most > kPieceWidth ? kPieceWidth : most);
         pieces = cdiv(a.classes, most);
         width = cdiv(cdiv(a.classes, pieces), 256) * 256;
         pieces = cdiv(a.classes, width);
@@ -1292,8 +1377,13 @@ struct CeBwdPlan {
         dh = up256(gt + few * width * 64);
         dw = up256(dh + (a.dh && gather() ? dh_parts * rows * a.c * 4 : 0));
         colsum = up256(dw + (a.dw && dw_parts > 1 ? dw_parts * wide * a.c * 4 : 0));
-        own = up256(colsum + (a.dbias ? cdiv(a.m, grad_tile.bi) * (grad_tile.bi / grad_rows) * a.classes * 4 : 0));
-        end = up256(own + (grad_tile.small && a.classes <= kFewClasses ? cdiv(a.classes, grad_tile.bj) * a.m * 8 : 0));
+        // (its place does not depend on smoothing, which the size query does not know)
+        const bool shows = a.classes <= kFewClasses || a.dtype == DT_F32 || few;
+        const int64_t parts = pieces == 1 && shows ? cdiv(a.classes, grad_tile.bj) : 0;
+        own_parts = a.smoothing >= kOwnSmoothing && a.classes > kFewClasses ? 0 : (int)parts;
+        others = up256(colsum + (a.dbias ? cdiv(a.m, grad_tile.bi) * (grad_tile.bi / grad_rows) * a.classes * 4 : 0));
+        prob = up256(others + parts * a.m * 4);
+        end = up256(prob + (parts ? a.m * 4 : 0));
     }
 };
 
@@ -1410,9 +1500,10 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
         q.j = weights; q.j_ld = a.w_ld * es;
         q.bias = a.bias ? a.bias + first : nullptr;
         q.colsum = a.dbias ? (float *)(ws + w.colsum) + first : nullptr;
-        q.own = w.again() ? (float2 *)(ws + w.own) : nullptr;
+        q.others = w.own_parts ? (float *)(ws + w.others) : nullptr;
+        q.prob = (float *)(ws + w.prob);
         CE_TRY(gemm<CE_GRAD>(a, q, w.grad_tile, a.m, wide, a.c, s));
-        if (w.again()) CE_TRY(launch_own(a, q, w.grad_tile, s));
+        if (w.own_parts) CE_TRY(launch_own(a, q, w.grad_rows, w.own_parts, s));
         CeGemm dh = p, dw = p;
         dh.i = dw.i = p.g; dh.i_ld = dw.i_ld = w.width * es;
         dh.j = weights; dh.j_ld = a.w_ld * es;

@@ -476,9 +476,9 @@ def test_few_rows_of_more_threads_than_a_dimension_of_a_grid_holds():
 
 
 def test_gradient_of_rows_of_more_threads_than_a_dimension_of_a_grid_holds():
-    """2^24 rows of 1024 channels whose dh adds up over two pieces: 2^32 threads add the parts (180 GB)."""
-    m, c, v = 1 << 24, 1024, 300
-    _room(170 << 30)
+    """2^24 rows of 1024 channels whose dh adds up over two pieces: 2^32 threads add the parts (190 GB)."""
+    m, c, v = 1 << 24, 1024, 600
+    _room(180 << 30)
     g = torch.Generator(device="cuda").manual_seed(8)
     h, dh = (torch.empty(m, c, dtype=torch.bfloat16, device="cuda") for _ in range(2))
     step = 1 << 20
@@ -487,7 +487,7 @@ def test_gradient_of_rows_of_more_threads_than_a_dimension_of_a_grid_holds():
     w = (torch.randn(v, c, generator=g, device="cuda") * (1.0 / 32)).bfloat16()
     labels = torch.randint(0, v, (m,), generator=g, device="cuda", dtype=torch.int32)
     labels[torch.rand(m, generator=g, device="cuda") < 0.1] = IGNORE
-    labels[m - 1] = 299
+    labels[m - 1] = v - 1
     lse = torch.full((1 + m,), float(np.log(v) + 0.5), device="cuda")        # any log sum: the formula's g of it
     n = int((labels != IGNORE).sum())
     lse[0] = n
@@ -507,3 +507,22 @@ def test_gradient_of_rows_of_more_threads_than_a_dimension_of_a_grid_holds():
         _close("dh from row %d" % s, dh[s:s + 400], gg @ ww, tol + half * ((gg @ ww).abs() + tol))
     del h, dh
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype,m,v,lean", [
+    (torch.float32, 20001, 3, 16.0), (torch.float32, 4100, 512, 16.0), (torch.float32, 60, 5000, 18.0),
+    (torch.float32, 1000, 1000, 18.0), (torch.float32, 2500, 1500, 18.0), (torch.float32, 70, 20000, 18.0),
+    (torch.bfloat16, 20001, 3, 16.0), (torch.bfloat16, 4100, 500, 16.0), (torch.bfloat16, 25000, 500, 16.0),
+    (torch.float32, 140001, 512, 16.0), (torch.bfloat16, 10, 3000, 18.0), (torch.bfloat16, 30, 3000, 18.0), (torch.bfloat16, 64, 6000, 18.0)])
+def test_many_rows_or_classes_sure_of_their_label(dtype, m, v, lean):
+    """Rows sure of their label in tiles of every size and of any number of classes of one piece: a logit of about
+    `lean` against others of about 0 leaves a 1 - p of v e^-lean."""
+    k = Case(m, 256, v, dtype, bias=True, std=1.0, ignored=0.2)
+    w = k.w.double()[k.labels.clamp(0, v - 1).long()]
+    k.h.copy_((k.h.double() + lean * w / (w * w).sum(1, keepdim=True)).to(dtype))
+    k.forward()
+    k.check_forward()
+    p = torch.exp(k.l - k.lse[:, None]).gather(1, k.at)[k.counts]
+    assert bool((p > 0.6).all())
+    k.backward()
+    k.check_backward(sure=True)
