@@ -1381,7 +1381,7 @@ struct CeBwdPlan {
         const bool shows = a.classes <= kFewClasses || a.dtype == DT_F32 || few;
         const int64_t parts = pieces == 1 && shows ? cdiv(a.classes, grad_tile.bj) : 0;
         own_parts = a.smoothing >= kOwnSmoothing && a.classes > kFewClasses ? 0 : (int)parts;
-        others = up256(colsum + (a.dbias ? cdiv(a.m, grad_tile.bi) * (grad_tile.bi / grad_rows) * a.classes * 4 : 0));
+        others = up256(colsum + (a.dbias ? cdiv(a.m, grad_tile.bi) * (grad_tile.bi / grad_rows) * wide * 4 : 0));   // (of a piece)
         prob = up256(others + parts * a.m * 4);
         end = up256(prob + (parts ? a.m * 4 : 0));
     }
@@ -1484,11 +1484,16 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
     p.c = a.c; p.m = a.m;
     p.z = a.z; p.hit = 1.f - a.smoothing; p.flat = a.smoothing / (float)a.classes;
     p.g = ws + w.g; p.g_ld = w.width;
-    p.colsum_ld = a.classes;
+    p.colsum_ld = w.width < a.classes ? w.width : a.classes;
     const char *copy = ws + w.head.copy;
     const bool gather_dh = w.gather();
     const int64_t dh_rows = w.few ? 2 * a.m : a.m;
     if (w.few) { p.gt = ws + w.gt; p.gt_rows = w.few; }
+    // dbias: of each piece, by the launch that adds up dh where that is behind all classes
+    const bool bias_behind = w.pieces == 1 && a.dh && gather_dh;
+    CeBias b{};
+    b.count = p.count; b.tile = w.grad_rows; b.factor = p.factor;
+    b.colsum = (const float *)(ws + w.colsum); b.ld = p.colsum_ld; b.out = a.dbias;
     for (int64_t n = 0; n < w.pieces; n++) {
         const int64_t first = n * w.width;
         const int64_t wide = a.classes - first < w.width ? a.classes - first : w.width;
@@ -1499,11 +1504,17 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
         q.i = copy; q.i_ld = (int64_t)a.c * es;
         q.j = weights; q.j_ld = a.w_ld * es;
         q.bias = a.bias ? a.bias + first : nullptr;
-        q.colsum = a.dbias ? (float *)(ws + w.colsum) + first : nullptr;
+        q.colsum = a.dbias ? (float *)(ws + w.colsum) : nullptr;
         q.others = w.own_parts ? (float *)(ws + w.others) : nullptr;
         q.prob = (float *)(ws + w.prob);
         CE_TRY(gemm<CE_GRAD>(a, q, w.grad_tile, a.m, wide, a.c, s));
         if (w.own_parts) CE_TRY(launch_own(a, q, w.grad_rows, w.own_parts, s));
+        b.classes = (int)wide;
+        if (a.dbias && !bias_behind) {
+            b.out = a.dbias + first;
+            TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 4.0 * wide * (cdiv(a.m, w.grad_rows) + 1), 0.0);
+            hipLaunchKernelGGL(k_ce_bias, dim3((unsigned)cdiv(wide, kThreads)), dim3(kThreads), 0, s, b);
+        }
         CeGemm dh = p, dw = p;
         dh.i = dw.i = p.g; dh.i_ld = dw.i_ld = w.width * es;
         dh.j = weights; dh.j_ld = a.w_ld * es;
@@ -1537,18 +1548,12 @@ hipError_t launch_ce_bwd(const CeCall &a, void *ws_, hipStream_t s)
         }
         if (a.dw && w.dw_parts > 1) CE_TRY(sum_parts(t, CeBias{}, a.dw_dtype, wide, s));
     }
-    CeBias b{};
-    b.count = p.count; b.tile = w.grad_rows; b.factor = p.factor; b.classes = a.classes;
-    b.colsum = (const float *)(ws + w.colsum); b.ld = a.classes; b.out = a.dbias;
     if (a.dh && gather_dh) {
         CeSum t{};
         t.part = (const float *)(ws + w.dh); t.part_stride = dh_rows * a.c; t.twice = w.few ? 1 : 0; t.parts = w.dh_parts; t.c = a.c;
         t.rows = p.rows; t.count = p.count; t.factor = p.factor;
         t.out = a.dh; t.out_ld = a.dh_ld;
-        CE_TRY(sum_parts(t, b, a.dtype, a.m, s));
-    } else if (a.dbias) {
-        TraceScope tr(KC_SMALL, KID_LINEAR_CE, s, 4.0 * a.classes * (cdiv(a.m, w.grad_rows) + 1), 0.0);
-        hipLaunchKernelGGL(k_ce_bias, dim3((unsigned)cdiv(a.classes, kThreads)), dim3(kThreads), 0, s, b);
+        CE_TRY(sum_parts(t, bias_behind ? b : CeBias{}, a.dtype, a.m, s));
     }
     return hipGetLastError();
 }

@@ -118,3 +118,12 @@ def test_binding_refuses(B):
     for bad in (dict(dh=torch.zeros(3, 8)), dict(dw=torch.zeros(5, 9)), dict(dbias=torch.zeros(6)), dict(dloss=torch.zeros(4))):
         with pytest.raises(ValueError):
             B.bnr_linear_ce_bwd(h, w, ce, **bad)
+
+
+@pytest.mark.parametrize("m,c,v,t", [(1 << 16, 1024, 131072, BF16), (1 << 18, 64, 131072, F32), (1 << 20, 64, 131072, BF16)])
+def test_backward_keeps_nothing_of_all_classes(B, m, c, v, t):
+    """The rows' copy, float32 sums of dh, a piece's g (256 MiB, or 512 classes) and 1/16 as much for dbias, whatever the
+    number of classes."""
+    es = 2 if t == BF16 else 4
+    most = m * c * (es + 4) + max(256 << 20, m * 512 * es) * 17 // 16 + m * 64 + (64 << 20)
+    assert B._lib_fns["bnr_linear_ce_workspace_size"](m, c, v, t, 1) < most
