@@ -694,7 +694,8 @@ bnr_status bnr_dropout_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy
  * (BNR_ERR_UNSUPPORTED).  A row whose label is `ignore` (padding) does not count: its loss, lse
  * and dh are zeros, and its features reach nothing, whatever they hold.  Any other
  * label outside [0, classes) gives its row (and the mean) a NaN loss and NaN
- * gradients.  A bias of -infinity takes its class out.  An infinity or NaN in a row
+ * gradients.  A bias of -infinity takes its class out (smoothing > 0 still gives it its
+ * share: the row's loss is infinite, the class's g is -r smoothing / classes).  An infinity or NaN in a row
  * of h makes its own loss NaN, and every row of dw. */
 typedef struct {
     const float *bias;     /* [classes] or NULL (0)                                */

@@ -256,3 +256,21 @@ def test_float32_weight_gradient_in_two_levels(m, c, v):
     dl = (c + 8) * U * (h[:1].double().abs() @ w.double().abs().t())
     rel = torch.expm1(dl + dl.amax() + 100 * U + U * torch.logsumexp(l, 1).abs() + 24 * U)
     _close("dw", dw[1:], ref, ref.abs() * (rel.t()[1:] + (64 + 64 + 64 + 4) * U))
+
+
+@pytest.mark.parametrize("dtype,m,c,v", TILES + [(torch.float32, 60, 64, 700), (torch.bfloat16, 60, 64, 700)])
+def test_classes_taken_out_keep_their_share_of_smoothing(dtype, m, c, v):
+    k = Case(m, c, v, dtype, bias=True, smoothing=0.1)
+    out = torch.zeros(v, dtype=torch.bool, device="cuda")
+    out[100:300] = True
+    keep = torch.nonzero(~out)[:, 0]
+    k.labels.copy_(keep[k.labels.long() % len(keep)].int())
+    k.bias[out] = float("-inf")
+    k.forward()
+    k.reference()
+    assert bool((k.loss == float("inf")).all())
+    _close("lse", k.ce.lse[1:], k.lse, k.t + U * k.lse.abs())
+    k.backward()
+    k.check_backward()
+    share = -k.s / v                                      # the rows' r add up to 1
+    assert bool(((k.dbias[out].double() - share).abs() <= (m + 70) * U * -share).all())
