@@ -2081,7 +2081,7 @@ bnr_status bnr_dropout_bwd(int64_t m, int32_t c, bnr_dtype dtype, const void *dy
 }  // extern "C"
 
 // ----------------------------------- linear layer and softmax cross entropy ----
-static bnr_status check_ce_rows(const void *p, int64_t rows, int32_t ld, int32_t c, bnr_dtype dtype, const char *name)
+static bnr_status check_ce_rows(const void *p, int32_t ld, int32_t c, bnr_dtype dtype, const char *name)
 {
     TRY(check_ptr(p, name));
     TRY(check_channels(c, ld, dtype, name));
@@ -2105,8 +2105,8 @@ static bnr_status check_ce(int64_t m, int32_t c, int32_t classes, bnr_dtype dtyp
                            const void *w, int32_t w_ld, const bnr_ce *ce)
 {
     TRY(check_ce_sizes(m, c, classes, dtype));
-    TRY(check_ce_rows(h, m, h_ld, c, dtype, "h"));
-    TRY(check_ce_rows(w, classes, w_ld, c, dtype, "w"));
+    TRY(check_ce_rows(h, h_ld, c, dtype, "h"));
+    TRY(check_ce_rows(w, w_ld, c, dtype, "w"));
     if (!ce) return fail(BNR_ERR_NULL, "ce is NULL");
     if (!ce->labels) return fail(BNR_ERR_NULL, "ce.labels is NULL");
     if (reinterpret_cast<uintptr_t>(ce->labels) % 4) return fail(BNR_ERR_ALIGN, "ce.labels is not 4-byte aligned");
@@ -2179,11 +2179,11 @@ bnr_status bnr_linear_ce_bwd(int64_t m, int32_t c, int32_t classes, bnr_dtype dt
     struct Out { Range r; const char *name; } out[3];
     int n = 0;
     if (dh) {
-        TRY(check_ce_rows(dh, m, dh_ld, c, dtype, "dh"));
+        TRY(check_ce_rows(dh, dh_ld, c, dtype, "dh"));
         out[n++] = Out{view_range(dh, m, c, dh_ld, es), "dh"};
     }
     if (dw) {
-        TRY(check_ce_rows(dw, classes, dw_ld, c, dw_dtype, "dw"));
+        TRY(check_ce_rows(dw, dw_ld, c, dw_dtype, "dw"));
         out[n++] = Out{view_range(dw, classes, c, dw_ld, esize(dw_dtype)), "dw"};
     }
     if (dbias) {

@@ -16,9 +16,10 @@
 // A thread takes eight channels of a row: one call of the generator.  Any stride and
 // alignment: the eight elements move as one 16-byte access (two in float32), which
 // gfx950 allows at element alignment, and one by one at a row's ragged end.  Bound by
-// HBM: 8192 bf16 rows of 4096 with an addition 36.9 us = 5.5 TB/s (two, four and eight
-// blocks a thread, whose loads all come first: 39.0, 42.3 and 46.0 us), rows of 4095, none
-// of them aligned, 54 us.
+// HBM: 8192 bf16 rows of 4096 with an addition 36.4 us = 5.5 TB/s on buffers that take turns
+// (two, four and eight blocks a thread, whose loads all come first: 2, 5 and 9 us more), rows
+// of 4095, none of them aligned, 47.7 us: an access of a wave ends inside a line, which the
+// next one moves again.
 #include "common.hpp"
 #include "kernels.hpp"
 #include "trace.hpp"

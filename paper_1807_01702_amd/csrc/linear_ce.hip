@@ -34,8 +34,9 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
 
-// exp(x) by the base-2 instruction: off by about |x| 2^-24 of itself, next to the
-// c 2^-24 sum |h w| that the logits are off by.
+// exp(x) by the base-2 instruction: its product's one rounding puts it off by about |x| 2^-24
+// of itself, next to the c 2^-24 sum |h w| that the logits are off by (gradients of 128 x 1024
+// x 1000 in float32: 4.9e-7 of their norm off float64, elementary float32 operations 3.6e-7).
 __device__ __forceinline__ float ce_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // A row's entry of g from its probability e
@@ -931,6 +932,10 @@ __global__ __launch_bounds__(NT) void k_ce_own(CeGemm p, int tile, int parts)
 // 16 rows of a class together, rounded, and then what the rounding left: the same
 // instruction adds both, so dw has no error of g's rounding.  Block b's row 4 g + r stands
 // for column 32 (b / 2) + 8 g + 4 (b % 2) + r, so that a lane stores eight neighbours.
+// Bound by its stores: 32000 classes of 2048 in 29.6 us = 4.4 TB/s with up to 16 rows, 38.6 up to
+// 32 and 57.4 up to 64, where g's share of the loads doubles and doubles again.  (With more than
+// 16 rows the scalars that the compiler spills are the conditions of the features' loads, before
+// the loop; none is read in it.)
 template <typename W, int KB>
 __global__ __launch_bounds__(kThreads) void k_ce_outer(CeGemm p, int chunk)
 {
@@ -1000,7 +1005,10 @@ __global__ __launch_bounds__(kThreads) void k_ce_outer(CeGemm p, int chunk)
 
 // ---- rows' losses ------------------------------------------------------------
 constexpr int kLossRows = 16;              // rows a workgroup takes, 16 threads each
-// or 8 threads each: one workgroup, no launch for the mean (128 x 1024 x 1000 float32 18.7 us -> 16.3)
+// or 8 threads each: one workgroup of 1024, no launch for the mean.  Two launches are 1 to 3 us longer
+// up to 63 tiles of classes (128 x 1024 x 1000 float32 16.5 us and 14.6, 40 x 1024 x 2500 22.3 and
+// 21.8; 17 rows of 4000 classes alone 16.0 and 17.0), as long at 125 (128 x 1024 x 16000 bf16 34.9
+// and 36.0, 40 x 1024 x 8000 16.5 and 15.8) and shorter from there on.
 constexpr int kLossWide = 128;
 
 __device__ __forceinline__ void ce_join(float &mx, double &sum, float mx2, double sum2)
@@ -1176,7 +1184,10 @@ inline int64_t up256(int64_t b) { return (b + 255) / 256 * 256; }
 // few rows or of too few tiles for that run as k_ce_small, 16 x i by 16 x j.
 // Up to kFewRows bf16 rows g is kept in two parts, rounded and the rest, in separate rows
 // (their products cost next to nothing beside reading the weights): with few rows the
-// rounding of one label's g is no longer one of many.
+// rounding of one label's g is no longer one of many.  Beyond, g is one bf16 operand, where
+// float32 products would take ten times as long: dw of 1001 x 776 x 40961 is off float64 by 1.85e-3
+// of its norm, where the result's own rounding alone is 1.65e-3, and by up to sqrt(2) times that
+// where one label's entry makes up a row of dw.
 constexpr int kFewRows = 64;
 // The labels' entries of g are formed a second time (k_ce_own) where one piece holds all
 // classes (kFewClasses always fit), so that the others' sum is whole before the products.  Not
@@ -1367,8 +1378,12 @@ struct CeBwdPlan {
         // few rows: dh streams the weights past them, dw writes more than it multiplies
         dh_tile = rows <= 32 ? CeTile{32, a.dtype == DT_BF16 ? 256 : 128, false} : ce_tile(a.dtype, rows, a.c);
         dw_tile = a.dtype == DT_BF16 && a.m <= 128 ? CeTile{128, 128, false} : ce_tile(a.dtype, wide, a.c);
-        // one launch for both: a dw of few stages in the smaller tiles, else a dh in the larger
-        // (1001 x 776 x 40961: 246 us and 266; 5037 x 792 x 101207: 2958 and 2917, apart 3460)
+        // one launch for both, which is shorter than two (5037 x 792 x 101207: 3301 us apart): a dw of
+        // few stages in the smaller tiles, else a dh in the larger.  Measured in the smaller and the
+        // larger, the crossing lies between 300 and 400 rows of 2048 channels (32768 classes: 178 us
+        // and 192 with 300 rows, 391 and 378 with 1001, 1774 and 1601 with 5037), between 300 and 1001
+        // of 792 (101207 classes: 283 and 321, 674 and 661, 2880 and 2788) and of 4096 (16384: 183 and
+        // 200, 382 and 369), and past 5037 of 776 (40961: 131 and 149, 256 and 267, 1130 and 1214).
         if (dw_tile.bi == 256 && dh_tile.bi == 128) (a.m < 1024 ? dw_tile : dh_tile) = a.m < 1024 ? dh_tile : dw_tile;
         dh_parts = ce_parts(dh_tile, rows, a.c, cdiv(wide, bk), 2);
         dw_parts = few ? 1 : ce_parts(dw_tile, wide, a.c, cdiv(a.m, bk), 4);
